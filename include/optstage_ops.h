@@ -2,7 +2,9 @@
  * Single-kernel entry points of liboptstage: each launches one step of a stage's F / B / W op graph
  * (paper Sec. 2.2: linear maps z = W x, grad_x = W^T grad_z, grad_W = grad_z x^T; everything else is the
  * non-linear part the paper folds into sigma).  They exist so that every kernel can be checked against
- * the CPU oracle and timed on its own; the stage calls in optstage.h launch exactly these kernels.
+ * the CPU oracle and timed on its own; the stage calls in optstage.h launch exactly these kernels.  Beside them stand operators that a
+ * training step needs around a stage and that its op graph does not have: activations kept in 8 bits, norms of queries and
+ * keys, and the embedding.
  *
  * All tensor pointers are DEVICE memory, caller-owned, 16-byte aligned, row-major with tokens as rows.
  * dtype is optstage_dtype (storage type; arithmetic is fp32 / bf16 MFMA with fp32 accumulation).
@@ -111,6 +113,72 @@ optstage_status optstage_op_attn_bwd(uint32_t dtype, const void* qkv, const void
                                      const float* lse, void* dqkv, float* ws, uint32_t seq, uint32_t batch,
                                      uint32_t n_q, uint32_t n_kv, uint32_t head_dim, void* stream);
 uint64_t optstage_op_attn_bwd_ws_floats(uint32_t seq, uint32_t batch, uint32_t n_q, uint32_t n_kv, uint32_t head_dim);
+/* ---- Values kept in 8 bits between a forward and a backward pass ----
+ * x [rows, cols] is kept as codes (DEVICE, rows * cols bytes) and scales (DEVICE, rows * ceil(cols / 32) bytes), 1.03 bytes a
+ * value.  Blocks of 32 consecutive values of a row (the last one of a row may be shorter) share a scale byte b, which stands for
+ * 2^(b - 127): the least power 2^k, -117 <= k <= 119, with max |x| <= 448 * 2^k.  A code is x / 2^k in e4m3 (4 exponent and 3 fraction
+ * bits, bias 7, no infinity, largest value 448), rounded to nearest, ties to even.  So a kept value is off by at most 2^-4 of the value, or
+ * 2^(k - 10) where that is more, and is exactly representable in bf16 and fp32.  A value that is not finite is kept as NaN, and
+ * its block's scale goes by the others; values above 448 * 2^119 are kept as that.
+ * The calls below that keep their operand ("_pack8") give what pack8 would and otherwise the results of their plain counterparts; those that
+ * read it ("8") compute in fp32 from the values kept, with one rounding of each result to the storage type.
+ * What is kept may lie in pinned host memory meanwhile; codes and scales are plain bytes. */
+/* ldx: distance of x's rows in elements, >= cols (a column range of wider rows). */
+optstage_status optstage_op_pack8(uint32_t dtype, const void* x, uint32_t ldx, uint8_t* codes, uint8_t* scales, uint32_t rows,
+                                  uint32_t cols, void* stream);
+optstage_status optstage_op_unpack8(uint32_t dtype, const uint8_t* codes, const uint8_t* scales, void* x, uint32_t ldx, uint32_t rows,
+                                    uint32_t cols, void* stream);
+/* optstage_op_norm_fwd that keeps x [rows, hidden].  hidden is a multiple of 8 (fp32: 4), at most 8192. */
+optstage_status optstage_op_norm_fwd_pack8(uint32_t dtype, uint32_t family, const void* x, const void* gamma, const void* beta, void* out,
+                                           float* stats, uint8_t* codes, uint8_t* scales, uint32_t rows, uint32_t hidden, float eps,
+                                           void* stream);
+/* optstage_op_norm_bwd from the kept x, with the forward pass's statistics.  out (may be null): the normalised rows once more, from the
+ * kept x, for the weight gradient of the projection that read them (dW = dY^T n); beta is read only for that.  dx may be dn or
+ * dres; out is a buffer of its own.  partial: fp32 scratch of 2 * min(rows, 512) * hidden elements. */
+optstage_status optstage_op_norm_bwd8(uint32_t dtype, uint32_t family, const void* dn, const uint8_t* codes, const uint8_t* scales,
+                                      const float* stats, const void* gamma, const void* beta, const void* dres, void* dx, void* out,
+                                      float* partial, float* dgamma, float* dbeta, uint32_t rows, uint32_t hidden, void* stream);
+/* optstage_op_act_fwd that keeps gu.  LLAMA: as 2 * rows rows of ffn values, row 2 r the gate's and 2 r + 1 the up projection's.  ffn is a
+ * multiple of 8 (fp32: 4). */
+optstage_status optstage_op_act_fwd_pack8(uint32_t dtype, uint32_t family, const void* gu, void* a, uint8_t* codes, uint8_t* scales,
+                                          uint32_t rows, uint32_t ffn, void* stream);
+/* optstage_op_act_bwd from the kept gu.  a (may be null): the activation's output once more, from the kept gu, for the weight
+ * gradient of the down projection; a may be da.  dgu is a buffer of its own (GPT: may be da, with a null or elsewhere). */
+optstage_status optstage_op_act_bwd8(uint32_t dtype, uint32_t family, const void* da, const uint8_t* codes, const uint8_t* scales, void* dgu,
+                                     void* a, uint32_t rows, uint32_t ffn, void* stream);
+
+/* ---- Norms of queries and keys with the position rotation ----
+ * Over packed qkv rows [rows, (n_q + 2 n_kv) * head_dim]: every q head x becomes R(x * r * gamma_q), every k head R(x * r * gamma_k) with
+ * r = 1 / sqrt(mean(x^2) + eps) and R the rotation of optstage_op_rope (position = row % seq, its table); one rounding.  gamma_q
+ * and gamma_k are [head_dim], shared by their heads.  stats (fp32 [rows, n_q + n_kv]) receives r.  dst may be src (in place); otherwise the
+ * v part is copied too.  codes / scales (both or neither): src kept in 8 bits as above, all of the row.  head_dim 64, 128, 192 or 256. */
+optstage_status optstage_op_qknorm_rope(uint32_t dtype, const void* src, void* dst, const void* gamma_q, const void* gamma_k, const float* table,
+                                        float* stats, uint8_t* codes, uint8_t* scales, uint32_t rows, uint32_t seq, uint32_t n_q, uint32_t n_kv,
+                                        uint32_t head_dim, float eps, void* stream);
+/* dst once more from what was kept, with the forward pass's stats: what the attention's gradient reads. */
+optstage_status optstage_op_qknorm_rope8(uint32_t dtype, const uint8_t* codes, const uint8_t* scales, const float* stats, const void* gamma_q,
+                                         const void* gamma_k, const float* table, void* dst, uint32_t rows, uint32_t seq, uint32_t n_q,
+                                         uint32_t n_kv, uint32_t head_dim, void* stream);
+/* dx from dy (the attention's gradient, rows as above) and either x (the rows before the norm) or codes and scales; dgamma_q and dgamma_k
+ * (fp32 [head_dim]) are ADDED to.  dx may be dy or x; the v part of dy is passed on.  partial: fp32 scratch of
+ * 2 * min(rows, 1024) * head_dim elements. */
+optstage_status optstage_op_qknorm_rope_bwd(uint32_t dtype, const void* dy, const void* x, const uint8_t* codes, const uint8_t* scales,
+                                            const float* stats, const void* gamma_q, const void* gamma_k, const float* table, void* dx,
+                                            float* partial, float* dgamma_q, float* dgamma_k, uint32_t rows, uint32_t seq, uint32_t n_q,
+                                            uint32_t n_kv, uint32_t head_dim, void* stream);
+
+/* ---- Embedding: the first stage's input and what becomes of its gradient ----
+ * out[r] = scale * weight[ids[r]]; weight is [vocab, hidden], ids int32 [rows].  A row whose id is negative or >= vocab (padding) is zero
+ * and has no gradient.  hidden is a multiple of 8 (fp32: 4). */
+optstage_status optstage_op_embed_fwd(uint32_t dtype, const int32_t* ids, const void* weight, void* out, uint32_t rows, uint32_t vocab,
+                                      uint32_t hidden, float scale, void* stream);
+/* grad[t] (fp32 [vocab, hidden]) += scale * sum of dy[r] over the rows r with ids[r] = t: the tokens are sorted, equal ones side by side,
+ * and their rows added in a fixed order, without atomics (the same bits every time); rows of grad whose token does not occur are neither
+ * read nor written.  ws: DEVICE scratch of at least optstage_op_embed_bwd_ws_bytes() bytes, used until the call's work has run. */
+optstage_status optstage_op_embed_bwd(uint32_t dtype, const int32_t* ids, const void* dy, float* grad, void* ws, uint64_t ws_bytes, uint32_t rows,
+                                      uint32_t vocab, uint32_t hidden, float scale, void* stream);
+uint64_t optstage_op_embed_bwd_ws_bytes(uint32_t rows, uint32_t hidden);
+
 /* out_dev[0] = sum of the buffer's 64-bit words mod 2^64, out_dev[1] = their xor.  bytes % 8 == 0. */
 optstage_status optstage_op_checksum(const void* buf, uint64_t bytes, uint64_t* out_dev, void* stream);
 

@@ -106,9 +106,20 @@ _SIGS = {
     "optstage_op_rope": [_u32, _vp, _vp, _vp, _u32, _u32, _u32, _u32, _u32, _u32, _vp],
     "optstage_op_attn_fwd": [_u32, _vp, _vp, _vp, _u32, _u32, _u32, _u32, _u32, _vp],
     "optstage_op_attn_bwd": [_u32, _vp, _vp, _vp, _vp, _vp, _vp, _u32, _u32, _u32, _u32, _u32, _vp],
+    "optstage_op_pack8": [_u32, _vp, _u32, _vp, _vp, _u32, _u32, _vp],
+    "optstage_op_unpack8": [_u32, _vp, _vp, _vp, _u32, _u32, _u32, _vp],
+    "optstage_op_norm_fwd_pack8": [_u32, _u32, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _u32, _u32, _f32, _vp],
+    "optstage_op_norm_bwd8": [_u32, _u32, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _u32, _u32, _vp],
+    "optstage_op_act_fwd_pack8": [_u32, _u32, _vp, _vp, _vp, _vp, _u32, _u32, _vp],
+    "optstage_op_act_bwd8": [_u32, _u32, _vp, _vp, _vp, _vp, _vp, _u32, _u32, _vp],
+    "optstage_op_qknorm_rope": [_u32, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _u32, _u32, _u32, _u32, _u32, _f32, _vp],
+    "optstage_op_qknorm_rope8": [_u32, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _u32, _u32, _u32, _u32, _u32, _vp],
+    "optstage_op_qknorm_rope_bwd": [_u32, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _u32, _u32, _u32, _u32, _u32, _vp],
+    "optstage_op_embed_fwd": [_u32, _vp, _vp, _vp, _u32, _u32, _u32, _f32, _vp],
+    "optstage_op_embed_bwd": [_u32, _vp, _vp, _vp, _vp, _u64, _u32, _u32, _u32, _f32, _vp],
     "optstage_op_checksum": [_vp, _u64, _vp, _vp],
 }
-EXPORTS = tuple(_SIGS) + ("optstage_destroy", "optstage_last_error", "optstage_op_attn_bwd_ws_floats")
+EXPORTS = tuple(_SIGS) + ("optstage_destroy", "optstage_last_error", "optstage_op_attn_bwd_ws_floats", "optstage_op_embed_bwd_ws_bytes")
 
 
 def lib():
@@ -135,6 +146,8 @@ def lib():
         L.optstage_last_error.restype = C.c_char_p
         L.optstage_op_attn_bwd_ws_floats.argtypes = [_u32] * 5
         L.optstage_op_attn_bwd_ws_floats.restype = _u64
+        L.optstage_op_embed_bwd_ws_bytes.argtypes = [_u32] * 2
+        L.optstage_op_embed_bwd_ws_bytes.restype = _u64
         _lib = L
     return _lib
 

@@ -173,3 +173,25 @@ hipError_t launch_attn_bwd_inplace(int dtype, void* qkv, const void* o, const vo
 uint64_t attn_bwd_ws_floats(int seq, int batch, int n_q, int n_kv, int d);
 // heads of 64: how many groups of waves share the keys of a dK / dV workgroup
 int attn_d64_key_groups(int seq, int batch, int n_q, int n_kv);
+// values kept in 8 bits (keep8.h): codes [rows][cols], scales [rows][ceil(cols / 32)]
+hipError_t launch_pack8(int dtype, const void* x, size_t ldx, uint8_t* codes, uint8_t* scales, int rows, int cols, hipStream_t s);
+hipError_t launch_unpack8(int dtype, const uint8_t* codes, const uint8_t* scales, void* x, size_t ldx, int rows, int cols, hipStream_t s);
+// whether norm_fwd_pack8 / norm_bwd8 serve rows of h
+bool norm8_shape_ok(int dtype, int h);
+hipError_t launch_norm_fwd_pack8(int dtype, int family, const void* x, const void* gamma, const void* beta, void* out, float* stats, uint8_t* codes,
+                                 uint8_t* scales, int rows, int h, float eps, hipStream_t s);
+hipError_t launch_norm_bwd8(int dtype, int family, const void* dn, const uint8_t* codes, const uint8_t* scales, const float* stats, const void* gamma, const void* beta,
+                            const void* dres, void* dx, void* out, float* partial, float* dgamma, float* dbeta, int rows, int h, hipStream_t s);
+hipError_t launch_act_fwd_pack8(int dtype, int family, const void* gu, void* a, uint8_t* codes, uint8_t* scales, int rows, int f, hipStream_t s);
+hipError_t launch_act_bwd8(int dtype, int family, const void* da, const uint8_t* codes, const uint8_t* scales, void* dgu, void* a, int rows, int f, hipStream_t s);
+// src or codes_in / scales_in; codes / scales: where src is kept, or null
+hipError_t launch_qknorm_rope(int dtype, const void* src, const uint8_t* codes_in, const uint8_t* scales_in, void* dst, const void* gamma_q, const void* gamma_k,
+                              const float* table, float* stats, uint8_t* codes, uint8_t* scales, int rows, int seq, int n_q, int n_kv, int d, float eps, hipStream_t s);
+// x or codes / scales; partial: fp32 scratch of 2 * min(rows, 1024) * d elements
+hipError_t launch_qknorm_rope_bwd(int dtype, const void* dy, const void* x, const uint8_t* codes, const uint8_t* scales, const float* stats, const void* gamma_q,
+                                  const void* gamma_k, const float* table, void* dx, float* partial, float* dgamma_q, float* dgamma_k, int rows, int seq, int n_q, int n_kv,
+                                  int d, hipStream_t s);
+hipError_t launch_embed_fwd(int dtype, const int* ids, const void* weight, void* out, int rows, unsigned vocab, int h, float scale, hipStream_t s);
+// ws: embed_bwd_ws_bytes() bytes
+hipError_t launch_embed_bwd(int dtype, const int* ids, const void* dy, float* grad, void* ws, int rows, unsigned vocab, int h, float scale, hipStream_t s);
+uint64_t embed_bwd_ws_bytes(int rows, int h);

@@ -1,0 +1,230 @@
+// Activations kept in 8 bits between the forward and the backward pass (keep8.h), and the non-linear parts of a layer that keep their
+// input that way and take their gradients from it.
+#include "keep8.h"
+
+namespace {
+
+constexpr int NT = 256;
+
+__device__ __forceinline__ uint32_t half_wave_max(uint32_t v) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) v = max(v, (uint32_t)__shfl_xor((int)v, o, 64));
+  return v;
+}
+
+// one value per lane, a block per half wave
+template <typename T>
+__global__ __launch_bounds__(NT) void pack8_kernel(const T* __restrict__ x, size_t ldx, uint8_t* __restrict__ codes, uint8_t* __restrict__ scales,
+                                                   int rows, int cols) {
+  const int nb = keep_blocks(cols), l = threadIdx.x & 31;
+  const size_t total = (size_t)rows * nb, step = (size_t)gridDim.x * (NT / 32);
+  for (size_t i = blockIdx.x * (size_t)(NT / 32) + (threadIdx.x >> 5); i < total; i += step) {
+    const size_t row = i / nb;
+    const int col = (int)(i % nb) * KEEP_BLOCK + l;
+    const float v = col < cols ? to_f32<T>(x[row * ldx + col]) : 0.f;
+    const uint32_t b = keep_scale_byte(half_wave_max(keep_magnitude(v)));
+    if (col < cols) codes[row * cols + col] = (uint8_t)keep_encode(v, keep_inverse(b));
+    if (l == 0) scales[i] = (uint8_t)b;
+  }
+}
+
+template <typename T>
+__global__ __launch_bounds__(NT) void unpack8_kernel(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales, T* __restrict__ x, size_t ldx,
+                                                     int rows, int cols) {
+  const int nb = keep_blocks(cols);
+  const size_t total = (size_t)rows * cols, step = (size_t)gridDim.x * NT;
+  for (size_t i = blockIdx.x * (size_t)NT + threadIdx.x; i < total; i += step) {
+    const size_t row = i / cols;
+    const int col = (int)(i % cols);
+    x[row * ldx + col] = from_f32<T>(keep_decode(codes[i], keep_scale(scales[row * nb + col / KEEP_BLOCK])));
+  }
+}
+
+__device__ __forceinline__ float block_sum(float v, float* red /* [NT / 64] */) {
+  v = wave_sum(v);
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
+  __syncthreads();
+  float t = 0.f;
+#pragma unroll
+  for (int w = 0; w < NT / 64; ++w) t += red[w];
+  return t;
+}
+
+// one row per workgroup
+template <typename T, bool LN>
+__global__ __launch_bounds__(NT) void norm_fwd_pack8_kernel(const T* __restrict__ x, const T* __restrict__ gamma, const T* __restrict__ beta, T* __restrict__ out,
+                                                            float* __restrict__ stats, uint8_t* __restrict__ codes, uint8_t* __restrict__ scales, int h, float eps) {
+  __shared__ float red[NT / 64];
+  const size_t row = blockIdx.x;
+  const int nb = keep_blocks(h), l = threadIdx.x & 31;
+  const T* xr = x + row * h;
+  float mean = 0.f, s = 0.f;
+  if (LN) {
+    for (int c = threadIdx.x; c < h; c += NT) s += to_f32<T>(xr[c]);
+    mean = block_sum(s, red) / h;
+  }
+  s = 0.f;
+  for (int c = threadIdx.x; c < h; c += NT) { const float d = to_f32<T>(xr[c]) - mean; s += d * d; }
+  const float r = rsqrtf(block_sum(s, red) / h + eps);
+  if (threadIdx.x == 0) {
+    if (LN) { stats[2 * row] = mean; stats[2 * row + 1] = r; } else stats[row] = r;
+  }
+  for (int b0 = 0; b0 < nb; b0 += NT / 32) {
+    const int b = b0 + (threadIdx.x >> 5), col = b * KEEP_BLOCK + l;
+    const float v = col < h ? to_f32<T>(xr[col]) : 0.f;
+    const uint32_t byte = keep_scale_byte(half_wave_max(keep_magnitude(v)));
+    if (col < h) {
+      codes[row * h + col] = (uint8_t)keep_encode(v, keep_inverse(byte));
+      float o = (v - mean) * r * to_f32<T>(gamma[col]);
+      if (LN) o += to_f32<T>(beta[col]);
+      out[row * h + col] = from_f32<T>(o);
+    }
+    if (b < nb && l == 0) scales[row * nb + b] = (uint8_t)byte;
+  }
+}
+
+// workgroup b takes rows b, b + gridDim.x, ...; its sums of the gains' and biases' gradients stand in its rows of `partial`
+template <typename T, bool LN>
+__global__ __launch_bounds__(NT) void norm_bwd8_kernel(const T* dn, const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales,
+                                                       const float* __restrict__ stats, const T* __restrict__ gamma, const T* __restrict__ beta, const T* dres, T* dx,
+                                                       T* __restrict__ out, float* __restrict__ partial, int rows, int h) {
+  __shared__ float red[NT / 64];
+  const int nb = keep_blocks(h);
+  float* pg = partial + (size_t)blockIdx.x * h;
+  float* pb = partial + ((size_t)gridDim.x + blockIdx.x) * h;
+  for (int c = threadIdx.x; c < h; c += NT) { pg[c] = 0.f; if (LN) pb[c] = 0.f; }
+  for (size_t row = blockIdx.x; row < (size_t)rows; row += gridDim.x) {
+    const float mean = LN ? stats[2 * row] : 0.f, r = LN ? stats[2 * row + 1] : stats[row];
+    const uint8_t* cr = codes + row * h;
+    const uint8_t* sr = scales + row * nb;
+    float sg = 0.f, sgx = 0.f;
+    for (int c = threadIdx.x; c < h; c += NT) {
+      const float xh = (keep_decode(cr[c], keep_scale(sr[c / KEEP_BLOCK])) - mean) * r, d = to_f32<T>(dn[row * h + c]), g = d * to_f32<T>(gamma[c]);
+      sg += g;
+      sgx += g * xh;
+      pg[c] += d * xh;
+      if (LN) pb[c] += d;
+    }
+    const float mgx = block_sum(sgx, red) / h, mg = LN ? block_sum(sg, red) / h : 0.f;
+    for (int c = threadIdx.x; c < h; c += NT) {
+      const float xh = (keep_decode(cr[c], keep_scale(sr[c / KEEP_BLOCK])) - mean) * r, gm = to_f32<T>(gamma[c]);
+      float v = r * (to_f32<T>(dn[row * h + c]) * gm - mg - xh * mgx);
+      if (dres) v += to_f32<T>(dres[row * h + c]);
+      dx[row * h + c] = from_f32<T>(v);
+      if (out) out[row * h + c] = from_f32<T>(LN ? xh * gm + to_f32<T>(beta[c]) : xh * gm);
+    }
+  }
+}
+
+// one value of the output per lane, its block (SwiGLU: the gate's and the up projection's) per half wave
+template <typename T, bool SWIGLU>
+__global__ __launch_bounds__(NT) void act_fwd_pack8_kernel(const T* __restrict__ gu, T* __restrict__ a, uint8_t* __restrict__ codes, uint8_t* __restrict__ scales,
+                                                           int rows, int f) {
+  const int nb = keep_blocks(f), l = threadIdx.x & 31, parts = SWIGLU ? 2 : 1;
+  const size_t total = (size_t)rows * nb, step = (size_t)gridDim.x * (NT / 32);
+  for (size_t i = blockIdx.x * (size_t)(NT / 32) + (threadIdx.x >> 5); i < total; i += step) {
+    const size_t row = i / nb;
+    const int b = (int)(i % nb), col = b * KEEP_BLOCK + l;
+    float v[2] = {0.f, 0.f};
+#pragma unroll
+    for (int p = 0; p < parts; ++p) {
+      const size_t at = (row * parts + p) * f + col;
+      if (col < f) v[p] = to_f32<T>(gu[at]);
+      const uint32_t byte = keep_scale_byte(half_wave_max(keep_magnitude(v[p])));
+      if (col < f) codes[at] = (uint8_t)keep_encode(v[p], keep_inverse(byte));
+      if (l == 0) scales[(row * parts + p) * nb + b] = (uint8_t)byte;
+    }
+    if (col < f) a[row * f + col] = from_f32<T>(SWIGLU ? v[0] * sigmoidf_(v[0]) * v[1] : gelu(v[0]));
+  }
+}
+
+template <typename T, bool SWIGLU>
+__global__ __launch_bounds__(NT) void act_bwd8_kernel(const T* da, const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales, T* dgu, T* a, int rows, int f) {
+  const int nb = keep_blocks(f), parts = SWIGLU ? 2 : 1;
+  const size_t total = (size_t)rows * f, step = (size_t)gridDim.x * NT;
+  for (size_t i = blockIdx.x * (size_t)NT + threadIdx.x; i < total; i += step) {
+    const size_t row = i / f;
+    const int col = (int)(i % f);
+    float v[2] = {0.f, 0.f};
+#pragma unroll
+    for (int p = 0; p < parts; ++p) v[p] = keep_decode(codes[(row * parts + p) * f + col], keep_scale(scales[(row * parts + p) * nb + col / KEEP_BLOCK]));
+    const float d = to_f32<T>(da[i]);
+    if (SWIGLU) {
+      float dg, du;
+      dswiglu(v[0], v[1], d, dg, du);
+      dgu[row * 2 * f + col] = from_f32<T>(dg);
+      dgu[row * 2 * f + f + col] = from_f32<T>(du);
+    } else {
+      dgu[i] = from_f32<T>(dgelu(v[0], d));
+    }
+    if (a) a[i] = from_f32<T>(SWIGLU ? v[0] * sigmoidf_(v[0]) * v[1] : gelu(v[0]));
+  }
+}
+
+int grid_of(size_t workgroups) { return (int)(workgroups > 8192 ? 8192 : workgroups); }
+
+template <typename T> hipError_t run_pack8(const void* x, size_t ldx, uint8_t* codes, uint8_t* scales, int rows, int cols, hipStream_t s) {
+  const size_t blocks = (size_t)rows * keep_blocks(cols);
+  hipLaunchKernelGGL(pack8_kernel<T>, dim3(grid_of((blocks + 7) / 8)), dim3(NT), 0, s, (const T*)x, ldx, codes, scales, rows, cols);
+  return hipGetLastError();
+}
+template <typename T> hipError_t run_unpack8(const uint8_t* codes, const uint8_t* scales, void* x, size_t ldx, int rows, int cols, hipStream_t s) {
+  hipLaunchKernelGGL(unpack8_kernel<T>, dim3(grid_of(((size_t)rows * cols + NT - 1) / NT)), dim3(NT), 0, s, codes, scales, (T*)x, ldx, rows, cols);
+  return hipGetLastError();
+}
+template <typename T, bool LN>
+hipError_t run_norm_fwd_pack8(const void* x, const void* gamma, const void* beta, void* out, float* stats, uint8_t* codes, uint8_t* scales, int rows, int h, float eps,
+                              hipStream_t s) {
+  hipLaunchKernelGGL((norm_fwd_pack8_kernel<T, LN>), dim3(rows), dim3(NT), 0, s, (const T*)x, (const T*)gamma, (const T*)beta, (T*)out, stats, codes, scales, h, eps);
+  return hipGetLastError();
+}
+template <typename T, bool LN>
+hipError_t run_norm_bwd8(const void* dn, const uint8_t* codes, const uint8_t* scales, const float* stats, const void* gamma, const void* beta, const void* dres, void* dx,
+                         void* out, float* partial, int rows, int h, hipStream_t s) {
+  hipLaunchKernelGGL((norm_bwd8_kernel<T, LN>), dim3(norm_bwd_partial_rows(rows)), dim3(NT), 0, s, (const T*)dn, codes, scales, stats, (const T*)gamma, (const T*)beta,
+                     (const T*)dres, (T*)dx, (T*)out, partial, rows, h);
+  return hipGetLastError();
+}
+template <typename T, bool SWIGLU>
+hipError_t run_act_fwd_pack8(const void* gu, void* a, uint8_t* codes, uint8_t* scales, int rows, int f, hipStream_t s) {
+  hipLaunchKernelGGL((act_fwd_pack8_kernel<T, SWIGLU>), dim3(grid_of(((size_t)rows * keep_blocks(f) + 7) / 8)), dim3(NT), 0, s, (const T*)gu, (T*)a, codes, scales, rows, f);
+  return hipGetLastError();
+}
+template <typename T, bool SWIGLU>
+hipError_t run_act_bwd8(const void* da, const uint8_t* codes, const uint8_t* scales, void* dgu, void* a, int rows, int f, hipStream_t s) {
+  hipLaunchKernelGGL((act_bwd8_kernel<T, SWIGLU>), dim3(grid_of(((size_t)rows * f + NT - 1) / NT)), dim3(NT), 0, s, (const T*)da, codes, scales, (T*)dgu, (T*)a, rows, f);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+// f<T, true / false>(...) by type and family
+#define KEEP_BY_TYPE(f, ...) (dtype == DT_BF16 ? f<bf16_t>(__VA_ARGS__) : f<float>(__VA_ARGS__))
+#define KEEP_BY_BOTH(f, flag, ...)                                                       \
+  (dtype == DT_BF16 ? ((flag) ? f<bf16_t, true>(__VA_ARGS__) : f<bf16_t, false>(__VA_ARGS__)) \
+                    : ((flag) ? f<float, true>(__VA_ARGS__) : f<float, false>(__VA_ARGS__)))
+
+hipError_t launch_pack8(int dtype, const void* x, size_t ldx, uint8_t* codes, uint8_t* scales, int rows, int cols, hipStream_t s) {
+  return KEEP_BY_TYPE(run_pack8, x, ldx, codes, scales, rows, cols, s);
+}
+hipError_t launch_unpack8(int dtype, const uint8_t* codes, const uint8_t* scales, void* x, size_t ldx, int rows, int cols, hipStream_t s) {
+  return KEEP_BY_TYPE(run_unpack8, codes, scales, x, ldx, rows, cols, s);
+}
+bool norm8_shape_ok(int dtype, int h) { return h > 0 && h <= 8192 && h % (dtype == DT_BF16 ? 8 : 4) == 0; }
+hipError_t launch_norm_fwd_pack8(int dtype, int family, const void* x, const void* gamma, const void* beta, void* out, float* stats, uint8_t* codes,
+                                 uint8_t* scales, int rows, int h, float eps, hipStream_t s) {
+  return KEEP_BY_BOTH(run_norm_fwd_pack8, family == FAM_GPT, x, gamma, beta, out, stats, codes, scales, rows, h, eps, s);
+}
+hipError_t launch_norm_bwd8(int dtype, int family, const void* dn, const uint8_t* codes, const uint8_t* scales, const float* stats, const void* gamma, const void* beta,
+                            const void* dres, void* dx, void* out, float* partial, float* dgamma, float* dbeta, int rows, int h, hipStream_t s) {
+  const hipError_t e = KEEP_BY_BOTH(run_norm_bwd8, family == FAM_GPT, dn, codes, scales, stats, gamma, beta, dres, dx, out, partial, rows, h, s);
+  if (e != hipSuccess) return e;
+  return launch_norm_reduce(family, NormReduce{{partial}, {dgamma}, {dbeta}, 1}, rows, h, 0, s);
+}
+hipError_t launch_act_fwd_pack8(int dtype, int family, const void* gu, void* a, uint8_t* codes, uint8_t* scales, int rows, int f, hipStream_t s) {
+  return KEEP_BY_BOTH(run_act_fwd_pack8, family == FAM_LLAMA, gu, a, codes, scales, rows, f, s);
+}
+hipError_t launch_act_bwd8(int dtype, int family, const void* da, const uint8_t* codes, const uint8_t* scales, void* dgu, void* a, int rows, int f, hipStream_t s) {
+  return KEEP_BY_BOTH(run_act_bwd8, family == FAM_LLAMA, da, codes, scales, dgu, a, rows, f, s);
+}

@@ -289,4 +289,137 @@ optstage_status optstage_op_checksum(const void* buf, uint64_t bytes, uint64_t* 
   return wrap(launch_checksum(buf, bytes, out_dev, (hipStream_t)stream), "checksum");
 }
 
+// ---- values kept in 8 bits ---------------------------------------------------------------------------------
+optstage_status optstage_op_pack8(uint32_t dtype, const void* x, uint32_t ldx, uint8_t* codes, uint8_t* scales, uint32_t rows,
+                                  uint32_t cols, void* stream) {
+  REQ(x && codes && scales, "pack8: null operand");
+  REQ(aligned16(x) && aligned16(codes) && aligned16(scales), "pack8: operands must be 16-byte aligned");
+  REQ(dtype <= 1 && rows && cols && rows < (1u << 30) && cols < (1u << 30) && ldx >= cols, "pack8: bad argument");
+  return wrap(launch_pack8((int)dtype, x, ldx, codes, scales, (int)rows, (int)cols, (hipStream_t)stream), "pack8");
+}
+
+optstage_status optstage_op_unpack8(uint32_t dtype, const uint8_t* codes, const uint8_t* scales, void* x, uint32_t ldx, uint32_t rows,
+                                    uint32_t cols, void* stream) {
+  REQ(x && codes && scales, "unpack8: null operand");
+  REQ(aligned16(x) && aligned16(codes) && aligned16(scales), "unpack8: operands must be 16-byte aligned");
+  REQ(dtype <= 1 && rows && cols && rows < (1u << 30) && cols < (1u << 30) && ldx >= cols, "unpack8: bad argument");
+  return wrap(launch_unpack8((int)dtype, codes, scales, x, ldx, (int)rows, (int)cols, (hipStream_t)stream), "unpack8");
+}
+
+optstage_status optstage_op_norm_fwd_pack8(uint32_t dtype, uint32_t family, const void* x, const void* gamma, const void* beta, void* out,
+                                           float* stats, uint8_t* codes, uint8_t* scales, uint32_t rows, uint32_t hidden, float eps,
+                                           void* stream) {
+  REQ(dtype <= 1 && family <= 1 && rows && hidden && rows < (1u << 30), "norm_fwd_pack8: bad argument");
+  REQ(x && gamma && out && stats && codes && scales && (family == OPTSTAGE_LLAMA || beta), "norm_fwd_pack8: null operand");
+  REQ(aligned16(x) && aligned16(gamma) && aligned16(beta) && aligned16(out) && aligned16(stats) && aligned16(codes) && aligned16(scales),
+      "norm_fwd_pack8: operands must be 16-byte aligned");
+  REQ(hidden <= 8192 && norm8_shape_ok((int)dtype, (int)hidden), "norm_fwd_pack8: hidden must be a multiple of 8 (fp32: 4), at most 8192");
+  return wrap(launch_norm_fwd_pack8((int)dtype, (int)family, x, gamma, beta, out, stats, codes, scales, (int)rows, (int)hidden, eps, (hipStream_t)stream),
+              "norm_fwd_pack8");
+}
+
+optstage_status optstage_op_norm_bwd8(uint32_t dtype, uint32_t family, const void* dn, const uint8_t* codes, const uint8_t* scales,
+                                      const float* stats, const void* gamma, const void* beta, const void* dres, void* dx, void* out,
+                                      float* partial, float* dgamma, float* dbeta, uint32_t rows, uint32_t hidden, void* stream) {
+  REQ(dtype <= 1 && family <= 1 && rows && hidden && rows < (1u << 30), "norm_bwd8: bad argument");
+  REQ(dn && codes && scales && stats && gamma && dx && partial && dgamma && (family == OPTSTAGE_LLAMA || (dbeta && (beta || !out))), "norm_bwd8: null operand");
+  REQ(aligned16(dn) && aligned16(codes) && aligned16(scales) && aligned16(stats) && aligned16(gamma) && aligned16(beta) && aligned16(dres) && aligned16(dx) &&
+          aligned16(out) && aligned16(partial) && aligned16(dgamma) && aligned16(dbeta),
+      "norm_bwd8: operands must be 16-byte aligned");
+  REQ(out != dx && (!out || (out != dn && out != dres)), "norm_bwd8: out must be a buffer of its own");
+  REQ(hidden <= 8192 && norm8_shape_ok((int)dtype, (int)hidden), "norm_bwd8: hidden must be a multiple of 8 (fp32: 4), at most 8192");
+  return wrap(launch_norm_bwd8((int)dtype, (int)family, dn, codes, scales, stats, gamma, beta, dres, dx, out, partial, dgamma, dbeta, (int)rows, (int)hidden,
+                               (hipStream_t)stream),
+              "norm_bwd8");
+}
+
+optstage_status optstage_op_act_fwd_pack8(uint32_t dtype, uint32_t family, const void* gu, void* a, uint8_t* codes, uint8_t* scales,
+                                          uint32_t rows, uint32_t ffn, void* stream) {
+  REQ(gu && a && codes && scales, "act_fwd_pack8: null operand");
+  REQ(aligned16(gu) && aligned16(a) && aligned16(codes) && aligned16(scales), "act_fwd_pack8: operands must be 16-byte aligned");
+  REQ(dtype <= 1 && family <= 1 && rows && ffn && rows < (1u << 30) && ffn < (1u << 29), "act_fwd_pack8: bad argument");
+  REQ(ffn % (dtype == OPTSTAGE_BF16 ? 8 : 4) == 0, "act_fwd_pack8: ffn must be a multiple of 8 (fp32: 4)");
+  return wrap(launch_act_fwd_pack8((int)dtype, (int)family, gu, a, codes, scales, (int)rows, (int)ffn, (hipStream_t)stream), "act_fwd_pack8");
+}
+
+optstage_status optstage_op_act_bwd8(uint32_t dtype, uint32_t family, const void* da, const uint8_t* codes, const uint8_t* scales, void* dgu,
+                                     void* a, uint32_t rows, uint32_t ffn, void* stream) {
+  REQ(da && codes && scales && dgu, "act_bwd8: null operand");
+  REQ(aligned16(da) && aligned16(codes) && aligned16(scales) && aligned16(dgu) && aligned16(a), "act_bwd8: operands must be 16-byte aligned");
+  REQ(dgu != a && (family == OPTSTAGE_GPT || dgu != da), "act_bwd8: dgu must be a buffer of its own");
+  REQ(dtype <= 1 && family <= 1 && rows && ffn && rows < (1u << 30) && ffn < (1u << 29), "act_bwd8: bad argument");
+  REQ(ffn % (dtype == OPTSTAGE_BF16 ? 8 : 4) == 0, "act_bwd8: ffn must be a multiple of 8 (fp32: 4)");
+  return wrap(launch_act_bwd8((int)dtype, (int)family, da, codes, scales, dgu, a, (int)rows, (int)ffn, (hipStream_t)stream), "act_bwd8");
+}
+
+// ---- norms of queries and keys -----------------------------------------------------------------------------
+static bool qknorm_shape_ok(uint32_t rows, uint32_t seq, uint32_t n_q, uint32_t n_kv, uint32_t d) {
+  return rows && rows < (1u << 30) && seq && seq < (1u << 24) && n_q && n_q < 65536 && n_kv && n_kv < 65536 && (d == 64 || d == 128 || d == 192 || d == 256);
+}
+
+optstage_status optstage_op_qknorm_rope(uint32_t dtype, const void* src, void* dst, const void* gamma_q, const void* gamma_k, const float* table,
+                                        float* stats, uint8_t* codes, uint8_t* scales, uint32_t rows, uint32_t seq, uint32_t n_q, uint32_t n_kv,
+                                        uint32_t head_dim, float eps, void* stream) {
+  REQ(src && dst && gamma_q && gamma_k && table && stats && !codes == !scales, "qknorm_rope: null operand");
+  REQ(aligned16(src) && aligned16(dst) && aligned16(gamma_q) && aligned16(gamma_k) && aligned16(table) && aligned16(stats) && aligned16(codes) && aligned16(scales),
+      "qknorm_rope: operands must be 16-byte aligned");
+  REQ(dtype <= 1 && qknorm_shape_ok(rows, seq, n_q, n_kv, head_dim), "qknorm_rope: bad argument (head_dim is 64, 128, 192 or 256)");
+  return wrap(launch_qknorm_rope((int)dtype, src, nullptr, nullptr, dst, gamma_q, gamma_k, table, stats, codes, scales, (int)rows, (int)seq, (int)n_q, (int)n_kv,
+                                 (int)head_dim, eps, (hipStream_t)stream),
+              "qknorm_rope");
+}
+
+optstage_status optstage_op_qknorm_rope8(uint32_t dtype, const uint8_t* codes, const uint8_t* scales, const float* stats, const void* gamma_q,
+                                         const void* gamma_k, const float* table, void* dst, uint32_t rows, uint32_t seq, uint32_t n_q,
+                                         uint32_t n_kv, uint32_t head_dim, void* stream) {
+  REQ(codes && scales && stats && gamma_q && gamma_k && table && dst, "qknorm_rope8: null operand");
+  REQ(aligned16(codes) && aligned16(scales) && aligned16(stats) && aligned16(gamma_q) && aligned16(gamma_k) && aligned16(table) && aligned16(dst),
+      "qknorm_rope8: operands must be 16-byte aligned");
+  REQ(dtype <= 1 && qknorm_shape_ok(rows, seq, n_q, n_kv, head_dim), "qknorm_rope8: bad argument (head_dim is 64, 128, 192 or 256)");
+  return wrap(launch_qknorm_rope((int)dtype, nullptr, codes, scales, dst, gamma_q, gamma_k, table, const_cast<float*>(stats), nullptr, nullptr, (int)rows, (int)seq,
+                                 (int)n_q, (int)n_kv, (int)head_dim, 0.f, (hipStream_t)stream),
+              "qknorm_rope8");
+}
+
+optstage_status optstage_op_qknorm_rope_bwd(uint32_t dtype, const void* dy, const void* x, const uint8_t* codes, const uint8_t* scales,
+                                            const float* stats, const void* gamma_q, const void* gamma_k, const float* table, void* dx,
+                                            float* partial, float* dgamma_q, float* dgamma_k, uint32_t rows, uint32_t seq, uint32_t n_q,
+                                            uint32_t n_kv, uint32_t head_dim, void* stream) {
+  REQ(dy && stats && gamma_q && gamma_k && table && dx && partial && dgamma_q && dgamma_k, "qknorm_rope_bwd: null operand");
+  REQ(!codes == !scales && !x == !!codes, "qknorm_rope_bwd: either x or codes and scales");
+  REQ(aligned16(dy) && aligned16(x) && aligned16(codes) && aligned16(scales) && aligned16(stats) && aligned16(gamma_q) && aligned16(gamma_k) && aligned16(table) &&
+          aligned16(dx) && aligned16(partial) && aligned16(dgamma_q) && aligned16(dgamma_k),
+      "qknorm_rope_bwd: operands must be 16-byte aligned");
+  REQ(dtype <= 1 && qknorm_shape_ok(rows, seq, n_q, n_kv, head_dim), "qknorm_rope_bwd: bad argument (head_dim is 64, 128, 192 or 256)");
+  return wrap(launch_qknorm_rope_bwd((int)dtype, dy, x, codes, scales, stats, gamma_q, gamma_k, table, dx, partial, dgamma_q, dgamma_k, (int)rows, (int)seq, (int)n_q,
+                                     (int)n_kv, (int)head_dim, (hipStream_t)stream),
+              "qknorm_rope_bwd");
+}
+
+// ---- embedding ---------------------------------------------------------------------------------------------
+static bool embed_shape_ok(uint32_t dtype, uint32_t rows, uint32_t vocab, uint32_t hidden) {
+  return dtype <= 1 && rows && rows < (1u << 26) && vocab && vocab < (1u << 31) && hidden && hidden < (1u << 24) && hidden % (dtype == OPTSTAGE_BF16 ? 8 : 4) == 0;
+}
+
+optstage_status optstage_op_embed_fwd(uint32_t dtype, const int32_t* ids, const void* weight, void* out, uint32_t rows, uint32_t vocab,
+                                      uint32_t hidden, float scale, void* stream) {
+  REQ(ids && weight && out, "embed_fwd: null operand");
+  REQ(aligned16(ids) && aligned16(weight) && aligned16(out), "embed_fwd: operands must be 16-byte aligned");
+  REQ(embed_shape_ok(dtype, rows, vocab, hidden), "embed_fwd: bad argument (hidden must be a multiple of 8, fp32: 4)");
+  return wrap(launch_embed_fwd((int)dtype, ids, weight, out, (int)rows, vocab, (int)hidden, scale, (hipStream_t)stream), "embed_fwd");
+}
+
+uint64_t optstage_op_embed_bwd_ws_bytes(uint32_t rows, uint32_t hidden) {
+  return rows < (1u << 26) && hidden < (1u << 24) ? embed_bwd_ws_bytes((int)rows, (int)hidden) : 0;
+}
+
+optstage_status optstage_op_embed_bwd(uint32_t dtype, const int32_t* ids, const void* dy, float* grad, void* ws, uint64_t ws_bytes, uint32_t rows,
+                                      uint32_t vocab, uint32_t hidden, float scale, void* stream) {
+  REQ(ids && dy && grad && ws, "embed_bwd: null operand");
+  REQ(aligned16(ids) && aligned16(dy) && aligned16(grad) && aligned16(ws), "embed_bwd: operands must be 16-byte aligned");
+  REQ(embed_shape_ok(dtype, rows, vocab, hidden), "embed_bwd: bad argument (hidden must be a multiple of 8, fp32: 4)");
+  REQ(ws_bytes >= embed_bwd_ws_bytes((int)rows, (int)hidden), "embed_bwd: workspace smaller than optstage_op_embed_bwd_ws_bytes()");
+  return wrap(launch_embed_bwd((int)dtype, ids, dy, grad, ws, (int)rows, vocab, (int)hidden, scale, (hipStream_t)stream), "embed_bwd");
+}
+
 }  // extern "C"
