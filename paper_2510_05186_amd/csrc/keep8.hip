@@ -40,6 +40,84 @@ __global__ __launch_bounds__(NT) void unpack8_kernel(const uint8_t* __restrict__
   }
 }
 
+// ---- the same, 16 bytes of x per lane and access ----------------------------------------------------------
+// The chunks of a row, padded to whole blocks, are numbered through all rows; a workgroup takes NT * U numbers at a time and all of its
+// loads are in flight before the first is used.
+struct Chunks {
+  size_t total;          // rows * per_row
+  unsigned per_row;      // chunks of a row, padded to whole blocks
+};
+template <typename T> Chunks chunks_of(int rows, int cols) {
+  const unsigned per_row = (unsigned)keep_blocks(cols) * KeepChunk<T>::LANES;
+  return {(size_t)rows * per_row, per_row};
+}
+struct At { size_t row; int col; };
+// chunk base + i, for base a multiple of NT * U and i < NT * U
+template <typename T> struct Walk {
+  size_t row0;
+  unsigned c0, per_row;
+  __device__ __forceinline__ Walk(size_t base, const Chunks& k) : per_row(k.per_row) {
+    row0 = k.total >> 32 ? base / k.per_row : (size_t)((unsigned)base / k.per_row);
+    c0 = (unsigned)(base - row0 * k.per_row);
+  }
+  __device__ __forceinline__ At at(unsigned i) const {
+    const unsigned n = c0 + i, r = n / per_row;
+    return {row0 + r, (int)((n - r * per_row) * Vec16<T>::N)};
+  }
+};
+
+template <typename T, int U>
+__global__ __launch_bounds__(NT) void pack8_vec_kernel(const T* __restrict__ x, size_t ldx, uint8_t* __restrict__ codes, uint8_t* __restrict__ scales, const Chunks k,
+                                                       int rows, int cols) {
+  typedef Vec16<T> V;
+  typedef typename KeepChunk<T>::codes_t codes_t;
+  const int nb = keep_blocks(cols);
+  for (size_t base = blockIdx.x * (size_t)(NT * U); base < k.total; base += (size_t)gridDim.x * (NT * U)) {
+    const Walk<T> walk(base, k);
+    V v[U] = {};
+    At at[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      at[u] = walk.at(u * NT + threadIdx.x);
+      if (at[u].row < (size_t)rows && at[u].col < cols) v[u] = *reinterpret_cast<const V*>(x + at[u].row * ldx + at[u].col);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      uint32_t byte;
+      const codes_t c = keep_chunk<T>(v[u], byte);
+      if (at[u].row < (size_t)rows) {
+        if (at[u].col < cols) *reinterpret_cast<codes_t*>(codes + at[u].row * cols + at[u].col) = c;
+        if (at[u].col % KEEP_BLOCK == 0) scales[at[u].row * nb + at[u].col / KEEP_BLOCK] = (uint8_t)byte;
+      }
+    }
+  }
+}
+
+template <typename T, int U>
+__global__ __launch_bounds__(NT) void unpack8_vec_kernel(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales, T* __restrict__ x, size_t ldx, const Chunks k,
+                                                         int rows, int cols) {
+  typedef Vec16<T> V;
+  typedef typename KeepChunk<T>::codes_t codes_t;
+  const int nb = keep_blocks(cols);
+  for (size_t base = blockIdx.x * (size_t)(NT * U); base < k.total; base += (size_t)gridDim.x * (NT * U)) {
+    const Walk<T> walk(base, k);
+    codes_t c[U];
+    uint32_t b[U];
+    At at[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      at[u] = walk.at(u * NT + threadIdx.x);
+      if (at[u].row < (size_t)rows && at[u].col < cols) {
+        c[u] = *reinterpret_cast<const codes_t*>(codes + at[u].row * cols + at[u].col);
+        b[u] = scales[at[u].row * nb + at[u].col / KEEP_BLOCK];
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (at[u].row < (size_t)rows && at[u].col < cols) *reinterpret_cast<V*>(x + at[u].row * ldx + at[u].col) = keep_stored(c[u], keep_scale(b[u]), V());
+  }
+}
+
 __device__ __forceinline__ float block_sum(float v, float* red /* [NT / 64] */) {
   v = wave_sum(v);
   __syncthreads();
@@ -164,12 +242,28 @@ __global__ __launch_bounds__(NT) void act_bwd8_kernel(const T* da, const uint8_t
 
 int grid_of(size_t workgroups) { return (int)(workgroups > 8192 ? 8192 : workgroups); }
 
+// rows of x and of the codes start on whole chunks
+template <typename T> bool chunked(size_t ldx, int cols) { return ldx % Vec16<T>::N == 0 && cols % Vec16<T>::N == 0; }
+constexpr int U = 4;
+
 template <typename T> hipError_t run_pack8(const void* x, size_t ldx, uint8_t* codes, uint8_t* scales, int rows, int cols, hipStream_t s) {
+  if (chunked<T>(ldx, cols)) {
+    const Chunks k = chunks_of<T>(rows, cols);
+    const size_t groups = (k.total + NT * U - 1) / (NT * U);
+    hipLaunchKernelGGL((pack8_vec_kernel<T, U>), dim3((unsigned)(groups > (1u << 20) ? 1u << 20 : groups)), dim3(NT), 0, s, (const T*)x, ldx, codes, scales, k, rows, cols);
+    return hipGetLastError();
+  }
   const size_t blocks = (size_t)rows * keep_blocks(cols);
   hipLaunchKernelGGL(pack8_kernel<T>, dim3(grid_of((blocks + 7) / 8)), dim3(NT), 0, s, (const T*)x, ldx, codes, scales, rows, cols);
   return hipGetLastError();
 }
 template <typename T> hipError_t run_unpack8(const uint8_t* codes, const uint8_t* scales, void* x, size_t ldx, int rows, int cols, hipStream_t s) {
+  if (chunked<T>(ldx, cols)) {
+    const Chunks k = chunks_of<T>(rows, cols);
+    const size_t groups = (k.total + NT * U - 1) / (NT * U);
+    hipLaunchKernelGGL((unpack8_vec_kernel<T, U>), dim3((unsigned)(groups > (1u << 20) ? 1u << 20 : groups)), dim3(NT), 0, s, codes, scales, (T*)x, ldx, k, rows, cols);
+    return hipGetLastError();
+  }
   hipLaunchKernelGGL(unpack8_kernel<T>, dim3(grid_of(((size_t)rows * cols + NT - 1) / NT)), dim3(NT), 0, s, codes, scales, (T*)x, ldx, rows, cols);
   return hipGetLastError();
 }
