@@ -195,48 +195,131 @@ __global__ __launch_bounds__(NT) void norm_bwd8_kernel(const T* dn, const uint8_
   }
 }
 
-// one value of the output per lane, its block (SwiGLU: the gate's and the up projection's) per half wave
-template <typename T, bool SWIGLU>
+// ---- the MLP activation -----------------------------------------------------------------------------------
+// The functions of common.h cost some 50 instructions a value (a division, expf, erff), more than the time of its bytes allows in bf16, where results keep
+// 8 bits of them.  There: exp2 and the reciprocal of the hardware (relative error of a few 2^-23), and for GELU the normal
+// distribution from Abramowitz and Stegun 7.1.26, erfc(u) = (a1 t + ... + a5 t^5) exp(-u^2) with t = 1 / (1 + p u), u >= 0, off by at most
+// 1.5e-7, whose exponential the gradient needs anyway.
+template <typename T> struct Math {
+  static __device__ __forceinline__ float sigmoid(float x) { return sigmoidf_(x); }
+  static __device__ __forceinline__ void normal(float x, float& cdf, float& density) {
+    cdf = 0.5f * (1.f + erff(x * 0.70710678118654752f));
+    density = 0.39894228040143268f * expf(-0.5f * x * x);
+  }
+};
+template <> struct Math<bf16_t> {
+  static __device__ __forceinline__ float sigmoid(float x) {
+    return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(x * -1.44269504088896341f));
+  }
+  static __device__ __forceinline__ void normal(float x, float& cdf, float& density) {
+    const float t = __builtin_amdgcn_rcpf(fmaf(fabsf(x), 0.3275911f * 0.70710678118654752f, 1.f));
+    const float e = __builtin_amdgcn_exp2f(x * x * -0.72134752044448170f);                 // exp(-x^2 / 2)
+    float s = fmaf(t, 1.061405429f, -1.453152027f);
+    s = fmaf(t, s, 1.421413741f);
+    s = fmaf(t, s, -0.284496736f);
+    s = fmaf(t, s, 0.254829592f);
+    const float tail = 0.5f * t * s * e;
+    cdf = x < 0.f ? tail : 1.f - tail;
+    density = 0.39894228040143268f * e;
+  }
+};
+template <typename T, bool SWIGLU> __device__ __forceinline__ float activation(float x, float up) {
+  if (SWIGLU) return x * Math<T>::sigmoid(x) * up;
+  float cdf, density;
+  Math<T>::normal(x, cdf, density);
+  return x * cdf;
+}
+
+template <typename T, bool SWIGLU, int U>
 __global__ __launch_bounds__(NT) void act_fwd_pack8_kernel(const T* __restrict__ gu, T* __restrict__ a, uint8_t* __restrict__ codes, uint8_t* __restrict__ scales,
-                                                           int rows, int f) {
-  const int nb = keep_blocks(f), l = threadIdx.x & 31, parts = SWIGLU ? 2 : 1;
-  const size_t total = (size_t)rows * nb, step = (size_t)gridDim.x * (NT / 32);
-  for (size_t i = blockIdx.x * (size_t)(NT / 32) + (threadIdx.x >> 5); i < total; i += step) {
-    const size_t row = i / nb;
-    const int b = (int)(i % nb), col = b * KEEP_BLOCK + l;
-    float v[2] = {0.f, 0.f};
+                                                           const Chunks k, int rows, int f) {
+  typedef Vec16<T> V;
+  typedef typename KeepChunk<T>::codes_t codes_t;
+  constexpr int P = SWIGLU ? 2 : 1;
+  const int nb = keep_blocks(f);
+  for (size_t base = blockIdx.x * (size_t)(NT * U); base < k.total; base += (size_t)gridDim.x * (NT * U)) {
+    const Walk<T> walk(base, k);
+    V v[U][P] = {};
+    At at[U];
 #pragma unroll
-    for (int p = 0; p < parts; ++p) {
-      const size_t at = (row * parts + p) * f + col;
-      if (col < f) v[p] = to_f32<T>(gu[at]);
-      const uint32_t byte = keep_scale_byte(half_wave_max(keep_magnitude(v[p])));
-      if (col < f) codes[at] = (uint8_t)keep_encode(v[p], keep_inverse(byte));
-      if (l == 0) scales[(row * parts + p) * nb + b] = (uint8_t)byte;
+    for (int u = 0; u < U; ++u) {
+      at[u] = walk.at(u * NT + threadIdx.x);
+      if (at[u].row < (size_t)rows && at[u].col < f)
+#pragma unroll
+        for (int p = 0; p < P; ++p) v[u][p] = *reinterpret_cast<const V*>(gu + (at[u].row * P + p) * f + at[u].col);
     }
-    if (col < f) a[row * f + col] = from_f32<T>(SWIGLU ? v[0] * sigmoidf_(v[0]) * v[1] : gelu(v[0]));
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+#pragma unroll
+      for (int p = 0; p < P; ++p) {
+        uint32_t byte;
+        const codes_t c = keep_chunk<T>(v[u][p], byte);
+        const size_t row = at[u].row * P + p;
+        if (at[u].row < (size_t)rows) {
+          if (at[u].col < f) *reinterpret_cast<codes_t*>(codes + row * f + at[u].col) = c;
+          if (at[u].col % KEEP_BLOCK == 0) scales[row * nb + at[u].col / KEEP_BLOCK] = (uint8_t)byte;
+        }
+      }
+      V o;
+#pragma unroll
+      for (int e = 0; e < V::N; ++e) o.set(e, activation<T, SWIGLU>(v[u][0].get(e), v[u][P - 1].get(e)));
+      if (at[u].row < (size_t)rows && at[u].col < f) *reinterpret_cast<V*>(a + at[u].row * f + at[u].col) = o;
+    }
   }
 }
 
-template <typename T, bool SWIGLU>
-__global__ __launch_bounds__(NT) void act_bwd8_kernel(const T* da, const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales, T* dgu, T* a, int rows, int f) {
-  const int nb = keep_blocks(f), parts = SWIGLU ? 2 : 1;
-  const size_t total = (size_t)rows * f, step = (size_t)gridDim.x * NT;
-  for (size_t i = blockIdx.x * (size_t)NT + threadIdx.x; i < total; i += step) {
-    const size_t row = i / f;
-    const int col = (int)(i % f);
-    float v[2] = {0.f, 0.f};
+// a and dgu may be da: a thread reads its chunk of da before it writes there
+template <typename T, bool SWIGLU, int U>
+__global__ __launch_bounds__(NT) void act_bwd8_kernel(const T* da, const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales, T* dgu, T* a, const Chunks k,
+                                                      int rows, int f) {
+  typedef Vec16<T> V;
+  typedef typename KeepChunk<T>::codes_t codes_t;
+  constexpr int P = SWIGLU ? 2 : 1;
+  const int nb = keep_blocks(f);
+  for (size_t base = blockIdx.x * (size_t)(NT * U); base < k.total; base += (size_t)gridDim.x * (NT * U)) {
+    const Walk<T> walk(base, k);
+    V d[U];
+    codes_t c[U][P];
+    uint32_t b[U][P];
+    At at[U];
 #pragma unroll
-    for (int p = 0; p < parts; ++p) v[p] = keep_decode(codes[(row * parts + p) * f + col], keep_scale(scales[(row * parts + p) * nb + col / KEEP_BLOCK]));
-    const float d = to_f32<T>(da[i]);
-    if (SWIGLU) {
-      float dg, du;
-      dswiglu(v[0], v[1], d, dg, du);
-      dgu[row * 2 * f + col] = from_f32<T>(dg);
-      dgu[row * 2 * f + f + col] = from_f32<T>(du);
-    } else {
-      dgu[i] = from_f32<T>(dgelu(v[0], d));
+    for (int u = 0; u < U; ++u) {
+      at[u] = walk.at(u * NT + threadIdx.x);
+      if (at[u].row < (size_t)rows && at[u].col < f) {
+        d[u] = *reinterpret_cast<const V*>(da + at[u].row * f + at[u].col);
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+          c[u][p] = *reinterpret_cast<const codes_t*>(codes + (at[u].row * P + p) * f + at[u].col);
+          b[u][p] = scales[(at[u].row * P + p) * nb + at[u].col / KEEP_BLOCK];
+        }
+      }
     }
-    if (a) a[i] = from_f32<T>(SWIGLU ? v[0] * sigmoidf_(v[0]) * v[1] : gelu(v[0]));
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (!(at[u].row < (size_t)rows && at[u].col < f)) continue;
+      float x[P][V::N];
+#pragma unroll
+      for (int p = 0; p < P; ++p) keep_values(c[u][p], keep_scale(b[u][p]), x[p]);
+      V o[P], act;
+#pragma unroll
+      for (int e = 0; e < V::N; ++e) {
+        const float v = x[0][e], g = d[u].get(e);
+        if constexpr (SWIGLU) {
+          const float s = Math<T>::sigmoid(v), silu = v * s;
+          o[0].set(e, g * x[1][e] * s * fmaf(v, 1.f - s, 1.f));
+          o[1].set(e, g * silu);
+          act.set(e, silu * x[1][e]);
+        } else {
+          float cdf, density;
+          Math<T>::normal(v, cdf, density);
+          o[0].set(e, g * fmaf(v, density, cdf));
+          act.set(e, v * cdf);
+        }
+      }
+#pragma unroll
+      for (int p = 0; p < P; ++p) *reinterpret_cast<V*>(dgu + (at[u].row * P + p) * f + at[u].col) = o[p];
+      if (a) *reinterpret_cast<V*>(a + at[u].row * f + at[u].col) = act;
+    }
   }
 }
 
@@ -244,13 +327,16 @@ int grid_of(size_t workgroups) { return (int)(workgroups > 8192 ? 8192 : workgro
 
 // rows of x and of the codes start on whole chunks
 template <typename T> bool chunked(size_t ldx, int cols) { return ldx % Vec16<T>::N == 0 && cols % Vec16<T>::N == 0; }
-constexpr int U = 4;
+constexpr int U = 4, UA = 2;
+unsigned groups_of(const Chunks& k, int u) {
+  const size_t groups = (k.total + (size_t)NT * u - 1) / ((size_t)NT * u);
+  return (unsigned)(groups > (1u << 20) ? 1u << 20 : groups);
+}
 
 template <typename T> hipError_t run_pack8(const void* x, size_t ldx, uint8_t* codes, uint8_t* scales, int rows, int cols, hipStream_t s) {
   if (chunked<T>(ldx, cols)) {
     const Chunks k = chunks_of<T>(rows, cols);
-    const size_t groups = (k.total + NT * U - 1) / (NT * U);
-    hipLaunchKernelGGL((pack8_vec_kernel<T, U>), dim3((unsigned)(groups > (1u << 20) ? 1u << 20 : groups)), dim3(NT), 0, s, (const T*)x, ldx, codes, scales, k, rows, cols);
+    hipLaunchKernelGGL((pack8_vec_kernel<T, U>), dim3(groups_of(k, U)), dim3(NT), 0, s, (const T*)x, ldx, codes, scales, k, rows, cols);
     return hipGetLastError();
   }
   const size_t blocks = (size_t)rows * keep_blocks(cols);
@@ -260,8 +346,7 @@ template <typename T> hipError_t run_pack8(const void* x, size_t ldx, uint8_t* c
 template <typename T> hipError_t run_unpack8(const uint8_t* codes, const uint8_t* scales, void* x, size_t ldx, int rows, int cols, hipStream_t s) {
   if (chunked<T>(ldx, cols)) {
     const Chunks k = chunks_of<T>(rows, cols);
-    const size_t groups = (k.total + NT * U - 1) / (NT * U);
-    hipLaunchKernelGGL((unpack8_vec_kernel<T, U>), dim3((unsigned)(groups > (1u << 20) ? 1u << 20 : groups)), dim3(NT), 0, s, codes, scales, (T*)x, ldx, k, rows, cols);
+    hipLaunchKernelGGL((unpack8_vec_kernel<T, U>), dim3(groups_of(k, U)), dim3(NT), 0, s, codes, scales, (T*)x, ldx, k, rows, cols);
     return hipGetLastError();
   }
   hipLaunchKernelGGL(unpack8_kernel<T>, dim3(grid_of(((size_t)rows * cols + NT - 1) / NT)), dim3(NT), 0, s, codes, scales, (T*)x, ldx, rows, cols);
@@ -282,12 +367,14 @@ hipError_t run_norm_bwd8(const void* dn, const uint8_t* codes, const uint8_t* sc
 }
 template <typename T, bool SWIGLU>
 hipError_t run_act_fwd_pack8(const void* gu, void* a, uint8_t* codes, uint8_t* scales, int rows, int f, hipStream_t s) {
-  hipLaunchKernelGGL((act_fwd_pack8_kernel<T, SWIGLU>), dim3(grid_of(((size_t)rows * keep_blocks(f) + 7) / 8)), dim3(NT), 0, s, (const T*)gu, (T*)a, codes, scales, rows, f);
+  const Chunks k = chunks_of<T>(rows, f);
+  hipLaunchKernelGGL((act_fwd_pack8_kernel<T, SWIGLU, UA>), dim3(groups_of(k, UA)), dim3(NT), 0, s, (const T*)gu, (T*)a, codes, scales, k, rows, f);
   return hipGetLastError();
 }
 template <typename T, bool SWIGLU>
 hipError_t run_act_bwd8(const void* da, const uint8_t* codes, const uint8_t* scales, void* dgu, void* a, int rows, int f, hipStream_t s) {
-  hipLaunchKernelGGL((act_bwd8_kernel<T, SWIGLU>), dim3(grid_of(((size_t)rows * f + NT - 1) / NT)), dim3(NT), 0, s, (const T*)da, codes, scales, (T*)dgu, (T*)a, rows, f);
+  const Chunks k = chunks_of<T>(rows, f);
+  hipLaunchKernelGGL((act_bwd8_kernel<T, SWIGLU, UA>), dim3(groups_of(k, UA)), dim3(NT), 0, s, (const T*)da, codes, scales, (T*)dgu, (T*)a, k, rows, f);
   return hipGetLastError();
 }
 

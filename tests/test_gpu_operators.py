@@ -141,13 +141,15 @@ def test_pack8_offsets_beyond_32_bits():
 # ------------------------------------------------------------------ the MLP activation
 def act_bounds(family, gu, da, dtype):
     """Bounds on a, dgu.  SwiGLU: exp's argument is rounded (|g| EPS of the sigmoid) and some 12 roundings follow; 1 - sigmoid is off by EPS outright.
-    GELU: the normal distribution's value is good to 8 EPS outright (bf16: 1.5e-7 of a fitted formula besides)."""
+    GELU: the normal distribution's value is good to 8 EPS outright (bf16: 1.5e-7 of a fitted formula besides).
+    The hardware's reciprocal (bf16) gives 0 where its result is below the least normal number: a sigmoid is then off by up to 2^-126 outright,
+    which reaches a times |g u|, the gate's gradient times |da u| (1 + |g|) and the up projection's times |da g|."""
     if family == LLAMA:
         g, u = np.split(gu, 2, axis=1)
-        n = 16 * EPS * (2 + np.abs(g))
         s = 1 / (1 + np.exp(-g))
-        a = n * np.abs(g * s * u)
-        d = np.concatenate([n * np.abs(da * u) * s * (1 + np.abs(g)), n * np.abs(da * g) * s], 1) if da is not None else None
+        n = 16 * EPS * (2 + np.abs(g)) * s + (2.0 ** -126 if dtype == BF16 else 0)
+        a = n * np.abs(g * u)
+        d = np.concatenate([n * np.abs(da * u) * (1 + np.abs(g)), n * np.abs(da * g)], 1) if da is not None else None
     else:
         n = (8 * EPS + (2e-7 if dtype == BF16 else 0)) * np.ones_like(gu)
         a = np.abs(gu) * n + 8 * EPS * np.abs(P.activation(GPT, gu))
