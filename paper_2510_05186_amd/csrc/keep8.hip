@@ -2,6 +2,8 @@
 // input that way and take their gradients from it.
 #include "keep8.h"
 
+#include <type_traits>
+
 namespace {
 
 constexpr int NT = 256;
@@ -118,79 +120,198 @@ __global__ __launch_bounds__(NT) void unpack8_vec_kernel(const uint8_t* __restri
   }
 }
 
-__device__ __forceinline__ float block_sum(float v, float* red /* [NT / 64] */) {
+// ---- norms ------------------------------------------------------------------------------------------------
+// A row belongs to W waves, R rows to a workgroup; a lane holds C chunks of its row, W * 64 chunks apart.  The W waves of a row add up their sums
+// through LDS (`red`, of its own for every use).
+template <int W> __device__ __forceinline__ float row_sum(float v, float* red /* [R * W] */, int slot, int wave) {
   v = wave_sum(v);
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
+  if (W == 1) return v;
+  if ((threadIdx.x & 63) == 0) red[slot * W + wave] = v;
   __syncthreads();
   float t = 0.f;
 #pragma unroll
-  for (int w = 0; w < NT / 64; ++w) t += red[w];
+  for (int w = 0; w < W; ++w) t += red[slot * W + w];
   return t;
 }
 
-// one row per workgroup
-template <typename T, bool LN>
-__global__ __launch_bounds__(NT) void norm_fwd_pack8_kernel(const T* __restrict__ x, const T* __restrict__ gamma, const T* __restrict__ beta, T* __restrict__ out,
-                                                            float* __restrict__ stats, uint8_t* __restrict__ codes, uint8_t* __restrict__ scales, int h, float eps) {
-  __shared__ float red[NT / 64];
-  const size_t row = blockIdx.x;
-  const int nb = keep_blocks(h), l = threadIdx.x & 31;
-  const T* xr = x + row * h;
+template <typename T, bool LN, int W, int C, int R>
+__global__ __launch_bounds__(W * R * 64) void norm_fwd_pack8_kernel(const T* __restrict__ x, const T* __restrict__ gamma, const T* __restrict__ beta, T* __restrict__ out,
+                                                                    float* __restrict__ stats, uint8_t* __restrict__ codes, uint8_t* __restrict__ scales, int rows, int h,
+                                                                    float eps) {
+  typedef Vec16<T> V;
+  typedef typename KeepChunk<T>::codes_t codes_t;
+  __shared__ float red[2][R * W];
+  const int slot = threadIdx.x / (W * 64), l = threadIdx.x % (W * 64), wave = l >> 6, nb = keep_blocks(h);
+  const size_t row = (size_t)blockIdx.x * R + slot;
+  const bool on = row < (size_t)rows;
+  V v[C] = {};
+#pragma unroll
+  for (int c = 0; c < C; ++c) {
+    const int col = (l + c * W * 64) * V::N;
+    if (on && col < h) v[c] = *reinterpret_cast<const V*>(x + row * h + col);
+  }
   float mean = 0.f, s = 0.f;
   if (LN) {
-    for (int c = threadIdx.x; c < h; c += NT) s += to_f32<T>(xr[c]);
-    mean = block_sum(s, red) / h;
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+#pragma unroll
+      for (int e = 0; e < V::N; ++e) s += v[c].get(e);
+    mean = row_sum<W>(s, red[0], slot, wave) / h;
+    s = 0.f;
   }
-  s = 0.f;
-  for (int c = threadIdx.x; c < h; c += NT) { const float d = to_f32<T>(xr[c]) - mean; s += d * d; }
-  const float r = rsqrtf(block_sum(s, red) / h + eps);
-  if (threadIdx.x == 0) {
+#pragma unroll
+  for (int c = 0; c < C; ++c) {
+    if ((l + c * W * 64) * V::N < h)
+#pragma unroll
+      for (int e = 0; e < V::N; ++e) { const float d = v[c].get(e) - mean; s += d * d; }
+  }
+  const float r = rsqrtf(row_sum<W>(s, red[1], slot, wave) / h + eps);
+  if (on && l == 0) {
     if (LN) { stats[2 * row] = mean; stats[2 * row + 1] = r; } else stats[row] = r;
   }
-  for (int b0 = 0; b0 < nb; b0 += NT / 32) {
-    const int b = b0 + (threadIdx.x >> 5), col = b * KEEP_BLOCK + l;
-    const float v = col < h ? to_f32<T>(xr[col]) : 0.f;
-    const uint32_t byte = keep_scale_byte(half_wave_max(keep_magnitude(v)));
-    if (col < h) {
-      codes[row * h + col] = (uint8_t)keep_encode(v, keep_inverse(byte));
-      float o = (v - mean) * r * to_f32<T>(gamma[col]);
-      if (LN) o += to_f32<T>(beta[col]);
-      out[row * h + col] = from_f32<T>(o);
+#pragma unroll
+  for (int c = 0; c < C; ++c) {
+    const int col = (l + c * W * 64) * V::N;
+    uint32_t byte;
+    const codes_t code = keep_chunk<T>(v[c], byte);
+    if (on && col < h) {
+      *reinterpret_cast<codes_t*>(codes + row * h + col) = code;
+      if (col % KEEP_BLOCK == 0) scales[row * nb + col / KEEP_BLOCK] = (uint8_t)byte;
+      const V g = *reinterpret_cast<const V*>(gamma + col);
+      V o, b;
+      if (LN) b = *reinterpret_cast<const V*>(beta + col);
+#pragma unroll
+      for (int e = 0; e < V::N; ++e) {
+        float f = (v[c].get(e) - mean) * r * g.get(e);
+        if (LN) f += b.get(e);
+        o.set(e, f);
+      }
+      *reinterpret_cast<V*>(out + row * h + col) = o;
     }
-    if (b < nb && l == 0) scales[row * nb + b] = (uint8_t)byte;
   }
 }
 
-// workgroup b takes rows b, b + gridDim.x, ...; its sums of the gains' and biases' gradients stand in its rows of `partial`
-template <typename T, bool LN>
-__global__ __launch_bounds__(NT) void norm_bwd8_kernel(const T* dn, const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales,
-                                                       const float* __restrict__ stats, const T* __restrict__ gamma, const T* __restrict__ beta, const T* dres, T* dx,
-                                                       T* __restrict__ out, float* __restrict__ partial, int rows, int h) {
-  __shared__ float red[NT / 64];
-  const int nb = keep_blocks(h);
-  float* pg = partial + (size_t)blockIdx.x * h;
-  float* pb = partial + ((size_t)gridDim.x + blockIdx.x) * h;
-  for (int c = threadIdx.x; c < h; c += NT) { pg[c] = 0.f; if (LN) pb[c] = 0.f; }
-  for (size_t row = blockIdx.x; row < (size_t)rows; row += gridDim.x) {
-    const float mean = LN ? stats[2 * row] : 0.f, r = LN ? stats[2 * row + 1] : stats[row];
-    const uint8_t* cr = codes + row * h;
-    const uint8_t* sr = scales + row * nb;
-    float sg = 0.f, sgx = 0.f;
-    for (int c = threadIdx.x; c < h; c += NT) {
-      const float xh = (keep_decode(cr[c], keep_scale(sr[c / KEEP_BLOCK])) - mean) * r, d = to_f32<T>(dn[row * h + c]), g = d * to_f32<T>(gamma[c]);
-      sg += g;
-      sgx += g * xh;
-      pg[c] += d * xh;
-      if (LN) pb[c] += d;
+// Workgroup b takes the rows b R .. b R + R - 1, (b + gridDim.x) R .., the loads of the next ones in flight while the present ones are reduced and written.
+// Its sums of the gains' and biases' gradients stay in registers and end in its rows of `partial`, those of its R rows added in order.  dx may be dn or
+// dres: rows in flight are other rows, and a lane has read its chunks of the present one.
+template <typename T, bool LN, int W, int C, int R>
+__global__ __launch_bounds__(W * R * 64) void norm_bwd8_kernel(const T* dn, const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales,
+                                                               const float* __restrict__ stats, const T* __restrict__ gamma, const T* __restrict__ beta, const T* dres, T* dx,
+                                                               T* __restrict__ out, float* __restrict__ partial, int rows, int h) {
+  typedef Vec16<T> V;
+  typedef typename KeepChunk<T>::codes_t codes_t;
+  __shared__ float red[2][2][R * W];
+  __shared__ float sums[R > 1 ? W * 64 * C * V::N : 1];
+  const int slot = threadIdx.x / (W * 64), l = threadIdx.x % (W * 64), wave = l >> 6, nb = keep_blocks(h);
+  float pg[C][V::N] = {}, pb[LN ? C : 1][V::N] = {};
+  V gv[C];
+#pragma unroll
+  for (int c = 0; c < C; ++c) {
+    const int col = (l + c * W * 64) * V::N;
+    if (col < h) gv[c] = *reinterpret_cast<const V*>(gamma + col);
+  }
+  struct Row { V d[C], res[C]; codes_t q[C]; uint32_t b[C]; float mean, r; } buf[2];
+  auto load = [&](Row& k, size_t row) {
+    if (row >= (size_t)rows) return;
+    k.mean = LN ? stats[2 * row] : 0.f;
+    k.r = LN ? stats[2 * row + 1] : stats[row];
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      const int col = (l + c * W * 64) * V::N;
+      if (col < h) {
+        k.d[c] = *reinterpret_cast<const V*>(dn + row * h + col);
+        k.q[c] = *reinterpret_cast<const codes_t*>(codes + row * h + col);
+        k.b[c] = scales[row * nb + col / KEEP_BLOCK];
+        if (dres) k.res[c] = *reinterpret_cast<const V*>(dres + row * h + col);
+      }
     }
-    const float mgx = block_sum(sgx, red) / h, mg = LN ? block_sum(sg, red) / h : 0.f;
-    for (int c = threadIdx.x; c < h; c += NT) {
-      const float xh = (keep_decode(cr[c], keep_scale(sr[c / KEEP_BLOCK])) - mean) * r, gm = to_f32<T>(gamma[c]);
-      float v = r * (to_f32<T>(dn[row * h + c]) * gm - mg - xh * mgx);
-      if (dres) v += to_f32<T>(dres[row * h + c]);
-      dx[row * h + c] = from_f32<T>(v);
-      if (out) out[row * h + c] = from_f32<T>(LN ? xh * gm + to_f32<T>(beta[c]) : xh * gm);
+  };
+  auto process = [&](const Row& k, size_t row, int turn) {
+    const bool on = row < (size_t)rows;
+    float xh[C][V::N], sg = 0.f, sgx = 0.f;
+    if (on) {
+#pragma unroll
+      for (int c = 0; c < C; ++c) {
+        if ((l + c * W * 64) * V::N < h) {
+          keep_values(k.q[c], keep_scale(k.b[c]), xh[c]);
+#pragma unroll
+          for (int e = 0; e < V::N; ++e) {
+            xh[c][e] = (xh[c][e] - k.mean) * k.r;
+            const float d = k.d[c].get(e), g = d * gv[c].get(e);
+            if (LN) sg += g;
+            sgx += g * xh[c][e];
+            pg[c][e] += d * xh[c][e];
+            if (LN) pb[c][e] += d;
+          }
+        }
+      }
+    }
+    // both sums behind one barrier; the next row's take the other half of red
+    sgx = wave_sum(sgx);
+    if (LN) sg = wave_sum(sg);
+    if (W > 1) {
+      if ((threadIdx.x & 63) == 0) {
+        red[turn][0][slot * W + wave] = sgx;
+        if (LN) red[turn][1][slot * W + wave] = sg;
+      }
+      __syncthreads();
+      sgx = sg = 0.f;
+#pragma unroll
+      for (int w = 0; w < W; ++w) {
+        sgx += red[turn][0][slot * W + w];
+        if (LN) sg += red[turn][1][slot * W + w];
+      }
+    }
+    const float mgx = sgx / h, mg = LN ? sg / h : 0.f;
+    if (!on) return;
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      const int col = (l + c * W * 64) * V::N;
+      if (col < h) {
+        V o, n, b;
+        if (LN && out) b = *reinterpret_cast<const V*>(beta + col);
+#pragma unroll
+        for (int e = 0; e < V::N; ++e) {
+          float v = k.r * (k.d[c].get(e) * gv[c].get(e) - mg - xh[c][e] * mgx);
+          if (dres) v += k.res[c].get(e);
+          o.set(e, v);
+          float y = xh[c][e] * gv[c].get(e);
+          if (LN && out) y += b.get(e);
+          n.set(e, y);
+        }
+        *reinterpret_cast<V*>(dx + row * h + col) = o;
+        if (out) *reinterpret_cast<V*>(out + row * h + col) = n;
+      }
+    }
+  };
+  const size_t step = (size_t)gridDim.x * R;
+  size_t row = (size_t)blockIdx.x * R + slot;
+  load(buf[0], row);
+  for (size_t first = (size_t)blockIdx.x * R; first < (size_t)rows; first += 2 * step, row += 2 * step) {
+    load(buf[1], row + step);
+    process(buf[0], row, 0);
+    load(buf[0], row + 2 * step);
+    process(buf[1], row + step, 1);
+  }
+#pragma unroll
+  for (int part = 0; part < (LN ? 2 : 1); ++part) {
+    float (&p)[C][V::N] = part ? reinterpret_cast<float (&)[C][V::N]>(pb) : pg;
+    float* to = partial + ((size_t)part * gridDim.x + blockIdx.x) * h;
+    for (int i = 0; i < R; ++i) {
+      if (R > 1) __syncthreads();
+      if (slot != i) continue;
+#pragma unroll
+      for (int c = 0; c < C; ++c) {
+        const int at = (l + c * W * 64) * V::N;
+        if (at < h)
+#pragma unroll
+          for (int e = 0; e < V::N; ++e) {
+            float t = p[c][e];
+            if (R > 1 && i > 0) t += sums[at + e];
+            if (R > 1 && i < R - 1) sums[at + e] = t;
+            else to[at + e] = t;
+          }
+      }
     }
   }
 }
@@ -327,7 +448,10 @@ int grid_of(size_t workgroups) { return (int)(workgroups > 8192 ? 8192 : workgro
 
 // rows of x and of the codes start on whole chunks
 template <typename T> bool chunked(size_t ldx, int cols) { return ldx % Vec16<T>::N == 0 && cols % Vec16<T>::N == 0; }
-constexpr int U = 4, UA = 2;
+// Chunks in flight per thread.  16384 x 15360 bf16, pack and unpack: 285 us with 1, 269 with 2, 277 with 4, 296 with 8; the activation holds two or three
+// operands of each: SwiGLU 4096 x 11008, forward and backward, 155 us with 1 or 2, 164 with 4; GELU 4999 x 4088 53 us with 1, 58 with 2.
+constexpr int U = 2, UA = 1;
+constexpr int NORM_GROUPS = 256;                                       // workgroups of norm_bwd8_kernel, one row of sums each
 unsigned groups_of(const Chunks& k, int u) {
   const size_t groups = (k.total + (size_t)NT * u - 1) / ((size_t)NT * u);
   return (unsigned)(groups > (1u << 20) ? 1u << 20 : groups);
@@ -352,18 +476,40 @@ template <typename T> hipError_t run_unpack8(const uint8_t* codes, const uint8_t
   hipLaunchKernelGGL(unpack8_kernel<T>, dim3(grid_of(((size_t)rows * cols + NT - 1) / NT)), dim3(NT), 0, s, codes, scales, (T*)x, ldx, rows, cols);
   return hipGetLastError();
 }
+// f(W, C, R) for rows of h: the fewest waves that hold a row with at most two chunks a lane
+template <typename T, typename F> auto norm_division(int h, F f) {
+  const int chunks = h / Vec16<T>::N;
+#define NORM_DIVISION(W, C, R) f(std::integral_constant<int, W>(), std::integral_constant<int, C>(), std::integral_constant<int, R>())
+  if (chunks <= 64) return NORM_DIVISION(1, 1, 8);
+  if (chunks <= 128) return NORM_DIVISION(1, 2, 8);
+  if (chunks <= 256) return NORM_DIVISION(2, 2, 4);
+  if (chunks <= 512) return NORM_DIVISION(4, 2, 2);
+  if (chunks <= 1024) return NORM_DIVISION(8, 2, 1);
+  return NORM_DIVISION(16, 2, 1);                                      // fp32 rows of more than 4096
+#undef NORM_DIVISION
+}
+
 template <typename T, bool LN>
 hipError_t run_norm_fwd_pack8(const void* x, const void* gamma, const void* beta, void* out, float* stats, uint8_t* codes, uint8_t* scales, int rows, int h, float eps,
                               hipStream_t s) {
-  hipLaunchKernelGGL((norm_fwd_pack8_kernel<T, LN>), dim3(rows), dim3(NT), 0, s, (const T*)x, (const T*)gamma, (const T*)beta, (T*)out, stats, codes, scales, h, eps);
+  norm_division<T>(h, [&](auto w, auto c, auto r) {
+    hipLaunchKernelGGL((norm_fwd_pack8_kernel<T, LN, w, c, r>), dim3((rows + r - 1) / r), dim3(w * r * 64), 0, s, (const T*)x, (const T*)gamma, (const T*)beta, (T*)out, stats,
+                       codes, scales, rows, h, eps);
+  });
   return hipGetLastError();
 }
 template <typename T, bool LN>
 hipError_t run_norm_bwd8(const void* dn, const uint8_t* codes, const uint8_t* scales, const float* stats, const void* gamma, const void* beta, const void* dres, void* dx,
-                         void* out, float* partial, int rows, int h, hipStream_t s) {
-  hipLaunchKernelGGL((norm_bwd8_kernel<T, LN>), dim3(norm_bwd_partial_rows(rows)), dim3(NT), 0, s, (const T*)dn, codes, scales, stats, (const T*)gamma, (const T*)beta,
-                     (const T*)dres, (T*)dx, (T*)out, partial, rows, h);
-  return hipGetLastError();
+                         void* out, float* partial, float* dgamma, float* dbeta, int rows, int h, hipStream_t s) {
+  int nb = 0;
+  norm_division<T>(h, [&](auto w, auto c, auto r) {
+    nb = min((rows + r - 1) / r, NORM_GROUPS);
+    hipLaunchKernelGGL((norm_bwd8_kernel<T, LN, w, c, r>), dim3(nb), dim3(w * r * 64), 0, s, (const T*)dn, codes, scales, stats, (const T*)gamma, (const T*)beta, (const T*)dres,
+                       (T*)dx, (T*)out, partial, rows, h);
+  });
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  return launch_norm_reduce(LN ? FAM_GPT : FAM_LLAMA, NormReduce{{partial}, {dgamma}, {dbeta}, 1}, nb, h, 0, s);
 }
 template <typename T, bool SWIGLU>
 hipError_t run_act_fwd_pack8(const void* gu, void* a, uint8_t* codes, uint8_t* scales, int rows, int f, hipStream_t s) {
@@ -399,9 +545,7 @@ hipError_t launch_norm_fwd_pack8(int dtype, int family, const void* x, const voi
 }
 hipError_t launch_norm_bwd8(int dtype, int family, const void* dn, const uint8_t* codes, const uint8_t* scales, const float* stats, const void* gamma, const void* beta,
                             const void* dres, void* dx, void* out, float* partial, float* dgamma, float* dbeta, int rows, int h, hipStream_t s) {
-  const hipError_t e = KEEP_BY_BOTH(run_norm_bwd8, family == FAM_GPT, dn, codes, scales, stats, gamma, beta, dres, dx, out, partial, rows, h, s);
-  if (e != hipSuccess) return e;
-  return launch_norm_reduce(family, NormReduce{{partial}, {dgamma}, {dbeta}, 1}, rows, h, 0, s);
+  return KEEP_BY_BOTH(run_norm_bwd8, family == FAM_GPT, dn, codes, scales, stats, gamma, beta, dres, dx, out, partial, dgamma, dbeta, rows, h, s);
 }
 hipError_t launch_act_fwd_pack8(int dtype, int family, const void* gu, void* a, uint8_t* codes, uint8_t* scales, int rows, int f, hipStream_t s) {
   return KEEP_BY_BOTH(run_act_fwd_pack8, family == FAM_LLAMA, gu, a, codes, scales, rows, f, s);
