@@ -173,6 +173,8 @@ hipError_t launch_attn_bwd_inplace(int dtype, void* qkv, const void* o, const vo
 uint64_t attn_bwd_ws_floats(int seq, int batch, int n_q, int n_kv, int d);
 // heads of 64: how many groups of waves share the keys of a dK / dV workgroup
 int attn_d64_key_groups(int seq, int batch, int n_q, int n_kv);
+// dst[i][c] += the sum over b < rows of partial[(i rows + b) cols + c], i = 0, and 1 where dst[1] is given
+hipError_t launch_add_columns(const float* partial, float* dst0, float* dst1, int rows, int cols, hipStream_t s);
 // values kept in 8 bits (keep8.h): codes [rows][cols], scales [rows][ceil(cols / 32)]
 hipError_t launch_pack8(int dtype, const void* x, size_t ldx, uint8_t* codes, uint8_t* scales, int rows, int cols, hipStream_t s);
 hipError_t launch_unpack8(int dtype, const uint8_t* codes, const uint8_t* scales, void* x, size_t ldx, int rows, int cols, hipStream_t s);

@@ -316,6 +316,31 @@ __global__ __launch_bounds__(W * R * 64) void norm_bwd8_kernel(const T* dn, cons
   }
 }
 
+// Workgroups' sums, one row each, into the accumulators: 32 columns x 32 groups of rows, eight loads of a lane in flight, a fixed order (the
+// lane's rows one after the other, then the 32 groups).  Bound by the latency of its few loads and of the launch.
+__global__ __launch_bounds__(1024) void add_columns_kernel(const float* __restrict__ partial, float* dst0, float* dst1, int rows, int cols) {
+  __shared__ float red[32][33];
+  const int cx = threadIdx.x & 31, g = threadIdx.x >> 5, col = blockIdx.x * 32 + cx;
+  const float* p = partial + (size_t)blockIdx.y * rows * cols + col;
+  float s = 0.f;
+  if (col < cols)
+    for (int b0 = g; b0 < rows; b0 += 256) {
+      float v[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = b0 + 32 * i < rows ? p[(size_t)(b0 + 32 * i) * cols] : 0.f;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) s += v[i];
+    }
+  red[g][cx] = s;
+  __syncthreads();
+  // a wave adds up two columns, 32 lanes each
+  float t = red[threadIdx.x & 31][threadIdx.x >> 5];
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) t += __shfl_xor(t, o, 64);
+  const int out = blockIdx.x * 32 + (threadIdx.x >> 5);
+  if ((threadIdx.x & 31) == 0 && out < cols) (blockIdx.y ? dst1 : dst0)[out] += t;
+}
+
 // ---- the MLP activation -----------------------------------------------------------------------------------
 // The functions of common.h cost some 50 instructions a value (a division, expf, erff), more than the time of its bytes allows in bf16, where results keep
 // 8 bits of them.  There: exp2 and the reciprocal of the hardware (relative error of a few 2^-23), and for GELU the normal
@@ -509,7 +534,7 @@ hipError_t run_norm_bwd8(const void* dn, const uint8_t* codes, const uint8_t* sc
   });
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  return launch_norm_reduce(LN ? FAM_GPT : FAM_LLAMA, NormReduce{{partial}, {dgamma}, {dbeta}, 1}, nb, h, 0, s);
+  return launch_add_columns(partial, dgamma, LN ? dbeta : nullptr, nb, h, s);
 }
 template <typename T, bool SWIGLU>
 hipError_t run_act_fwd_pack8(const void* gu, void* a, uint8_t* codes, uint8_t* scales, int rows, int f, hipStream_t s) {
@@ -525,6 +550,11 @@ hipError_t run_act_bwd8(const void* da, const uint8_t* codes, const uint8_t* sca
 }
 
 }  // namespace
+
+hipError_t launch_add_columns(const float* partial, float* dst0, float* dst1, int rows, int cols, hipStream_t s) {
+  hipLaunchKernelGGL(add_columns_kernel, dim3((cols + 31) / 32, dst1 ? 2 : 1), dim3(1024), 0, s, partial, dst0, dst1, rows, cols);
+  return hipGetLastError();
+}
 
 // f<T, true / false>(...) by type and family
 #define KEEP_BY_TYPE(f, ...) (dtype == DT_BF16 ? f<bf16_t>(__VA_ARGS__) : f<float>(__VA_ARGS__))
