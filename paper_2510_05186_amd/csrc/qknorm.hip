@@ -1,179 +1,312 @@
 // Norms of queries and keys with the position rotation, in one pass over packed qkv rows: every q and k head x becomes
 // R(position) (x * r * gamma), r = 1 / sqrt(mean(x^2) + eps), and its gradient goes back the same way:
 // dn = R^T dy, g = dn * gamma, dx = r (g - xh mean(g xh)) with xh = x r, dgamma = sum of dn * xh over rows and heads.
+//
+// Bound by memory.  A head belongs to G lanes, each with the same chunk of both halves, so that the rotation's pairs are a lane's own and a
+// head's sum is a few lane swaps.  Heads are numbered through all rows, a workgroup takes 256 / G of them at a time whatever the
+// number of heads; cos and sin (fp32, 512 bytes a row at d = 128) come out of the caches again for every head.
 #include "keep8.h"
+
+#include <type_traits>
 
 namespace {
 
 constexpr int NT = 256;
+constexpr int FWD_GROUPS = 4096, BWD_GROUPS = 1024;
 
-__device__ __forceinline__ uint32_t half_wave_max(uint32_t v) {
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) v = max(v, (uint32_t)__shfl_xor((int)v, o, 64));
+template <int G> __device__ __forceinline__ float group_sum(float v) {
+  v += __uint_as_float(lane_swap<0xB1>(__float_as_uint(v)));          // lane ^ 1
+  v += __uint_as_float(lane_swap<0x4E>(__float_as_uint(v)));          // lane ^ 2
+  if (G >= 8) v += __uint_as_float(lane_swap<0x141>(__float_as_uint(v)));    // 7 - lane of eight
+  if (G >= 16) v += __uint_as_float(lane_swap<0x140>(__float_as_uint(v)));   // 15 - lane of sixteen
+  if (G >= 32) v += __shfl_xor(v, 16, 64);
   return v;
 }
+
+// item = row * heads + head
+struct Items {
+  size_t total;
+  unsigned heads, n_q, n_rot, seq;
+};
+struct Head {
+  size_t row;
+  unsigned head;
+  bool on;
+};
+// item base + i; base is the workgroup's
+struct Walk {
+  size_t row0, left;
+  unsigned h0, heads;
+  __device__ __forceinline__ Walk(size_t base, const Items& k) : left(k.total - base), heads(k.heads) {
+    row0 = k.total >> 32 ? base / k.heads : (size_t)((unsigned)base / k.heads);
+    h0 = (unsigned)(base - row0 * k.heads);
+  }
+  __device__ __forceinline__ Head at(unsigned i) const {
+    const unsigned n = h0 + i, r = n / heads;
+    return {row0 + r, n - r * heads, i < left};
+  }
+};
+__device__ __forceinline__ unsigned position(size_t row, unsigned seq) { return (unsigned)row % seq; }   // rows < 2^30
+
+// the chunk's cos and sin
+template <typename T> struct Angles {
+  float c[Vec16<T>::N], s[Vec16<T>::N];
+  __device__ __forceinline__ void load(const float2* __restrict__ table) {
+#pragma unroll
+    for (int e = 0; e < Vec16<T>::N; e += 2) {
+      const f32x4_t v = *reinterpret_cast<const f32x4_t*>(table + e);
+      c[e] = v[0]; s[e] = v[1]; c[e + 1] = v[2]; s[e + 1] = v[3];
+    }
+  }
+};
 
 struct QkNorm {
   const void* src; const uint8_t* codes_in; const uint8_t* scales_in;   // the projection's output, or its kept form
   void* dst; const void* gamma_q; const void* gamma_k; const float2* table; float* stats;
-  uint8_t* codes; uint8_t* scales;                                      // where src is kept, or null
-  int rows, seq, n_q, n_kv, d; float eps;
+  uint8_t* codes; uint8_t* scales;                                      // where src is kept (KEEP)
+  Items items;
+  int d; float eps;
 };
 
-// one head per wave: lane l holds elements l + 64 i, i < d / 64 (at most 4); its partner in the rotation is d / 2 away
-template <typename T, bool FROM8>
+template <typename T, int G, bool FROM8, bool KEEP>
 __global__ __launch_bounds__(NT) void qknorm_kernel(const QkNorm p) {
-  __shared__ float line[NT / 64][256];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, d = p.d, half = d / 2, heads = p.n_q + 2 * p.n_kv, n_rot = p.n_q + p.n_kv;
-  const size_t items = (size_t)p.rows * heads, w = (size_t)heads * d;
-  for (size_t i0 = (size_t)blockIdx.x * (NT / 64); i0 < items; i0 += (size_t)gridDim.x * (NT / 64)) {
-    const size_t i = i0 + wave;
-    const bool on = i < items;
-    const size_t row = on ? i / heads : 0;
-    const int head = on ? (int)(i % heads) : 0;
-    float ss = 0.f;
-    for (int c = lane; c < d; c += 64) {
-      const size_t at = row * w + (size_t)head * d + c;
-      const float v = FROM8 ? keep_decode(p.codes_in[at], keep_scale(p.scales_in[at / KEEP_BLOCK])) : to_f32<T>(((const T*)p.src)[at]);
-      if (!FROM8 && p.codes) {
-        const uint32_t b = keep_scale_byte(half_wave_max(keep_magnitude(v)));
-        if (on) p.codes[at] = (uint8_t)keep_encode(v, keep_inverse(b));
-        if (on && (lane & 31) == 0) p.scales[at / KEEP_BLOCK] = (uint8_t)b;
-      }
-      line[wave][c] = v;
-      ss += v * v;
+  typedef Vec16<T> V;
+  typedef typename KeepChunk<T>::codes_t codes_t;
+  constexpr int S = NT / G;
+  const int half = p.d / 2, col = (threadIdx.x % G) * V::N;
+  const unsigned slot = threadIdx.x / G, n_rot = p.items.n_rot;
+  const bool mine = col < half;                                        // d = 192: lanes of a head that hold nothing
+  V gain[2][2];                                                        // q, k; lower, upper half
+  if (mine)
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      gain[0][i] = *reinterpret_cast<const V*>((const T*)p.gamma_q + i * half + col);
+      gain[1][i] = *reinterpret_cast<const V*>((const T*)p.gamma_k + i * half + col);
     }
-    __syncthreads();
-    if (on && head < n_rot) {
-      float r;
-      if (FROM8) r = p.stats[row * n_rot + head];
-      else {
-        r = rsqrtf(wave_sum(ss) / d + p.eps);
-        if (lane == 0) p.stats[row * n_rot + head] = r;
+  for (size_t base = (size_t)blockIdx.x * S; base < p.items.total; base += (size_t)gridDim.x * S) {
+    const Head k = Walk(base, p.items).at(slot);
+    const bool on = k.on && mine, turn = k.head < n_rot;
+    const size_t at = (k.row * p.items.heads + k.head) * p.d + col;
+    V x[2] = {};
+    float v[2][V::N];
+    Angles<T> a;
+    float r = 0.f;
+    if (on) {
+      if (turn) a.load(p.table + (size_t)position(k.row, p.items.seq) * half + col);
+      if constexpr (FROM8) {
+        codes_t c[2];
+        uint32_t b[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          c[i] = *reinterpret_cast<const codes_t*>(p.codes_in + at + i * half);
+          b[i] = p.scales_in[(at + i * half) / KEEP_BLOCK];
+        }
+        if (turn) r = p.stats[k.row * n_rot + k.head];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          if (turn) keep_values(c[i], keep_scale(b[i]), v[i]);
+          else x[i] = keep_stored(c[i], keep_scale(b[i]), V());
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) x[i] = *reinterpret_cast<const V*>((const T*)p.src + at + i * half);
       }
-      const T* gamma = (const T*)(head < p.n_q ? p.gamma_q : p.gamma_k);
-      for (int k = lane; k < half; k += 64) {
-        const float2 cs = p.table[(row % p.seq) * half + k];
-        const float lo = line[wave][k] * r * to_f32<T>(gamma[k]), hi = line[wave][k + half] * r * to_f32<T>(gamma[k + half]);
-        T* o = (T*)p.dst + row * w + (size_t)head * d + k;
-        o[0] = from_f32<T>(lo * cs.x - hi * cs.y);
-        o[half] = from_f32<T>(hi * cs.x + lo * cs.y);
-      }
-    } else if (on && p.dst != p.src) {
-      for (int c = lane; c < d; c += 64) ((T*)p.dst)[row * w + (size_t)head * d + c] = from_f32<T>(line[wave][c]);
     }
-    __syncthreads();
+    if constexpr (!FROM8) {
+      float s = 0.f;
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int e = 0; e < V::N; ++e) {
+          v[i][e] = x[i].get(e);
+          s += v[i][e] * v[i][e];
+        }
+      r = rsqrtf(group_sum<G>(s) / p.d + p.eps);
+      if (on && turn && col == 0) p.stats[k.row * n_rot + k.head] = r;
+      if constexpr (KEEP) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          uint32_t byte;
+          const codes_t c = keep_chunk<T>(x[i], byte);
+          if (on) {
+            *reinterpret_cast<codes_t*>(p.codes + at + i * half) = c;
+            if (col % KEEP_BLOCK == 0) p.scales[(at + i * half) / KEEP_BLOCK] = (uint8_t)byte;
+          }
+        }
+      }
+    }
+    if (!on) continue;
+    T* out = (T*)p.dst + at;
+    if (turn) {
+      const bool is_k = k.head >= p.items.n_q;
+      V o[2];
+#pragma unroll
+      for (int e = 0; e < V::N; ++e) {
+        const float lo = v[0][e] * r * (is_k ? gain[1][0] : gain[0][0]).get(e), hi = v[1][e] * r * (is_k ? gain[1][1] : gain[0][1]).get(e);
+        o[0].set(e, lo * a.c[e] - hi * a.s[e]);
+        o[1].set(e, hi * a.c[e] + lo * a.s[e]);
+      }
+#pragma unroll
+      for (int i = 0; i < 2; ++i) *reinterpret_cast<V*>(out + i * half) = o[i];
+    } else if (FROM8 || p.dst != p.src) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) *reinterpret_cast<V*>(out + i * half) = x[i];
+    }
   }
 }
 
 struct QkNormBwd {
   const void* dy; const void* x; const uint8_t* codes; const uint8_t* scales; const float* stats;
   const void* gamma_q; const void* gamma_k; const float2* table; void* dx; float* partial;
-  int rows, seq, n_q, n_kv, d;
+  Items items;
+  int d;
 };
 
-// workgroup b takes rows b, b + gridDim.x, ...; its sums of the gains' gradients stand in partial[b] (q) and partial[gridDim.x + b] (k)
-template <typename T, bool FROM8>
+// dx may be dy or x: a lane has read its chunks before it writes there.  The gains' gradients of a workgroup's heads stay in registers, 2 N of q and of k a lane,
+// and end in partial[blockIdx.x] (q) and partial[gridDim.x + blockIdx.x] (k), added up in a fixed order.
+template <typename T, int G, bool FROM8>
 __global__ __launch_bounds__(NT) void qknorm_bwd_kernel(const QkNormBwd p) {
-  __shared__ float sums[NT / 64][2][256];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, d = p.d, half = d / 2, heads = p.n_q + 2 * p.n_kv, n_rot = p.n_q + p.n_kv;
-  const size_t w = (size_t)heads * d;
-  for (int i = threadIdx.x; i < (NT / 64) * 512; i += NT) (&sums[0][0][0])[i] = 0.f;
-  __syncthreads();
-  for (size_t row = blockIdx.x; row < (size_t)p.rows; row += gridDim.x) {
-    for (int head = wave; head < heads; head += NT / 64) {
-      const size_t at = row * w + (size_t)head * d;
-      const T* dy = (const T*)p.dy + at;
-      T* dx = (T*)p.dx + at;
-      if (head >= n_rot) {
-        if (p.dx != p.dy)
-          for (int c = lane; c < d; c += 64) dx[c] = dy[c];
-        continue;
-      }
-      const float r = p.stats[row * n_rot + head];
-      const T* gamma = (const T*)(head < p.n_q ? p.gamma_q : p.gamma_k);
-      float* sum = sums[wave][head < p.n_q ? 0 : 1];
-      float glo[2], ghi[2], xlo[2], xhi[2], s = 0.f;
+  typedef Vec16<T> V;
+  typedef typename KeepChunk<T>::codes_t codes_t;
+  constexpr int S = NT / G, N = V::N;
+  __shared__ float sums[NT / 64][2][2][G * N];
+  const int half = p.d / 2, col = (threadIdx.x % G) * N;
+  const unsigned slot = threadIdx.x / G, n_rot = p.items.n_rot;
+  const bool mine = col < half;
+  V gain[2][2];
+  if (mine)
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const int k = lane + 64 * i;
-        if (k < half) {
-          const float2 cs = p.table[(row % p.seq) * half + k];
-          const float a = to_f32<T>(dy[k]), b = to_f32<T>(dy[k + half]);
-          const float nlo = a * cs.x + b * cs.y, nhi = b * cs.x - a * cs.y;
-          const float vlo = FROM8 ? keep_decode(p.codes[at + k], keep_scale(p.scales[(at + k) / KEEP_BLOCK])) : to_f32<T>(((const T*)p.x)[at + k]);
-          const float vhi = FROM8 ? keep_decode(p.codes[at + k + half], keep_scale(p.scales[(at + k + half) / KEEP_BLOCK])) : to_f32<T>(((const T*)p.x)[at + k + half]);
-          xlo[i] = vlo * r;
-          xhi[i] = vhi * r;
-          sum[k] += nlo * xlo[i];
-          sum[k + half] += nhi * xhi[i];
-          glo[i] = nlo * to_f32<T>(gamma[k]);
-          ghi[i] = nhi * to_f32<T>(gamma[k + half]);
-          s += glo[i] * xlo[i] + ghi[i] * xhi[i];
+    for (int i = 0; i < 2; ++i) {
+      gain[0][i] = *reinterpret_cast<const V*>((const T*)p.gamma_q + i * half + col);
+      gain[1][i] = *reinterpret_cast<const V*>((const T*)p.gamma_k + i * half + col);
+    }
+  float dg[2][2][N] = {};
+  for (size_t base = (size_t)blockIdx.x * S; base < p.items.total; base += (size_t)gridDim.x * S) {
+    const Head k = Walk(base, p.items).at(slot);
+    const bool on = k.on && mine, turn = k.head < n_rot, is_k = k.head >= p.items.n_q;
+    const size_t at = (k.row * p.items.heads + k.head) * p.d + col;
+    V dy[2] = {};
+    float xh[2][N] = {}, g[2][N] = {}, r = 0.f, s = 0.f;
+    if (on) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) dy[i] = *reinterpret_cast<const V*>((const T*)p.dy + at + i * half);
+      if (turn) {
+        Angles<T> a;
+        a.load(p.table + (size_t)position(k.row, p.items.seq) * half + col);
+        r = p.stats[k.row * n_rot + k.head];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          if constexpr (FROM8) {
+            keep_values(*reinterpret_cast<const codes_t*>(p.codes + at + i * half), keep_scale(p.scales[(at + i * half) / KEEP_BLOCK]), xh[i]);
+          } else {
+            const V x = *reinterpret_cast<const V*>((const T*)p.x + at + i * half);
+#pragma unroll
+            for (int e = 0; e < N; ++e) xh[i][e] = x.get(e);
+          }
         }
-      }
-      const float m = wave_sum(s) / d;
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const int k = lane + 64 * i;
-        if (k < half) {
-          dx[k] = from_f32<T>(r * (glo[i] - xlo[i] * m));
-          dx[k + half] = from_f32<T>(r * (ghi[i] - xhi[i] * m));
+        for (int e = 0; e < N; ++e) {
+          const float lo = dy[0].get(e), hi = dy[1].get(e), n[2] = {lo * a.c[e] + hi * a.s[e], hi * a.c[e] - lo * a.s[e]};
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            xh[i][e] *= r;
+            const float t = n[i] * xh[i][e];
+            dg[0][i][e] += is_k ? 0.f : t;
+            dg[1][i][e] += is_k ? t : 0.f;
+            g[i][e] = n[i] * (is_k ? gain[1][i] : gain[0][i]).get(e);
+            s += g[i][e] * xh[i][e];
+          }
         }
       }
     }
+    const float m = group_sum<G>(s) / p.d;
+    if (!on) continue;
+    T* out = (T*)p.dx + at;
+    if (turn) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        V o;
+#pragma unroll
+        for (int e = 0; e < N; ++e) o.set(e, r * (g[i][e] - xh[i][e] * m));
+        *reinterpret_cast<V*>(out + i * half) = o;
+      }
+    } else if (p.dx != p.dy) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) *reinterpret_cast<V*>(out + i * half) = dy[i];
+    }
   }
+  // lanes of a wave with the same chunk, then the waves
+#pragma unroll
+  for (int q = 0; q < 2; ++q)
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int e = 0; e < N; ++e) {
+        float t = dg[q][i][e];
+#pragma unroll
+        for (int o = G; o < 64; o <<= 1) t += __shfl_xor(t, o, 64);
+        if ((threadIdx.x & 63) < G) sums[threadIdx.x >> 6][q][i][col + e] = t;
+      }
   __syncthreads();
-  for (int i = threadIdx.x; i < 2 * d; i += NT) {
-    const int g = i / d, c = i % d;
-    p.partial[((size_t)g * gridDim.x + blockIdx.x) * d + c] = ((sums[0][g][c] + sums[1][g][c]) + sums[2][g][c]) + sums[3][g][c];
+  for (int j = threadIdx.x; j < 2 * p.d; j += NT) {
+    const int q = j / p.d, c = j % p.d, i = c / half, e = c % half;
+    p.partial[((size_t)q * gridDim.x + blockIdx.x) * p.d + c] = ((sums[0][q][i][e] + sums[1][q][i][e]) + sums[2][q][i][e]) + sums[3][q][i][e];
   }
 }
 
-// adds the workgroups' sums into the accumulators: one column per workgroup, in a fixed order
-__global__ __launch_bounds__(NT) void qknorm_reduce_kernel(const float* __restrict__ partial, float* dgamma_q, float* dgamma_k, int nb, int d) {
-  __shared__ float red[NT / 64];
-  const int c = blockIdx.x;
-  const float* src = partial + (size_t)blockIdx.y * nb * d;
-  float s = 0.f;
-  for (int b = threadIdx.x; b < nb; b += NT) s += src[(size_t)b * d + c];
-  s = wave_sum(s);
-  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = s;
-  __syncthreads();
-  if (threadIdx.x == 0) (blockIdx.y ? dgamma_k : dgamma_q)[c] += ((red[0] + red[1]) + red[2]) + red[3];
+// lanes of a head: half a head's chunks, the next power of two
+template <typename T, typename F> hipError_t by_head(int d, F f) {
+  const int lanes = d / 2 / Vec16<T>::N;
+  if constexpr (Vec16<T>::N == 8) {
+    if (lanes <= 4) f(std::integral_constant<int, 4>());
+    else if (lanes <= 8) f(std::integral_constant<int, 8>());
+    else f(std::integral_constant<int, 16>());
+  } else {
+    if (lanes <= 8) f(std::integral_constant<int, 8>());
+    else if (lanes <= 16) f(std::integral_constant<int, 16>());
+    else f(std::integral_constant<int, 32>());
+  }
+  return hipGetLastError();
+}
+unsigned groups_of(const Items& k, int slots, unsigned most) {
+  const size_t n = (k.total + slots - 1) / slots;
+  return (unsigned)(n > most ? most : n);
+}
+
+template <typename T> hipError_t run_qknorm(const QkNorm& p, hipStream_t s) {
+  return by_head<T>(p.d, [&](auto g) {
+    const dim3 grid(groups_of(p.items, NT / g, FWD_GROUPS));
+    if (p.codes_in) hipLaunchKernelGGL((qknorm_kernel<T, g, true, false>), grid, dim3(NT), 0, s, p);
+    else if (p.codes) hipLaunchKernelGGL((qknorm_kernel<T, g, false, true>), grid, dim3(NT), 0, s, p);
+    else hipLaunchKernelGGL((qknorm_kernel<T, g, false, false>), grid, dim3(NT), 0, s, p);
+  });
+}
+template <typename T> hipError_t run_qknorm_bwd(const QkNormBwd& p, float* dgamma_q, float* dgamma_k, int rows, hipStream_t s) {
+  unsigned nb = 0;
+  const hipError_t e = by_head<T>(p.d, [&](auto g) {
+    nb = groups_of(p.items, NT / g, (unsigned)(rows < BWD_GROUPS ? rows : BWD_GROUPS));
+    if (p.codes) hipLaunchKernelGGL((qknorm_bwd_kernel<T, g, true>), dim3(nb), dim3(NT), 0, s, p);
+    else hipLaunchKernelGGL((qknorm_bwd_kernel<T, g, false>), dim3(nb), dim3(NT), 0, s, p);
+  });
+  if (e != hipSuccess) return e;
+  return launch_add_columns(p.partial, dgamma_q, dgamma_k, (int)nb, p.d, s);
 }
 
 }  // namespace
 
 hipError_t launch_qknorm_rope(int dtype, const void* src, const uint8_t* codes_in, const uint8_t* scales_in, void* dst, const void* gamma_q, const void* gamma_k,
                               const float* table, float* stats, uint8_t* codes, uint8_t* scales, int rows, int seq, int n_q, int n_kv, int d, float eps, hipStream_t s) {
-  const QkNorm p = {src, codes_in, scales_in, dst, gamma_q, gamma_k, (const float2*)table, stats, codes, scales, rows, seq, n_q, n_kv, d, eps};
-  const size_t groups = ((size_t)rows * (n_q + 2 * n_kv) + 3) / 4;
-  const dim3 grid((unsigned)(groups > 16384 ? 16384 : groups));
-  if (dtype == DT_BF16) {
-    if (codes_in) hipLaunchKernelGGL((qknorm_kernel<bf16_t, true>), grid, dim3(NT), 0, s, p);
-    else hipLaunchKernelGGL((qknorm_kernel<bf16_t, false>), grid, dim3(NT), 0, s, p);
-  } else {
-    if (codes_in) hipLaunchKernelGGL((qknorm_kernel<float, true>), grid, dim3(NT), 0, s, p);
-    else hipLaunchKernelGGL((qknorm_kernel<float, false>), grid, dim3(NT), 0, s, p);
-  }
-  return hipGetLastError();
+  const unsigned heads = n_q + 2 * n_kv;
+  const QkNorm p = {src, codes_in, scales_in, dst, gamma_q, gamma_k, (const float2*)table, stats, codes, scales,
+                    {(size_t)rows * heads, heads, (unsigned)n_q, (unsigned)(n_q + n_kv), (unsigned)seq}, d, eps};
+  return dtype == DT_BF16 ? run_qknorm<bf16_t>(p, s) : run_qknorm<float>(p, s);
 }
 
 hipError_t launch_qknorm_rope_bwd(int dtype, const void* dy, const void* x, const uint8_t* codes, const uint8_t* scales, const float* stats, const void* gamma_q,
                                   const void* gamma_k, const float* table, void* dx, float* partial, float* dgamma_q, float* dgamma_k, int rows, int seq, int n_q, int n_kv,
                                   int d, hipStream_t s) {
-  const QkNormBwd p = {dy, x, codes, scales, stats, gamma_q, gamma_k, (const float2*)table, dx, partial, rows, seq, n_q, n_kv, d};
-  const int nb = rows < 1024 ? rows : 1024;
-  if (dtype == DT_BF16) {
-    if (codes) hipLaunchKernelGGL((qknorm_bwd_kernel<bf16_t, true>), dim3(nb), dim3(NT), 0, s, p);
-    else hipLaunchKernelGGL((qknorm_bwd_kernel<bf16_t, false>), dim3(nb), dim3(NT), 0, s, p);
-  } else {
-    if (codes) hipLaunchKernelGGL((qknorm_bwd_kernel<float, true>), dim3(nb), dim3(NT), 0, s, p);
-    else hipLaunchKernelGGL((qknorm_bwd_kernel<float, false>), dim3(nb), dim3(NT), 0, s, p);
-  }
-  const hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(qknorm_reduce_kernel, dim3(d, 2), dim3(NT), 0, s, partial, dgamma_q, dgamma_k, nb, d);
-  return hipGetLastError();
+  const unsigned heads = n_q + 2 * n_kv;
+  const QkNormBwd p = {dy, x, codes, scales, stats, gamma_q, gamma_k, (const float2*)table, dx, partial,
+                       {(size_t)rows * heads, heads, (unsigned)n_q, (unsigned)(n_q + n_kv), (unsigned)seq}, d};
+  return dtype == DT_BF16 ? run_qknorm_bwd<bf16_t>(p, dgamma_q, dgamma_k, rows, s) : run_qknorm_bwd<float>(p, dgamma_q, dgamma_k, rows, s);
 }
