@@ -12,7 +12,9 @@
 namespace {
 
 constexpr int NT = 256;
-constexpr int FWD_GROUPS = 4096, BWD_GROUPS = 1024;
+// Workgroups: forward 154 us with 2048 to 8192 of them each taking several turns, 163 with one turn each (8192 rows of 80 heads of 128); backward as many as
+// the compute units hold at once, four on each (768: 100 us, 1024: 94), and the sums of so many
+constexpr int FWD_GROUPS = 8192, BWD_GROUPS = 1024;
 
 template <int G> __device__ __forceinline__ float group_sum(float v) {
   v += __uint_as_float(lane_swap<0xB1>(__float_as_uint(v)));          // lane ^ 1
@@ -29,24 +31,43 @@ struct Items {
   unsigned heads, n_q, n_rot, seq;
 };
 struct Head {
-  size_t row;
-  unsigned head;
+  unsigned row, head, pos;
   bool on;
 };
-// item base + i; base is the workgroup's
-struct Walk {
-  size_t row0, left;
-  unsigned h0, heads;
-  __device__ __forceinline__ Walk(size_t base, const Items& k) : left(k.total - base), heads(k.heads) {
-    row0 = k.total >> 32 ? base / k.heads : (size_t)((unsigned)base / k.heads);
-    h0 = (unsigned)(base - row0 * k.heads);
+// The workgroup's items base .. base + S - 1 of every turn.  All of it is the same for the whole workgroup and advances without a division; a lane's address is
+// a pointer to the workgroup's first head plus an offset that never changes (these and the divisions were a third of the gradient kernel's instructions).
+template <int S> struct Cursor {
+  size_t base;
+  unsigned row, head, pos;
+  size_t step;
+  unsigned step_row, step_head, step_pos;
+  __device__ __forceinline__ explicit Cursor(const Items& k) {
+    base = (size_t)blockIdx.x * S;
+    step = (size_t)gridDim.x * S;                                      // < 2^32
+    row = (unsigned)(k.total >> 32 ? base / k.heads : (unsigned)base / k.heads);
+    head = (unsigned)(base - (size_t)row * k.heads);
+    pos = row % k.seq;
+    step_row = (unsigned)step / k.heads;
+    step_head = (unsigned)step - step_row * k.heads;
+    step_pos = step_row % k.seq;
   }
-  __device__ __forceinline__ Head at(unsigned i) const {
-    const unsigned n = h0 + i, r = n / heads;
-    return {row0 + r, n - r * heads, i < left};
+  __device__ __forceinline__ void advance(const Items& k) {
+    base += step;
+    head += step_head;
+    const unsigned carry = head >= k.heads;
+    head -= carry ? k.heads : 0u;
+    row += step_row + carry;
+    pos += step_pos + carry;
+    pos -= pos >= k.seq ? k.seq : 0u;
+  }
+  __device__ __forceinline__ Head lane(unsigned slot, const Items& k) const {
+    const unsigned n = head + slot, r = k.heads >= S ? (n >= k.heads ? 1u : 0u) : n / k.heads;
+    unsigned at = pos + r;                                              // r <= S
+    if (k.seq >= S) at -= at >= k.seq ? k.seq : 0u;
+    else at %= k.seq;
+    return {row + r, n - r * k.heads, at, base + slot < k.total};
   }
 };
-__device__ __forceinline__ unsigned position(size_t row, unsigned seq) { return (unsigned)row % seq; }   // rows < 2^30
 
 // the chunk's cos and sin
 template <typename T> struct Angles {
@@ -76,6 +97,7 @@ __global__ __launch_bounds__(NT) void qknorm_kernel(const QkNorm p) {
   const int half = p.d / 2, col = (threadIdx.x % G) * V::N;
   const unsigned slot = threadIdx.x / G, n_rot = p.items.n_rot;
   const bool mine = col < half;                                        // d = 192: lanes of a head that hold nothing
+  const unsigned off[2] = {slot * p.d + col, slot * p.d + col + half};
   V gain[2][2];                                                        // q, k; lower, upper half
   if (mine)
 #pragma unroll
@@ -83,25 +105,27 @@ __global__ __launch_bounds__(NT) void qknorm_kernel(const QkNorm p) {
       gain[0][i] = *reinterpret_cast<const V*>((const T*)p.gamma_q + i * half + col);
       gain[1][i] = *reinterpret_cast<const V*>((const T*)p.gamma_k + i * half + col);
     }
-  for (size_t base = (size_t)blockIdx.x * S; base < p.items.total; base += (size_t)gridDim.x * S) {
-    const Head k = Walk(base, p.items).at(slot);
+  for (Cursor<S> cur(p.items); cur.base < p.items.total; cur.advance(p.items)) {
+    const Head k = cur.lane(slot, p.items);
     const bool on = k.on && mine, turn = k.head < n_rot;
-    const size_t at = (k.row * p.items.heads + k.head) * p.d + col;
+    const size_t first = cur.base * p.d;
     V x[2] = {};
     float v[2][V::N];
     Angles<T> a;
     float r = 0.f;
     if (on) {
-      if (turn) a.load(p.table + (size_t)position(k.row, p.items.seq) * half + col);
       if constexpr (FROM8) {
         codes_t c[2];
         uint32_t b[2];
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-          c[i] = *reinterpret_cast<const codes_t*>(p.codes_in + at + i * half);
-          b[i] = p.scales_in[(at + i * half) / KEEP_BLOCK];
+          c[i] = *reinterpret_cast<const codes_t*>(p.codes_in + first + off[i]);
+          b[i] = p.scales_in[first / KEEP_BLOCK + off[i] / KEEP_BLOCK];
         }
-        if (turn) r = p.stats[k.row * n_rot + k.head];
+        if (turn) {
+          a.load(p.table + (size_t)k.pos * half + col);
+          r = p.stats[(size_t)k.row * n_rot + k.head];
+        }
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
           if (turn) keep_values(c[i], keep_scale(b[i]), v[i]);
@@ -109,7 +133,8 @@ __global__ __launch_bounds__(NT) void qknorm_kernel(const QkNorm p) {
         }
       } else {
 #pragma unroll
-        for (int i = 0; i < 2; ++i) x[i] = *reinterpret_cast<const V*>((const T*)p.src + at + i * half);
+        for (int i = 0; i < 2; ++i) x[i] = *reinterpret_cast<const V*>((const T*)p.src + first + off[i]);
+        if (turn) a.load(p.table + (size_t)k.pos * half + col);
       }
     }
     if constexpr (!FROM8) {
@@ -122,21 +147,21 @@ __global__ __launch_bounds__(NT) void qknorm_kernel(const QkNorm p) {
           s += v[i][e] * v[i][e];
         }
       r = rsqrtf(group_sum<G>(s) / p.d + p.eps);
-      if (on && turn && col == 0) p.stats[k.row * n_rot + k.head] = r;
+      if (on && turn && col == 0) p.stats[(size_t)k.row * n_rot + k.head] = r;
       if constexpr (KEEP) {
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
           uint32_t byte;
           const codes_t c = keep_chunk<T>(x[i], byte);
           if (on) {
-            *reinterpret_cast<codes_t*>(p.codes + at + i * half) = c;
-            if (col % KEEP_BLOCK == 0) p.scales[(at + i * half) / KEEP_BLOCK] = (uint8_t)byte;
+            *reinterpret_cast<codes_t*>(p.codes + first + off[i]) = c;
+            if (col % KEEP_BLOCK == 0) p.scales[first / KEEP_BLOCK + off[i] / KEEP_BLOCK] = (uint8_t)byte;
           }
         }
       }
     }
     if (!on) continue;
-    T* out = (T*)p.dst + at;
+    T* out = (T*)p.dst + first;
     if (turn) {
       const bool is_k = k.head >= p.items.n_q;
       V o[2];
@@ -147,10 +172,10 @@ __global__ __launch_bounds__(NT) void qknorm_kernel(const QkNorm p) {
         o[1].set(e, hi * a.c[e] + lo * a.s[e]);
       }
 #pragma unroll
-      for (int i = 0; i < 2; ++i) *reinterpret_cast<V*>(out + i * half) = o[i];
+      for (int i = 0; i < 2; ++i) *reinterpret_cast<V*>(out + off[i]) = o[i];
     } else if (FROM8 || p.dst != p.src) {
 #pragma unroll
-      for (int i = 0; i < 2; ++i) *reinterpret_cast<V*>(out + i * half) = x[i];
+      for (int i = 0; i < 2; ++i) *reinterpret_cast<V*>(out + off[i]) = x[i];
     }
   }
 }
@@ -162,14 +187,15 @@ struct QkNormBwd {
   int d;
 };
 
-// dx may be dy or x: a lane has read its chunks before it writes there.  The gains' gradients of a workgroup's heads stay in registers, 2 N of q and of k a lane,
-// and end in partial[blockIdx.x] (q) and partial[gridDim.x + blockIdx.x] (k), added up in a fixed order.
+// dx may be dy or x: a lane has read its chunks before it writes there.  The gains' gradients of a
+// workgroup's heads stay in registers, 2 N of q and of k a lane, and end in partial[blockIdx.x] (q) and partial[gridDim.x + blockIdx.x] (k), added up in a
+// fixed order.
 template <typename T, int G, bool FROM8>
 __global__ __launch_bounds__(NT) void qknorm_bwd_kernel(const QkNormBwd p) {
   typedef Vec16<T> V;
   typedef typename KeepChunk<T>::codes_t codes_t;
-  constexpr int S = NT / G, N = V::N;
-  __shared__ float sums[NT / 64][2][2][G * N];
+  constexpr int S = NT / G, N = V::N, W = G * N;
+  __shared__ float sums[S][2][2][W];
   const int half = p.d / 2, col = (threadIdx.x % G) * N;
   const unsigned slot = threadIdx.x / G, n_rot = p.items.n_rot;
   const bool mine = col < half;
@@ -181,76 +207,93 @@ __global__ __launch_bounds__(NT) void qknorm_bwd_kernel(const QkNormBwd p) {
       gain[1][i] = *reinterpret_cast<const V*>((const T*)p.gamma_k + i * half + col);
     }
   float dg[2][2][N] = {};
-  for (size_t base = (size_t)blockIdx.x * S; base < p.items.total; base += (size_t)gridDim.x * S) {
-    const Head k = Walk(base, p.items).at(slot);
+  const unsigned off[2] = {slot * p.d + col, slot * p.d + col + half};
+  for (Cursor<S> cur(p.items); cur.base < p.items.total; cur.advance(p.items)) {
+    const Head k = cur.lane(slot, p.items);
     const bool on = k.on && mine, turn = k.head < n_rot, is_k = k.head >= p.items.n_q;
-    const size_t at = (k.row * p.items.heads + k.head) * p.d + col;
+    const size_t first = cur.base * p.d;
     V dy[2] = {};
     float xh[2][N] = {}, g[2][N] = {}, r = 0.f, s = 0.f;
     if (on) {
 #pragma unroll
-      for (int i = 0; i < 2; ++i) dy[i] = *reinterpret_cast<const V*>((const T*)p.dy + at + i * half);
+      for (int i = 0; i < 2; ++i) dy[i] = *reinterpret_cast<const V*>((const T*)p.dy + first + off[i]);
       if (turn) {
+        codes_t c[2];
+        uint32_t b[2];
+        V x[2];
         Angles<T> a;
-        a.load(p.table + (size_t)position(k.row, p.items.seq) * half + col);
-        r = p.stats[k.row * n_rot + k.head];
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
           if constexpr (FROM8) {
-            keep_values(*reinterpret_cast<const codes_t*>(p.codes + at + i * half), keep_scale(p.scales[(at + i * half) / KEEP_BLOCK]), xh[i]);
+            c[i] = *reinterpret_cast<const codes_t*>(p.codes + first + off[i]);
+            b[i] = p.scales[first / KEEP_BLOCK + off[i] / KEEP_BLOCK];
           } else {
-            const V x = *reinterpret_cast<const V*>((const T*)p.x + at + i * half);
-#pragma unroll
-            for (int e = 0; e < N; ++e) xh[i][e] = x.get(e);
+            x[i] = *reinterpret_cast<const V*>((const T*)p.x + first + off[i]);
           }
         }
+        a.load(p.table + (size_t)k.pos * half + col);
+        r = p.stats[(size_t)k.row * n_rot + k.head];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          if constexpr (FROM8) {
+            keep_values(c[i], keep_scale(b[i]), xh[i]);
+          } else {
+#pragma unroll
+            for (int e = 0; e < N; ++e) xh[i][e] = x[i].get(e);
+          }
+        }
+        float n[2][N];
 #pragma unroll
         for (int e = 0; e < N; ++e) {
-          const float lo = dy[0].get(e), hi = dy[1].get(e), n[2] = {lo * a.c[e] + hi * a.s[e], hi * a.c[e] - lo * a.s[e]};
+          const float lo = dy[0].get(e), hi = dy[1].get(e);
+          n[0][e] = lo * a.c[e] + hi * a.s[e];
+          n[1][e] = hi * a.c[e] - lo * a.s[e];
 #pragma unroll
           for (int i = 0; i < 2; ++i) {
             xh[i][e] *= r;
-            const float t = n[i] * xh[i][e];
-            dg[0][i][e] += is_k ? 0.f : t;
-            dg[1][i][e] += is_k ? t : 0.f;
-            g[i][e] = n[i] * (is_k ? gain[1][i] : gain[0][i]).get(e);
+            g[i][e] = n[i][e] * (is_k ? gain[1][i] : gain[0][i]).get(e);
             s += g[i][e] * xh[i][e];
           }
         }
+        // one of two branches for nearly every wave
+#pragma unroll
+        for (int q = 0; q < 2; ++q)
+          if (is_k == (q == 1))
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+              for (int e = 0; e < N; ++e) dg[q][i][e] = fmaf(n[i][e], xh[i][e], dg[q][i][e]);
       }
     }
     const float m = group_sum<G>(s) / p.d;
     if (!on) continue;
-    T* out = (T*)p.dx + at;
+    T* out = (T*)p.dx + first;
     if (turn) {
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         V o;
 #pragma unroll
         for (int e = 0; e < N; ++e) o.set(e, r * (g[i][e] - xh[i][e] * m));
-        *reinterpret_cast<V*>(out + i * half) = o;
+        *reinterpret_cast<V*>(out + off[i]) = o;
       }
     } else if (p.dx != p.dy) {
 #pragma unroll
-      for (int i = 0; i < 2; ++i) *reinterpret_cast<V*>(out + i * half) = dy[i];
+      for (int i = 0; i < 2; ++i) *reinterpret_cast<V*>(out + off[i]) = dy[i];
     }
   }
-  // lanes of a wave with the same chunk, then the waves
 #pragma unroll
   for (int q = 0; q < 2; ++q)
 #pragma unroll
     for (int i = 0; i < 2; ++i)
 #pragma unroll
-      for (int e = 0; e < N; ++e) {
-        float t = dg[q][i][e];
-#pragma unroll
-        for (int o = G; o < 64; o <<= 1) t += __shfl_xor(t, o, 64);
-        if ((threadIdx.x & 63) < G) sums[threadIdx.x >> 6][q][i][col + e] = t;
-      }
+      for (int e = 0; e < N; ++e) sums[slot][q][i][col + e] = dg[q][i][e];
   __syncthreads();
   for (int j = threadIdx.x; j < 2 * p.d; j += NT) {
-    const int q = j / p.d, c = j % p.d, i = c / half, e = c % half;
-    p.partial[((size_t)q * gridDim.x + blockIdx.x) * p.d + c] = ((sums[0][q][i][e] + sums[1][q][i][e]) + sums[2][q][i][e]) + sums[3][q][i][e];
+    const int q = j / p.d, c = j % p.d, i = c >= half, e = c - i * half;
+    float t = 0.f;
+#pragma unroll 8
+    for (int w = 0; w < S; ++w) t += sums[w][q][i][e];
+    p.partial[((size_t)q * gridDim.x + blockIdx.x) * p.d + c] = t;
   }
 }
 
