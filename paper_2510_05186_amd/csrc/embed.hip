@@ -1,89 +1,354 @@
 // Embedding: out[r] = scale * weight[ids[r]], and its gradient grad[t] += scale * (sum of dy[r] over the rows r with ids[r] = t).
 // A row whose id is no word of the vocabulary (negative, or vocab and more: padding) is zero and has no gradient.
+//
+// The gradient sorts the tokens, so that equal ones stand side by side and every row of the accumulator that occurs is read and written once, without
+// atomics and in an order that the ids alone decide: the rows of a token in their order, up to PIECE of them by one wave.  The runs of frequent
+// tokens are cut at multiples of PIECE, and their pieces' sums are added by a second launch.  Bound by memory (dy once, the accumulator's rows in and out)
+// from some thousand tokens of some thousand columns on, by the latency of the launches below that.
 #include "common.h"
 
 namespace {
 
 constexpr int NT = 256;
 
-template <typename T>
-__global__ __launch_bounds__(NT) void embed_fwd_kernel(const int* __restrict__ ids, const T* __restrict__ weight, T* __restrict__ out, int rows, unsigned vocab, int h,
-                                                       float scale) {
+// ---- lookup -----------------------------------------------------------------------------------------------
+// 16 bytes a lane; chunks numbered through all rows
+template <typename T, int U>
+__global__ __launch_bounds__(NT) void embed_fwd_kernel(const int* __restrict__ ids, const T* __restrict__ weight, T* __restrict__ out, size_t total, unsigned per_row,
+                                                       unsigned vocab, float scale) {
   typedef Vec16<T> V;
-  const int nvec = h / V::N;
-  const size_t total = (size_t)rows * nvec, step = (size_t)gridDim.x * NT;
-  for (size_t i = blockIdx.x * (size_t)NT + threadIdx.x; i < total; i += step) {
-    const size_t row = i / nvec;
-    const int c = (int)(i % nvec);
-    const unsigned id = (unsigned)ids[row];
-    V v;
+  for (size_t base = blockIdx.x * (size_t)(NT * U); base < total; base += (size_t)gridDim.x * (NT * U)) {
+    const size_t row0 = total >> 32 ? base / per_row : (size_t)((unsigned)base / per_row);
+    const unsigned c0 = (unsigned)(base - row0 * per_row);
+    V v[U];
+    bool word[U];
 #pragma unroll
-    for (int e = 0; e < V::N; ++e) v.set(e, 0.f);
-    if (id < vocab) {
-      v = *reinterpret_cast<const V*>(weight + (size_t)id * h + (size_t)c * V::N);
-#pragma unroll
-      for (int e = 0; e < V::N; ++e) v.set(e, v.get(e) * scale);
+    for (int u = 0; u < U; ++u) {
+      const unsigned i = u * NT + threadIdx.x, n = c0 + i, r = n / per_row;
+      word[u] = false;
+      if (base + i < total) {
+        const unsigned id = (unsigned)ids[row0 + r];
+        word[u] = id < vocab;
+        if (word[u]) v[u] = *reinterpret_cast<const V*>(weight + ((size_t)id * per_row + (n - r * per_row)) * V::N);
+      }
     }
-    *reinterpret_cast<V*>(out + row * h + (size_t)c * V::N) = v;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const size_t i = base + u * NT + threadIdx.x;
+#pragma unroll
+      for (int e = 0; e < V::N; ++e) v[u].set(e, word[u] ? v[u].get(e) * scale : 0.f);
+      if (i < total) *reinterpret_cast<V*>(out + i * V::N) = v[u];
+    }
   }
 }
 
-// place of every row among all rows in the order of (id, row), by counting; ids outside the vocabulary come last
-__global__ __launch_bounds__(NT) void embed_rank_kernel(const int* __restrict__ ids, unsigned* __restrict__ key, unsigned* __restrict__ row_of, int rows, unsigned vocab) {
-  __shared__ unsigned tile[NT];
-  const int i = blockIdx.x * NT + threadIdx.x;
-  unsigned mine = i < rows ? (unsigned)ids[i] : 0u;
-  if (mine >= vocab) mine = 0xffffffffu;
-  unsigned place = 0;
-  for (int j0 = 0; j0 < rows; j0 += NT) {
-    const int j = j0 + threadIdx.x;
-    unsigned k = j < rows ? (unsigned)ids[j] : 0u;
-    if (k >= vocab) k = 0xffffffffu;
-    __syncthreads();
-    tile[threadIdx.x] = k;
-    __syncthreads();
-    const int n = min(NT, rows - j0);
-    for (int q = 0; q < n; ++q) place += tile[q] < mine || (tile[q] == mine && j0 + q < i);
+// ---- sort ---------------------------------------------------------------------------------------------------
+// One pass of a stable radix sort by up to 9 bits of the id in one launch: every workgroup counts the digits of ALL keys (they come out of the L2;
+// 16384 keys are 64 KB), those ahead of its own range apart, which gives it the place of each of its digits without waiting for the others.  The first
+// pass takes the ids themselves and leaves out those that are no words.
+constexpr int SORT_T = 1024, RADIX = 512, COPIES = 8;                   // counters in 8 copies by lane: equal digits of a wave meet 8 at a time at most
+constexpr int SORT_MAX_GROUPS = 256;
+
+struct Sorted {
+  unsigned* count;                                                      // [0] valid tokens, [1] runs in `long_runs`
+  unsigned* long_runs;
+  unsigned *key[2], *row[2];
+  float* partial;
+};
+
+template <bool FIRST>
+__global__ __launch_bounds__(SORT_T) void embed_sort_kernel(const int* __restrict__ ids, const unsigned* __restrict__ key_in, const unsigned* __restrict__ row_in,
+                                                            unsigned* __restrict__ key_out, unsigned* __restrict__ row_out, unsigned* count, unsigned n, unsigned vocab,
+                                                            int shift, int bits, unsigned per_group) {
+  __shared__ unsigned hist[2][RADIX * COPIES];                          // ahead of the range, and the rest
+  __shared__ unsigned place[RADIX], wave_total[SORT_T / 64];
+  const unsigned tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, digits = 1u << bits, mask = digits - 1;
+  if (!FIRST) n = count[0];
+  const unsigned begin = min(n, blockIdx.x * per_group), end = min(n, begin + per_group);
+  for (unsigned i = tid; i < digits * COPIES; i += SORT_T) hist[0][i] = hist[1][i] = 0;
+  __syncthreads();
+  auto key_at = [&](unsigned i) { return FIRST ? (unsigned)ids[i] : key_in[i]; };
+  for (unsigned i0 = 0; i0 < n; i0 += SORT_T * 8) {
+    unsigned k[8];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+      const unsigned i = i0 + u * SORT_T + tid;
+      k[u] = i < n ? key_at(i) : 0xffffffffu;
+    }
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+      const unsigned i = i0 + u * SORT_T + tid;
+      if (i < n && k[u] < vocab) atomicAdd(&hist[i < begin ? 0 : 1][(k[u] >> shift & mask) * COPIES + (lane & (COPIES - 1))], 1u);
+    }
   }
-  if (i < rows) { key[place] = mine; row_of[place] = (unsigned)i; }
+  __syncthreads();
+  // place[d]: keys of smaller digits, and those of digit d ahead of the range
+  unsigned ahead = 0, all = 0;
+  if (tid < digits) {
+#pragma unroll
+    for (int c = 0; c < COPIES; ++c) {
+      ahead += hist[0][tid * COPIES + c];
+      all += hist[1][tid * COPIES + c];
+    }
+    all += ahead;
+  }
+  unsigned before = all;                                                // inclusive scan over the wave, then over the waves
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const unsigned t = (unsigned)__shfl_up((int)before, o, 64);
+    if (lane >= (unsigned)o) before += t;
+  }
+  if (lane == 63) wave_total[wave] = before;
+  __syncthreads();
+  unsigned sum = 0;
+#pragma unroll
+  for (int w = 0; w < SORT_T / 64; ++w) {
+    if ((unsigned)w == wave) before += sum;
+    sum += wave_total[w];
+  }
+  if (tid < digits) place[tid] = before - all + ahead;
+  if (FIRST && blockIdx.x == 0 && tid == 0) { count[0] = sum; count[1] = 0; }
+  // the range, SORT_T keys at a time: a lane's place is its digit's, past the waves ahead and the lanes of its own wave ahead with the same digit
+  unsigned (&wave_count)[SORT_T / 64][RADIX] = reinterpret_cast<unsigned (&)[SORT_T / 64][RADIX]>(hist);
+  for (unsigned i0 = begin; i0 < end; i0 += SORT_T) {
+    __syncthreads();
+    for (unsigned i = tid; i < (SORT_T / 64) * RADIX; i += SORT_T) (&wave_count[0][0])[i] = 0;
+    __syncthreads();
+    const unsigned i = i0 + tid;
+    const unsigned key = i < end ? key_at(i) : 0xffffffffu;
+    const bool on = key < vocab;
+    const unsigned d = key >> shift & mask;
+    unsigned long long same = __ballot(on);
+    for (int b = 0; b < bits; ++b) {
+      const unsigned long long set = __ballot(d >> b & 1);
+      same &= d >> b & 1 ? set : ~set;
+    }
+    const unsigned rank = __popcll(same & ((1ull << lane) - 1));
+    if (on && rank == 0) wave_count[wave][d] = __popcll(same);
+    __syncthreads();
+    if (tid < digits) {
+      unsigned at = place[tid];
+#pragma unroll
+      for (int w = 0; w < SORT_T / 64; ++w) {
+        const unsigned c = wave_count[w][tid];
+        wave_count[w][tid] = at;
+        at += c;
+      }
+      place[tid] = at;
+    }
+    __syncthreads();
+    if (on) {
+      const unsigned at = wave_count[wave][d] + rank;
+      key_out[at] = key;
+      row_out[at] = FIRST ? i : row_in[i];
+    }
+  }
+}
+static_assert(sizeof(unsigned) * 2 * RADIX * COPIES >= sizeof(unsigned) * (SORT_T / 64) * RADIX, "the waves' counts lie in the histogram's place");
+
+// ---- sums -----------------------------------------------------------------------------------------------------
+constexpr int PIECE = 32;                                               // rows that one wave adds up
+constexpr int FLIGHT = 16;                                              // of them in flight
+
+// The sum over the `n` rows whose numbers the lanes hold, n <= 64, of the lane's chunk at column col.
+template <typename T> __device__ __forceinline__ void add_rows(const T* __restrict__ dy, unsigned row, int n, size_t h, int col, bool on, float* s) {
+  typedef Vec16<T> V;
+  for (int i0 = 0; i0 < n; i0 += FLIGHT) {
+    V v[FLIGHT];
+#pragma unroll
+    for (int u = 0; u < FLIGHT; ++u)
+      if (i0 + u < n) {
+        const size_t r = (unsigned)__builtin_amdgcn_readlane((int)row, i0 + u);
+        if (on) v[u] = *reinterpret_cast<const V*>(dy + r * h + col);
+      }
+#pragma unroll
+    for (int u = 0; u < FLIGHT; ++u)
+      if (i0 + u < n)
+#pragma unroll
+        for (int e = 0; e < V::N; ++e) s[e] += v[u].get(e);
+  }
+}
+template <int N> __device__ __forceinline__ void add_to(float* g, const float* s, float scale) {
+#pragma unroll
+  for (int i = 0; i < N; i += 4) {
+    f32x4_t v = *reinterpret_cast<f32x4_t*>(g + i);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] += scale * s[i + e];
+    *reinterpret_cast<f32x4_t*>(g + i) = v;
+  }
 }
 
-// one run of equal ids per workgroup (the workgroups of places where none begins end at once), its rows added in order
+// Wave (p, slice): place p of the sorted tokens, 64 chunks of columns.  It has work where a run of equal tokens begins at p, and at multiples of PIECE inside a run of more
+// than PIECE.  partial[2 k] is the sum of the piece that begins at place k PIECE, partial[2 k + 1] that of the piece of a long run that begins later in
+// that range (only one can: it goes on behind it).
 template <typename T>
-__global__ __launch_bounds__(NT) void embed_sum_kernel(const unsigned* __restrict__ key, const unsigned* __restrict__ row_of, const T* __restrict__ dy,
-                                                       float* __restrict__ grad, int rows, int h, float scale) {
-  const int p = blockIdx.x;
-  const unsigned id = key[p];
-  if (id == 0xffffffffu || (p > 0 && key[p - 1] == id)) return;
-  int end = p + 1;
-  while (end < rows && key[end] == id) ++end;
-  for (int c = threadIdx.x; c < h; c += NT) {
-    float s = 0.f;
-    for (int q = p; q < end; ++q) s += to_f32<T>(dy[(size_t)row_of[q] * h + c]);
-    float* g = grad + (size_t)id * h + c;
-    *g += scale * s;
+__global__ __launch_bounds__(NT) void embed_sum_kernel(const unsigned* __restrict__ key, const unsigned* __restrict__ row_of, const T* __restrict__ dy, float* __restrict__ grad,
+                                                       unsigned* count, unsigned* long_runs, float* __restrict__ partial, int h, float scale) {
+  constexpr int N = Vec16<T>::N;
+  const int lane = threadIdx.x & 63, slice = blockIdx.y * (NT / 64) + (threadIdx.x >> 6), col = (slice * 64 + lane) * N;
+  const unsigned m = count[0];
+  if (slice * 64 * N >= h) return;
+  for (unsigned p = blockIdx.x; p < m; p += gridDim.x) {
+    // bit j: place p - PIECE + j holds the same token
+    const unsigned id = key[p];
+    const long long j = (long long)p - PIECE + lane;
+    const unsigned long long same = __ballot(j >= 0 && j < (long long)m && key[j < 0 ? 0 : j] == id);
+    const bool first = !(same >> (PIECE - 1) & 1);
+    if (!first && p % PIECE) continue;
+    const int ahead = first ? 0 : __clzll((long long)~(same << (64 - PIECE)));        // places before p with the same token, of the last PIECE
+    const int here = __ffsll((long long)~(same >> PIECE)) - 1;                        // from p on, of the next PIECE (the bits shifted in are zero)
+    const bool longer = here == PIECE && p + PIECE < m && key[p + PIECE] == id;
+    // whether the run has more than PIECE places
+    const bool cut = first ? longer : ahead + here > PIECE || longer;
+    if (!first && !cut) continue;
+    const int n = cut ? min(here, (int)(PIECE - p % PIECE)) : here;
+    const unsigned row = lane < n ? row_of[p + lane] : 0u;
+    float s[N] = {};
+    add_rows(dy, row, n, (size_t)h, col, col < h, s);
+    if (cut && first && slice == 0 && lane == 0) long_runs[atomicAdd(&count[1], 1u)] = p;
+    if (col >= h) continue;
+    if (!cut) add_to<N>(grad + (size_t)id * h + col, s, scale);
+    else {
+      float* to = partial + (size_t)(p / PIECE * 2 + (p % PIECE ? 1 : 0)) * h + col;
+#pragma unroll
+      for (int i = 0; i < N; i += 4) *reinterpret_cast<f32x4_t*>(to + i) = (f32x4_t){s[i], s[i + 1], s[i + 2], s[i + 3]};
+    }
   }
+}
+
+// The pieces of a long run, 256 columns of it per workgroup: eight waves take every eighth piece, eight loads of a lane in flight, and are added in order.  The order
+// of the list does not matter: a run's pieces are found from its first place.
+constexpr int JOIN_T = 512;
+__global__ __launch_bounds__(JOIN_T) void embed_join_kernel(const unsigned* __restrict__ key, const unsigned* __restrict__ count, const unsigned* __restrict__ long_runs,
+                                                            const float* __restrict__ partial, float* __restrict__ grad, int h, float scale) {
+  constexpr int W = JOIN_T / 64;
+  __shared__ f32x4_t red[W][64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const unsigned m = count[0], slices = (h + 255) / 256;
+  const unsigned long long items = (unsigned long long)count[1] * slices;
+  for (unsigned long long item = blockIdx.x; item < items; item += gridDim.x) {
+    const unsigned p = long_runs[item / slices], id = key[p];
+    const int col = (int)(item % slices) * 256 + lane * 4;
+    unsigned lo = p, hi = m;                                             // the run's end: the first place of a larger token
+    while (hi - lo > 1) {
+      const unsigned mid = lo + (hi - lo) / 2;
+      if (key[mid] == id) lo = mid; else hi = mid;
+    }
+    const unsigned k0 = p / PIECE + 1, pieces = (hi - 1) / PIECE + 1 - k0;   // behind the first piece
+    f32x4_t s = {0.f, 0.f, 0.f, 0.f};
+    if (col < h) {
+      if (wave == 0) s = *reinterpret_cast<const f32x4_t*>(partial + (size_t)(p / PIECE * 2 + (p % PIECE ? 1 : 0)) * h + col);
+      for (unsigned i0 = wave; i0 < pieces; i0 += W * 8) {
+        f32x4_t v[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u)
+          if (i0 + u * W < pieces) v[u] = *reinterpret_cast<const f32x4_t*>(partial + (size_t)(k0 + i0 + u * W) * 2 * h + col);
+#pragma unroll
+        for (int u = 0; u < 8; ++u)
+          if (i0 + u * W < pieces) s += v[u];
+      }
+    }
+    red[wave][lane] = s;
+    __syncthreads();
+    if (wave == 0 && col < h) {
+      for (int w = 1; w < W; ++w) s += red[w][lane];
+      const float t[4] = {s[0], s[1], s[2], s[3]};
+      add_to<4>(grad + (size_t)id * h + col, t, scale);
+    }
+    __syncthreads();
+  }
+}
+
+// A few tokens, in one launch: wave (r, slice) compares all ids with row r's and adds up its token's rows if r is the first of them.
+constexpr int FEW = 256;
+template <typename T>
+__global__ __launch_bounds__(NT) void embed_few_kernel(const int* __restrict__ ids, const T* __restrict__ dy, float* __restrict__ grad, int rows, unsigned vocab, int h,
+                                                       float scale) {
+  constexpr int N = Vec16<T>::N;
+  const int lane = threadIdx.x & 63, slice = blockIdx.y * (NT / 64) + (threadIdx.x >> 6), col = (slice * 64 + lane) * N, r = blockIdx.x;
+  if (slice * 64 * N >= h) return;
+  const int id = ids[r];
+  if ((unsigned)id >= vocab) return;
+  unsigned long long same[FEW / 64];
+#pragma unroll
+  for (int i = 0; i < FEW / 64; ++i) same[i] = __ballot(i * 64 + lane < rows && ids[min(i * 64 + lane, rows - 1)] == id);
+#pragma unroll
+  for (int i = 0; i < FEW / 64; ++i)
+    if (r > i * 64 && (same[i] & (r - i * 64 >= 64 ? ~0ull : (1ull << (r - i * 64)) - 1))) return;
+  float s[N] = {};
+#pragma unroll
+  for (int i = 0; i < FEW / 64; ++i) {
+    if (!same[i]) continue;
+    // lane k gets the number of the k-th row of the 64
+    const int n = __popcll(same[i]), k = __popcll(same[i] & ((1ull << lane) - 1));
+    const unsigned row = (unsigned)__builtin_amdgcn_ds_permute((same[i] >> lane & 1 ? k : 63) * 4, i * 64 + lane);
+    add_rows(dy, row, n, (size_t)h, col, col < h, s);
+  }
+  if (col < h) add_to<N>(grad + (size_t)id * h + col, s, scale);
+}
+
+Sorted layout(void* ws, int rows, int h, uint64_t* bytes) {
+  uint64_t at = 0;
+  auto take = [&](uint64_t n) { void* p = (char*)ws + at; at += (n + 255) / 256 * 256; return p; };
+  Sorted s;
+  s.count = (unsigned*)take(8);
+  s.long_runs = (unsigned*)take(((uint64_t)rows / (PIECE + 1) + 1) * 4);
+  for (int i = 0; i < 2; ++i) {
+    s.key[i] = (unsigned*)take((uint64_t)rows * 4);
+    s.row[i] = (unsigned*)take((uint64_t)rows * 4);
+  }
+  s.partial = (float*)take(((uint64_t)rows + PIECE - 1) / PIECE * 2 * h * 4);
+  *bytes = at;
+  return s;
+}
+
+template <typename T>
+hipError_t run_embed_bwd(const int* ids, const void* dy, float* grad, void* ws, int rows, unsigned vocab, int h, float scale, hipStream_t s) {
+  const unsigned slices = (unsigned)((h / Vec16<T>::N + NT - 1) / NT);
+  if (rows <= FEW) {
+    hipLaunchKernelGGL(embed_few_kernel<T>, dim3(rows, slices), dim3(NT), 0, s, ids, (const T*)dy, grad, rows, vocab, h, scale);
+    return hipGetLastError();
+  }
+  uint64_t bytes;
+  const Sorted w = layout(ws, rows, h, &bytes);
+  int bits = 1;
+  while (bits < 31 && (vocab - 1) >> bits) ++bits;
+  const int passes = (bits + 8) / 9, per_pass = (bits + passes - 1) / passes;
+  const unsigned tiles = ((unsigned)rows + SORT_T - 1) / SORT_T, per_group = (tiles + SORT_MAX_GROUPS - 1) / SORT_MAX_GROUPS * SORT_T;
+  const dim3 grid(((unsigned)rows + per_group - 1) / per_group);
+  for (int i = 0; i < passes; ++i) {
+    const int to = i & 1, now = i == passes - 1 ? bits - per_pass * i : per_pass;
+    if (i == 0) hipLaunchKernelGGL(embed_sort_kernel<true>, grid, dim3(SORT_T), 0, s, ids, nullptr, nullptr, w.key[to], w.row[to], w.count, (unsigned)rows, vocab, 0, now, per_group);
+    else hipLaunchKernelGGL(embed_sort_kernel<false>, grid, dim3(SORT_T), 0, s, nullptr, w.key[to ^ 1], w.row[to ^ 1], w.key[to], w.row[to], w.count, 0u, vocab, per_pass * i, now, per_group);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  const int last = (passes - 1) & 1;
+  hipLaunchKernelGGL(embed_sum_kernel<T>, dim3(min(rows, 1 << 20), slices), dim3(NT), 0, s, w.key[last], w.row[last], (const T*)dy, grad, w.count, w.long_runs, w.partial, h, scale);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL(embed_join_kernel, dim3(512), dim3(JOIN_T), 0, s, w.key[last], w.count, w.long_runs, w.partial, grad, h, scale);
+  return hipGetLastError();
 }
 
 }  // namespace
 
-uint64_t embed_bwd_ws_bytes(int rows, int h) { (void)h; return (uint64_t)rows * 8; }
+uint64_t embed_bwd_ws_bytes(int rows, int h) {
+  uint64_t bytes;
+  layout(nullptr, rows, h, &bytes);
+  return bytes;
+}
 
 hipError_t launch_embed_fwd(int dtype, const int* ids, const void* weight, void* out, int rows, unsigned vocab, int h, float scale, hipStream_t s) {
-  const size_t groups = ((size_t)rows * h / (dtype == DT_BF16 ? 8 : 4) + NT - 1) / NT;
-  const dim3 grid((unsigned)(groups > 8192 ? 8192 : groups));
-  if (dtype == DT_BF16) hipLaunchKernelGGL(embed_fwd_kernel<bf16_t>, grid, dim3(NT), 0, s, ids, (const bf16_t*)weight, (bf16_t*)out, rows, vocab, h, scale);
-  else hipLaunchKernelGGL(embed_fwd_kernel<float>, grid, dim3(NT), 0, s, ids, (const float*)weight, (float*)out, rows, vocab, h, scale);
+  constexpr int U = 2;
+  const unsigned per_row = (unsigned)h / (dtype == DT_BF16 ? 8 : 4);
+  const size_t total = (size_t)rows * per_row, groups = (total + NT * U - 1) / (NT * U);
+  const dim3 grid((unsigned)(groups > (1u << 20) ? 1u << 20 : groups));
+  if (dtype == DT_BF16) hipLaunchKernelGGL((embed_fwd_kernel<bf16_t, U>), grid, dim3(NT), 0, s, ids, (const bf16_t*)weight, (bf16_t*)out, total, per_row, vocab, scale);
+  else hipLaunchKernelGGL((embed_fwd_kernel<float, U>), grid, dim3(NT), 0, s, ids, (const float*)weight, (float*)out, total, per_row, vocab, scale);
   return hipGetLastError();
 }
 
 hipError_t launch_embed_bwd(int dtype, const int* ids, const void* dy, float* grad, void* ws, int rows, unsigned vocab, int h, float scale, hipStream_t s) {
-  unsigned* key = (unsigned*)ws;
-  unsigned* row_of = key + rows;
-  hipLaunchKernelGGL(embed_rank_kernel, dim3((rows + NT - 1) / NT), dim3(NT), 0, s, ids, key, row_of, rows, vocab);
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
-  if (dtype == DT_BF16) hipLaunchKernelGGL(embed_sum_kernel<bf16_t>, dim3(rows), dim3(NT), 0, s, key, row_of, (const bf16_t*)dy, grad, rows, h, scale);
-  else hipLaunchKernelGGL(embed_sum_kernel<float>, dim3(rows), dim3(NT), 0, s, key, row_of, (const float*)dy, grad, rows, h, scale);
-  return hipGetLastError();
+  return dtype == DT_BF16 ? run_embed_bwd<bf16_t>(ids, dy, grad, ws, rows, vocab, h, scale, s) : run_embed_bwd<float>(ids, dy, grad, ws, rows, vocab, h, scale, s);
 }

@@ -140,53 +140,56 @@ __global__ __launch_bounds__(W * R * 64) void norm_fwd_pack8_kernel(const T* __r
                                                                     float eps) {
   typedef Vec16<T> V;
   typedef typename KeepChunk<T>::codes_t codes_t;
-  __shared__ float red[2][R * W];
+  __shared__ float red[2][2][R * W];
   const int slot = threadIdx.x / (W * 64), l = threadIdx.x % (W * 64), wave = l >> 6, nb = keep_blocks(h);
-  const size_t row = (size_t)blockIdx.x * R + slot;
-  const bool on = row < (size_t)rows;
-  V v[C] = {};
+  int turn = 0;                                                        // what the last rows' sums stand in is not written again before the next barrier
+  for (size_t first = (size_t)blockIdx.x * R; first < (size_t)rows; first += (size_t)gridDim.x * R, turn ^= 1) {
+    const size_t row = first + slot;
+    const bool on = row < (size_t)rows;
+    V v[C] = {};
 #pragma unroll
-  for (int c = 0; c < C; ++c) {
-    const int col = (l + c * W * 64) * V::N;
-    if (on && col < h) v[c] = *reinterpret_cast<const V*>(x + row * h + col);
-  }
-  float mean = 0.f, s = 0.f;
-  if (LN) {
+    for (int c = 0; c < C; ++c) {
+      const int col = (l + c * W * 64) * V::N;
+      if (on && col < h) v[c] = *reinterpret_cast<const V*>(x + row * h + col);
+    }
+    float mean = 0.f, s = 0.f;
+    if (LN) {
 #pragma unroll
-    for (int c = 0; c < C; ++c)
+      for (int c = 0; c < C; ++c)
 #pragma unroll
-      for (int e = 0; e < V::N; ++e) s += v[c].get(e);
-    mean = row_sum<W>(s, red[0], slot, wave) / h;
-    s = 0.f;
-  }
+        for (int e = 0; e < V::N; ++e) s += v[c].get(e);
+      mean = row_sum<W>(s, red[turn][0], slot, wave) / h;
+      s = 0.f;
+    }
 #pragma unroll
-  for (int c = 0; c < C; ++c) {
-    if ((l + c * W * 64) * V::N < h)
+    for (int c = 0; c < C; ++c) {
+      if ((l + c * W * 64) * V::N < h)
 #pragma unroll
-      for (int e = 0; e < V::N; ++e) { const float d = v[c].get(e) - mean; s += d * d; }
-  }
-  const float r = rsqrtf(row_sum<W>(s, red[1], slot, wave) / h + eps);
-  if (on && l == 0) {
-    if (LN) { stats[2 * row] = mean; stats[2 * row + 1] = r; } else stats[row] = r;
-  }
+        for (int e = 0; e < V::N; ++e) { const float d = v[c].get(e) - mean; s += d * d; }
+    }
+    const float r = rsqrtf(row_sum<W>(s, red[turn][1], slot, wave) / h + eps);
+    if (on && l == 0) {
+      if (LN) { stats[2 * row] = mean; stats[2 * row + 1] = r; } else stats[row] = r;
+    }
 #pragma unroll
-  for (int c = 0; c < C; ++c) {
-    const int col = (l + c * W * 64) * V::N;
-    uint32_t byte;
-    const codes_t code = keep_chunk<T>(v[c], byte);
-    if (on && col < h) {
-      *reinterpret_cast<codes_t*>(codes + row * h + col) = code;
-      if (col % KEEP_BLOCK == 0) scales[row * nb + col / KEEP_BLOCK] = (uint8_t)byte;
-      const V g = *reinterpret_cast<const V*>(gamma + col);
-      V o, b;
-      if (LN) b = *reinterpret_cast<const V*>(beta + col);
+    for (int c = 0; c < C; ++c) {
+      const int col = (l + c * W * 64) * V::N;
+      uint32_t byte;
+      const codes_t code = keep_chunk<T>(v[c], byte);
+      if (on && col < h) {
+        *reinterpret_cast<codes_t*>(codes + row * h + col) = code;
+        if (col % KEEP_BLOCK == 0) scales[row * nb + col / KEEP_BLOCK] = (uint8_t)byte;
+        const V g = *reinterpret_cast<const V*>(gamma + col);
+        V o, b;
+        if (LN) b = *reinterpret_cast<const V*>(beta + col);
 #pragma unroll
-      for (int e = 0; e < V::N; ++e) {
-        float f = (v[c].get(e) - mean) * r * g.get(e);
-        if (LN) f += b.get(e);
-        o.set(e, f);
+        for (int e = 0; e < V::N; ++e) {
+          float f = (v[c].get(e) - mean) * r * g.get(e);
+          if (LN) f += b.get(e);
+          o.set(e, f);
+        }
+        *reinterpret_cast<V*>(out + row * h + col) = o;
       }
-      *reinterpret_cast<V*>(out + row * h + col) = o;
     }
   }
 }
@@ -518,7 +521,7 @@ template <typename T, bool LN>
 hipError_t run_norm_fwd_pack8(const void* x, const void* gamma, const void* beta, void* out, float* stats, uint8_t* codes, uint8_t* scales, int rows, int h, float eps,
                               hipStream_t s) {
   norm_division<T>(h, [&](auto w, auto c, auto r) {
-    hipLaunchKernelGGL((norm_fwd_pack8_kernel<T, LN, w, c, r>), dim3((rows + r - 1) / r), dim3(w * r * 64), 0, s, (const T*)x, (const T*)gamma, (const T*)beta, (T*)out, stats,
+    hipLaunchKernelGGL((norm_fwd_pack8_kernel<T, LN, w, c, r>), dim3(min((rows + r - 1) / r, 1 << 20)), dim3(w * r * 64), 0, s, (const T*)x, (const T*)gamma, (const T*)beta, (T*)out, stats,
                        codes, scales, rows, h, eps);
   });
   return hipGetLastError();
