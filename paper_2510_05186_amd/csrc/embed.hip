@@ -178,40 +178,96 @@ template <int N> __device__ __forceinline__ void add_to(float* g, const float* s
   }
 }
 
-// Wave (p, slice): place p of the sorted tokens, 64 chunks of columns.  It has work where a run of equal tokens begins at p, and at multiples of PIECE inside a run of more
-// than PIECE.  partial[2 k] is the sum of the piece that begins at place k PIECE, partial[2 k + 1] that of the piece of a long run that begins later in
-// that range (only one can: it goes on behind it).
+// Wave (w, slice): places w Q .. w Q + Q - 1 of the sorted tokens, 64 chunks of columns.  Its are the runs of equal tokens that begin there, to their ends, which lie up to
+// PIECE places on: one stretch of places, BATCH rows of dy in flight together with the accumulator's rows of the runs that end among them (with one run
+// to a wave, 4096 tokens took 41 us instead of 27: half of the waves find no run, the others wait for one row).  A run of more than PIECE places is cut at
+// multiples of PIECE: partial[2 k] is the sum of the piece that begins at place k PIECE, partial[2 k + 1] that of the piece of a long run that begins
+// later in that range (only one can: it goes on behind it).
+constexpr int Q = 8, BATCH = 8;
+static_assert(PIECE == 32 && PIECE % Q == 0 && Q + PIECE <= 63, "masks of 64 places");
 template <typename T>
 __global__ __launch_bounds__(NT) void embed_sum_kernel(const unsigned* __restrict__ key, const unsigned* __restrict__ row_of, const T* __restrict__ dy, float* __restrict__ grad,
-                                                       unsigned* count, unsigned* long_runs, float* __restrict__ partial, int h, float scale) {
-  constexpr int N = Vec16<T>::N;
-  const int lane = threadIdx.x & 63, slice = blockIdx.y * (NT / 64) + (threadIdx.x >> 6), col = (slice * 64 + lane) * N;
-  const unsigned m = count[0];
+                                                       unsigned* count, unsigned* long_runs, float* __restrict__ partial, int rows, int h, unsigned groups, float scale) {
+  typedef Vec16<T> V;
+  constexpr int N = V::N;
+  const int lane = threadIdx.x & 63, slice = (int)(blockIdx.x % groups) * (NT / 64) + (threadIdx.x >> 6), col = (slice * 64 + lane) * N;
   if (slice * 64 * N >= h) return;
-  for (unsigned p = blockIdx.x; p < m; p += gridDim.x) {
-    // bit j: place p - PIECE + j holds the same token
-    const unsigned id = key[p];
-    const long long j = (long long)p - PIECE + lane;
-    const unsigned long long same = __ballot(j >= 0 && j < (long long)m && key[j < 0 ? 0 : j] == id);
-    const bool first = !(same >> (PIECE - 1) & 1);
-    if (!first && p % PIECE) continue;
-    const int ahead = first ? 0 : __clzll((long long)~(same << (64 - PIECE)));        // places before p with the same token, of the last PIECE
-    const int here = __ffsll((long long)~(same >> PIECE)) - 1;                        // from p on, of the next PIECE (the bits shifted in are zero)
-    const bool longer = here == PIECE && p + PIECE < m && key[p + PIECE] == id;
-    // whether the run has more than PIECE places
-    const bool cut = first ? longer : ahead + here > PIECE || longer;
-    if (!first && !cut) continue;
-    const int n = cut ? min(here, (int)(PIECE - p % PIECE)) : here;
-    const unsigned row = lane < n ? row_of[p + lane] : 0u;
+  const bool on = col < h;
+  for (long long base = (long long)(blockIdx.x / groups) * Q; base < rows; base += (long long)(gridDim.x / groups) * Q) {
+    const long long m = count[0], xa = base - PIECE + lane, xb = base + PIECE + lane;
+    const auto inside = [&](long long x) { return x < 0 ? 0 : x < rows ? x : (long long)rows - 1; };
+    const unsigned ka = key[inside(xa)], kb = key[inside(xb)], row = row_of[inside(base + lane)];
+    if (base >= m) return;
+    // bit i of `starts`: a run begins at place base + i (or the tokens have ended); of `back`: at base - PIECE + i, the first of them not looked at
+    const unsigned pa = (unsigned)__shfl_up((int)ka, 1, 64), pb = (unsigned)__shfl_up((int)kb, 1, 64), last_a = (unsigned)__builtin_amdgcn_readlane((int)ka, 63);
+    const unsigned long long sa = __ballot(xa <= 0 || xa >= m || (lane > 0 && ka != pa)), sb = __ballot(xb >= m || kb != (lane > 0 ? pb : last_a));
+    const unsigned long long starts = sa >> 32 | sb << 32;
+    const unsigned back = (unsigned)sa & ~1u;
+    // a piece of a long run that began earlier: it has more than PIECE places, PIECE of them before this or from its begin to its end
+    bool resumed = base % PIECE == 0 && !(starts & 1);
+    if (resumed && back) {
+      const int ahead = __clz((int)back) + 1, here = starts ? __ffsll((long long)starts) - 1 : 64;
+      resumed = ahead + here > PIECE;
+    }
+    const int many = m - base < Q ? (int)(m - base) : Q;
+    const unsigned long long mine = starts & ((1ull << many) - 1);
+    if (!resumed && !mine) continue;
+    const int first = resumed ? 0 : __ffsll((long long)mine) - 1, last = mine ? 63 - __clzll((long long)mine) : 0;   // places of the first and last run or piece
+    const unsigned long long behind = starts & ~((2ull << last) - 1);
+    int end = behind ? __ffsll((long long)behind) - 1 : 64;
+    const bool cut = !mine || end - last > PIECE;                       // the last one is a piece
+    if (cut) end = min(end, (int)(PIECE - (base + last) % PIECE) + last);
+    const int resumed_end = !resumed ? -1 : (mine ? __ffsll((long long)mine) - 1 : end);
+    if (cut && mine && slice == 0 && lane == 0) long_runs[atomicAdd(&count[1], 1u)] = (unsigned)(base + last);
     float s[N] = {};
-    add_rows(dy, row, n, (size_t)h, col, col < h, s);
-    if (cut && first && slice == 0 && lane == 0) long_runs[atomicAdd(&count[1], 1u)] = p;
-    if (col >= h) continue;
-    if (!cut) add_to<N>(grad + (size_t)id * h + col, s, scale);
-    else {
-      float* to = partial + (size_t)(p / PIECE * 2 + (p % PIECE ? 1 : 0)) * h + col;
+    for (int i = first; i < end; i += BATCH) {
+      V v[BATCH];
+      f32x4_t g[BATCH][N / 4];
+      float* to[BATCH];
 #pragma unroll
-      for (int i = 0; i < N; i += 4) *reinterpret_cast<f32x4_t*>(to + i) = (f32x4_t){s[i], s[i + 1], s[i + 2], s[i + 3]};
+      for (int u = 0; u < BATCH; ++u)
+        if (i + u < end) {
+          const size_t r = (unsigned)__builtin_amdgcn_readlane((int)row, i + u);
+          if (on) v[u] = *reinterpret_cast<const V*>(dy + r * h + col);
+        }
+#pragma unroll
+      for (int u = 0; u < BATCH; ++u) {
+        const int next = i + u + 1;
+        to[u] = nullptr;
+        if (next <= end && (next == end || (starts >> next & 1))) {
+          const bool piece = next == resumed_end || (cut && next == end);
+          if (piece) {
+            const unsigned long long at = (unsigned long long)base + (next == resumed_end ? 0 : last);
+            to[u] = partial + (size_t)(at / PIECE * 2 + (at % PIECE ? 1 : 0)) * h + col;
+#pragma unroll
+            for (int c = 0; c < N / 4; ++c) g[u][c] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
+          } else {
+            const int x = next - 1;
+            const size_t id = (unsigned)(x < PIECE ? __builtin_amdgcn_readlane((int)ka, x + PIECE) : __builtin_amdgcn_readlane((int)kb, x - PIECE));
+            to[u] = grad + id * h + col;
+            if (on)
+#pragma unroll
+              for (int c = 0; c < N / 4; ++c) g[u][c] = *reinterpret_cast<const f32x4_t*>(to[u] + 4 * c);
+          }
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < BATCH; ++u) {
+        if (i + u < end)
+#pragma unroll
+          for (int e = 0; e < N; ++e) s[e] += v[u].get(e);
+        if (to[u]) {
+          const float by = (i + u + 1 == resumed_end || (cut && i + u + 1 == end)) ? 1.f : scale;
+#pragma unroll
+          for (int e = 0; e < N; ++e) {
+            g[u][e / 4][e % 4] += by * s[e];
+            s[e] = 0.f;
+          }
+          if (on)
+#pragma unroll
+            for (int c = 0; c < N / 4; ++c) *reinterpret_cast<f32x4_t*>(to[u] + 4 * c) = g[u][c];
+        }
+      }
     }
   }
 }
@@ -229,12 +285,12 @@ __global__ __launch_bounds__(JOIN_T) void embed_join_kernel(const unsigned* __re
   for (unsigned long long item = blockIdx.x; item < items; item += gridDim.x) {
     const unsigned p = long_runs[item / slices], id = key[p];
     const int col = (int)(item % slices) * 256 + lane * 4;
-    unsigned lo = p, hi = m;                                             // the run's end: the first place of a larger token
-    while (hi - lo > 1) {
-      const unsigned mid = lo + (hi - lo) / 2;
-      if (key[mid] == id) lo = mid; else hi = mid;
+    const unsigned k0 = p / PIECE + 1;
+    unsigned pieces = 0;                                                 // behind the first one: places k PIECE that still hold the token
+    for (unsigned long long more = ~0ull; more == ~0ull; pieces += more == ~0ull ? 64 : __ffsll((long long)~more) - 1) {
+      const unsigned long long x = ((unsigned long long)k0 + pieces + lane) * PIECE;
+      more = __ballot(x < m && key[x < m ? x : 0] == id);
     }
-    const unsigned k0 = p / PIECE + 1, pieces = (hi - 1) / PIECE + 1 - k0;   // behind the first piece
     f32x4_t s = {0.f, 0.f, 0.f, 0.f};
     if (col < h) {
       if (wave == 0) s = *reinterpret_cast<const f32x4_t*>(partial + (size_t)(p / PIECE * 2 + (p % PIECE ? 1 : 0)) * h + col);
@@ -324,7 +380,8 @@ hipError_t run_embed_bwd(const int* ids, const void* dy, float* grad, void* ws, 
     if (e != hipSuccess) return e;
   }
   const int last = (passes - 1) & 1;
-  hipLaunchKernelGGL(embed_sum_kernel<T>, dim3(min(rows, 1 << 20), slices), dim3(NT), 0, s, w.key[last], w.row[last], (const T*)dy, grad, w.count, w.long_runs, w.partial, h, scale);
+  hipLaunchKernelGGL(embed_sum_kernel<T>, dim3(min((rows + Q - 1) / Q, max(1, (1 << 22) / (int)slices)) * slices), dim3(NT), 0, s, w.key[last], w.row[last],
+                     (const T*)dy, grad, w.count, w.long_runs, w.partial, rows, h, slices, scale);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   hipLaunchKernelGGL(embed_join_kernel, dim3(512), dim3(JOIN_T), 0, s, w.key[last], w.count, w.long_runs, w.partial, grad, h, scale);
