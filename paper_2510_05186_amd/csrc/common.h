@@ -97,6 +97,21 @@ __device__ __forceinline__ float wave_max(float v) {
   return v;
 }
 
+// n / d for n < 2^31 by a multiplication: with 2^(l - 1) < d <= 2^l and m = ceil(2^(31 + l) / d) < 2^32, m d = 2^(31 + l) + e with e < d <= 2^l, so that
+// n m / 2^(31 + l) is n / d plus less than 1 / d: the same whole part
+struct Divisor {
+  unsigned d, m, shift;
+  Divisor() = default;
+  explicit Divisor(unsigned divisor) : d(divisor) {
+    int l = 1;
+    while (l < 31 && (1u << l) < d) ++l;
+    m = (unsigned)(((1ull << (31 + l)) + d - 1) / d);
+    shift = (unsigned)(l - 1);
+    if (d == 1) m = 0;
+  }
+  __device__ __forceinline__ unsigned quotient(unsigned n) const { return d == 1 ? n : __umulhi(n, m) >> shift; }
+};
+
 // launchers implemented in the .hip files; all return hipError_t from the launch
 int attn_dkv_split(int seq, int batch, int n_q, int n_kv);
 struct GemmProblem { const void* A; const void* B; void* C; const void* R; int M, N, lda, ldb, ldc; };

@@ -14,22 +14,26 @@ constexpr int NT = 256;
 // ---- lookup -----------------------------------------------------------------------------------------------
 // 16 bytes a lane; chunks numbered through all rows
 template <typename T, int U>
-__global__ __launch_bounds__(NT) void embed_fwd_kernel(const int* __restrict__ ids, const T* __restrict__ weight, T* __restrict__ out, size_t total, unsigned per_row,
+__global__ __launch_bounds__(NT) void embed_fwd_kernel(const int* __restrict__ ids, const T* __restrict__ weight, T* __restrict__ out, size_t total, const Divisor per_row,
                                                        unsigned vocab, float scale) {
   typedef Vec16<T> V;
   for (size_t base = blockIdx.x * (size_t)(NT * U); base < total; base += (size_t)gridDim.x * (NT * U)) {
-    const size_t row0 = total >> 32 ? base / per_row : (size_t)((unsigned)base / per_row);
-    const unsigned c0 = (unsigned)(base - row0 * per_row);
+    size_t row0 = 0;
+    unsigned c0 = (unsigned)base;
+    if (total >> 31) {
+      row0 = base / per_row.d;
+      c0 = (unsigned)(base - row0 * per_row.d);
+    }
     V v[U];
     bool word[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const unsigned i = u * NT + threadIdx.x, n = c0 + i, r = n / per_row;
+      const unsigned i = u * NT + threadIdx.x, n = c0 + i, r = per_row.quotient(n);
       word[u] = false;
       if (base + i < total) {
         const unsigned id = (unsigned)ids[row0 + r];
         word[u] = id < vocab;
-        if (word[u]) v[u] = *reinterpret_cast<const V*>(weight + ((size_t)id * per_row + (n - r * per_row)) * V::N);
+        if (word[u]) v[u] = *reinterpret_cast<const V*>(weight + ((size_t)id * per_row.d + (n - r * per_row.d)) * V::N);
       }
     }
 #pragma unroll
@@ -401,8 +405,8 @@ hipError_t launch_embed_fwd(int dtype, const int* ids, const void* weight, void*
   const unsigned per_row = (unsigned)h / (dtype == DT_BF16 ? 8 : 4);
   const size_t total = (size_t)rows * per_row, groups = (total + NT * U - 1) / (NT * U);
   const dim3 grid((unsigned)(groups > (1u << 20) ? 1u << 20 : groups));
-  if (dtype == DT_BF16) hipLaunchKernelGGL((embed_fwd_kernel<bf16_t, U>), grid, dim3(NT), 0, s, ids, (const bf16_t*)weight, (bf16_t*)out, total, per_row, vocab, scale);
-  else hipLaunchKernelGGL((embed_fwd_kernel<float, U>), grid, dim3(NT), 0, s, ids, (const float*)weight, (float*)out, total, per_row, vocab, scale);
+  if (dtype == DT_BF16) hipLaunchKernelGGL((embed_fwd_kernel<bf16_t, U>), grid, dim3(NT), 0, s, ids, (const bf16_t*)weight, (bf16_t*)out, total, Divisor(per_row), vocab, scale);
+  else hipLaunchKernelGGL((embed_fwd_kernel<float, U>), grid, dim3(NT), 0, s, ids, (const float*)weight, (float*)out, total, Divisor(per_row), vocab, scale);
   return hipGetLastError();
 }
 

@@ -44,6 +44,22 @@ template <> struct KeepChunk<float> {
   static constexpr int LANES = 8;
 };
 template <int CTRL> __device__ __forceinline__ uint32_t lane_swap(uint32_t v) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xf, 0xf, true); }
+// The sum over G lanes side by side (a power of two from 4 to 64), in all of them: lane swaps, no LDS
+template <int G> __device__ __forceinline__ float lanes_sum(float v) {
+  v += __uint_as_float(lane_swap<0xB1>(__float_as_uint(v)));          // lane ^ 1
+  v += __uint_as_float(lane_swap<0x4E>(__float_as_uint(v)));          // lane ^ 2
+  if (G >= 8) v += __uint_as_float(lane_swap<0x141>(__float_as_uint(v)));    // 7 - lane of eight
+  if (G >= 16) v += __uint_as_float(lane_swap<0x140>(__float_as_uint(v)));   // 15 - lane of sixteen
+  if (G >= 32) {
+    const auto p = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = __uint_as_float(p[0]) + __uint_as_float(p[1]);
+  }
+  if (G >= 64) {
+    const auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = __uint_as_float(p[0]) + __uint_as_float(p[1]);
+  }
+  return v;
+}
 template <typename T> __device__ __forceinline__ uint32_t keep_block_max(uint32_t v) {
   v = max(v, lane_swap<0xB1>(v));                                     // lane ^ 1
   v = max(v, lane_swap<0x4E>(v));                                     // lane ^ 2

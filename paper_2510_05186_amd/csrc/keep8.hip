@@ -47,24 +47,27 @@ __global__ __launch_bounds__(NT) void unpack8_kernel(const uint8_t* __restrict__
 // loads are in flight before the first is used.
 struct Chunks {
   size_t total;          // rows * per_row
-  unsigned per_row;      // chunks of a row, padded to whole blocks
+  Divisor per_row;       // chunks of a row, padded to whole blocks: less than 2^28
 };
 template <typename T> Chunks chunks_of(int rows, int cols) {
   const unsigned per_row = (unsigned)keep_blocks(cols) * KeepChunk<T>::LANES;
-  return {(size_t)rows * per_row, per_row};
+  return {(size_t)rows * per_row, Divisor(per_row)};
 }
 struct At { size_t row; int col; };
 // chunk base + i, for base a multiple of NT * U and i < NT * U
 template <typename T> struct Walk {
-  size_t row0;
-  unsigned c0, per_row;
-  __device__ __forceinline__ Walk(size_t base, const Chunks& k) : per_row(k.per_row) {
-    row0 = k.total >> 32 ? base / k.per_row : (size_t)((unsigned)base / k.per_row);
-    c0 = (unsigned)(base - row0 * k.per_row);
+  size_t row0 = 0;
+  unsigned c0;
+  Divisor per_row;
+  __device__ __forceinline__ Walk(size_t base, const Chunks& k) : c0((unsigned)base), per_row(k.per_row) {
+    if (k.total >> 31) {
+      row0 = base / per_row.d;
+      c0 = (unsigned)(base - row0 * per_row.d);
+    }
   }
   __device__ __forceinline__ At at(unsigned i) const {
-    const unsigned n = c0 + i, r = n / per_row;
-    return {row0 + r, (int)((n - r * per_row) * Vec16<T>::N)};
+    const unsigned n = c0 + i, r = per_row.quotient(n);
+    return {row0 + r, (int)((n - r * per_row.d) * Vec16<T>::N)};
   }
 };
 
@@ -124,7 +127,7 @@ __global__ __launch_bounds__(NT) void unpack8_vec_kernel(const uint8_t* __restri
 // A row belongs to W waves, R rows to a workgroup; a lane holds C chunks of its row, W * 64 chunks apart.  The W waves of a row add up their sums
 // through LDS (`red`, of its own for every use).
 template <int W> __device__ __forceinline__ float row_sum(float v, float* red /* [R * W] */, int slot, int wave) {
-  v = wave_sum(v);
+  v = lanes_sum<64>(v);
   if (W == 1) return v;
   if ((threadIdx.x & 63) == 0) red[slot * W + wave] = v;
   __syncthreads();
@@ -204,7 +207,7 @@ __global__ __launch_bounds__(W * R * 64) void norm_bwd8_kernel(const T* dn, cons
   typedef Vec16<T> V;
   typedef typename KeepChunk<T>::codes_t codes_t;
   __shared__ float red[2][2][R * W];
-  __shared__ float sums[R > 1 ? W * 64 * C * V::N : 1];
+  __shared__ f32x4_t sums[R > 1 ? R : 1][R > 1 ? C * V::N / 4 : 1][W * 64];      // 32 KB
   const int slot = threadIdx.x / (W * 64), l = threadIdx.x % (W * 64), wave = l >> 6, nb = keep_blocks(h);
   float pg[C][V::N] = {}, pb[LN ? C : 1][V::N] = {};
   V gv[C];
@@ -250,8 +253,8 @@ __global__ __launch_bounds__(W * R * 64) void norm_bwd8_kernel(const T* dn, cons
       }
     }
     // both sums behind one barrier; the next row's take the other half of red
-    sgx = wave_sum(sgx);
-    if (LN) sg = wave_sum(sg);
+    sgx = lanes_sum<64>(sgx);
+    if (LN) sg = lanes_sum<64>(sg);
     if (W > 1) {
       if ((threadIdx.x & 63) == 0) {
         red[turn][0][slot * W + wave] = sgx;
@@ -300,20 +303,27 @@ __global__ __launch_bounds__(W * R * 64) void norm_bwd8_kernel(const T* dn, cons
   for (int part = 0; part < (LN ? 2 : 1); ++part) {
     float (&p)[C][V::N] = part ? reinterpret_cast<float (&)[C][V::N]>(pb) : pg;
     float* to = partial + ((size_t)part * gridDim.x + blockIdx.x) * h;
-    for (int i = 0; i < R; ++i) {
-      if (R > 1) __syncthreads();
-      if (slot != i) continue;
+    if (R > 1) {
+      if (part) __syncthreads();
+#pragma unroll
+      for (int c = 0; c < C; ++c)
+#pragma unroll
+        for (int e = 0; e < V::N; e += 4) sums[slot][(c * V::N + e) / 4][l] = (f32x4_t){p[c][e], p[c][e + 1], p[c][e + 2], p[c][e + 3]};
+      __syncthreads();
+      for (int i = threadIdx.x; i < C * V::N / 4 * W * 64; i += W * R * 64) {
+        const int q = i / (W * 64), lane = i % (W * 64), at = (lane + q / (V::N / 4) * W * 64) * V::N + q % (V::N / 4) * 4;
+        f32x4_t t = sums[0][q][lane];
+#pragma unroll
+        for (int k = 1; k < R; ++k) t += sums[k][q][lane];
+        if (at < h) *reinterpret_cast<f32x4_t*>(to + at) = t;
+      }
+    } else {
 #pragma unroll
       for (int c = 0; c < C; ++c) {
         const int at = (l + c * W * 64) * V::N;
         if (at < h)
 #pragma unroll
-          for (int e = 0; e < V::N; ++e) {
-            float t = p[c][e];
-            if (R > 1 && i > 0) t += sums[at + e];
-            if (R > 1 && i < R - 1) sums[at + e] = t;
-            else to[at + e] = t;
-          }
+          for (int e = 0; e < V::N; e += 4) *reinterpret_cast<f32x4_t*>(to + at + e) = (f32x4_t){p[c][e], p[c][e + 1], p[c][e + 2], p[c][e + 3]};
       }
     }
   }
@@ -338,8 +348,7 @@ __global__ __launch_bounds__(1024) void add_columns_kernel(const float* __restri
   __syncthreads();
   // a wave adds up two columns, 32 lanes each
   float t = red[threadIdx.x & 31][threadIdx.x >> 5];
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) t += __shfl_xor(t, o, 64);
+  t = lanes_sum<32>(t);
   const int out = blockIdx.x * 32 + (threadIdx.x >> 5);
   if ((threadIdx.x & 31) == 0 && out < cols) (blockIdx.y ? dst1 : dst0)[out] += t;
 }

@@ -16,15 +16,6 @@ constexpr int NT = 256;
 // backward as many as the compute units hold at once, four on each (512: 118 us, 768: 100, 1024: 94).
 constexpr int FWD_GROUPS = 8192, BWD_GROUPS = 1024;
 
-template <int G> __device__ __forceinline__ float group_sum(float v) {
-  v += __uint_as_float(lane_swap<0xB1>(__float_as_uint(v)));          // lane ^ 1
-  v += __uint_as_float(lane_swap<0x4E>(__float_as_uint(v)));          // lane ^ 2
-  if (G >= 8) v += __uint_as_float(lane_swap<0x141>(__float_as_uint(v)));    // 7 - lane of eight
-  if (G >= 16) v += __uint_as_float(lane_swap<0x140>(__float_as_uint(v)));   // 15 - lane of sixteen
-  if (G >= 32) v += __shfl_xor(v, 16, 64);
-  return v;
-}
-
 // item = row * heads + head
 struct Items {
   size_t total;
@@ -44,7 +35,7 @@ template <int S> struct Cursor {
   __device__ __forceinline__ explicit Cursor(const Items& k) {
     base = (size_t)blockIdx.x * S;
     step = (size_t)gridDim.x * S;                                      // < 2^32
-    row = (unsigned)(k.total >> 32 ? base / k.heads : (unsigned)base / k.heads);
+    row = (unsigned)(base / k.heads);
     head = (unsigned)(base - (size_t)row * k.heads);
     pos = row % k.seq;
     step_row = (unsigned)step / k.heads;
@@ -146,7 +137,7 @@ __global__ __launch_bounds__(NT) void qknorm_kernel(const QkNorm p) {
           v[i][e] = x[i].get(e);
           s += v[i][e] * v[i][e];
         }
-      r = rsqrtf(group_sum<G>(s) / p.d + p.eps);
+      r = rsqrtf(lanes_sum<G>(s) / p.d + p.eps);
       if (on && turn && col == 0) p.stats[(size_t)k.row * n_rot + k.head] = r;
       if constexpr (KEEP) {
 #pragma unroll
@@ -265,7 +256,7 @@ __global__ __launch_bounds__(NT) void qknorm_bwd_kernel(const QkNormBwd p) {
               for (int e = 0; e < N; ++e) dg[q][i][e] = fmaf(n[i][e], xh[i][e], dg[q][i][e]);
       }
     }
-    const float m = group_sum<G>(s) / p.d;
+    const float m = lanes_sum<G>(s) / p.d;
     if (!on) continue;
     T* out = (T*)p.dx + first;
     if (turn) {
