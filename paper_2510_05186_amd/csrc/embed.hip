@@ -47,55 +47,102 @@ __global__ __launch_bounds__(NT) void embed_fwd_kernel(const int* __restrict__ i
 }
 
 // ---- sort ---------------------------------------------------------------------------------------------------
-// One pass of a stable radix sort by up to 9 bits of the id in one launch: every workgroup counts the digits of ALL keys (they come out of the L2;
-// 16384 keys are 64 KB), those ahead of its own range apart, which gives it the place of each of its digits without waiting for the others.  The first
-// pass takes the ids themselves and leaves out those that are no words.
-constexpr int SORT_T = 1024, RADIX = 512, COPIES = 8;                   // counters in 8 copies by lane: equal digits of a wave meet 8 at a time at most
-constexpr int SORT_MAX_GROUPS = 256;
+// A stable radix sort by up to 9 bits of the id per pass.  Up to 16384 keys a pass is one launch: every workgroup counts the digits of ALL keys (they come out
+// of the L2, 64 KB at most), those ahead of its own range apart, which gives it the place of each of its digits without waiting for the others.
+// Beyond that a launch ahead of it counts each range once (65536 tokens, 256 columns: TABLE_US us with it, 75 without).  The first pass takes the ids
+// themselves and leaves out those that are no words.
+constexpr int RADIX = 512, COPIES = 8;                                  // counters in 8 copies by lane: equal digits of a wave meet 8 at a time at most
+constexpr int SORT_MAX_GROUPS = 256, SORT_COUNTED = 16384;
 
 struct Sorted {
   unsigned* count;                                                      // [0] valid tokens, [1] runs in `long_runs`
   unsigned* long_runs;
-  unsigned *key[2], *row[2];
+  unsigned *key[2], *row[2];                                            // pass i leaves its order in i & 1
+  unsigned* table;                                                      // keys of each range by digit, beyond SORT_COUNTED
   float* partial;
 };
 
-template <bool FIRST>
-__global__ __launch_bounds__(SORT_T) void embed_sort_kernel(const int* __restrict__ ids, const unsigned* __restrict__ key_in, const unsigned* __restrict__ row_in,
-                                                            unsigned* __restrict__ key_out, unsigned* __restrict__ row_out, unsigned* count, unsigned n, unsigned vocab,
-                                                            int shift, int bits, unsigned per_group) {
-  __shared__ unsigned hist[2][RADIX * COPIES];                          // ahead of the range, and the rest
-  __shared__ unsigned place[RADIX], wave_total[SORT_T / 64];
-  const unsigned tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, digits = 1u << bits, mask = digits - 1;
-  if (!FIRST) n = count[0];
-  const unsigned begin = min(n, blockIdx.x * per_group), end = min(n, begin + per_group);
-  for (unsigned i = tid; i < digits * COPIES; i += SORT_T) hist[0][i] = hist[1][i] = 0;
+struct Pass {
+  int shift, bits, number;
+  unsigned rows, vocab, per_group;
+};
+__device__ __forceinline__ void count_digits(unsigned (&hist)[RADIX * COPIES], unsigned digit) { atomicAdd(&hist[digit * COPIES + (threadIdx.x & (COPIES - 1))], 1u); }
+
+// table[g][d]: keys of digit d in range g
+__global__ __launch_bounds__(1024) void embed_count_kernel(const unsigned* __restrict__ ids, const Sorted w, const Pass p) {
+  __shared__ unsigned hist[RADIX * COPIES];
+  const unsigned tid = threadIdx.x, digits = 1u << p.bits, n = p.number == 0 ? p.rows : w.count[0];
+  const unsigned* key_in = p.number == 0 ? ids : w.key[(p.number - 1) & 1];
+  const unsigned begin = min(n, blockIdx.x * p.per_group), end = min(n, begin + p.per_group);
+  for (unsigned i = tid; i < digits * COPIES; i += 1024) hist[i] = 0;
   __syncthreads();
-  auto key_at = [&](unsigned i) { return FIRST ? (unsigned)ids[i] : key_in[i]; };
-  for (unsigned i0 = 0; i0 < n; i0 += SORT_T * 8) {
-    unsigned k[8];
-#pragma unroll
-    for (int u = 0; u < 8; ++u) {
-      const unsigned i = i0 + u * SORT_T + tid;
-      k[u] = i < n ? key_at(i) : 0xffffffffu;
-    }
-#pragma unroll
-    for (int u = 0; u < 8; ++u) {
-      const unsigned i = i0 + u * SORT_T + tid;
-      if (i < n && k[u] < vocab) atomicAdd(&hist[i < begin ? 0 : 1][(k[u] >> shift & mask) * COPIES + (lane & (COPIES - 1))], 1u);
-    }
+  for (unsigned i = begin + tid; i < end; i += 1024) {
+    const unsigned k = key_in[i];
+    if (k < p.vocab) count_digits(hist, k >> p.shift & (digits - 1));
   }
   __syncthreads();
+  for (unsigned d = tid; d < digits; d += 1024) {
+    unsigned s = 0;
+#pragma unroll
+    for (int c = 0; c < COPIES; ++c) s += hist[d * COPIES + c];
+    w.table[blockIdx.x * digits + d] = s;
+  }
+}
+
+template <int THREADS>
+__global__ __launch_bounds__(THREADS) void embed_sort_kernel(const unsigned* __restrict__ ids, const Sorted w, const Pass p, int counted) {
+  constexpr int WAVES = THREADS / 64;
+  __shared__ union {
+    unsigned hist[2][RADIX * COPIES];                                   // ahead of the range, and the rest
+    unsigned wave_count[WAVES][RADIX];
+  } lds;
+  __shared__ unsigned place[RADIX], wave_total[WAVES];
+  const unsigned tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, digits = 1u << p.bits, mask = digits - 1;
+  const unsigned n = p.number == 0 ? p.rows : w.count[0];
+  const unsigned* key_in = p.number == 0 ? ids : w.key[(p.number - 1) & 1];
+  const unsigned* row_in = w.row[(p.number - 1) & 1];
+  unsigned *key_out = w.key[p.number & 1], *row_out = w.row[p.number & 1];
+  const unsigned begin = min(n, blockIdx.x * p.per_group), end = min(n, begin + p.per_group);
+  unsigned ahead = 0, all = 0;                                          // of digit tid: keys ahead of the range, and all
+  if (counted) {
+    if (tid < digits)
+      for (unsigned g0 = 0; g0 < gridDim.x; g0 += 16) {
+        unsigned c[16];
+#pragma unroll
+        for (int u = 0; u < 16; ++u) c[u] = g0 + u < gridDim.x ? w.table[(g0 + u) * digits + tid] : 0u;
+#pragma unroll
+        for (int u = 0; u < 16; ++u) {
+          ahead += g0 + u < blockIdx.x ? c[u] : 0u;
+          all += c[u];
+        }
+      }
+  } else {
+    for (unsigned i = tid; i < digits * COPIES; i += THREADS) lds.hist[0][i] = lds.hist[1][i] = 0;
+    __syncthreads();
+    for (unsigned i0 = 0; i0 < n; i0 += THREADS * 8) {
+      unsigned k[8];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        const unsigned i = i0 + u * THREADS + tid;
+        k[u] = i < n ? key_in[i] : 0xffffffffu;
+      }
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        const unsigned i = i0 + u * THREADS + tid;
+        if (i < n && k[u] < p.vocab) count_digits(lds.hist[i < begin ? 0 : 1], k[u] >> p.shift & mask);
+      }
+    }
+    __syncthreads();
+    if (tid < digits) {
+#pragma unroll
+      for (int c = 0; c < COPIES; ++c) {
+        ahead += lds.hist[0][tid * COPIES + c];
+        all += lds.hist[1][tid * COPIES + c];
+      }
+      all += ahead;
+    }
+  }
   // place[d]: keys of smaller digits, and those of digit d ahead of the range
-  unsigned ahead = 0, all = 0;
-  if (tid < digits) {
-#pragma unroll
-    for (int c = 0; c < COPIES; ++c) {
-      ahead += hist[0][tid * COPIES + c];
-      all += hist[1][tid * COPIES + c];
-    }
-    all += ahead;
-  }
   unsigned before = all;                                                // inclusive scan over the wave, then over the waves
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) {
@@ -106,49 +153,47 @@ __global__ __launch_bounds__(SORT_T) void embed_sort_kernel(const int* __restric
   __syncthreads();
   unsigned sum = 0;
 #pragma unroll
-  for (int w = 0; w < SORT_T / 64; ++w) {
-    if ((unsigned)w == wave) before += sum;
-    sum += wave_total[w];
+  for (int v = 0; v < WAVES; ++v) {
+    if ((unsigned)v == wave) before += sum;
+    sum += wave_total[v];
   }
   if (tid < digits) place[tid] = before - all + ahead;
-  if (FIRST && blockIdx.x == 0 && tid == 0) { count[0] = sum; count[1] = 0; }
-  // the range, SORT_T keys at a time: a lane's place is its digit's, past the waves ahead and the lanes of its own wave ahead with the same digit
-  unsigned (&wave_count)[SORT_T / 64][RADIX] = reinterpret_cast<unsigned (&)[SORT_T / 64][RADIX]>(hist);
-  for (unsigned i0 = begin; i0 < end; i0 += SORT_T) {
+  if (p.number == 0 && blockIdx.x == 0 && tid == 0) { w.count[0] = sum; w.count[1] = 0; }
+  // the range, THREADS keys at a time: a lane's place is its digit's, past the waves ahead and the lanes of its own wave ahead with the same digit
+  for (unsigned i0 = begin; i0 < end; i0 += THREADS) {
     __syncthreads();
-    for (unsigned i = tid; i < (SORT_T / 64) * RADIX; i += SORT_T) (&wave_count[0][0])[i] = 0;
+    for (unsigned i = tid; i < (unsigned)WAVES << p.bits; i += THREADS) lds.wave_count[i >> p.bits][i & mask] = 0;
     __syncthreads();
     const unsigned i = i0 + tid;
-    const unsigned key = i < end ? key_at(i) : 0xffffffffu;
-    const bool on = key < vocab;
-    const unsigned d = key >> shift & mask;
+    const unsigned key = i < end ? key_in[i] : 0xffffffffu;
+    const bool on = key < p.vocab;
+    const unsigned d = key >> p.shift & mask;
     unsigned long long same = __ballot(on);
-    for (int b = 0; b < bits; ++b) {
+    for (int b = 0; b < p.bits; ++b) {
       const unsigned long long set = __ballot(d >> b & 1);
       same &= d >> b & 1 ? set : ~set;
     }
     const unsigned rank = __popcll(same & ((1ull << lane) - 1));
-    if (on && rank == 0) wave_count[wave][d] = __popcll(same);
+    if (on && rank == 0) lds.wave_count[wave][d] = __popcll(same);
     __syncthreads();
     if (tid < digits) {
       unsigned at = place[tid];
 #pragma unroll
-      for (int w = 0; w < SORT_T / 64; ++w) {
-        const unsigned c = wave_count[w][tid];
-        wave_count[w][tid] = at;
+      for (int v = 0; v < WAVES; ++v) {
+        const unsigned c = lds.wave_count[v][tid];
+        lds.wave_count[v][tid] = at;
         at += c;
       }
       place[tid] = at;
     }
     __syncthreads();
     if (on) {
-      const unsigned at = wave_count[wave][d] + rank;
+      const unsigned at = lds.wave_count[wave][d] + rank;
       key_out[at] = key;
-      row_out[at] = FIRST ? i : row_in[i];
+      row_out[at] = p.number == 0 ? i : row_in[i];
     }
   }
 }
-static_assert(sizeof(unsigned) * 2 * RADIX * COPIES >= sizeof(unsigned) * (SORT_T / 64) * RADIX, "the waves' counts lie in the histogram's place");
 
 // ---- sums -----------------------------------------------------------------------------------------------------
 constexpr int PIECE = 32;                                               // rows that one wave adds up
@@ -227,12 +272,12 @@ __global__ __launch_bounds__(NT) void embed_sum_kernel(const unsigned* __restric
     for (int i = first; i < end; i += BATCH) {
       V v[BATCH];
       f32x4_t g[BATCH][N / 4];
-      float* to[BATCH];
+      float* to[BATCH];                                                 // rows, the same for the whole wave
 #pragma unroll
       for (int u = 0; u < BATCH; ++u)
         if (i + u < end) {
           const size_t r = (unsigned)__builtin_amdgcn_readlane((int)row, i + u);
-          if (on) v[u] = *reinterpret_cast<const V*>(dy + r * h + col);
+          if (on) v[u].v = __builtin_nontemporal_load(&reinterpret_cast<const V*>(dy + r * h + col)->v);   // read once: 86 -> 75 us at 16384 x 5120
         }
 #pragma unroll
       for (int u = 0; u < BATCH; ++u) {
@@ -242,16 +287,16 @@ __global__ __launch_bounds__(NT) void embed_sum_kernel(const unsigned* __restric
           const bool piece = next == resumed_end || (cut && next == end);
           if (piece) {
             const unsigned long long at = (unsigned long long)base + (next == resumed_end ? 0 : last);
-            to[u] = partial + (size_t)(at / PIECE * 2 + (at % PIECE ? 1 : 0)) * h + col;
+            to[u] = partial + (size_t)(at / PIECE * 2 + (at % PIECE ? 1 : 0)) * h;
 #pragma unroll
             for (int c = 0; c < N / 4; ++c) g[u][c] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
           } else {
             const int x = next - 1;
             const size_t id = (unsigned)(x < PIECE ? __builtin_amdgcn_readlane((int)ka, x + PIECE) : __builtin_amdgcn_readlane((int)kb, x - PIECE));
-            to[u] = grad + id * h + col;
+            to[u] = grad + id * h;
             if (on)
 #pragma unroll
-              for (int c = 0; c < N / 4; ++c) g[u][c] = *reinterpret_cast<const f32x4_t*>(to[u] + 4 * c);
+              for (int c = 0; c < N / 4; ++c) g[u][c] = *reinterpret_cast<const f32x4_t*>(to[u] + col + 4 * c);
           }
         }
       }
@@ -269,7 +314,7 @@ __global__ __launch_bounds__(NT) void embed_sum_kernel(const unsigned* __restric
           }
           if (on)
 #pragma unroll
-            for (int c = 0; c < N / 4; ++c) *reinterpret_cast<f32x4_t*>(to[u] + 4 * c) = g[u][c];
+            for (int c = 0; c < N / 4; ++c) *reinterpret_cast<f32x4_t*>(to[u] + col + 4 * c) = g[u][c];
         }
       }
     }
@@ -320,7 +365,7 @@ __global__ __launch_bounds__(JOIN_T) void embed_join_kernel(const unsigned* __re
 }
 
 // A few tokens, in one launch: wave (r, slice) compares all ids with row r's and adds up its token's rows if r is the first of them.
-constexpr int FEW = 256;
+constexpr int FEW = 512;
 template <typename T>
 __global__ __launch_bounds__(NT) void embed_few_kernel(const int* __restrict__ ids, const T* __restrict__ dy, float* __restrict__ grad, int rows, unsigned vocab, int h,
                                                        float scale) {
@@ -347,6 +392,12 @@ __global__ __launch_bounds__(NT) void embed_few_kernel(const int* __restrict__ i
   if (col < h) add_to<N>(grad + (size_t)id * h + col, s, scale);
 }
 
+unsigned sort_range(int rows) {
+  if (rows <= 8192) return 512;
+  const unsigned tiles = ((unsigned)rows + 1023) / 1024;
+  return (tiles + SORT_MAX_GROUPS - 1) / SORT_MAX_GROUPS * 1024;
+}
+
 Sorted layout(void* ws, int rows, int h, uint64_t* bytes) {
   uint64_t at = 0;
   auto take = [&](uint64_t n) { void* p = (char*)ws + at; at += (n + 255) / 256 * 256; return p; };
@@ -357,6 +408,8 @@ Sorted layout(void* ws, int rows, int h, uint64_t* bytes) {
     s.key[i] = (unsigned*)take((uint64_t)rows * 4);
     s.row[i] = (unsigned*)take((uint64_t)rows * 4);
   }
+  const unsigned range = sort_range(rows);
+  s.table = (unsigned*)take(rows > SORT_COUNTED ? (uint64_t)((unsigned)rows + range - 1) / range * RADIX * 4 : 0);
   s.partial = (float*)take(((uint64_t)rows + PIECE - 1) / PIECE * 2 * h * 4);
   *bytes = at;
   return s;
@@ -374,12 +427,14 @@ hipError_t run_embed_bwd(const int* ids, const void* dy, float* grad, void* ws, 
   int bits = 1;
   while (bits < 31 && (vocab - 1) >> bits) ++bits;
   const int passes = (bits + 8) / 9, per_pass = (bits + passes - 1) / passes;
-  const unsigned tiles = ((unsigned)rows + SORT_T - 1) / SORT_T, per_group = (tiles + SORT_MAX_GROUPS - 1) / SORT_MAX_GROUPS * SORT_T;
-  const dim3 grid(((unsigned)rows + per_group - 1) / per_group);
+  // keys of a workgroup: 512 of them up to 8192 tokens (4096 tokens of 256 columns 24.2 us, 25.8 with 1024), 1024 beyond (16384: 33.6 us, 34.3 with 512)
+  const bool counted = rows > SORT_COUNTED;
+  const unsigned threads = rows <= 8192 ? 512 : 1024, per_group = sort_range(rows), groups = ((unsigned)rows + per_group - 1) / per_group;
   for (int i = 0; i < passes; ++i) {
-    const int to = i & 1, now = i == passes - 1 ? bits - per_pass * i : per_pass;
-    if (i == 0) hipLaunchKernelGGL(embed_sort_kernel<true>, grid, dim3(SORT_T), 0, s, ids, nullptr, nullptr, w.key[to], w.row[to], w.count, (unsigned)rows, vocab, 0, now, per_group);
-    else hipLaunchKernelGGL(embed_sort_kernel<false>, grid, dim3(SORT_T), 0, s, nullptr, w.key[to ^ 1], w.row[to ^ 1], w.key[to], w.row[to], w.count, 0u, vocab, per_pass * i, now, per_group);
+    const Pass p = {per_pass * i, min(per_pass, bits - per_pass * i), i, (unsigned)rows, vocab, per_group};
+    if (counted) hipLaunchKernelGGL(embed_count_kernel, dim3(groups), dim3(1024), 0, s, (const unsigned*)ids, w, p);
+    if (threads == 512) hipLaunchKernelGGL(embed_sort_kernel<512>, dim3(groups), dim3(512), 0, s, (const unsigned*)ids, w, p, 0);
+    else hipLaunchKernelGGL(embed_sort_kernel<1024>, dim3(groups), dim3(1024), 0, s, (const unsigned*)ids, w, p, counted ? 1 : 0);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
