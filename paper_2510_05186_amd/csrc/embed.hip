@@ -49,7 +49,7 @@ __global__ __launch_bounds__(NT) void embed_fwd_kernel(const int* __restrict__ i
 // ---- sort ---------------------------------------------------------------------------------------------------
 // A stable radix sort by up to 9 bits of the id per pass.  Up to 16384 keys a pass is one launch: every workgroup counts the digits of ALL keys (they come out
 // of the L2, 64 KB at most), those ahead of its own range apart, which gives it the place of each of its digits without waiting for the others.
-// Beyond that a launch ahead of it counts each range once (65536 tokens, 256 columns: TABLE_US us with it, 75 without).  The first pass takes the ids
+// Beyond that a launch ahead of it counts each range once (65536 tokens, 256 columns: 69 us with it, 76 without).  The first pass takes the ids
 // themselves and leaves out those that are no words.
 constexpr int RADIX = 512, COPIES = 8;                                  // counters in 8 copies by lane: equal digits of a wave meet 8 at a time at most
 constexpr int SORT_MAX_GROUPS = 256, SORT_COUNTED = 16384;
@@ -239,7 +239,7 @@ __global__ __launch_bounds__(NT) void embed_sum_kernel(const unsigned* __restric
                                                        unsigned* count, unsigned* long_runs, float* __restrict__ partial, int rows, int h, unsigned groups, float scale) {
   typedef Vec16<T> V;
   constexpr int N = V::N;
-  const int lane = threadIdx.x & 63, slice = (int)(blockIdx.x % groups) * (NT / 64) + (threadIdx.x >> 6), col = (slice * 64 + lane) * N;
+  const int lane = threadIdx.x & 63, slice = (int)((blockIdx.x % groups) * blockDim.x + threadIdx.x) >> 6, col = (slice * 64 + lane) * N;
   if (slice * 64 * N >= h) return;
   const bool on = col < h;
   for (long long base = (long long)(blockIdx.x / groups) * Q; base < rows; base += (long long)(gridDim.x / groups) * Q) {
@@ -370,7 +370,7 @@ template <typename T>
 __global__ __launch_bounds__(NT) void embed_few_kernel(const int* __restrict__ ids, const T* __restrict__ dy, float* __restrict__ grad, int rows, unsigned vocab, int h,
                                                        float scale) {
   constexpr int N = Vec16<T>::N;
-  const int lane = threadIdx.x & 63, slice = blockIdx.y * (NT / 64) + (threadIdx.x >> 6), col = (slice * 64 + lane) * N, r = blockIdx.x;
+  const int lane = threadIdx.x & 63, slice = (int)(blockIdx.y * blockDim.x + threadIdx.x) >> 6, col = (slice * 64 + lane) * N, r = blockIdx.x;
   if (slice * 64 * N >= h) return;
   const int id = ids[r];
   if ((unsigned)id >= vocab) return;
@@ -417,9 +417,9 @@ Sorted layout(void* ws, int rows, int h, uint64_t* bytes) {
 
 template <typename T>
 hipError_t run_embed_bwd(const int* ids, const void* dy, float* grad, void* ws, int rows, unsigned vocab, int h, float scale, hipStream_t s) {
-  const unsigned slices = (unsigned)((h / Vec16<T>::N + NT - 1) / NT);
+  const unsigned waves = (unsigned)(h / Vec16<T>::N + 63) / 64, threads = 64 * min(waves, 4u), slices = (waves + 3) / 4;
   if (rows <= FEW) {
-    hipLaunchKernelGGL(embed_few_kernel<T>, dim3(rows, slices), dim3(NT), 0, s, ids, (const T*)dy, grad, rows, vocab, h, scale);
+    hipLaunchKernelGGL(embed_few_kernel<T>, dim3(rows, slices), dim3(threads), 0, s, ids, (const T*)dy, grad, rows, vocab, h, scale);
     return hipGetLastError();
   }
   uint64_t bytes;
@@ -429,17 +429,17 @@ hipError_t run_embed_bwd(const int* ids, const void* dy, float* grad, void* ws, 
   const int passes = (bits + 8) / 9, per_pass = (bits + passes - 1) / passes;
   // keys of a workgroup: 512 of them up to 8192 tokens (4096 tokens of 256 columns 24.2 us, 25.8 with 1024), 1024 beyond (16384: 33.6 us, 34.3 with 512)
   const bool counted = rows > SORT_COUNTED;
-  const unsigned threads = rows <= 8192 ? 512 : 1024, per_group = sort_range(rows), groups = ((unsigned)rows + per_group - 1) / per_group;
+  const unsigned keys = rows <= 8192 ? 512 : 1024, per_group = sort_range(rows), groups = ((unsigned)rows + per_group - 1) / per_group;
   for (int i = 0; i < passes; ++i) {
     const Pass p = {per_pass * i, min(per_pass, bits - per_pass * i), i, (unsigned)rows, vocab, per_group};
     if (counted) hipLaunchKernelGGL(embed_count_kernel, dim3(groups), dim3(1024), 0, s, (const unsigned*)ids, w, p);
-    if (threads == 512) hipLaunchKernelGGL(embed_sort_kernel<512>, dim3(groups), dim3(512), 0, s, (const unsigned*)ids, w, p, 0);
+    if (keys == 512) hipLaunchKernelGGL(embed_sort_kernel<512>, dim3(groups), dim3(512), 0, s, (const unsigned*)ids, w, p, 0);
     else hipLaunchKernelGGL(embed_sort_kernel<1024>, dim3(groups), dim3(1024), 0, s, (const unsigned*)ids, w, p, counted ? 1 : 0);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
   const int last = (passes - 1) & 1;
-  hipLaunchKernelGGL(embed_sum_kernel<T>, dim3(min((rows + Q - 1) / Q, max(1, (1 << 22) / (int)slices)) * slices), dim3(NT), 0, s, w.key[last], w.row[last],
+  hipLaunchKernelGGL(embed_sum_kernel<T>, dim3(min((rows + Q - 1) / Q, max(1, (1 << 22) / (int)slices)) * slices), dim3(threads), 0, s, w.key[last], w.row[last],
                      (const T*)dy, grad, w.count, w.long_runs, w.partial, rows, h, slices, scale);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;

@@ -8,41 +8,52 @@ namespace {
 
 constexpr int NT = 256;
 
-__device__ __forceinline__ uint32_t half_wave_max(uint32_t v) {
+// ---- keep and restore, 16 bytes of x per lane and access ------------------------------------------------------
+// Rows may start anywhere (an odd number of columns, a column range of wider rows): the memory system takes 16-byte accesses at any address
+// of an element (4096 x 9079 bf16: 53 us, 130 with one value a lane), and only a row's last chunk goes value by value.
+template <typename T> struct Loose;
+template <> struct Loose<bf16_t> {
+  typedef bf16_t x_t __attribute__((ext_vector_type(8), aligned(2)));
+  typedef uint32_t codes_t __attribute__((ext_vector_type(2), aligned(1)));
+};
+template <> struct Loose<float> {
+  typedef float x_t __attribute__((ext_vector_type(4), aligned(4)));
+  typedef uint32_t codes_t __attribute__((aligned(1)));
+};
+template <typename T> __device__ __forceinline__ Vec16<T> load_values(const T* x, int left) {
+  Vec16<T> v = {};
+  if (left >= Vec16<T>::N) v.v = *reinterpret_cast<const typename Loose<T>::x_t*>(x);
+  else
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) v = max(v, (uint32_t)__shfl_xor((int)v, o, 64));
+    for (int e = 0; e < Vec16<T>::N - 1; ++e)
+      if (e < left) v.v[e] = x[e];
   return v;
 }
-
-// one value per lane, a block per half wave
-template <typename T>
-__global__ __launch_bounds__(NT) void pack8_kernel(const T* __restrict__ x, size_t ldx, uint8_t* __restrict__ codes, uint8_t* __restrict__ scales,
-                                                   int rows, int cols) {
-  const int nb = keep_blocks(cols), l = threadIdx.x & 31;
-  const size_t total = (size_t)rows * nb, step = (size_t)gridDim.x * (NT / 32);
-  for (size_t i = blockIdx.x * (size_t)(NT / 32) + (threadIdx.x >> 5); i < total; i += step) {
-    const size_t row = i / nb;
-    const int col = (int)(i % nb) * KEEP_BLOCK + l;
-    const float v = col < cols ? to_f32<T>(x[row * ldx + col]) : 0.f;
-    const uint32_t b = keep_scale_byte(half_wave_max(keep_magnitude(v)));
-    if (col < cols) codes[row * cols + col] = (uint8_t)keep_encode(v, keep_inverse(b));
-    if (l == 0) scales[i] = (uint8_t)b;
-  }
+template <typename T> __device__ __forceinline__ void store_values(T* x, const Vec16<T>& v, int left) {
+  if (left >= Vec16<T>::N) *reinterpret_cast<typename Loose<T>::x_t*>(x) = v.v;
+  else
+#pragma unroll
+    for (int e = 0; e < Vec16<T>::N - 1; ++e)
+      if (e < left) x[e] = v.v[e];
+}
+__device__ __forceinline__ uint32_t code_of(uint2 c, int e) { return (e < 4 ? c.x : c.y) >> 8 * (e & 3); }
+__device__ __forceinline__ uint32_t code_of(uint32_t c, int e) { return c >> 8 * e; }
+template <typename T> __device__ __forceinline__ typename KeepChunk<T>::codes_t load_codes(const uint8_t* p, int left) {
+  typename KeepChunk<T>::codes_t c = {};
+  if (left >= Vec16<T>::N) return __builtin_bit_cast(typename KeepChunk<T>::codes_t, *reinterpret_cast<const typename Loose<T>::codes_t*>(p));
+#pragma unroll
+  for (int e = 0; e < Vec16<T>::N - 1; ++e)
+    if (e < left) keep_put(c, e, p[e]);
+  return c;
+}
+template <typename T> __device__ __forceinline__ void store_codes(uint8_t* p, typename KeepChunk<T>::codes_t c, int left) {
+  if (left >= Vec16<T>::N) *reinterpret_cast<typename Loose<T>::codes_t*>(p) = __builtin_bit_cast(typename Loose<T>::codes_t, c);
+  else
+#pragma unroll
+    for (int e = 0; e < Vec16<T>::N - 1; ++e)
+      if (e < left) p[e] = (uint8_t)code_of(c, e);
 }
 
-template <typename T>
-__global__ __launch_bounds__(NT) void unpack8_kernel(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales, T* __restrict__ x, size_t ldx,
-                                                     int rows, int cols) {
-  const int nb = keep_blocks(cols);
-  const size_t total = (size_t)rows * cols, step = (size_t)gridDim.x * NT;
-  for (size_t i = blockIdx.x * (size_t)NT + threadIdx.x; i < total; i += step) {
-    const size_t row = i / cols;
-    const int col = (int)(i % cols);
-    x[row * ldx + col] = from_f32<T>(keep_decode(codes[i], keep_scale(scales[row * nb + col / KEEP_BLOCK])));
-  }
-}
-
-// ---- the same, 16 bytes of x per lane and access ----------------------------------------------------------
 // The chunks of a row, padded to whole blocks, are numbered through all rows; a workgroup takes NT * U numbers at a time and all of its
 // loads are in flight before the first is used.
 struct Chunks {
@@ -71,55 +82,53 @@ template <typename T> struct Walk {
   }
 };
 
-template <typename T, int U>
-__global__ __launch_bounds__(NT) void pack8_vec_kernel(const T* __restrict__ x, size_t ldx, uint8_t* __restrict__ codes, uint8_t* __restrict__ scales, const Chunks k,
-                                                       int rows, int cols) {
-  typedef Vec16<T> V;
-  typedef typename KeepChunk<T>::codes_t codes_t;
+// WHOLE: every chunk of a row is whole (the test for it costs unpack 131 -> 140 us at 16384 x 15360)
+template <typename T, int U, bool WHOLE>
+__global__ __launch_bounds__(NT) void pack8_kernel(const T* __restrict__ x, size_t ldx, uint8_t* __restrict__ codes, uint8_t* __restrict__ scales, const Chunks k, int rows,
+                                                   int cols) {
   const int nb = keep_blocks(cols);
   for (size_t base = blockIdx.x * (size_t)(NT * U); base < k.total; base += (size_t)gridDim.x * (NT * U)) {
     const Walk<T> walk(base, k);
-    V v[U] = {};
+    Vec16<T> v[U] = {};
     At at[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       at[u] = walk.at(u * NT + threadIdx.x);
-      if (at[u].row < (size_t)rows && at[u].col < cols) v[u] = *reinterpret_cast<const V*>(x + at[u].row * ldx + at[u].col);
+      if (at[u].row < (size_t)rows && at[u].col < cols) v[u] = load_values(x + at[u].row * ldx + at[u].col, WHOLE ? Vec16<T>::N : cols - at[u].col);
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       uint32_t byte;
-      const codes_t c = keep_chunk<T>(v[u], byte);
+      const auto c = keep_chunk<T>(v[u], byte);
       if (at[u].row < (size_t)rows) {
-        if (at[u].col < cols) *reinterpret_cast<codes_t*>(codes + at[u].row * cols + at[u].col) = c;
+        if (at[u].col < cols) store_codes<T>(codes + at[u].row * cols + at[u].col, c, WHOLE ? Vec16<T>::N : cols - at[u].col);
         if (at[u].col % KEEP_BLOCK == 0) scales[at[u].row * nb + at[u].col / KEEP_BLOCK] = (uint8_t)byte;
       }
     }
   }
 }
 
-template <typename T, int U>
-__global__ __launch_bounds__(NT) void unpack8_vec_kernel(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales, T* __restrict__ x, size_t ldx, const Chunks k,
-                                                         int rows, int cols) {
-  typedef Vec16<T> V;
-  typedef typename KeepChunk<T>::codes_t codes_t;
+template <typename T, int U, bool WHOLE>
+__global__ __launch_bounds__(NT) void unpack8_kernel(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales, T* __restrict__ x, size_t ldx, const Chunks k,
+                                                     int rows, int cols) {
   const int nb = keep_blocks(cols);
   for (size_t base = blockIdx.x * (size_t)(NT * U); base < k.total; base += (size_t)gridDim.x * (NT * U)) {
     const Walk<T> walk(base, k);
-    codes_t c[U];
+    typename KeepChunk<T>::codes_t c[U];
     uint32_t b[U];
     At at[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       at[u] = walk.at(u * NT + threadIdx.x);
       if (at[u].row < (size_t)rows && at[u].col < cols) {
-        c[u] = *reinterpret_cast<const codes_t*>(codes + at[u].row * cols + at[u].col);
+        c[u] = load_codes<T>(codes + at[u].row * cols + at[u].col, WHOLE ? Vec16<T>::N : cols - at[u].col);
         b[u] = scales[at[u].row * nb + at[u].col / KEEP_BLOCK];
       }
     }
 #pragma unroll
     for (int u = 0; u < U; ++u)
-      if (at[u].row < (size_t)rows && at[u].col < cols) *reinterpret_cast<V*>(x + at[u].row * ldx + at[u].col) = keep_stored(c[u], keep_scale(b[u]), V());
+      if (at[u].row < (size_t)rows && at[u].col < cols)
+        store_values(x + at[u].row * ldx + at[u].col, keep_stored(c[u], keep_scale(b[u]), Vec16<T>()), WHOLE ? Vec16<T>::N : cols - at[u].col);
   }
 }
 
@@ -481,10 +490,7 @@ __global__ __launch_bounds__(NT) void act_bwd8_kernel(const T* da, const uint8_t
   }
 }
 
-int grid_of(size_t workgroups) { return (int)(workgroups > 8192 ? 8192 : workgroups); }
 
-// rows of x and of the codes start on whole chunks
-template <typename T> bool chunked(size_t ldx, int cols) { return ldx % Vec16<T>::N == 0 && cols % Vec16<T>::N == 0; }
 // Chunks in flight per thread.  16384 x 15360 bf16, pack and unpack: 285 us with 1, 269 with 2, 277 with 4, 296 with 8; the activation holds two or three
 // operands of each: SwiGLU 4096 x 11008, forward and backward, 155 us with 1 or 2, 164 with 4; GELU 4999 x 4088 53 us with 1, 58 with 2.
 constexpr int U = 2, UA = 1;
@@ -495,22 +501,15 @@ unsigned groups_of(const Chunks& k, int u) {
 }
 
 template <typename T> hipError_t run_pack8(const void* x, size_t ldx, uint8_t* codes, uint8_t* scales, int rows, int cols, hipStream_t s) {
-  if (chunked<T>(ldx, cols)) {
-    const Chunks k = chunks_of<T>(rows, cols);
-    hipLaunchKernelGGL((pack8_vec_kernel<T, U>), dim3(groups_of(k, U)), dim3(NT), 0, s, (const T*)x, ldx, codes, scales, k, rows, cols);
-    return hipGetLastError();
-  }
-  const size_t blocks = (size_t)rows * keep_blocks(cols);
-  hipLaunchKernelGGL(pack8_kernel<T>, dim3(grid_of((blocks + 7) / 8)), dim3(NT), 0, s, (const T*)x, ldx, codes, scales, rows, cols);
+  const Chunks k = chunks_of<T>(rows, cols);
+  if (cols % Vec16<T>::N == 0) hipLaunchKernelGGL((pack8_kernel<T, U, true>), dim3(groups_of(k, U)), dim3(NT), 0, s, (const T*)x, ldx, codes, scales, k, rows, cols);
+  else hipLaunchKernelGGL((pack8_kernel<T, U, false>), dim3(groups_of(k, U)), dim3(NT), 0, s, (const T*)x, ldx, codes, scales, k, rows, cols);
   return hipGetLastError();
 }
 template <typename T> hipError_t run_unpack8(const uint8_t* codes, const uint8_t* scales, void* x, size_t ldx, int rows, int cols, hipStream_t s) {
-  if (chunked<T>(ldx, cols)) {
-    const Chunks k = chunks_of<T>(rows, cols);
-    hipLaunchKernelGGL((unpack8_vec_kernel<T, U>), dim3(groups_of(k, U)), dim3(NT), 0, s, codes, scales, (T*)x, ldx, k, rows, cols);
-    return hipGetLastError();
-  }
-  hipLaunchKernelGGL(unpack8_kernel<T>, dim3(grid_of(((size_t)rows * cols + NT - 1) / NT)), dim3(NT), 0, s, codes, scales, (T*)x, ldx, rows, cols);
+  const Chunks k = chunks_of<T>(rows, cols);
+  if (cols % Vec16<T>::N == 0) hipLaunchKernelGGL((unpack8_kernel<T, U, true>), dim3(groups_of(k, U)), dim3(NT), 0, s, codes, scales, (T*)x, ldx, k, rows, cols);
+  else hipLaunchKernelGGL((unpack8_kernel<T, U, false>), dim3(groups_of(k, U)), dim3(NT), 0, s, codes, scales, (T*)x, ldx, k, rows, cols);
   return hipGetLastError();
 }
 // f(W, C, R) for rows of h: the fewest waves that hold a row with at most two chunks a lane
