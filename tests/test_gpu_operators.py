@@ -122,9 +122,7 @@ def test_pack8_at_the_ends_of_the_range(dtype, cols):
 def test_pack8_offsets_beyond_32_bits():
     """2^31 values and more: rows of the same few patterns, checked at both ends and around the place where 32 bits end."""
     cols, rows = 32768 + 8, 65537
-    free = torch.cuda.mem_get_info()[0]
-    if free < 24 * 2 ** 30:
-        pytest.skip("too little memory free")
+    room(24)
     pattern = torch.from_numpy(wide((7, cols), rng(2), BF16)).to(torch.bfloat16).cuda()
     X = pattern.repeat(rows // 7 + 1, 1)[:rows].contiguous()
     codes = torch.zeros((rows, cols), dtype=torch.uint8, device="cuda")
@@ -136,6 +134,40 @@ def test_pack8_offsets_beyond_32_bits():
     c, s, v = P.pack8(host(pattern))
     for r in (0, 1, 32760, 32767, 32768, 65529, 65535, 65536):
         assert np.array_equal(codes[r].cpu().numpy(), c[r % 7]) and np.array_equal(scales[r].cpu().numpy(), s[r % 7]) and np.array_equal(host(X[r]), v[r % 7]), r
+
+
+def room(gib):
+    if torch.cuda.mem_get_info()[0] < gib * 2 ** 30:
+        pytest.skip("too little memory free")
+
+
+@pytest.mark.parametrize("dtype,rows,cols", [(BF16, (1 << 29) + 5, 8), (FP32, (1 << 28) + 3, 4)])
+def test_more_than_two_to_the_31_chunks(dtype, rows, cols):
+    """Short rows, each padded to a block of chunks: their number passes 31 bits.  pack, unpack and the MLP activation."""
+    room(60)
+    pattern = q(rng(20).standard_normal((1009, cols)), dtype)
+    x = dev(pattern, dtype).repeat(rows // 1009 + 1, 1)[:rows].contiguous()
+    at = [0, 1, (1 << 28) - 1, rows // 2, rows - 2, rows - 1]
+    want = P.pack8(pattern)
+    codes, scales = torch.zeros((rows, cols), dtype=torch.uint8, device="cuda"), torch.zeros((rows, 1), dtype=torch.uint8, device="cuda")
+    y, dgu = torch.zeros_like(x), torch.zeros_like(x)
+    ok(lib().optstage_op_pack8(dtype, x.data_ptr(), cols, codes.data_ptr(), scales.data_ptr(), rows, cols, stream()))
+    ok(lib().optstage_op_unpack8(dtype, codes.data_ptr(), scales.data_ptr(), y.data_ptr(), cols, rows, cols, stream()))
+    torch.cuda.synchronize()
+    for r in at:
+        assert np.array_equal(codes[r].cpu().numpy(), want[0][r % 1009]) and scales[r].item() == want[1][r % 1009, 0] and np.array_equal(host(y[r]), want[2][r % 1009]), r
+    codes.zero_()
+    y.zero_()
+    ok(lib().optstage_op_act_fwd_pack8(dtype, GPT, x.data_ptr(), y.data_ptr(), codes.data_ptr(), scales.data_ptr(), rows, cols, stream()))
+    ok(lib().optstage_op_act_bwd8(dtype, GPT, x.data_ptr(), codes.data_ptr(), scales.data_ptr(), dgu.data_ptr(), 0, rows, cols, stream()))
+    torch.cuda.synchronize()
+    for r in at:
+        k, g = want[2][r % 1009], pattern[r % 1009]
+        assert np.array_equal(codes[r].cpu().numpy(), want[0][r % 1009])
+        ref, b = P.activation(GPT, g[None]), act_bounds(GPT, g[None], None, dtype)
+        within(host(y[r])[None], ref, HALF[dtype] * np.abs(ref) + b[0])
+        ref, b = P.activation_bwd(GPT, k[None], g[None]), act_bounds(GPT, k[None], g[None], dtype)
+        within(host(dgu[r])[None], ref, HALF[dtype] * np.abs(ref) + b[1])
 
 
 # ------------------------------------------------------------------ the MLP activation
@@ -307,6 +339,27 @@ def test_norm_gradient_in_place_without_residual_or_second_output_and_repeatable
     st = host(first["stats"])
     dx, _, _ = P.norm_bwd(family, t["dn"], v, st[:, :1] if family == GPT else 0.0, st[:, -1:], t["gamma"], None)
     assert np.max(np.abs(host(g2["dx"]) - dx)) <= 2 * HALF[dtype] * np.max(np.abs(dx)) + 100 * EPS * np.max(np.abs(dx))
+
+
+def test_norm_of_more_rows_than_workgroups():
+    """More rows of a few columns than one launch has workgroups for: the forward pass goes round again."""
+    rows, h = (1 << 23) + 9, 8
+    pattern = q(rng(21).standard_normal((1009, h)), BF16)
+    x = dev(pattern, BF16).repeat(rows // 1009 + 1, 1)[:rows].contiguous()
+    gamma, beta = torch.ones(h, dtype=torch.bfloat16, device="cuda"), torch.zeros(h, dtype=torch.bfloat16, device="cuda")
+    out, stats = torch.zeros_like(x), torch.zeros((rows, 2), device="cuda")
+    codes, scales, whole = kept(rows, h)
+    ok(lib().optstage_op_norm_fwd_pack8(BF16, GPT, x.data_ptr(), gamma.data_ptr(), beta.data_ptr(), out.data_ptr(), stats.data_ptr(), codes.data_ptr(), scales.data_ptr(), rows, h, 1e-5,
+                                        stream()))
+    torch.cuda.synchronize()
+    mean, r = P.norm_stats(GPT, pattern, 1e-5)
+    c, s, _ = P.pack8(pattern)
+    for i in (0, 1 << 20, (1 << 23) - 1, 1 << 23, rows - 1):
+        k = i % 1009
+        ref = P.norm(GPT, pattern[k:k + 1], 1.0, 0.0, mean[k:k + 1], r[k:k + 1])
+        within(host(out[i])[None], ref, HALF[BF16] * np.abs(ref) + 100 * EPS * (1 + np.abs(ref)))
+        assert np.array_equal(codes[i].cpu().numpy(), c[k]) and scales[i].item() == s[k, 0]
+    assert whole()
 
 
 def test_norm_keeps_what_is_not_finite_to_its_row():
@@ -495,8 +548,7 @@ def test_embedding_and_its_gradient(dtype, rows, vocab, h, kind):
 def test_embedding_offsets_beyond_32_bits():
     """A table of more than 2^31 values: tokens on both sides of that place."""
     vocab, h = 540000, 4096
-    if torch.cuda.mem_get_info()[0] < 40 * 2 ** 30:
-        pytest.skip("too little memory free")
+    room(40)
     ids = np.array([0, vocab - 1, 524287, 524288, 524289, vocab - 1, vocab, 262144, 0], np.int32)
     W = torch.empty((vocab, h), dtype=torch.bfloat16, device="cuda")
     G = torch.empty((vocab, h), dtype=torch.float32, device="cuda")
@@ -520,7 +572,99 @@ def test_embedding_offsets_beyond_32_bits():
         assert np.max(np.abs(host(G[int(t)]) - want)) <= 4 * EPS * np.abs(dy[ids == t]).sum(0).max()
 
 
+@pytest.mark.parametrize("dtype,rows,vocab,h,bits", [(FP32, 3000, 1 << 28, 4, 28), (BF16, 700, (1 << 27) + 1, 8, 28)])
+def test_embedding_gradient_of_a_vocabulary_that_takes_four_passes_of_the_sort(dtype, rows, vocab, h, bits):
+    room(12)
+    r = rng(22, rows)
+    ids = (r.integers(0, vocab, 40)[r.integers(0, 40, rows)]).astype(np.int32)
+    ids[5], ids[6], ids[7] = vocab - 1, 0, -1
+    dy = q(r.standard_normal((rows, h)), dtype)
+    G = torch.zeros((vocab, h), device="cuda")
+    need = lib().optstage_op_embed_bwd_ws_bytes(rows, h)
+    ws, I, DY = torch.empty(need, dtype=torch.uint8, device="cuda"), torch.from_numpy(ids).cuda(), dev(dy, dtype)
+    ok(lib().optstage_op_embed_bwd(dtype, I.data_ptr(), DY.data_ptr(), G.data_ptr(), ws.data_ptr(), need, rows, vocab, h, 1.0, stream()))
+    torch.cuda.synchronize()
+    for t in set(ids.tolist()) - {-1}:
+        want, size = dy[ids == t].sum(0), np.abs(dy[ids == t]).sum(0)
+        within(host(G[t])[None], want[None], (EPS * 90 * size)[None], str(t))
+    assert int((G != 0).any(1).sum()) == len(set(ids.tolist()) - {-1})
+
+
+def test_embedding_of_more_tokens_than_one_launch_s_workgroups_and_more_than_two_to_the_31_chunks():
+    """2^25 tokens and some: every token of dy is a row of ones, so that the gradient counts tokens, exactly.  The lookup at 512 columns has more than
+    2^31 chunks."""
+    room(80)
+    rows, vocab, h = (1 << 25) + 77, 5000, 8
+    g = torch.Generator(device="cuda")
+    g.manual_seed(5)
+    ids = (torch.exp(torch.rand(rows, generator=g, device="cuda") * float(np.log(vocab + 20.0))) - 1).int()       # some beyond the vocabulary
+    dy, G = torch.ones((rows, h), dtype=torch.bfloat16, device="cuda"), torch.zeros((vocab, h), device="cuda")
+    need = lib().optstage_op_embed_bwd_ws_bytes(rows, h)
+    ws = torch.empty(need, dtype=torch.uint8, device="cuda")
+    ok(lib().optstage_op_embed_bwd(BF16, ids.data_ptr(), dy.data_ptr(), G.data_ptr(), ws.data_ptr(), need, rows, vocab, h, 1.0, stream()))
+    torch.cuda.synchronize()
+    count = torch.bincount(ids.long(), minlength=vocab + 32)[:vocab].float()
+    assert torch.equal(G, count[:, None].expand(-1, h)) and float(count.max()) < 2 ** 24
+    del dy, ws, G
+    h = 512
+    W = torch.randn((vocab, h), generator=g, device="cuda").to(torch.bfloat16)
+    out = torch.zeros((rows, h), dtype=torch.bfloat16, device="cuda")
+    ok(lib().optstage_op_embed_fwd(BF16, ids.data_ptr(), W.data_ptr(), out.data_ptr(), rows, vocab, h, 1.0, stream()))
+    torch.cuda.synchronize()
+    for i in (0, 12345, (1 << 25) - 1, 1 << 25, rows - 1, *range(rows - 20, rows)):
+        t = int(ids[i])
+        assert torch.equal(out[i], W[t] if t < vocab else torch.zeros_like(out[i])), i
+
+
+def test_embedding_gradient_workspace_as_an_earlier_call_left_it():
+    h, vocab = 64, 3000
+    need = lib().optstage_op_embed_bwd_ws_bytes(30000, h)
+    ws = torch.full((need,), 0xFF, dtype=torch.uint8, device="cuda")
+    for i, (rows, kind) in enumerate([(30000, "zipf"), (900, "padded"), (9000, "one"), (513, "none"), (2000, "zipf"), (100, "zipf")]):
+        r = rng(23, i)
+        ids, dy = ids_of(kind, rows, vocab, r), q(r.standard_normal((rows, h)), BF16)
+        G, I, DY = torch.zeros((vocab, h), device="cuda"), torch.from_numpy(ids).cuda(), dev(dy, BF16)
+        ok(lib().optstage_op_embed_bwd(BF16, I.data_ptr(), DY.data_ptr(), G.data_ptr(), ws.data_ptr(), need, rows, vocab, h, 1.0, stream()))
+        torch.cuda.synchronize()
+        valid = (ids >= 0) & (ids < vocab)
+        ref, size = np.zeros((vocab, h)), np.zeros((vocab, h))
+        np.add.at(ref, ids[valid], dy[valid])
+        np.add.at(size, ids[valid], np.abs(dy[valid]))
+        within(G, ref, EPS * 90 * size, kind)
+
+
 # ------------------------------------------------------------------ streams, graphs, a run of them together
+def test_two_calls_at_once_on_two_streams():
+    """Each with buffers and scratch of its own: the results of one after the other."""
+    sets = [Heads(BF16, 3000, 1000, 8, 2, 128, seed=k) for k in range(2)]
+    ids = [torch.from_numpy(ids_of("zipf", 5000, 2000, rng(24, k))).cuda() for k in range(2)]
+    dy = [dev(rng(25, k).standard_normal((5000, 256)), BF16) for k in range(2)]
+    need = lib().optstage_op_embed_bwd_ws_bytes(5000, 256)
+    ws, G = [torch.empty(need, dtype=torch.uint8, device="cuda") for _ in range(2)], [torch.zeros((2000, 256), device="cuda") for _ in range(2)]
+    y, dx = [torch.empty_like(H.X) for H in sets], [torch.empty_like(H.X) for H in sets]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+
+    def call(k, s):
+        sets[k].fwd(sets[k].X, y[k], True, s)
+        ok(lib().optstage_op_embed_bwd(BF16, ids[k].data_ptr(), dy[k].data_ptr(), G[k].data_ptr(), ws[k].data_ptr(), need, 5000, 2000, 256, 1.0, s))
+        sets[k].bwd(sets[k].DY, None, dx[k], s)
+
+    for k in range(2):
+        call(k, stream())
+    torch.cuda.synchronize()
+    first = [[t.clone() for t in (y[k], dx[k], G[k], sets[k].DG)] for k in range(2)]
+    for _ in range(3):
+        for k in range(2):
+            sets[k].reset()
+            G[k].zero_()
+            y[k].zero_()
+        torch.cuda.synchronize()
+        for k in range(2):
+            call(k, streams[k].cuda_stream)
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for k in range(2) for a, b in zip(first[k], (y[k], dx[k], G[k], sets[k].DG)))
+
+
 def test_on_a_stream_of_its_own_and_in_a_graph():
     """Captured once, replayed after the inputs have changed, with eager work between the replays: every replay gives the eager result."""
     rows, seq, n_q, n_kv, d, f, vocab = 200, 100, 4, 2, 64, 352, 500
