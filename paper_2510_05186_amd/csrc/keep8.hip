@@ -207,12 +207,12 @@ __global__ __launch_bounds__(W * R * 64) void norm_fwd_pack8_kernel(const T* __r
 }
 
 // Workgroup b takes the rows b R .. b R + R - 1, (b + gridDim.x) R .., the loads of the next ones in flight while the present ones are reduced and written.
-// Its sums of the gains' and biases' gradients stay in registers and end in its rows of `partial`, those of its R rows added in order.  dx may be dn or
-// dres: rows in flight are other rows, and a lane has read its chunks of the present one.
+// Its sums of the gains' and biases' gradients stay in registers and end in its rows of `partial`, those of its R rows added in order; a workgroup alone adds
+// them to the accumulators itself.  dx may be dn or dres: rows in flight are other rows, and a lane has read its chunks of the present one.
 template <typename T, bool LN, int W, int C, int R>
 __global__ __launch_bounds__(W * R * 64) void norm_bwd8_kernel(const T* dn, const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales,
                                                                const float* __restrict__ stats, const T* __restrict__ gamma, const T* __restrict__ beta, const T* dres, T* dx,
-                                                               T* __restrict__ out, float* __restrict__ partial, int rows, int h) {
+                                                               T* __restrict__ out, float* __restrict__ partial, float* dgamma, float* dbeta, int rows, int h) {
   typedef Vec16<T> V;
   typedef typename KeepChunk<T>::codes_t codes_t;
   __shared__ float red[2][2][R * W];
@@ -311,7 +311,13 @@ __global__ __launch_bounds__(W * R * 64) void norm_bwd8_kernel(const T* dn, cons
 #pragma unroll
   for (int part = 0; part < (LN ? 2 : 1); ++part) {
     float (&p)[C][V::N] = part ? reinterpret_cast<float (&)[C][V::N]>(pb) : pg;
-    float* to = partial + ((size_t)part * gridDim.x + blockIdx.x) * h;
+    const bool alone = gridDim.x == 1;
+    float* to = alone ? (part ? dbeta : dgamma) : partial + ((size_t)part * gridDim.x + blockIdx.x) * h;
+    const auto put = [&](int at, f32x4_t v) {
+      if (at >= h) return;
+      if (alone) v += *reinterpret_cast<const f32x4_t*>(to + at);
+      *reinterpret_cast<f32x4_t*>(to + at) = v;
+    };
     if (R > 1) {
       if (part) __syncthreads();
 #pragma unroll
@@ -324,15 +330,13 @@ __global__ __launch_bounds__(W * R * 64) void norm_bwd8_kernel(const T* dn, cons
         f32x4_t t = sums[0][q][lane];
 #pragma unroll
         for (int k = 1; k < R; ++k) t += sums[k][q][lane];
-        if (at < h) *reinterpret_cast<f32x4_t*>(to + at) = t;
+        put(at, t);
       }
     } else {
 #pragma unroll
       for (int c = 0; c < C; ++c) {
-        const int at = (l + c * W * 64) * V::N;
-        if (at < h)
 #pragma unroll
-          for (int e = 0; e < V::N; e += 4) *reinterpret_cast<f32x4_t*>(to + at + e) = (f32x4_t){p[c][e], p[c][e + 1], p[c][e + 2], p[c][e + 3]};
+        for (int e = 0; e < V::N; e += 4) put((l + c * W * 64) * V::N + e, (f32x4_t){p[c][e], p[c][e + 1], p[c][e + 2], p[c][e + 3]});
       }
     }
   }
@@ -494,7 +498,10 @@ __global__ __launch_bounds__(NT) void act_bwd8_kernel(const T* da, const uint8_t
 // Chunks in flight per thread.  16384 x 15360 bf16, pack and unpack: 285 us with 1, 269 with 2, 277 with 4, 296 with 8; the activation holds two or three
 // operands of each: SwiGLU 4096 x 11008, forward and backward, 155 us with 1 or 2, 164 with 4; GELU 4999 x 4088 53 us with 1, 58 with 2.
 constexpr int U = 2, UA = 1;
-constexpr int NORM_GROUPS = 256;                                       // workgroups of norm_bwd8_kernel, one row of sums each
+// Workgroups of norm_bwd8_kernel, one row of sums each: one per compute unit (4096 x 8192: 512 of them 65 us instead of 60, 384 74).  Rows that one workgroup has
+// done in two turns are left to one, which saves the second launch (16 rows of 1024, forward and backward: 11.0 us a pass among others, 13.7 with it; four
+// turns, 8 rows of 4096: 14.6 against 13.9).
+constexpr int NORM_GROUPS = 256, NORM_TURNS = 2;
 unsigned groups_of(const Chunks& k, int u) {
   const size_t groups = (k.total + (size_t)NT * u - 1) / ((size_t)NT * u);
   return (unsigned)(groups > (1u << 20) ? 1u << 20 : groups);
@@ -539,12 +546,12 @@ hipError_t run_norm_bwd8(const void* dn, const uint8_t* codes, const uint8_t* sc
                          void* out, float* partial, float* dgamma, float* dbeta, int rows, int h, hipStream_t s) {
   int nb = 0;
   norm_division<T>(h, [&](auto w, auto c, auto r) {
-    nb = min((rows + r - 1) / r, NORM_GROUPS);
+    nb = rows <= NORM_TURNS * r ? 1 : min((rows + r - 1) / r, NORM_GROUPS);
     hipLaunchKernelGGL((norm_bwd8_kernel<T, LN, w, c, r>), dim3(nb), dim3(w * r * 64), 0, s, (const T*)dn, codes, scales, stats, (const T*)gamma, (const T*)beta, (const T*)dres,
-                       (T*)dx, (T*)out, partial, rows, h);
+                       (T*)dx, (T*)out, partial, dgamma, dbeta, rows, h);
   });
   const hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
+  if (e != hipSuccess || nb == 1) return e;
   return launch_add_columns(partial, dgamma, LN ? dbeta : nullptr, nb, h, s);
 }
 template <typename T, bool SWIGLU>

@@ -14,7 +14,9 @@ namespace {
 constexpr int NT = 256;
 // Workgroups (8192 rows of 80 heads of 128, bf16): forward and rebuilt together 136 us with 2048, 134 with 4096, 130 with 8192, 142 with one turn each;
 // backward as many as the compute units hold at once, four on each (512: 118 us, 768: 100, 1024: 94).
-constexpr int FWD_GROUPS = 8192, BWD_GROUPS = 1024;
+// Heads that one workgroup has done in three turns are left to one, which saves the launch that adds the sums (5 rows of 12 heads of 128, forward and
+// backward: 10.8 us a pass among others, 13.5 with it; eight turns 16.1).
+constexpr int FWD_GROUPS = 8192, BWD_GROUPS = 1024, BWD_TURNS = 3;
 
 // item = row * heads + head
 struct Items {
@@ -173,7 +175,7 @@ __global__ __launch_bounds__(NT) void qknorm_kernel(const QkNorm p) {
 
 struct QkNormBwd {
   const void* dy; const void* x; const uint8_t* codes; const uint8_t* scales; const float* stats;
-  const void* gamma_q; const void* gamma_k; const float2* table; void* dx; float* partial;
+  const void* gamma_q; const void* gamma_k; const float2* table; void* dx; float* partial; float* dgamma_q; float* dgamma_k;
   Items items;
   int d;
 };
@@ -284,7 +286,8 @@ __global__ __launch_bounds__(NT) void qknorm_bwd_kernel(const QkNormBwd p) {
     float t = 0.f;
 #pragma unroll 8
     for (int w = 0; w < S; ++w) t += sums[w][q][i][e];
-    p.partial[((size_t)q * gridDim.x + blockIdx.x) * p.d + c] = t;
+    if (gridDim.x == 1) (q ? p.dgamma_k : p.dgamma_q)[c] += t;
+    else p.partial[((size_t)q * gridDim.x + blockIdx.x) * p.d + c] = t;
   }
 }
 
@@ -315,15 +318,15 @@ template <typename T> hipError_t run_qknorm(const QkNorm& p, hipStream_t s) {
     else hipLaunchKernelGGL((qknorm_kernel<T, g, false, false>), grid, dim3(NT), 0, s, p);
   });
 }
-template <typename T> hipError_t run_qknorm_bwd(const QkNormBwd& p, float* dgamma_q, float* dgamma_k, int rows, hipStream_t s) {
+template <typename T> hipError_t run_qknorm_bwd(const QkNormBwd& p, int rows, hipStream_t s) {
   unsigned nb = 0;
   const hipError_t e = by_head<T>(p.d, [&](auto g) {
-    nb = groups_of(p.items, NT / g, (unsigned)(rows < BWD_GROUPS ? rows : BWD_GROUPS));
+    nb = p.items.total <= (size_t)BWD_TURNS * (NT / g) ? 1u : groups_of(p.items, NT / g, (unsigned)(rows < BWD_GROUPS ? rows : BWD_GROUPS));
     if (p.codes) hipLaunchKernelGGL((qknorm_bwd_kernel<T, g, true>), dim3(nb), dim3(NT), 0, s, p);
     else hipLaunchKernelGGL((qknorm_bwd_kernel<T, g, false>), dim3(nb), dim3(NT), 0, s, p);
   });
-  if (e != hipSuccess) return e;
-  return launch_add_columns(p.partial, dgamma_q, dgamma_k, (int)nb, p.d, s);
+  if (e != hipSuccess || nb == 1) return e;
+  return launch_add_columns(p.partial, p.dgamma_q, p.dgamma_k, (int)nb, p.d, s);
 }
 
 }  // namespace
@@ -340,7 +343,7 @@ hipError_t launch_qknorm_rope_bwd(int dtype, const void* dy, const void* x, cons
                                   const void* gamma_k, const float* table, void* dx, float* partial, float* dgamma_q, float* dgamma_k, int rows, int seq, int n_q, int n_kv,
                                   int d, hipStream_t s) {
   const unsigned heads = n_q + 2 * n_kv;
-  const QkNormBwd p = {dy, x, codes, scales, stats, gamma_q, gamma_k, (const float2*)table, dx, partial,
+  const QkNormBwd p = {dy, x, codes, scales, stats, gamma_q, gamma_k, (const float2*)table, dx, partial, dgamma_q, dgamma_k,
                        {(size_t)rows * heads, heads, (unsigned)n_q, (unsigned)(n_q + n_kv), (unsigned)seq}, d};
-  return dtype == DT_BF16 ? run_qknorm_bwd<bf16_t>(p, dgamma_q, dgamma_k, rows, s) : run_qknorm_bwd<float>(p, dgamma_q, dgamma_k, rows, s);
+  return dtype == DT_BF16 ? run_qknorm_bwd<bf16_t>(p, rows, s) : run_qknorm_bwd<float>(p, rows, s);
 }
