@@ -120,15 +120,16 @@ uint64_t optstage_op_attn_bwd_ws_floats(uint32_t seq, uint32_t batch, uint32_t n
  * bits, bias 7, no infinity, largest value 448), rounded to nearest, ties to even.  So a kept value is off by at most 2^-4 of the value, or
  * 2^(k - 10) where that is more, and is exactly representable in bf16 and fp32.  A value that is not finite is kept as NaN, and
  * its block's scale goes by the others; values above 448 * 2^119 are kept as that.
- * The calls below that keep their operand ("_pack8") give what pack8 would and otherwise the results of their plain counterparts; those that
- * read it ("8") compute in fp32 from the values kept, with one rounding of each result to the storage type.
- * What is kept may lie in pinned host memory meanwhile; codes and scales are plain bytes. */
+ * The calls below that keep their operand ("_pack8") keep what pack8 would and otherwise compute what their plain counterparts do (to a last bit here and
+ * there: sums in another order, bf16 activations with the hardware's exp2 and reciprocal); those that read it ("8") compute in fp32 from
+ * the values kept, with one rounding of each result to the storage type.  Codes and scales are plain bytes, which may lie in pinned host memory
+ * meanwhile.  Scratch (partial, ws) belongs to a call until its work has run: calls, or captured graphs, that may overlap in time need their own. */
 /* ldx: distance of x's rows in elements, >= cols (a column range of wider rows). */
 optstage_status optstage_op_pack8(uint32_t dtype, const void* x, uint32_t ldx, uint8_t* codes, uint8_t* scales, uint32_t rows,
                                   uint32_t cols, void* stream);
 optstage_status optstage_op_unpack8(uint32_t dtype, const uint8_t* codes, const uint8_t* scales, void* x, uint32_t ldx, uint32_t rows,
                                     uint32_t cols, void* stream);
-/* optstage_op_norm_fwd that keeps x [rows, hidden].  hidden is a multiple of 8 (fp32: 4), at most 8192. */
+/* optstage_op_norm_fwd that keeps x [rows, hidden] (out is not x).  hidden is a multiple of 8 (fp32: 4), at most 8192. */
 optstage_status optstage_op_norm_fwd_pack8(uint32_t dtype, uint32_t family, const void* x, const void* gamma, const void* beta, void* out,
                                            float* stats, uint8_t* codes, uint8_t* scales, uint32_t rows, uint32_t hidden, float eps,
                                            void* stream);

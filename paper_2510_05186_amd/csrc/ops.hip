@@ -313,6 +313,7 @@ optstage_status optstage_op_norm_fwd_pack8(uint32_t dtype, uint32_t family, cons
   REQ(x && gamma && out && stats && codes && scales && (family == OPTSTAGE_LLAMA || beta), "norm_fwd_pack8: null operand");
   REQ(aligned16(x) && aligned16(gamma) && aligned16(beta) && aligned16(out) && aligned16(stats) && aligned16(codes) && aligned16(scales),
       "norm_fwd_pack8: operands must be 16-byte aligned");
+  REQ(out != x, "norm_fwd_pack8: out must be a buffer of its own");
   REQ(hidden <= 8192 && norm8_shape_ok((int)dtype, (int)hidden), "norm_fwd_pack8: hidden must be a multiple of 8 (fp32: 4), at most 8192");
   return wrap(launch_norm_fwd_pack8((int)dtype, (int)family, x, gamma, beta, out, stats, codes, scales, (int)rows, (int)hidden, eps, (hipStream_t)stream),
               "norm_fwd_pack8");

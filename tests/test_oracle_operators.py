@@ -103,7 +103,8 @@ A = 1 << 20
 CALLS = {
     "optstage_op_pack8": dict(dtype=1, x=A, ldx=64, codes=A, scales=A, rows=4, cols=64, stream=0),
     "optstage_op_unpack8": dict(dtype=1, codes=A, scales=A, x=A, ldx=64, rows=4, cols=64, stream=0),
-    "optstage_op_norm_fwd_pack8": dict(dtype=1, family=0, x=A, gamma=A, beta=A, out=A, stats=A, codes=A, scales=A, rows=4, hidden=64, eps=1e-5, stream=0),
+    "optstage_op_norm_fwd_pack8": dict(dtype=1, family=0, x=A, gamma=A, beta=A, out=2 * A, stats=A, codes=A, scales=A, rows=4, hidden=64, eps=1e-5,
+                                       stream=0),
     "optstage_op_norm_bwd8": dict(dtype=1, family=0, dn=A, codes=A, scales=A, stats=A, gamma=A, beta=A, dres=A, dx=A, out=2 * A, partial=A, dgamma=A, dbeta=A, rows=4, hidden=64,
                                   stream=0),
     "optstage_op_act_fwd_pack8": dict(dtype=1, family=1, gu=A, a=A, codes=A, scales=A, rows=4, ffn=64, stream=0),
@@ -119,7 +120,7 @@ CALLS = {
 MAY_BE_NULL = {("optstage_op_norm_bwd8", "dres"), ("optstage_op_norm_bwd8", "out"), ("optstage_op_act_bwd8", "a")}
 MORE = [
     ("optstage_op_pack8", dict(ldx=63)), ("optstage_op_unpack8", dict(ldx=63)), ("optstage_op_pack8", dict(cols=1 << 30, ldx=1 << 30)), ("optstage_op_pack8", dict(rows=1 << 30)),
-    ("optstage_op_norm_fwd_pack8", dict(hidden=60)), ("optstage_op_norm_fwd_pack8", dict(hidden=8200)), ("optstage_op_norm_fwd_pack8", dict(family=2)),
+    ("optstage_op_norm_fwd_pack8", dict(hidden=60)), ("optstage_op_norm_fwd_pack8", dict(out=A)), ("optstage_op_norm_fwd_pack8", dict(hidden=8200)), ("optstage_op_norm_fwd_pack8", dict(family=2)),
     ("optstage_op_norm_fwd_pack8", dict(dtype=0, hidden=62)), ("optstage_op_norm_fwd_pack8", dict(hidden=(1 << 32) - 8)),
     ("optstage_op_norm_bwd8", dict(hidden=60)), ("optstage_op_norm_bwd8", dict(hidden=8200)), ("optstage_op_norm_bwd8", dict(out=A)), ("optstage_op_norm_bwd8", dict(dx=2 * A)),
     ("optstage_op_act_fwd_pack8", dict(ffn=60)), ("optstage_op_act_fwd_pack8", dict(family=2)), ("optstage_op_act_fwd_pack8", dict(ffn=1 << 29)),
