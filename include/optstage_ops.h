@@ -169,7 +169,8 @@ optstage_status optstage_op_qknorm_rope_bwd(uint32_t dtype, const void* dy, cons
                                             uint32_t n_kv, uint32_t head_dim, void* stream);
 
 /* ---- Embedding: the first stage's input and what becomes of its gradient ----
- * out[r] = scale * weight[ids[r]]; weight is [vocab, hidden], ids int32 [rows].  A row whose id is negative or >= vocab (padding) is zero
+ * out[r] = scale * weight[ids[r]]; weight is [vocab, hidden], ids int32 [rows] (any
+ * address of an int32: a part of a longer list).  A row whose id is negative or >= vocab (padding) is zero
  * and has no gradient.  hidden is a multiple of 8 (fp32: 4). */
 optstage_status optstage_op_embed_fwd(uint32_t dtype, const int32_t* ids, const void* weight, void* out, uint32_t rows, uint32_t vocab,
                                       uint32_t hidden, float scale, void* stream);

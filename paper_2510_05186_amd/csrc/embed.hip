@@ -169,7 +169,8 @@ __global__ __launch_bounds__(THREADS) void embed_sort_kernel(const unsigned* __r
     const bool on = key < p.vocab;
     const unsigned d = key >> p.shift & mask;
     unsigned long long same = __ballot(on);
-    for (int b = 0; b < p.bits; ++b) {
+#pragma unroll
+    for (int b = 0; b < 9; ++b) {                                       // bits beyond the pass's are zero in all lanes
       const unsigned long long set = __ballot(d >> b & 1);
       same &= d >> b & 1 ? set : ~set;
     }

@@ -405,7 +405,7 @@ static bool embed_shape_ok(uint32_t dtype, uint32_t rows, uint32_t vocab, uint32
 optstage_status optstage_op_embed_fwd(uint32_t dtype, const int32_t* ids, const void* weight, void* out, uint32_t rows, uint32_t vocab,
                                       uint32_t hidden, float scale, void* stream) {
   REQ(ids && weight && out, "embed_fwd: null operand");
-  REQ(aligned16(ids) && aligned16(weight) && aligned16(out), "embed_fwd: operands must be 16-byte aligned");
+  REQ(((uintptr_t)ids & 3) == 0 && aligned16(weight) && aligned16(out), "embed_fwd: weight and out must be 16-byte aligned, ids 4");
   REQ(embed_shape_ok(dtype, rows, vocab, hidden), "embed_fwd: bad argument (hidden must be a multiple of 8, fp32: 4)");
   return wrap(launch_embed_fwd((int)dtype, ids, weight, out, (int)rows, vocab, (int)hidden, scale, (hipStream_t)stream), "embed_fwd");
 }
@@ -417,7 +417,7 @@ uint64_t optstage_op_embed_bwd_ws_bytes(uint32_t rows, uint32_t hidden) {
 optstage_status optstage_op_embed_bwd(uint32_t dtype, const int32_t* ids, const void* dy, float* grad, void* ws, uint64_t ws_bytes, uint32_t rows,
                                       uint32_t vocab, uint32_t hidden, float scale, void* stream) {
   REQ(ids && dy && grad && ws, "embed_bwd: null operand");
-  REQ(aligned16(ids) && aligned16(dy) && aligned16(grad) && aligned16(ws), "embed_bwd: operands must be 16-byte aligned");
+  REQ(((uintptr_t)ids & 3) == 0 && aligned16(dy) && aligned16(grad) && aligned16(ws), "embed_bwd: dy, grad and ws must be 16-byte aligned, ids 4");
   REQ(embed_shape_ok(dtype, rows, vocab, hidden), "embed_bwd: bad argument (hidden must be a multiple of 8, fp32: 4)");
   REQ(ws_bytes >= embed_bwd_ws_bytes((int)rows, (int)hidden), "embed_bwd: workspace smaller than optstage_op_embed_bwd_ws_bytes()");
   return wrap(launch_embed_bwd((int)dtype, ids, dy, grad, ws, (int)rows, vocab, (int)hidden, scale, (hipStream_t)stream), "embed_bwd");

@@ -142,7 +142,7 @@ def _one_bad_argument():
             if v in (A, 2 * A):
                 if (name, key) not in MAY_BE_NULL:
                     yield name, {key: 0}
-                yield name, {key: v + 8}                                 # 16-byte alignment
+                yield name, {key: v + (2 if key == "ids" else 8)}        # 16-byte alignment; ids of 4 bytes
             elif key == "dtype":
                 yield name, {key: 2}
             elif key in ("rows", "cols", "hidden", "ffn", "seq", "n_q", "n_kv", "head_dim", "vocab"):
