@@ -7,6 +7,8 @@
 // from some thousand tokens of some thousand columns on, by the latency of the launches below that.
 #include "common.h"
 
+#include <type_traits>
+
 namespace {
 
 constexpr int NT = 256;
@@ -198,22 +200,21 @@ __global__ __launch_bounds__(THREADS) void embed_sort_kernel(const unsigned* __r
 
 // ---- sums -----------------------------------------------------------------------------------------------------
 constexpr int PIECE = 32;                                               // rows that one wave adds up
-constexpr int FLIGHT = 16;                                              // of them in flight
 
-// The sum over the `n` rows whose numbers the lanes hold, n <= 64, of the lane's chunk at column col.
-template <typename T> __device__ __forceinline__ void add_rows(const T* __restrict__ dy, unsigned row, int n, size_t h, int col, bool on, float* s) {
+// s += the lane's chunk at column col over the rows whose numbers lanes first .. end - 1 hold, in their order; FLIGHT loads in flight, those behind the end
+// of its last row again
+template <int FLIGHT, typename T> __device__ __forceinline__ void add_rows(const T* __restrict__ dy, unsigned row, int first, int end, size_t h, int col, float* s) {
   typedef Vec16<T> V;
-  for (int i0 = 0; i0 < n; i0 += FLIGHT) {
+  for (int i0 = first; i0 < end; i0 += FLIGHT) {
     V v[FLIGHT];
 #pragma unroll
-    for (int u = 0; u < FLIGHT; ++u)
-      if (i0 + u < n) {
-        const size_t r = (unsigned)__builtin_amdgcn_readlane((int)row, i0 + u);
-        if (on) v[u] = *reinterpret_cast<const V*>(dy + r * h + col);
-      }
+    for (int u = 0; u < FLIGHT; ++u) {
+      const size_t r = (unsigned)__builtin_amdgcn_readlane((int)row, min(i0 + u, end - 1));
+      v[u].v = __builtin_nontemporal_load(&reinterpret_cast<const V*>(dy + r * h + col)->v);
+    }
 #pragma unroll
     for (int u = 0; u < FLIGHT; ++u)
-      if (i0 + u < n)
+      if (i0 + u < end)
 #pragma unroll
         for (int e = 0; e < V::N; ++e) s[e] += v[u].get(e);
   }
@@ -230,19 +231,20 @@ template <int N> __device__ __forceinline__ void add_to(float* g, const float* s
 
 // Wave (w, slice): places w Q .. w Q + Q - 1 of the sorted tokens, 64 chunks of columns.  Its are the runs of equal tokens that begin there, to their ends, which lie up to
 // PIECE places on: one stretch of places, BATCH rows of dy in flight together with the accumulator's rows of the runs that end among them (with one run
-// to a wave, 4096 tokens took 41 us instead of 27: half of the waves find no run, the others wait for one row).  A run of more than PIECE places is cut at
+// to a wave, 4096 tokens took 41 us instead of 26: half of the waves find no run, the others wait for one row).  A run of more than PIECE places is cut at
 // multiples of PIECE: partial[2 k] is the sum of the piece that begins at place k PIECE, partial[2 k + 1] that of the piece of a long run that begins
 // later in that range (only one can: it goes on behind it).
-constexpr int Q = 8, BATCH = 8;
-static_assert(PIECE == 32 && PIECE % Q == 0 && Q + PIECE <= 63, "masks of 64 places");
-template <typename T>
+constexpr int BATCH = 8;
+template <typename T, int Q>
 __global__ __launch_bounds__(NT) void embed_sum_kernel(const unsigned* __restrict__ key, const unsigned* __restrict__ row_of, const T* __restrict__ dy, float* __restrict__ grad,
                                                        unsigned* count, unsigned* long_runs, float* __restrict__ partial, int rows, int h, unsigned groups, float scale) {
+  static_assert(PIECE == 32 && PIECE % Q == 0 && Q + PIECE <= 64, "masks of 64 places");
   typedef Vec16<T> V;
   constexpr int N = V::N;
   const int lane = threadIdx.x & 63, slice = (int)((blockIdx.x % groups) * blockDim.x + threadIdx.x) >> 6, col = (slice * 64 + lane) * N;
   if (slice * 64 * N >= h) return;
   const bool on = col < h;
+  const int at = on ? col : 0;                                          // lanes behind the last column load, and store nothing
   for (long long base = (long long)(blockIdx.x / groups) * Q; base < rows; base += (long long)(gridDim.x / groups) * Q) {
     const long long m = count[0], xa = base - PIECE + lane, xb = base + PIECE + lane;
     const auto inside = [&](long long x) { return x < 0 ? 0 : x < rows ? x : (long long)rows - 1; };
@@ -269,55 +271,53 @@ __global__ __launch_bounds__(NT) void embed_sum_kernel(const unsigned* __restric
     if (cut) end = min(end, (int)(PIECE - (base + last) % PIECE) + last);
     const int resumed_end = !resumed ? -1 : (mine ? __ffsll((long long)mine) - 1 : end);
     if (cut && mine && slice == 0 && lane == 0) long_runs[atomicAdd(&count[1], 1u)] = (unsigned)(base + last);
+    // whole runs, and the rest of a resumed one: BATCH rows in flight together with the accumulator's rows of the runs that end among them
+    const int whole = cut ? last : end;
     float s[N] = {};
-    for (int i = first; i < end; i += BATCH) {
+    for (int i = first; i < whole; i += BATCH) {
       V v[BATCH];
       f32x4_t g[BATCH][N / 4];
       float* to[BATCH];                                                 // rows, the same for the whole wave
+      const unsigned ends = (unsigned)(starts >> (i + 1));              // bit u: a run ends with place i + u
+#pragma unroll
+      for (int u = 0; u < BATCH; ++u) {
+        const size_t r = (unsigned)__builtin_amdgcn_readlane((int)row, min(i + u, whole - 1));
+        v[u].v = __builtin_nontemporal_load(&reinterpret_cast<const V*>(dy + r * h + at)->v);   // read once: 86 -> 75 us at 16384 x 5120
+      }
 #pragma unroll
       for (int u = 0; u < BATCH; ++u)
-        if (i + u < end) {
-          const size_t r = (unsigned)__builtin_amdgcn_readlane((int)row, i + u);
-          if (on) v[u].v = __builtin_nontemporal_load(&reinterpret_cast<const V*>(dy + r * h + col)->v);   // read once: 86 -> 75 us at 16384 x 5120
+        if (i + u < whole && (ends >> u & 1)) {
+          const int x = i + u;
+          const size_t id = (unsigned)(x < PIECE ? __builtin_amdgcn_readlane((int)ka, x + PIECE) : __builtin_amdgcn_readlane((int)kb, x - PIECE));
+          to[u] = x + 1 == resumed_end ? partial + (size_t)(base / PIECE * 2) * h : grad + id * h;
+#pragma unroll
+          for (int c = 0; c < N / 4; ++c) g[u][c] = *reinterpret_cast<const f32x4_t*>(to[u] + at + 4 * c);
         }
 #pragma unroll
-      for (int u = 0; u < BATCH; ++u) {
-        const int next = i + u + 1;
-        to[u] = nullptr;
-        if (next <= end && (next == end || (starts >> next & 1))) {
-          const bool piece = next == resumed_end || (cut && next == end);
-          if (piece) {
-            const unsigned long long at = (unsigned long long)base + (next == resumed_end ? 0 : last);
-            to[u] = partial + (size_t)(at / PIECE * 2 + (at % PIECE ? 1 : 0)) * h;
-#pragma unroll
-            for (int c = 0; c < N / 4; ++c) g[u][c] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
-          } else {
-            const int x = next - 1;
-            const size_t id = (unsigned)(x < PIECE ? __builtin_amdgcn_readlane((int)ka, x + PIECE) : __builtin_amdgcn_readlane((int)kb, x - PIECE));
-            to[u] = grad + id * h;
-            if (on)
-#pragma unroll
-              for (int c = 0; c < N / 4; ++c) g[u][c] = *reinterpret_cast<const f32x4_t*>(to[u] + col + 4 * c);
-          }
-        }
-      }
-#pragma unroll
-      for (int u = 0; u < BATCH; ++u) {
-        if (i + u < end)
+      for (int u = 0; u < BATCH; ++u)
+        if (i + u < whole) {
 #pragma unroll
           for (int e = 0; e < N; ++e) s[e] += v[u].get(e);
-        if (to[u]) {
-          const float by = (i + u + 1 == resumed_end || (cut && i + u + 1 == end)) ? 1.f : scale;
+          if (ends >> u & 1) {
+            const bool piece = i + u + 1 == resumed_end;
 #pragma unroll
-          for (int e = 0; e < N; ++e) {
-            g[u][e / 4][e % 4] += by * s[e];
-            s[e] = 0.f;
+            for (int e = 0; e < N; ++e) {
+              g[u][e / 4][e % 4] = piece ? s[e] : fmaf(scale, s[e], g[u][e / 4][e % 4]);
+              s[e] = 0.f;
+            }
+            if (on)
+#pragma unroll
+              for (int c = 0; c < N / 4; ++c) *reinterpret_cast<f32x4_t*>(to[u] + at + 4 * c) = g[u][c];
           }
-          if (on)
-#pragma unroll
-            for (int c = 0; c < N / 4; ++c) *reinterpret_cast<f32x4_t*>(to[u] + col + 4 * c) = g[u][c];
         }
-      }
+    }
+    if (cut) {
+      add_rows<16>(dy, row, last, end, (size_t)h, at, s);
+      const unsigned long long p = (unsigned long long)base + last;
+      float* piece = partial + (size_t)(p / PIECE * 2 + (p % PIECE ? 1 : 0)) * h + at;
+      if (on)
+#pragma unroll
+        for (int i = 0; i < N; i += 4) *reinterpret_cast<f32x4_t*>(piece + i) = (f32x4_t){s[i], s[i + 1], s[i + 2], s[i + 3]};
     }
   }
 }
@@ -388,7 +388,8 @@ __global__ __launch_bounds__(NT) void embed_few_kernel(const int* __restrict__ i
     // lane k gets the number of the k-th row of the 64
     const int n = __popcll(same[i]), k = __popcll(same[i] & ((1ull << lane) - 1));
     const unsigned row = (unsigned)__builtin_amdgcn_ds_permute((same[i] >> lane & 1 ? k : 63) * 4, i * 64 + lane);
-    add_rows(dy, row, n, (size_t)h, col, col < h, s);
+    if (n == 1) add_rows<1>(dy, row, 0, 1, (size_t)h, col < h ? col : 0, s);
+    else add_rows<8>(dy, row, 0, n, (size_t)h, col < h ? col : 0, s);
   }
   if (col < h) add_to<N>(grad + (size_t)id * h + col, s, scale);
 }
@@ -440,8 +441,17 @@ hipError_t run_embed_bwd(const int* ids, const void* dy, float* grad, void* ws, 
     if (e != hipSuccess) return e;
   }
   const int last = (passes - 1) & 1;
-  hipLaunchKernelGGL(embed_sum_kernel<T>, dim3(min((rows + Q - 1) / Q, max(1, (1 << 22) / (int)slices)) * slices), dim3(threads), 0, s, w.key[last], w.row[last],
-                     (const T*)dy, grad, w.count, w.long_runs, w.partial, rows, h, slices, scale);
+  const auto sum = [&](auto q) {
+    hipLaunchKernelGGL((embed_sum_kernel<T, q>), dim3(min((rows + q - 1) / q, max(1, (1 << 22) / (int)slices)) * slices), dim3(threads), 0, s, w.key[last], w.row[last],
+                       (const T*)dy, grad, w.count, w.long_runs, w.partial, rows, h, slices, scale);
+  };
+  // Places of a wave: the more of them, the fewer waves find only the middle of a run, but there have to be waves enough, and where most runs are of one or
+  // two places a wave has to wait for many rows of the accumulator.  us with 8, 16, 32: 1000 x 4096 of 32000 words 13, 15, 21; 4096 x 4096 of 32000 words
+  // 27, 26, 27; 49000 x 200 of 10190 words 23, 16, 19; 16384 x 5120 of 131072 words 77, 79, 84; 22713 x 1352 fp32 of 821 words 73, 50, 39.
+  const uint64_t all = (uint64_t)rows * waves;
+  if (all < 16384) sum(std::integral_constant<int, 8>());
+  else if ((unsigned)rows < vocab || all < 98304) sum(std::integral_constant<int, 16>());
+  else sum(std::integral_constant<int, 32>());
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   hipLaunchKernelGGL(embed_join_kernel, dim3(512), dim3(JOIN_T), 0, s, w.key[last], w.count, w.long_runs, w.partial, grad, h, scale);
