@@ -219,11 +219,15 @@ __global__ __launch_bounds__(W * R * 64) void norm_bwd8_kernel(const T* dn, cons
   __shared__ f32x4_t sums[R > 1 ? R : 1][R > 1 ? C * V::N / 4 : 1][W * 64];      // 32 KB
   const int slot = threadIdx.x / (W * 64), l = threadIdx.x % (W * 64), wave = l >> 6, nb = keep_blocks(h);
   float pg[C][V::N] = {}, pb[LN ? C : 1][V::N] = {};
-  V gv[C];
+  V gv[C], bv[LN ? C : 1];
 #pragma unroll
   for (int c = 0; c < C; ++c) {
     const int col = (l + c * W * 64) * V::N;
-    if (col < h) gv[c] = *reinterpret_cast<const V*>(gamma + col);
+    if (col < h) {
+      gv[c] = *reinterpret_cast<const V*>(gamma + col);
+      if constexpr (LN)
+        if (out) bv[c] = *reinterpret_cast<const V*>(beta + col);
+    }
   }
   struct Row { V d[C], res[C]; codes_t q[C]; uint32_t b[C]; float mean, r; } buf[2];
   auto load = [&](Row& k, size_t row) {
@@ -283,15 +287,14 @@ __global__ __launch_bounds__(W * R * 64) void norm_bwd8_kernel(const T* dn, cons
     for (int c = 0; c < C; ++c) {
       const int col = (l + c * W * 64) * V::N;
       if (col < h) {
-        V o, n, b;
-        if (LN && out) b = *reinterpret_cast<const V*>(beta + col);
+        V o, n;
 #pragma unroll
         for (int e = 0; e < V::N; ++e) {
           float v = k.r * (k.d[c].get(e) * gv[c].get(e) - mg - xh[c][e] * mgx);
           if (dres) v += k.res[c].get(e);
           o.set(e, v);
           float y = xh[c][e] * gv[c].get(e);
-          if (LN && out) y += b.get(e);
+          if constexpr (LN) y += bv[c].get(e);
           n.set(e, y);
         }
         *reinterpret_cast<V*>(dx + row * h + col) = o;
