@@ -139,7 +139,7 @@ optstage_status optstage_op_norm_fwd_pack8(uint32_t dtype, uint32_t family, cons
 optstage_status optstage_op_norm_bwd8(uint32_t dtype, uint32_t family, const void* dn, const uint8_t* codes, const uint8_t* scales,
                                       const float* stats, const void* gamma, const void* beta, const void* dres, void* dx, void* out,
                                       float* partial, float* dgamma, float* dbeta, uint32_t rows, uint32_t hidden, void* stream);
-/* optstage_op_act_fwd that keeps gu.  LLAMA: as 2 * rows rows of ffn values, row 2 r the gate's and 2 r + 1 the up projection's.  ffn is a
+/* optstage_op_act_fwd that keeps gu (a is not gu).  LLAMA: as 2 * rows rows of ffn values, row 2 r the gate's and 2 r + 1 the up projection's.  ffn is a
  * multiple of 8 (fp32: 4). */
 optstage_status optstage_op_act_fwd_pack8(uint32_t dtype, uint32_t family, const void* gu, void* a, uint8_t* codes, uint8_t* scales,
                                           uint32_t rows, uint32_t ffn, void* stream);
@@ -161,7 +161,7 @@ optstage_status optstage_op_qknorm_rope8(uint32_t dtype, const uint8_t* codes, c
                                          const void* gamma_k, const float* table, void* dst, uint32_t rows, uint32_t seq, uint32_t n_q,
                                          uint32_t n_kv, uint32_t head_dim, void* stream);
 /* dx from dy (the attention's gradient, rows as above) and either x (the rows before the norm) or codes and scales; dgamma_q and dgamma_k
- * (fp32 [head_dim]) are ADDED to.  dx may be dy or x; the v part of dy is passed on.  partial: fp32 scratch of
+ * (fp32 [head_dim], two buffers also where q and k share a gain) are ADDED to.  dx may be dy or x; the v part of dy is passed on.  partial: fp32 scratch of
  * 2 * min(rows, 1024) * head_dim elements. */
 optstage_status optstage_op_qknorm_rope_bwd(uint32_t dtype, const void* dy, const void* x, const uint8_t* codes, const uint8_t* scales,
                                             const float* stats, const void* gamma_q, const void* gamma_k, const float* table, void* dx,

@@ -328,6 +328,7 @@ optstage_status optstage_op_norm_bwd8(uint32_t dtype, uint32_t family, const voi
           aligned16(out) && aligned16(partial) && aligned16(dgamma) && aligned16(dbeta),
       "norm_bwd8: operands must be 16-byte aligned");
   REQ(out != dx && (!out || (out != dn && out != dres)), "norm_bwd8: out must be a buffer of its own");
+  REQ(family == OPTSTAGE_LLAMA || dgamma != dbeta, "norm_bwd8: dgamma and dbeta must be two buffers");
   REQ(hidden <= 8192 && norm8_shape_ok((int)dtype, (int)hidden), "norm_bwd8: hidden must be a multiple of 8 (fp32: 4), at most 8192");
   return wrap(launch_norm_bwd8((int)dtype, (int)family, dn, codes, scales, stats, gamma, beta, dres, dx, out, partial, dgamma, dbeta, (int)rows, (int)hidden,
                                (hipStream_t)stream),
@@ -338,6 +339,7 @@ optstage_status optstage_op_act_fwd_pack8(uint32_t dtype, uint32_t family, const
                                           uint32_t rows, uint32_t ffn, void* stream) {
   REQ(gu && a && codes && scales, "act_fwd_pack8: null operand");
   REQ(aligned16(gu) && aligned16(a) && aligned16(codes) && aligned16(scales), "act_fwd_pack8: operands must be 16-byte aligned");
+  REQ(a != gu, "act_fwd_pack8: a must be a buffer of its own");
   REQ(dtype <= 1 && family <= 1 && rows && ffn && rows < (1u << 30) && ffn < (1u << 29), "act_fwd_pack8: bad argument");
   REQ(ffn % (dtype == OPTSTAGE_BF16 ? 8 : 4) == 0, "act_fwd_pack8: ffn must be a multiple of 8 (fp32: 4)");
   return wrap(launch_act_fwd_pack8((int)dtype, (int)family, gu, a, codes, scales, (int)rows, (int)ffn, (hipStream_t)stream), "act_fwd_pack8");
@@ -388,6 +390,7 @@ optstage_status optstage_op_qknorm_rope_bwd(uint32_t dtype, const void* dy, cons
                                             uint32_t n_kv, uint32_t head_dim, void* stream) {
   REQ(dy && stats && gamma_q && gamma_k && table && dx && partial && dgamma_q && dgamma_k, "qknorm_rope_bwd: null operand");
   REQ(!codes == !scales && !x == !!codes, "qknorm_rope_bwd: either x or codes and scales");
+  REQ(dgamma_q != dgamma_k, "qknorm_rope_bwd: dgamma_q and dgamma_k must be two buffers");
   REQ(aligned16(dy) && aligned16(x) && aligned16(codes) && aligned16(scales) && aligned16(stats) && aligned16(gamma_q) && aligned16(gamma_k) && aligned16(table) &&
           aligned16(dx) && aligned16(partial) && aligned16(dgamma_q) && aligned16(dgamma_k),
       "qknorm_rope_bwd: operands must be 16-byte aligned");

@@ -182,7 +182,7 @@ struct QkNormBwd {
 
 // dx may be dy or x: a lane has read its chunks before it writes there.  The gains' gradients of a
 // workgroup's heads stay in registers, 2 N of q and of k a lane, and end in partial[blockIdx.x] (q) and partial[gridDim.x + blockIdx.x] (k), added up in a
-// fixed order.
+// fixed order; a workgroup alone adds them to the accumulators itself.
 template <typename T, int G, bool FROM8>
 __global__ __launch_bounds__(NT) void qknorm_bwd_kernel(const QkNormBwd p) {
   typedef Vec16<T> V;

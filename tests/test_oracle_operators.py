@@ -105,14 +105,14 @@ CALLS = {
     "optstage_op_unpack8": dict(dtype=1, codes=A, scales=A, x=A, ldx=64, rows=4, cols=64, stream=0),
     "optstage_op_norm_fwd_pack8": dict(dtype=1, family=0, x=A, gamma=A, beta=A, out=2 * A, stats=A, codes=A, scales=A, rows=4, hidden=64, eps=1e-5,
                                        stream=0),
-    "optstage_op_norm_bwd8": dict(dtype=1, family=0, dn=A, codes=A, scales=A, stats=A, gamma=A, beta=A, dres=A, dx=A, out=2 * A, partial=A, dgamma=A, dbeta=A, rows=4, hidden=64,
+    "optstage_op_norm_bwd8": dict(dtype=1, family=0, dn=A, codes=A, scales=A, stats=A, gamma=A, beta=A, dres=A, dx=A, out=2 * A, partial=A, dgamma=A, dbeta=2 * A, rows=4, hidden=64,
                                   stream=0),
-    "optstage_op_act_fwd_pack8": dict(dtype=1, family=1, gu=A, a=A, codes=A, scales=A, rows=4, ffn=64, stream=0),
+    "optstage_op_act_fwd_pack8": dict(dtype=1, family=1, gu=A, a=2 * A, codes=A, scales=A, rows=4, ffn=64, stream=0),
     "optstage_op_act_bwd8": dict(dtype=1, family=1, da=A, codes=A, scales=A, dgu=2 * A, a=A, rows=4, ffn=64, stream=0),
     "optstage_op_qknorm_rope": dict(dtype=1, src=A, dst=A, gamma_q=A, gamma_k=A, table=A, stats=A, codes=A, scales=A, rows=4, seq=4, n_q=2, n_kv=1, head_dim=64, eps=1e-5,
                                     stream=0),
     "optstage_op_qknorm_rope8": dict(dtype=1, codes=A, scales=A, stats=A, gamma_q=A, gamma_k=A, table=A, dst=A, rows=4, seq=4, n_q=2, n_kv=1, head_dim=64, stream=0),
-    "optstage_op_qknorm_rope_bwd": dict(dtype=1, dy=A, x=A, codes=0, scales=0, stats=A, gamma_q=A, gamma_k=A, table=A, dx=A, partial=A, dgamma_q=A, dgamma_k=A, rows=4, seq=4,
+    "optstage_op_qknorm_rope_bwd": dict(dtype=1, dy=A, x=A, codes=0, scales=0, stats=A, gamma_q=A, gamma_k=A, table=A, dx=A, partial=A, dgamma_q=A, dgamma_k=2 * A, rows=4, seq=4,
                                         n_q=2, n_kv=1, head_dim=64, stream=0),
     "optstage_op_embed_fwd": dict(dtype=1, ids=A, weight=A, out=A, rows=4, vocab=10, hidden=64, scale=1.0, stream=0),
     "optstage_op_embed_bwd": dict(dtype=1, ids=A, dy=A, grad=A, ws=A, ws_bytes=1 << 30, rows=4, vocab=10, hidden=64, scale=1.0, stream=0),
@@ -124,6 +124,7 @@ MORE = [
     ("optstage_op_norm_fwd_pack8", dict(dtype=0, hidden=62)), ("optstage_op_norm_fwd_pack8", dict(hidden=(1 << 32) - 8)),
     ("optstage_op_norm_bwd8", dict(hidden=60)), ("optstage_op_norm_bwd8", dict(hidden=8200)), ("optstage_op_norm_bwd8", dict(out=A)), ("optstage_op_norm_bwd8", dict(dx=2 * A)),
     ("optstage_op_act_fwd_pack8", dict(ffn=60)), ("optstage_op_act_fwd_pack8", dict(family=2)), ("optstage_op_act_fwd_pack8", dict(ffn=1 << 29)),
+    ("optstage_op_act_fwd_pack8", dict(a=A)), ("optstage_op_norm_bwd8", dict(dbeta=A)), ("optstage_op_qknorm_rope_bwd", dict(dgamma_k=A)),
     ("optstage_op_act_bwd8", dict(ffn=60)), ("optstage_op_act_bwd8", dict(dgu=A)), ("optstage_op_act_bwd8", dict(a=2 * A)), ("optstage_op_act_bwd8", dict(dtype=0, ffn=62)),
     ("optstage_op_qknorm_rope", dict(codes=0)), ("optstage_op_qknorm_rope", dict(scales=0)), ("optstage_op_qknorm_rope", dict(head_dim=96)),
     ("optstage_op_qknorm_rope", dict(head_dim=320)), ("optstage_op_qknorm_rope", dict(n_q=65536)), ("optstage_op_qknorm_rope8", dict(head_dim=32)),
