@@ -1,7 +1,7 @@
 // Embedding: out[r] = scale * weight[ids[r]], and its gradient grad[t] += scale * (sum of dy[r] over the rows r with ids[r] = t).
 // A row whose id is no word of the vocabulary (negative, or vocab and more: padding) is zero and has no gradient.
 //
-// The gradient sorts the tokens, so that equal ones stand side by side and every row of the accumulator that occurs is read and written once, without
+// The gradient puts the tokens in order, so that equal ones stand side by side and every row of the accumulator that occurs is read and written once, without
 // atomics and in an order that the ids alone decide: the rows of a token in their order, up to PIECE of them by one wave.  The runs of frequent
 // tokens are cut at multiples of PIECE, and their pieces' sums are added by a second launch.  Bound by memory (dy once, the accumulator's rows in and out)
 // from some thousand tokens of some thousand columns on, by the latency of the launches below that.
@@ -54,7 +54,7 @@ __global__ __launch_bounds__(NT) void embed_fwd_kernel(const int* __restrict__ i
 // Beyond that a launch ahead of it counts each range once (65536 tokens, 256 columns: 69 us with it, 76 without).  The first pass takes the ids
 // themselves and leaves out those that are no words.
 constexpr int RADIX = 512, COPIES = 8;                                  // counters in 8 copies by lane: equal digits of a wave meet 8 at a time at most
-constexpr int SORT_MAX_GROUPS = 256, SORT_COUNTED = 16384;
+constexpr int SORT_T = 1024, SORT_MAX_GROUPS = 256, SORT_COUNTED = 16384;
 
 struct Sorted {
   unsigned* count;                                                      // [0] valid tokens, [1] runs in `long_runs`
@@ -71,19 +71,19 @@ struct Pass {
 __device__ __forceinline__ void count_digits(unsigned (&hist)[RADIX * COPIES], unsigned digit) { atomicAdd(&hist[digit * COPIES + (threadIdx.x & (COPIES - 1))], 1u); }
 
 // table[g][d]: keys of digit d in range g
-__global__ __launch_bounds__(1024) void embed_count_kernel(const unsigned* __restrict__ ids, const Sorted w, const Pass p) {
+__global__ __launch_bounds__(SORT_T) void embed_count_kernel(const unsigned* __restrict__ ids, const Sorted w, const Pass p) {
   __shared__ unsigned hist[RADIX * COPIES];
   const unsigned tid = threadIdx.x, digits = 1u << p.bits, n = p.number == 0 ? p.rows : w.count[0];
   const unsigned* key_in = p.number == 0 ? ids : w.key[(p.number - 1) & 1];
   const unsigned begin = min(n, blockIdx.x * p.per_group), end = min(n, begin + p.per_group);
-  for (unsigned i = tid; i < digits * COPIES; i += 1024) hist[i] = 0;
+  for (unsigned i = tid; i < digits * COPIES; i += SORT_T) hist[i] = 0;
   __syncthreads();
-  for (unsigned i = begin + tid; i < end; i += 1024) {
+  for (unsigned i = begin + tid; i < end; i += SORT_T) {
     const unsigned k = key_in[i];
     if (k < p.vocab) count_digits(hist, k >> p.shift & (digits - 1));
   }
   __syncthreads();
-  for (unsigned d = tid; d < digits; d += 1024) {
+  for (unsigned d = tid; d < digits; d += SORT_T) {
     unsigned s = 0;
 #pragma unroll
     for (int c = 0; c < COPIES; ++c) s += hist[d * COPIES + c];
@@ -91,9 +91,8 @@ __global__ __launch_bounds__(1024) void embed_count_kernel(const unsigned* __res
   }
 }
 
-template <int THREADS>
-__global__ __launch_bounds__(THREADS) void embed_sort_kernel(const unsigned* __restrict__ ids, const Sorted w, const Pass p, int counted) {
-  constexpr int WAVES = THREADS / 64;
+__global__ __launch_bounds__(SORT_T) void embed_sort_kernel(const unsigned* __restrict__ ids, const Sorted w, const Pass p, int counted) {
+  constexpr int WAVES = SORT_T / 64;
   __shared__ union {
     unsigned hist[2][RADIX * COPIES];                                   // ahead of the range, and the rest
     unsigned wave_count[WAVES][RADIX];
@@ -119,18 +118,18 @@ __global__ __launch_bounds__(THREADS) void embed_sort_kernel(const unsigned* __r
         }
       }
   } else {
-    for (unsigned i = tid; i < digits * COPIES; i += THREADS) lds.hist[0][i] = lds.hist[1][i] = 0;
+    for (unsigned i = tid; i < digits * COPIES; i += SORT_T) lds.hist[0][i] = lds.hist[1][i] = 0;
     __syncthreads();
-    for (unsigned i0 = 0; i0 < n; i0 += THREADS * 8) {
+    for (unsigned i0 = 0; i0 < n; i0 += SORT_T * 8) {
       unsigned k[8];
 #pragma unroll
       for (int u = 0; u < 8; ++u) {
-        const unsigned i = i0 + u * THREADS + tid;
+        const unsigned i = i0 + u * SORT_T + tid;
         k[u] = i < n ? key_in[i] : 0xffffffffu;
       }
 #pragma unroll
       for (int u = 0; u < 8; ++u) {
-        const unsigned i = i0 + u * THREADS + tid;
+        const unsigned i = i0 + u * SORT_T + tid;
         if (i < n && k[u] < p.vocab) count_digits(lds.hist[i < begin ? 0 : 1], k[u] >> p.shift & mask);
       }
     }
@@ -161,10 +160,10 @@ __global__ __launch_bounds__(THREADS) void embed_sort_kernel(const unsigned* __r
   }
   if (tid < digits) place[tid] = before - all + ahead;
   if (p.number == 0 && blockIdx.x == 0 && tid == 0) { w.count[0] = sum; w.count[1] = 0; }
-  // the range, THREADS keys at a time: a lane's place is its digit's, past the waves ahead and the lanes of its own wave ahead with the same digit
-  for (unsigned i0 = begin; i0 < end; i0 += THREADS) {
+  // the range, SORT_T keys at a time: a lane's place is its digit's, past the waves ahead and the lanes of its own wave ahead with the same digit
+  for (unsigned i0 = begin; i0 < end; i0 += SORT_T) {
     __syncthreads();
-    for (unsigned i = tid; i < (unsigned)WAVES << p.bits; i += THREADS) lds.wave_count[i >> p.bits][i & mask] = 0;
+    for (unsigned i = tid; i < (unsigned)WAVES << p.bits; i += SORT_T) lds.wave_count[i >> p.bits][i & mask] = 0;
     __syncthreads();
     const unsigned i = i0 + tid;
     const unsigned key = i < end ? key_in[i] : 0xffffffffu;
@@ -194,6 +193,62 @@ __global__ __launch_bounds__(THREADS) void embed_sort_kernel(const unsigned* __r
       const unsigned at = lds.wave_count[wave][d] + rank;
       key_out[at] = key;
       row_out[at] = p.number == 0 ? i : row_in[i];
+    }
+  }
+}
+
+// A single launch for fewer tokens, whatever the vocabulary: a token's place is the number of smaller ones and of equal ones in earlier rows.  The waves of a
+// workgroup hold all keys, 64 consecutive ones in a register; for each of the workgroup's 2 K rows a register takes one comparison and one count of bits.  The work
+// goes with the square of the tokens: 600 tokens 3.6 us, two passes of the sort 8.6; 4096 4.8 and 10.6, one pass 5.3; 8192 9.1 and 12.6, one pass 6.6; 16384 24
+// and 16.  Twice the rows to a workgroup: 4.8 us at 600 tokens, the same from 4096 on.
+template <int K> __global__ __launch_bounds__(1024) void embed_place_kernel(const int* __restrict__ ids, const Sorted w, int rows, unsigned vocab) {
+  constexpr int R = 2 * K, NONE = 0x7fffffff;                           // NONE: padding, behind all words
+  static_assert(64 % R == 0, "a workgroup's rows lie in one block of 64");
+  __shared__ int part[16][R], words[16];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, first = (int)blockIdx.x * R, own = first / 64;
+  const auto load = [&](int j) {
+    const int id = j < rows ? ids[j] : NONE;
+    return (unsigned)id < vocab ? id : NONE;
+  };
+  int k[K];
+#pragma unroll
+  for (int i = 0; i < K; ++i) k[i] = load((wave * K + i) * 64 + lane);
+  const int block = load(own * 64 + lane);
+  if (blockIdx.x == 0) {
+    int n = 0;
+#pragma unroll
+    for (int i = 0; i < K; ++i) n += __popcll(__ballot(k[i] != NONE));
+    if (lane == 0) words[wave] = n;
+  }
+  // k - 1 < key is k <= key: equal ones of earlier blocks count; those of the own block are the first wave's
+#pragma unroll
+  for (int i = 0; i < K; ++i) k[i] -= wave * K + i < own ? 1 : 0;
+  int ahead = 0;
+#pragma unroll 8
+  for (int q = 0; q < R; ++q) {
+    const int at = first % 64 + q, key = __builtin_amdgcn_readlane(block, at);
+    int n = 0;
+#pragma unroll
+    for (int i = 0; i < K; ++i) n += __popcll(__ballot(k[i] < key));
+    if (wave == 0) n += __popcll(__ballot(block == key) & ((1ull << at) - 1));
+    ahead = lane == q ? n : ahead;
+  }
+  if (lane < R) part[wave][lane] = ahead;
+  __syncthreads();
+  if (wave == 0) {
+    const int key = __shfl(block, first % 64 + lane % R, 64);
+    if (lane < R && key != NONE) {
+      int place = 0;
+#pragma unroll
+      for (int v = 0; v < 16; ++v) place += part[v][lane];
+      w.key[0][place] = (unsigned)key;
+      w.row[0][place] = (unsigned)(first + lane);
+    }
+    if (blockIdx.x == 0 && lane == 0) {
+      int n = 0;
+      for (int v = 0; v < 16; ++v) n += words[v];
+      w.count[0] = (unsigned)n;
+      w.count[1] = 0;
     }
   }
 }
@@ -366,7 +421,9 @@ __global__ __launch_bounds__(JOIN_T) void embed_join_kernel(const unsigned* __re
 }
 
 // A few tokens, in one launch: wave (r, slice) compares all ids with row r's and adds up its token's rows if r is the first of them.
-constexpr int FEW = 512;
+// In bf16, lookup and gradient in us, and with the launches above instead: 400 tokens of 32000 words and 512 columns 9.9, 14.6; of 50 words and 4096
+// columns 19.9, 18.0; 512 tokens 10.8, 15.6 and 26.9, 17.6.
+constexpr int FEW = 448;
 template <typename T>
 __global__ __launch_bounds__(NT) void embed_few_kernel(const int* __restrict__ ids, const T* __restrict__ dy, float* __restrict__ grad, int rows, unsigned vocab, int h,
                                                        float scale) {
@@ -395,9 +452,8 @@ __global__ __launch_bounds__(NT) void embed_few_kernel(const int* __restrict__ i
 }
 
 unsigned sort_range(int rows) {
-  if (rows <= 8192) return 512;
-  const unsigned tiles = ((unsigned)rows + 1023) / 1024;
-  return (tiles + SORT_MAX_GROUPS - 1) / SORT_MAX_GROUPS * 1024;
+  const unsigned tiles = ((unsigned)rows + SORT_T - 1) / SORT_T;
+  return (tiles + SORT_MAX_GROUPS - 1) / SORT_MAX_GROUPS * SORT_T;
 }
 
 Sorted layout(void* ws, int rows, int h, uint64_t* bytes) {
@@ -429,18 +485,23 @@ hipError_t run_embed_bwd(const int* ids, const void* dy, float* grad, void* ws, 
   int bits = 1;
   while (bits < 31 && (vocab - 1) >> bits) ++bits;
   const int passes = (bits + 8) / 9, per_pass = (bits + passes - 1) / passes;
-  // keys of a workgroup: 512 of them up to 8192 tokens (4096 tokens of 256 columns 24.2 us, 25.8 with 1024), 1024 beyond (16384: 33.6 us, 34.3 with 512)
-  const bool counted = rows > SORT_COUNTED;
-  const unsigned keys = rows <= 8192 ? 512 : 1024, per_group = sort_range(rows), groups = ((unsigned)rows + per_group - 1) / per_group;
-  for (int i = 0; i < passes; ++i) {
-    const Pass p = {per_pass * i, min(per_pass, bits - per_pass * i), i, (unsigned)rows, vocab, per_group};
-    if (counted) hipLaunchKernelGGL(embed_count_kernel, dim3(groups), dim3(1024), 0, s, (const unsigned*)ids, w, p);
-    if (keys == 512) hipLaunchKernelGGL(embed_sort_kernel<512>, dim3(groups), dim3(512), 0, s, (const unsigned*)ids, w, p, 0);
-    else hipLaunchKernelGGL(embed_sort_kernel<1024>, dim3(groups), dim3(1024), 0, s, (const unsigned*)ids, w, p, counted ? 1 : 0);
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
+  const bool placed = rows <= 4096 * min(passes, 2);
+  if (placed) {
+    const auto place = [&](auto k) { hipLaunchKernelGGL((embed_place_kernel<k>), dim3((rows + 2 * k - 1) / (2 * k)), dim3(1024), 0, s, ids, w, rows, vocab); };
+    if (rows <= 4096) place(std::integral_constant<int, 4>());
+    else place(std::integral_constant<int, 8>());
+  } else {
+    const bool counted = rows > SORT_COUNTED;
+    const unsigned per_group = sort_range(rows), groups = ((unsigned)rows + per_group - 1) / per_group;
+    for (int i = 0; i < passes; ++i) {
+      const Pass p = {per_pass * i, min(per_pass, bits - per_pass * i), i, (unsigned)rows, vocab, per_group};
+      if (counted) hipLaunchKernelGGL(embed_count_kernel, dim3(groups), dim3(SORT_T), 0, s, (const unsigned*)ids, w, p);
+      hipLaunchKernelGGL(embed_sort_kernel, dim3(groups), dim3(SORT_T), 0, s, (const unsigned*)ids, w, p, counted ? 1 : 0);
+      const hipError_t e = hipGetLastError();
+      if (e != hipSuccess) return e;
+    }
   }
-  const int last = (passes - 1) & 1;
+  const int last = placed ? 0 : (passes - 1) & 1;
   const auto sum = [&](auto q) {
     hipLaunchKernelGGL((embed_sum_kernel<T, q>), dim3(min((rows + q - 1) / q, max(1, (1 << 22) / (int)slices)) * slices), dim3(threads), 0, s, w.key[last], w.row[last],
                        (const T*)dy, grad, w.count, w.long_runs, w.partial, rows, h, slices, scale);

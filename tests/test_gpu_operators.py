@@ -502,7 +502,9 @@ def ids_of(kind, rows, vocab, r):
 EMB = [(BF16, 1, 1, 8, "one"), (BF16, 1, 5, 64, "none"), (BF16, 64, 10, 8, "zipf"), (BF16, 65, 1000, 264, "all"), (BF16, 300, 50, 1024, "padded"), (BF16, 1000, 7, 40, "zipf"),
        (BF16, 2000, 3000, 512, "all"), (BF16, 3000, 32000, 128, "zipf"), (BF16, 257, 100, 4096, "one"), (BF16, 5000, 128, 16, "one"), (BF16, 9001, 70000, 64, "zipf"), (BF16, 20000, 300, 24, "padded"),
        (BF16, 40000, 200000, 8, "zipf"), (BF16, 66000, 131072, 8, "all"), (BF16, 70000, 5, 8, "padded"), (FP32, 1, 3, 4, "all"), (FP32, 128, 1000, 256, "zipf"), (FP32, 500, 20, 36, "padded"),
-       (FP32, 130, 64, 8192, "zipf"), (FP32, 10000, 30, 12, "one"), (BF16, 4097, 100000, 32, "none"), (FP32, 8193, 65536, 4, "zipf"), (BF16, 12000, 1 << 20, 8, "zipf")]
+       (FP32, 130, 64, 8192, "zipf"), (FP32, 10000, 30, 12, "one"), (BF16, 4097, 100000, 32, "none"), (FP32, 8193, 65536, 4, "zipf"), (BF16, 12000, 1 << 20, 8, "zipf"),
+       (BF16, 513, 9, 8, "padded"), (BF16, 4096, 40000, 16, "zipf"), (FP32, 4097, 513, 8, "one"), (BF16, 7001, 30000, 40, "padded"), (FP32, 8192, 600, 8, "zipf"), (BF16, 8191, 512, 8, "zipf"),
+       (BF16, 448, 30, 40, "padded"), (FP32, 449, 3000, 264, "all")]
 
 
 def run_embed(dtype, rows, vocab, h, kind, scale, seed=0, s=None):
