@@ -212,3 +212,8 @@ hipError_t launch_embed_fwd(int dtype, const int* ids, const void* weight, void*
 // ws: embed_bwd_ws_bytes() bytes
 hipError_t launch_embed_bwd(int dtype, const int* ids, const void* dy, float* grad, void* ws, int rows, unsigned vocab, int h, float scale, hipStream_t s);
 uint64_t embed_bwd_ws_bytes(int rows, int h);
+// how launch_embed_bwd orders its tokens: not at all (a few, one launch), by counting the keys ahead of each (one launch), or by that many passes of the sort
+enum { EMBED_FEW = 0, EMBED_PLACED = -1 };
+int embed_bwd_order(int rows, unsigned vocab);
+// the sorted places that a wave of its sums takes
+int embed_bwd_places(int dtype, int rows, unsigned vocab, int h);

@@ -473,24 +473,39 @@ Sorted layout(void* ws, int rows, int h, uint64_t* bytes) {
   return s;
 }
 
+int id_bits(unsigned vocab) {
+  int bits = 1;
+  while (bits < 31 && (vocab - 1) >> bits) ++bits;
+  return bits;
+}
+// waves side by side over a row's columns, n of them to a lane
+unsigned sum_waves(int h, int n) { return (unsigned)(h / n + 63) / 64; }
+// Places of a wave: the more of them, the fewer waves find only the middle of a run, but there have to be waves enough, and where most runs are of one or
+// two places a wave has to wait for many rows of the accumulator.  us with 8, 16, 32: 1000 x 4096 of 32000 words 13, 15, 21; 4096 x 4096 of 32000 words
+// 27, 26, 27; 49000 x 200 of 10190 words 23, 16, 19; 16384 x 5120 of 131072 words 77, 79, 84; 22713 x 1352 fp32 of 821 words 73, 50, 39.
+int sum_places(int rows, unsigned vocab, unsigned waves) {
+  const uint64_t all = (uint64_t)rows * waves;
+  if (all < 16384) return 8;
+  return (unsigned)rows < vocab || all < 98304 ? 16 : 32;
+}
+
 template <typename T>
 hipError_t run_embed_bwd(const int* ids, const void* dy, float* grad, void* ws, int rows, unsigned vocab, int h, float scale, hipStream_t s) {
-  const unsigned waves = (unsigned)(h / Vec16<T>::N + 63) / 64, threads = 64 * min(waves, 4u), slices = (waves + 3) / 4;
-  if (rows <= FEW) {
+  const unsigned waves = sum_waves(h, Vec16<T>::N), threads = 64 * min(waves, 4u), slices = (waves + 3) / 4;
+  const int order = embed_bwd_order(rows, vocab);
+  if (order == EMBED_FEW) {
     hipLaunchKernelGGL(embed_few_kernel<T>, dim3(rows, slices), dim3(threads), 0, s, ids, (const T*)dy, grad, rows, vocab, h, scale);
     return hipGetLastError();
   }
   uint64_t bytes;
   const Sorted w = layout(ws, rows, h, &bytes);
-  int bits = 1;
-  while (bits < 31 && (vocab - 1) >> bits) ++bits;
-  const int passes = (bits + 8) / 9, per_pass = (bits + passes - 1) / passes;
-  const bool placed = rows <= 4096 * min(passes, 2);
+  const bool placed = order == EMBED_PLACED;
   if (placed) {
     const auto place = [&](auto k) { hipLaunchKernelGGL((embed_place_kernel<k>), dim3((rows + 2 * k - 1) / (2 * k)), dim3(1024), 0, s, ids, w, rows, vocab); };
     if (rows <= 4096) place(std::integral_constant<int, 4>());
     else place(std::integral_constant<int, 8>());
   } else {
+    const int passes = order, bits = id_bits(vocab), per_pass = (bits + passes - 1) / passes;
     const bool counted = rows > SORT_COUNTED;
     const unsigned per_group = sort_range(rows), groups = ((unsigned)rows + per_group - 1) / per_group;
     for (int i = 0; i < passes; ++i) {
@@ -501,18 +516,16 @@ hipError_t run_embed_bwd(const int* ids, const void* dy, float* grad, void* ws, 
       if (e != hipSuccess) return e;
     }
   }
-  const int last = placed ? 0 : (passes - 1) & 1;
+  const int last = placed ? 0 : (order - 1) & 1;
   const auto sum = [&](auto q) {
     hipLaunchKernelGGL((embed_sum_kernel<T, q>), dim3(min((rows + q - 1) / q, max(1, (1 << 22) / (int)slices)) * slices), dim3(threads), 0, s, w.key[last], w.row[last],
                        (const T*)dy, grad, w.count, w.long_runs, w.partial, rows, h, slices, scale);
   };
-  // Places of a wave: the more of them, the fewer waves find only the middle of a run, but there have to be waves enough, and where most runs are of one or
-  // two places a wave has to wait for many rows of the accumulator.  us with 8, 16, 32: 1000 x 4096 of 32000 words 13, 15, 21; 4096 x 4096 of 32000 words
-  // 27, 26, 27; 49000 x 200 of 10190 words 23, 16, 19; 16384 x 5120 of 131072 words 77, 79, 84; 22713 x 1352 fp32 of 821 words 73, 50, 39.
-  const uint64_t all = (uint64_t)rows * waves;
-  if (all < 16384) sum(std::integral_constant<int, 8>());
-  else if ((unsigned)rows < vocab || all < 98304) sum(std::integral_constant<int, 16>());
-  else sum(std::integral_constant<int, 32>());
+  switch (sum_places(rows, vocab, waves)) {
+    case 8: sum(std::integral_constant<int, 8>()); break;
+    case 16: sum(std::integral_constant<int, 16>()); break;
+    default: sum(std::integral_constant<int, 32>());
+  }
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   hipLaunchKernelGGL(embed_join_kernel, dim3(512), dim3(JOIN_T), 0, s, w.key[last], w.count, w.long_runs, w.partial, grad, h, scale);
@@ -520,6 +533,13 @@ hipError_t run_embed_bwd(const int* ids, const void* dy, float* grad, void* ws, 
 }
 
 }  // namespace
+
+int embed_bwd_order(int rows, unsigned vocab) {
+  if (rows <= FEW) return EMBED_FEW;
+  const int passes = (id_bits(vocab) + 8) / 9;
+  return rows <= 4096 * (passes < 2 ? 1 : 2) ? EMBED_PLACED : passes;
+}
+int embed_bwd_places(int dtype, int rows, unsigned vocab, int h) { return sum_places(rows, vocab, sum_waves(h, dtype == DT_BF16 ? 8 : 4)); }
 
 uint64_t embed_bwd_ws_bytes(int rows, int h) {
   uint64_t bytes;
