@@ -124,3 +124,35 @@ def test_gradient_by_passes_of_the_sort(dtype, rows, vocab, h, kind, passes):
     g.call()
     torch.cuda.synchronize()
     assert torch.equal(g.grad[at], first)
+
+
+# ------------------------------------------------------------------ rows of several waves, runs around the pieces, every number of places
+# dtype, rows, vocab, hidden, ids, places of a wave.  More than 2048 columns (fp32: 1024) take workgroups side by side
+SUMS = [(BF16, 600, 900, 4104, "zipf", 8), (BF16, 2100, 7, 2056, "one", 8), (BF16, 1500, 300, 1544, "lengths", 8), (BF16, 5000, 300, 2056, "zipf", 16), (BF16, 5000, 300, 2056, "padded", 16),
+        (BF16, 9000, 2000, 2056, "lengths", 16), (BF16, 33000, 500, 1032, "padded", 32), (BF16, 20000, 3, 2600, "zipf", 32), (BF16, 25000, 1100, 2056, "lengths", 32),
+        (FP32, 2000, 50, 1352, "zipf", 8), (FP32, 2000, 50, 1352, "one", 8), (FP32, 2000, 5000, 516, "lengths", 8), (FP32, 3000, 64, 1352, "padded", 16), (FP32, 4097, 5000, 1100, "all", 16),
+        (FP32, 4500, 200, 1028, "lengths", 16), (FP32, 17000, 821, 1352, "zipf", 32), (FP32, 20000, 900, 1284, "lengths", 32), (FP32, 17000, 40, 1352, "one", 32)]
+
+
+@pytest.mark.parametrize("dtype,rows,vocab,h,kind,places", SUMS)
+def test_a_case_for_a_number_of_places_takes_them(dtype, rows, vocab, h, kind, places):
+    assert route(dtype, rows, vocab, h)[2] == places
+
+
+def test_the_cases_reach_every_number_of_places_in_rows_of_several_workgroups():
+    for dtype, one_group in ((BF16, 2048), (FP32, 1024)):
+        assert {c[5] for c in SUMS if c[0] == dtype and c[3] > one_group} == {8, 16, 32}
+        assert {c[5] for c in SUMS if c[0] == dtype and c[4] == "lengths"} == {8, 16, 32}
+    ids = ids_for("lengths", 25000, 1100, np.random.default_rng(1))
+    assert set(np.bincount(ids)) >= {1, 31, 32, 33, 63, 64, 65, 96, 200}
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,rows,vocab,h,kind,places", SUMS)
+def test_gradient_of_rows_of_several_waves(dtype, rows, vocab, h, kind, places):
+    g = Gradient(dtype, rows, vocab, h, kind)
+    g.call()
+    at, first = g.check()
+    g.call()
+    torch.cuda.synchronize()
+    assert torch.equal(g.grad[at], first)
