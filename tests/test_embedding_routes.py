@@ -156,3 +156,70 @@ def test_gradient_of_rows_of_several_waves(dtype, rows, vocab, h, kind, places):
     g.call()
     torch.cuda.synchronize()
     assert torch.equal(g.grad[at], first)
+
+
+# ------------------------------------------------------------------ replayed with other tokens, and several calls at once
+# counting the keys ahead; the sort by itself; with a launch that counts: all of them several launches that leave their order, and how many runs
+# are long, in the workspace for the next one
+LAUNCHES = [(BF16, 600, 500, 264, PLACED), (FP32, 9000, 2000, 36, 2), (BF16, 20000, 2000, 40, 2)]
+
+
+def test_the_cases_for_replays_take_several_launches():
+    assert [route(*c[:4])[:2] for c in LAUNCHES] == [(PLACED, False), (2, False), (2, True)]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("shared", [False, True], ids=["own workspaces", "one workspace after the other"])
+def test_gradient_captured_once_and_replayed_with_other_tokens(shared):
+    """Long runs, none, tokens of one word, padding alone: every replay gives what the eager call gives for those tokens."""
+    sets = [Gradient(*c[:4], "none", seed=3) for c in LAUNCHES]
+    if shared:
+        most = max(sets, key=lambda g: g.need)
+        for g in sets:
+            g.ws, g.c2 = most.ws, most.c2
+    side = torch.cuda.Stream()
+    graphs = []
+    for g in sets:
+        g.call()                                                   # once before the capture, which may load no code
+        torch.cuda.synchronize()
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1], stream=side):
+            g.call(torch.cuda.current_stream().cuda_stream)
+    for turn, kind in enumerate(["zipf", "all", "one", "none", "lengths", "padded", "one", "all"]):
+        for g in sets:
+            rows, vocab, _ = g.shape
+            g.ids.copy_(torch.from_numpy(ids_for(kind, rows, vocab, np.random.default_rng([89, rows, turn]))))
+            g.reset()
+        torch.cuda.synchronize()
+        for graph in graphs:
+            graph.replay()
+        torch.cuda.synchronize()
+        replayed = [g.check() for g in sets]
+        for g, (at, got) in zip(sets, replayed):
+            g.reset()
+            g.call()
+            torch.cuda.synchronize()
+            assert torch.equal(g.grad[at], got), (g.shape, kind)
+        torch.ones(1 << 20, device="cuda").sum().item()
+
+
+@pytest.mark.gpu
+def test_gradients_of_many_tokens_on_two_streams_at_once():
+    sets = [[Gradient(*c[:4], kind, seed=4 + k) for c in LAUNCHES] for k, kind in enumerate(("zipf", "lengths"))]
+    streams = [torch.cuda.Stream() for _ in sets]
+    alone = []
+    for k in range(2):
+        for g in sets[k]:
+            g.call()
+        alone.append([g.check() for g in sets[k]])
+    for _ in range(4):
+        for g in sets[0] + sets[1]:
+            g.reset()
+        torch.cuda.synchronize()
+        for i in range(len(LAUNCHES)):
+            for k in range(2):
+                sets[k][i].call(streams[k].cuda_stream)
+        torch.cuda.synchronize()
+        for k in range(2):
+            for g, (at, got) in zip(sets[k], alone[k]):
+                assert torch.equal(g.grad[at], got), (g.shape, k)
