@@ -1,0 +1,50 @@
+"""The GELU that keeps its input, against its definition value by value in relative terms, far into the lower tail.
+
+The tail of the normal distribution is formed as 0.5 t S(t) e with e = exp(-x^2 / 2), t = 1 / (1 + p |x|).  In units of EPS = 2^-24 of the value: the exponent's
+argument is rounded three times (1.5 x^2), exp2 2, the fit 2^-22 (4), t's multiply-add, constant and reciprocal 4, which reach t S(t) up to 2.7-fold (11), the
+eight multiply-adds 10, the products 4: below 2 x^2 + 40.  The density has the exponent's and 4 more: below 2 x^2 + 8.  What lies below
+2^-126 may be flushed to zero on the way."""
+import numpy as np
+import pytest
+import torch
+from scipy.special import erfc
+
+from oracle import operators_fp64 as P
+from paper_2510_05186_amd import binding as B
+from gpu_util import TDT, host, ok, stream
+
+GPT, FP32, BF16 = 0, 0, 1
+EPS, HALF, LEAST = 2.0 ** -24, {FP32: 2.0 ** -24, BF16: 2.0 ** -8}, 2.0 ** -126
+
+
+def bounds(x, da):
+    """On x cdf(x) and on da (cdf(x) + x density(x)), ahead of the rounding to the storage type"""
+    cdf, density = 0.5 * erfc(-x / np.sqrt(2)), np.exp(-x * x / 2) / np.sqrt(2 * np.pi)
+    n = EPS * (2 * x * x + 40) * cdf + LEAST
+    return np.abs(x) * n + 2 * EPS * np.abs(x * cdf) + LEAST, np.abs(da) * (n + np.abs(x) * (EPS * (2 * x * x + 8) * density + LEAST) + 2 * EPS * (cdf + np.abs(x) * density)) + LEAST
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [FP32])
+def test_gelu_far_into_its_lower_tail(dtype):
+    """Random values from -13 to 13 and every value that is kept exactly, forward and backward."""
+    r = np.random.default_rng(31)
+    kept = np.concatenate([-P.E4M3[::-1], P.E4M3])[None] * np.array([[2.0 ** -5], [2.0 ** -6], [2.0 ** -7]])
+    x = np.concatenate([np.resize(kept[0], (2, 256)), np.resize(kept[1], (2, 256)), np.resize(kept[2], (2, 256)), r.uniform(-13, 13, (60, 256)), r.uniform(-13, -4, (60, 256))])
+    X = torch.from_numpy(x).to(TDT[dtype]).cuda()
+    x = host(X)
+    da = host(torch.from_numpy(r.standard_normal(x.shape)).to(TDT[dtype]))
+    DA = torch.from_numpy(da).to(TDT[dtype]).cuda()
+    rows, f = x.shape
+    codes, scales = torch.empty((rows, f), dtype=torch.uint8, device="cuda"), torch.empty((rows, f // 32), dtype=torch.uint8, device="cuda")
+    a, again, dgu = torch.empty_like(X), torch.empty_like(X), torch.empty_like(X)
+    ok(B.lib().optstage_op_act_fwd_pack8(dtype, GPT, X.data_ptr(), a.data_ptr(), codes.data_ptr(), scales.data_ptr(), rows, f, stream()))
+    ok(B.lib().optstage_op_act_bwd8(dtype, GPT, DA.data_ptr(), codes.data_ptr(), scales.data_ptr(), dgu.data_ptr(), again.data_ptr(), rows, f, stream()))
+    torch.cuda.synchronize()
+    v = P.pack8(x)[2]
+    assert v.min() < -12 and x.min() < -12.9
+    for what, got, at, ref, b in (("a", a, x, x * 0.5 * erfc(-x / np.sqrt(2)), bounds(x, da)[0]), ("a again", again, v, v * 0.5 * erfc(-v / np.sqrt(2)), bounds(v, da)[0]),
+                                  ("dgu", dgu, v, da * (0.5 * erfc(-v / np.sqrt(2)) + v * np.exp(-v * v / 2) / np.sqrt(2 * np.pi)), bounds(v, da)[1])):
+        off, b = np.abs(host(got) - ref), HALF[dtype] * np.abs(ref) + b
+        bad = ~(off <= b)
+        assert not bad.any(), (what, int(bad.sum()), at[bad][:6], host(got)[bad][:6], ref[bad][:6])
