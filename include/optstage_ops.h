@@ -121,7 +121,8 @@ uint64_t optstage_op_attn_bwd_ws_floats(uint32_t seq, uint32_t batch, uint32_t n
  * 2^(k - 10) where that is more, and is exactly representable in bf16 and fp32.  A value that is not finite is kept as NaN, and
  * its block's scale goes by the others; values above 448 * 2^119 are kept as that.
  * The calls below that keep their operand ("_pack8") keep what pack8 would and otherwise compute what their plain counterparts do (to a last bit here and
- * there: sums in another order, bf16 activations with the hardware's exp2 and reciprocal); those that read it ("8") compute in fp32 from
+ * there: sums in another order, the hardware's exp2 and reciprocal), but for GELU's lower tail, which the plain form loses (4 % off at -5, 0 from -6 on): here the
+ * normal distribution is within 2^-12 (bf16) or (2 x^2 + 40) 2^-24 (fp32) of itself wherever it is at least 2^-126.  Those that read it ("8") compute in fp32 from
  * the values kept, with one rounding of each result to the storage type.  Codes and scales are plain bytes, which may lie in pinned host memory
  * meanwhile.  Scratch (partial, ws) belongs to a call until its work has run: calls, or captured graphs, that may overlap in time need their own. */
 /* ldx: distance of x's rows in elements, >= cols (a column range of wider rows). */

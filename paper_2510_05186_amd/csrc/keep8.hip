@@ -370,53 +370,41 @@ __global__ __launch_bounds__(1024) void add_columns_kernel(const float* __restri
 }
 
 // ---- the MLP activation -----------------------------------------------------------------------------------
-// The functions of common.h cost some 50 instructions a value (a division, expf, erff), more than the time of its bytes allows in bf16, where results keep
-// 8 bits of them.  There: exp2 and the reciprocal of the hardware (relative error of a few 2^-23), and for GELU the normal
-// distribution from Abramowitz and Stegun 7.1.26, erfc(u) = (a1 t + ... + a5 t^5) exp(-u^2) with t = 1 / (1 + p u), u >= 0, off by at most
-// 1.5e-7, whose exponential the gradient needs anyway.
+// Bound by memory, in bf16 only without the functions of common.h: those cost some 50 instructions a value (a division, expf, erff) where results keep 8
+// bits of them.  There the sigmoid comes from the hardware's exp2 and reciprocal (relative error of a few 2^-23).
 //
-// fp32 GELU: 0.5 (1 + erf) would lose the lower tail (4 % off at -5, 0 from -6 on), and 0.5 erfc costs issue (4096 x 11008: 95 and 113 us, forward and
-// backward, instead of 69 and 101).  The tail is exp(-x^2 / 2) (c1 t + ... + c8 t^8), t = 1 / (1 + 0.42 u), u = |x| / sqrt(2); the c are a linear program's, over
-// u <= 9.6: the least worst ratio of the error to the lesser of 2^-22 of the value and 5e-9 outright.  With the roundings, of the exponent's argument above
-// all, it is off by less than (2 x^2 + 40) 2^-24 of itself down to 2^-126.
-__device__ __forceinline__ void normal8(float x, float& cdf, float& density) {
-  const float t = __builtin_amdgcn_rcpf(fmaf(fabsf(x), 0.42f * 0.70710678118654752f, 1.f));
+// GELU in both types: the normal distribution's tail is exp(-x^2 / 2) (c1 t + ... + cn t^n), t = 1 / (1 + p u), u = |x| / sqrt(2), whose exponential the
+// gradient needs anyway.  p and the c are a linear program's, over u <= 9.6: the least worst ratio of the error to the lesser of a share of the value and an amount
+// outright.  fp32: 8 terms, 2^-22 and 5e-9; with the roundings, of the exponent's argument above all, less than (2 x^2 + 40) 2^-24 of the tail down to
+// 2^-126.  0.5 (1 + erf) would lose it (4 % off at -5, 0 from -6 on), and 0.5 erfc costs issue (4096 x 11008: 95 and 113 us, forward and backward,
+// instead of 69 and 101).  bf16: 6 terms, 2^-12 and 5e-8 (8 terms: forward 41 us
+// instead of 37).
+template <typename T> struct Math;
+template <> struct Math<float> {
+  static constexpr int TERMS = 8;
+  static constexpr float P = 0.42f, C[TERMS] = {0.118404014f, 0.119930683f, 0.0964155011f, 0.137787986f, -0.0722499083f, 0.228464768f, -0.165131203f, 0.0363781628f};
+  static __device__ __forceinline__ float sigmoid(float x) { return sigmoidf_(x); }
+};
+template <> struct Math<bf16_t> {
+  static constexpr int TERMS = 6;
+  static constexpr float P = 0.41f, C[TERMS] = {0.116811496f, 0.100530932f, 0.180688379f, -0.0956544678f, 0.28699966f, -0.089376044f};
+  static __device__ __forceinline__ float sigmoid(float x) { return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(x * -1.44269504088896341f)); }
+};
+template <typename T> __device__ __forceinline__ void normal(float x, float& cdf, float& density) {
+  typedef Math<T> M;
+  const float t = __builtin_amdgcn_rcpf(fmaf(fabsf(x), M::P * 0.70710678118654752f, 1.f));
   const float e = __builtin_amdgcn_exp2f(x * x * -0.72134752044448170f);                   // exp(-x^2 / 2)
-  float s = fmaf(t, 0.0363781628f, -0.165131203f);
-  s = fmaf(t, s, 0.228464768f);
-  s = fmaf(t, s, -0.0722499083f);
-  s = fmaf(t, s, 0.137787986f);
-  s = fmaf(t, s, 0.0964155011f);
-  s = fmaf(t, s, 0.119930683f);
-  s = fmaf(t, s, 0.118404014f);
+  float s = M::C[M::TERMS - 1];
+#pragma unroll
+  for (int i = M::TERMS - 2; i >= 0; --i) s = fmaf(t, s, M::C[i]);
   const float tail = t * s * e;
   cdf = x < 0.f ? tail : 1.f - tail;
   density = 0.39894228040143268f * e;
 }
-template <typename T> struct Math {
-  static __device__ __forceinline__ float sigmoid(float x) { return sigmoidf_(x); }
-  static __device__ __forceinline__ void normal(float x, float& cdf, float& density) { normal8(x, cdf, density); }
-};
-template <> struct Math<bf16_t> {
-  static __device__ __forceinline__ float sigmoid(float x) {
-    return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(x * -1.44269504088896341f));
-  }
-  static __device__ __forceinline__ void normal(float x, float& cdf, float& density) {
-    const float t = __builtin_amdgcn_rcpf(fmaf(fabsf(x), 0.3275911f * 0.70710678118654752f, 1.f));
-    const float e = __builtin_amdgcn_exp2f(x * x * -0.72134752044448170f);                 // exp(-x^2 / 2)
-    float s = fmaf(t, 1.061405429f, -1.453152027f);
-    s = fmaf(t, s, 1.421413741f);
-    s = fmaf(t, s, -0.284496736f);
-    s = fmaf(t, s, 0.254829592f);
-    const float tail = 0.5f * t * s * e;
-    cdf = x < 0.f ? tail : 1.f - tail;
-    density = 0.39894228040143268f * e;
-  }
-};
 template <typename T, bool SWIGLU> __device__ __forceinline__ float activation(float x, float up) {
   if (SWIGLU) return x * Math<T>::sigmoid(x) * up;
   float cdf, density;
-  Math<T>::normal(x, cdf, density);
+  normal<T>(x, cdf, density);
   return x * cdf;
 }
 
@@ -501,7 +489,7 @@ __global__ __launch_bounds__(NT) void act_bwd8_kernel(const T* da, const uint8_t
           act.set(e, silu * x[1][e]);
         } else {
           float cdf, density;
-          Math<T>::normal(v, cdf, density);
+          normal<T>(v, cdf, density);
           o[0].set(e, g * fmaf(v, density, cdf));
           act.set(e, v * cdf);
         }
