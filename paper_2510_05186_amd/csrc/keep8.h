@@ -31,7 +31,6 @@ __device__ __forceinline__ uint32_t keep_encode(float x, float inverse) {
   const float y = fminf(fmaxf(x * inverse, -448.f), 448.f);
   return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(y, 0.f, 0, false) & 0xffu;
 }
-__device__ __forceinline__ float keep_decode(uint32_t code, float scale) { return __builtin_amdgcn_cvt_f32_fp8((int)code, 0) * scale; }
 
 // 16 bytes of T and their codes; the lanes whose chunks make up a block are next to each other, their number a divisor of 16
 template <typename T> struct KeepChunk;

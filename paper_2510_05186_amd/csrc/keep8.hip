@@ -534,8 +534,9 @@ template <typename T, typename F> auto norm_division(int h, F f) {
   if (chunks <= 128) return NORM_DIVISION(1, 2, 8);
   if (chunks <= 256) return NORM_DIVISION(2, 2, 4);
   if (chunks <= 512) return NORM_DIVISION(4, 2, 2);
-  if (chunks <= 1024) return NORM_DIVISION(8, 2, 1);
-  return NORM_DIVISION(16, 2, 1);                                      // fp32 rows of more than 4096
+  if constexpr (Vec16<T>::N == 4)
+    if (chunks > 1024) return NORM_DIVISION(16, 2, 1);                 // fp32 rows of more than 4096; bf16 rows of 8192, the widest, have 1024 chunks
+  return NORM_DIVISION(8, 2, 1);
 #undef NORM_DIVISION
 }
 

@@ -21,3 +21,21 @@ def test_no_counted_wait_stands_behind_the_epilogue_s_requests():
     # and no tile load is written between that wait and the end
     last_wait = max(at for at, _ in waits if at < min(requests))
     assert not re.search(r"trip\([^)]*, true, (?:true|false)\)|issue_one\(", body[last_wait:])
+
+
+def test_every_function_of_the_8_bit_keeping_has_a_caller():
+    text = open(os.path.join(CSRC, "keep8.h")).read()
+    everything = "\n".join(open(os.path.join(CSRC, f)).read() for f in sorted(os.listdir(CSRC)))
+    names = set(re.findall(r"__forceinline__ [\w:<> ]*?[ >](\w+)\(", text))
+    assert {"keep_values", "keep_chunk", "lanes_sum"} <= names
+    assert not [n for n in names if len(re.findall(rf"\b{n}\b", everything)) < 2]
+
+
+def test_the_library_holds_the_norm_kernels_that_a_call_can_reach():
+    """Rows of bf16 have at most 1024 chunks of 16 bytes, 8 waves; 16 waves are for fp32."""
+    from paper_2510_05186_amd import binding
+    held = open(binding.LIB_PATH, "rb").read()
+    for kernel in (b"norm_fwd_pack8_kernelI", b"norm_bwd8_kernelI"):
+        for layer_norm in b"01":
+            form = lambda t, waves: kernel + t + b"Lb%cELi%dE" % (layer_norm, waves)  # noqa: B023, E731
+            assert form(b"DF16b", 8) in held and form(b"f", 16) in held and form(b"DF16b", 16) not in held
