@@ -136,7 +136,7 @@ optstage_status optstage_op_norm_fwd_pack8(uint32_t dtype, uint32_t family, cons
                                            void* stream);
 /* optstage_op_norm_bwd from the kept x, with the forward pass's statistics.  out (may be null): the normalised rows once more, from the
  * kept x, for the weight gradient of the projection that read them (dW = dY^T n); beta is read only for that.  dx may be dn or
- * dres; out is a buffer of its own.  partial: fp32 scratch of 2 * min(rows, 512) * hidden elements. */
+ * dres; out is a buffer of its own.  partial: fp32 scratch of 2 * min(rows, 256) * hidden elements. */
 optstage_status optstage_op_norm_bwd8(uint32_t dtype, uint32_t family, const void* dn, const uint8_t* codes, const uint8_t* scales,
                                       const float* stats, const void* gamma, const void* beta, const void* dres, void* dx, void* out,
                                       float* partial, float* dgamma, float* dbeta, uint32_t rows, uint32_t hidden, void* stream);
