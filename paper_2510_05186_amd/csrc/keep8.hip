@@ -373,31 +373,42 @@ __global__ __launch_bounds__(1024) void add_columns_kernel(const float* __restri
 // Bound by memory, in bf16 only without the functions of common.h: those cost some 50 instructions a value (a division, expf, erff) where results keep 8
 // bits of them.  There the sigmoid comes from the hardware's exp2 and reciprocal (relative error of a few 2^-23).
 //
-// GELU in both types: the normal distribution's tail is exp(-x^2 / 2) (c1 t + ... + cn t^n), t = 1 / (1 + p u), u = |x| / sqrt(2), whose exponential the
-// gradient needs anyway.  p and the c are a linear program's, over u <= 9.6: the least worst ratio of the error to the lesser of a share of the value and an amount
-// outright.  fp32: 8 terms, 2^-22 and 5e-9; with the roundings, of the exponent's argument above all, less than (2 x^2 + 40) 2^-24 of the tail down to
-// 2^-126.  0.5 (1 + erf) would lose it (4 % off at -5, 0 from -6 on), and 0.5 erfc costs issue (4096 x 11008: 95 and 113 us, forward and backward,
-// instead of 69 and 101).  bf16: 6 terms, 2^-12 and 5e-8 (8 terms: forward 41 us
-// instead of 37).
+// GELU in both types: the tail of the normal distribution is exp(-x^2 / 2) F(u), u = |x| / sqrt(2), and the gradient needs the exponential anyway.  F is a polynomial in
+// t = 1 / (1 + p u) or in w = 1 - t = p u t.  Its coefficients are a linear program's, over u <= 9.6: the least worst ratio of the error to the lesser of a share of
+// F and an amount outright.  fp32: 2^-22 and 5e-9 by nine terms in w, of which the first is 1 / 2, so that little is rounded where x is small; with the
+// roundings, of the exponent's argument above all, less than (2 x^2 + 40) 2^-24 of the tail down to 2^-126.  0.5 (1 + erf) would lose it (4 % off at -5, 0
+// from -6 on), and 0.5 erfc costs issue (4096 x 11008: 95 and 113 us, forward and backward, instead of 69 and 101).  bf16: 2^-12 and 5e-8 by six terms in t
+// (eight: forward 41 us instead of 37; the form in w 38).
 template <typename T> struct Math;
 template <> struct Math<float> {
-  static constexpr int TERMS = 8;
-  static constexpr float P = 0.42f, C[TERMS] = {0.118404014f, 0.119930683f, 0.0964155011f, 0.137787986f, -0.0722499083f, 0.228464768f, -0.165131203f, 0.0363781628f};
   static __device__ __forceinline__ float sigmoid(float x) { return sigmoidf_(x); }
+  static __device__ __forceinline__ float tail_factor(float x) {
+    const float q = fminf(fabsf(x), 64.f) * (0.42f * 0.70710678118654752f);       // finite; the exponential is 0 long before
+    const float w = q * __builtin_amdgcn_rcpf(1.f + q);
+    float s = fmaf(w, 0.0361065609f, -0.125003526f);
+    s = fmaf(w, s, 0.0899473243f);
+    s = fmaf(w, s, 0.132865721f);
+    s = fmaf(w, s, -0.0299308343f);
+    s = fmaf(w, s, -0.75188043f);
+    s = fmaf(w, s, 1.49120338f);
+    s = fmaf(w, s, -1.34330943f);
+    return fmaf(w, s, 0.5f);
+  }
 };
 template <> struct Math<bf16_t> {
-  static constexpr int TERMS = 6;
-  static constexpr float P = 0.41f, C[TERMS] = {0.116811496f, 0.100530932f, 0.180688379f, -0.0956544678f, 0.28699966f, -0.089376044f};
   static __device__ __forceinline__ float sigmoid(float x) { return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(x * -1.44269504088896341f)); }
+  static __device__ __forceinline__ float tail_factor(float x) {
+    const float t = __builtin_amdgcn_rcpf(fmaf(fabsf(x), 0.41f * 0.70710678118654752f, 1.f));
+    float s = fmaf(t, -0.089376044f, 0.28699966f);
+    s = fmaf(t, s, -0.0956544678f);
+    s = fmaf(t, s, 0.180688379f);
+    s = fmaf(t, s, 0.100530932f);
+    s = fmaf(t, s, 0.116811496f);
+    return t * s;
+  }
 };
 template <typename T> __device__ __forceinline__ void normal(float x, float& cdf, float& density) {
-  typedef Math<T> M;
-  const float t = __builtin_amdgcn_rcpf(fmaf(fabsf(x), M::P * 0.70710678118654752f, 1.f));
-  const float e = __builtin_amdgcn_exp2f(x * x * -0.72134752044448170f);                   // exp(-x^2 / 2)
-  float s = M::C[M::TERMS - 1];
-#pragma unroll
-  for (int i = M::TERMS - 2; i >= 0; --i) s = fmaf(t, s, M::C[i]);
-  const float tail = t * s * e;
+  const float e = __builtin_amdgcn_exp2f(x * x * -0.72134752044448170f), tail = Math<T>::tail_factor(x) * e;       // e = exp(-x^2 / 2)
   cdf = x < 0.f ? tail : 1.f - tail;
   density = 0.39894228040143268f * e;
 }

@@ -1,10 +1,9 @@
 """The GELU that keeps its input, against its definition value by value in relative terms, far into the lower tail.
 
-The tail of the normal distribution is formed as 0.5 t S(t) e with e = exp(-x^2 / 2), t = 1 / (1 + p |x|).  In units of EPS = 2^-24 of the value: the exponent's
-argument is rounded three times (1.5 x^2), exp2 2, the fit 2^-22 (4), t's multiply-add, constant and reciprocal 4, which reach t S(t) up to 2.7-fold (11), the
-eight multiply-adds 10, the products 4: below 2 x^2 + 40.  bf16: the fit is good
-to 2^-12, a sixteenth of the storage type's rounding.  The density has the exponent's and 4 more: below 2 x^2 + 8.  What lies below
-2^-126 may be flushed to zero on the way."""
+The tail of the normal distribution is exp(-x^2 / 2) F(|x|), F a polynomial that falls from 1 / 2 as 0.4 / |x|.  In units of EPS = 2^-24 of the value: the
+exponent's argument is rounded three times (1.5 x^2), exp2 2, the fit 2^-22 (4), the products 4; F's reciprocal and multiply-adds 2 EPS outright, which are 4
+of F at 0, 20 at -4 and 5 |x| beyond: below 2 x^2 + 40.  The density has the exponent's and 4 more: below 2 x^2 + 8.  bf16: the fit is good to 2^-12, a
+sixteenth of the storage type's rounding.  What lies below 2^-126 may be flushed to zero on the way."""
 import numpy as np
 import pytest
 import torch
@@ -49,3 +48,24 @@ def test_gelu_far_into_its_lower_tail(dtype):
         off, b = np.abs(host(got) - ref), HALF[dtype] * np.abs(ref) + b
         bad = ~(off <= b)
         assert not bad.any(), (what, int(bad.sum()), at[bad][:6], host(got)[bad][:6], ref[bad][:6])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+def test_gelu_of_what_is_not_finite_and_of_the_largest_values(dtype):
+    """As the plain form: infinity stays, what has no limit is NaN, and the largest values are themselves or zero."""
+    top = float(torch.finfo(TDT[dtype]).max)
+    x = torch.zeros((1, 32), dtype=TDT[dtype], device="cuda")
+    x[0, :8] = torch.tensor([np.inf, -np.inf, np.nan, top, -top, 1e20, -1e20, -200.0])
+    a, plain = torch.empty_like(x), torch.empty_like(x)
+    codes, scales = torch.empty((1, 32), dtype=torch.uint8, device="cuda"), torch.empty((1, 1), dtype=torch.uint8, device="cuda")
+    ok(B.lib().optstage_op_act_fwd_pack8(dtype, GPT, x.data_ptr(), a.data_ptr(), codes.data_ptr(), scales.data_ptr(), 1, 32, stream()))
+    ok(B.lib().optstage_op_act_fwd(dtype, GPT, x.data_ptr(), plain.data_ptr(), 1, 32, stream()))
+    torch.cuda.synchronize()
+    assert np.array_equal(host(a), host(plain), equal_nan=True) and np.isinf(host(a)[0, 0]) and np.isnan(host(a)[0, [1, 2]]).all()
+    da, dgu = torch.ones_like(x), torch.empty_like(x)
+    for v, want in ((torch.full_like(x, top), 1.0), (torch.full_like(x, -top), 0.0), (torch.zeros_like(x), 0.5)):
+        ok(B.lib().optstage_op_act_fwd_pack8(dtype, GPT, v.data_ptr(), a.data_ptr(), codes.data_ptr(), scales.data_ptr(), 1, 32, stream()))
+        ok(B.lib().optstage_op_act_bwd8(dtype, GPT, da.data_ptr(), codes.data_ptr(), scales.data_ptr(), dgu.data_ptr(), 0, 1, 32, stream()))
+        torch.cuda.synchronize()
+        assert np.all(host(dgu) == want), (want, host(dgu)[0, 0])
