@@ -3,8 +3,9 @@
  * (paper Sec. 2.2: linear maps z = W x, grad_x = W^T grad_z, grad_W = grad_z x^T; everything else is the
  * non-linear part the paper folds into sigma).  They exist so that every kernel can be checked against
  * the CPU oracle and timed on its own; the stage calls in optstage.h launch exactly these kernels.  Beside them stand operators that a
- * training step needs around a stage and that its op graph does not have: activations kept in 8 bits, norms of queries and
- * keys, and the embedding.
+ * training step needs and a stage's op graph does not have, and that no stage call launches: the embedding, which goes around a stage (its input, its
+ * input's gradient), and, for layers that their caller writes from single calls as these, activations kept in 8 bits and norms of queries and keys.  A
+ * stage keeps its activations in its own arena, in its storage type.
  *
  * All tensor pointers are DEVICE memory, caller-owned, 16-byte aligned, row-major with tokens as rows.
  * dtype is optstage_dtype (storage type; arithmetic is fp32 / bf16 MFMA with fp32 accumulation).
