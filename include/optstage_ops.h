@@ -183,6 +183,53 @@ optstage_status optstage_op_embed_bwd(uint32_t dtype, const int32_t* ids, const 
                                       uint32_t vocab, uint32_t hidden, float scale, void* stream);
 uint64_t optstage_op_embed_bwd_ws_bytes(uint32_t rows, uint32_t hidden);
 
+/* ---- Rotary positions with several axes ----
+ * optstage_op_rope where a token has a place on n_axes (1..4) axes (time, height, width) instead of its row's number.  src rows lie ld_src elements apart, dst rows
+ * ld_dst: n_rot heads of head_dim that are rotated, then n_pass (may be 0) that are not (copied where dst is not src).  Pair i of a head, elements i and
+ * i + head_dim / 2, turns by table[p][i] (optstage_op_rope_table's entries, or the caller's own frequencies) with p = positions[axis[i]][row]; backward != 0 turns
+ * back (gradients).  positions: DEVICE int32 [n_axes][rows] (any address of an int32); axis: HOST, head_dim / 2 bytes, read before the call returns, each below
+ * n_axes, or 255 for a pair that does not turn.  Nor does one whose position is negative or >= n_positions (padding).  head_dim is a multiple of 16 (fp32:
+ * 8), at most 256; ld_src and ld_dst are multiples of 8 (fp32: 4).  dst may be src (with ld_dst = ld_src). */
+optstage_status optstage_op_rope_axes(uint32_t dtype, const void* src, uint32_t ld_src, void* dst, uint32_t ld_dst, const float* table, uint32_t n_positions,
+                                      const int32_t* positions, uint32_t n_axes, const uint8_t* axis, uint32_t rows, uint32_t n_rot, uint32_t n_pass,
+                                      uint32_t head_dim, uint32_t backward, void* stream);
+
+/* ---- Cross attention: queries of one sequence, keys and values of another (an encoder's states) ----
+ * Every query of sequence b attends to the first kv_len[b] of its seq_kv states; q-head a reads kv-head a*n_kv/n_q, scores are scaled by 1/sqrt(head_dim).
+ * q [batch*seq_q, n_q*d], rows ldq elements apart; k and v [batch*seq_kv, n_kv*d], rows ldkv apart (two column ranges of one packed projection, or two buffers).
+ * o, dout [batch*seq_q, n_q*d]; lse fp32 [batch][n_q][seq_q] (natural log).  kv_len: DEVICE int32 [batch] (any address of an int32), or null for all states; below 0
+ * counts as 0, above seq_kv as seq_kv.  States past it are not read: they may hold anything.  A sequence without states has o = 0, lse = -infinity and
+ * no gradients (0).  A padded query computes as any other; with dout = 0 it adds nothing to dk and dv.  head_dim 64 or 128.  ws: DEVICE scratch of at
+ * least optstage_op_cross_attn_ws_bytes() bytes for either direction, belonging to a call until its work has run.  bf16: products on the matrix units, sums and softmax in fp32. */
+optstage_status optstage_op_cross_attn_fwd(uint32_t dtype, const void* q, uint32_t ldq, const void* k, const void* v, uint32_t ldkv, const int32_t* kv_len, void* o,
+                                           float* lse, void* ws, uint64_t ws_bytes, uint32_t seq_q, uint32_t seq_kv, uint32_t batch, uint32_t n_q, uint32_t n_kv,
+                                           uint32_t head_dim, void* stream);
+/* dq like q (rows ldq apart), dk and dv like k and v (rows ldkv apart), every row written, buffers of their own.  o and lse are the forward pass's. */
+optstage_status optstage_op_cross_attn_bwd(uint32_t dtype, const void* q, uint32_t ldq, const void* k, const void* v, uint32_t ldkv, const int32_t* kv_len, const void* o,
+                                           const void* dout, const float* lse, void* dq, void* dk, void* dv, void* ws, uint64_t ws_bytes, uint32_t seq_q,
+                                           uint32_t seq_kv, uint32_t batch, uint32_t n_q, uint32_t n_kv, uint32_t head_dim, void* stream);
+uint64_t optstage_op_cross_attn_ws_bytes(uint32_t dtype, uint32_t seq_q, uint32_t seq_kv, uint32_t batch, uint32_t n_q, uint32_t n_kv, uint32_t head_dim);
+
+/* ---- Loss of the last stage against a teacher's top entries ----
+ * z: logits [rows, vocab], rows ldz elements apart.  ids int32, teacher fp32 [rows, k] (any addresses of theirs): the words that the teacher gave of a row and what it
+ * gave them.  An entry whose id is negative or >= vocab is not there; one word given twice counts with both.  With p = softmax(z / temperature) and t
+ * the teacher's probabilities, log_probs = 0: softmax(teacher / temperature) over the row's entries; log_probs = 1: exp(teacher), which need not add up to 1:
+ *   loss[r] = sum over j of t_j (log t_j - log p[ids_j]),  lse[r] = log of the sum of exp(z / temperature)                         (fp32 [rows])
+ *   dz[r][v] = dloss[r] / temperature * (p_v * sum of all t_j - sum of t_j with ids_j = v)
+ * A teacher's entry of minus infinity has t = 0 and adds nothing.  A row without entries has loss 0 and gradient 0, and so has the gradient of a row whose
+ * dloss is 0 (padding), whatever its logits are.  dz rows lie lddz apart; columns past vocab are neither read nor written; dz may be z (with lddz = ldz).
+ * k is at most 1024, temperature positive and finite.  z and dz: 16-byte aligned, any ldz and lddz >= vocab.  ws: DEVICE scratch of
+ * at least optstage_op_distill_ws_bytes() bytes, belonging to a call until its work has run. */
+optstage_status optstage_op_distill_fwd(uint32_t dtype, const void* z, uint32_t ldz, const int32_t* ids, const float* teacher, float* loss, float* lse, void* ws,
+                                        uint64_t ws_bytes, uint32_t rows, uint32_t vocab, uint32_t k, float temperature, uint32_t log_probs, void* stream);
+optstage_status optstage_op_distill_bwd(uint32_t dtype, const void* z, uint32_t ldz, const int32_t* ids, const float* teacher, const float* lse, const float* dloss,
+                                        void* dz, uint32_t lddz, uint32_t rows, uint32_t vocab, uint32_t k, float temperature, uint32_t log_probs, void* stream);
+/* Both, where dloss (fp32 [rows], e.g. 1 / rows, 0 for padding) is known beforehand: the logits are read once. */
+optstage_status optstage_op_distill(uint32_t dtype, const void* z, uint32_t ldz, const int32_t* ids, const float* teacher, const float* dloss, float* loss, float* lse,
+                                    void* dz, uint32_t lddz, void* ws, uint64_t ws_bytes, uint32_t rows, uint32_t vocab, uint32_t k, float temperature,
+                                    uint32_t log_probs, void* stream);
+uint64_t optstage_op_distill_ws_bytes(uint32_t rows, uint32_t vocab, uint32_t k);
+
 /* out_dev[0] = sum of the buffer's 64-bit words mod 2^64, out_dev[1] = their xor.  bytes % 8 == 0. */
 optstage_status optstage_op_checksum(const void* buf, uint64_t bytes, uint64_t* out_dev, void* stream);
 

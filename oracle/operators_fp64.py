@@ -1,5 +1,6 @@
 """Plain fp64 definitions of the operators around a stage's op graph: values kept in 8 bits, the non-linear parts of a layer
-from kept values, norms of queries and keys with the position rotation, the embedding.  Test infrastructure only."""
+from kept values, norms of queries and keys with the position rotation, the embedding, rotary positions with several axes, cross attention, and the loss
+against a teacher's top entries.  Test infrastructure only."""
 import numpy as np
 from scipy.special import erfc
 
@@ -131,3 +132,101 @@ def embed_bwd(ids, dy, vocab, scale):
         if 0 <= t < vocab:
             grad[t] += scale * dy[r]
     return grad
+
+
+def rope_axes(x, table, positions, axis, n_rot, sign=1):
+    """x [rows, heads, d]; pair i, elements i and i + d / 2 of the first n_rot heads, by table[positions[axis[i]][row]][i]; axis 255 or a position outside
+    the table: not turned"""
+    y = np.array(x, dtype=np.float64)
+    half = x.shape[2] // 2
+    for i, a in enumerate(axis):
+        if a == 255:
+            continue
+        for r in range(x.shape[0]):
+            at = positions[a][r]
+            if 0 <= at < len(table):
+                c, s = table[at, i, 0], sign * table[at, i, 1]
+                lo, hi = x[r, :n_rot, i], x[r, :n_rot, i + half]
+                y[r, :n_rot, i], y[r, :n_rot, i + half] = lo * c - hi * s, hi * c + lo * s
+    return y
+
+
+def cross_weights(q, k, n):
+    """q [queries, d], k [states, d], the first n of which count -> weights [queries, n], lse [queries]"""
+    score = q @ k[:n].T / np.sqrt(q.shape[1])
+    if n == 0:
+        return score, np.full(len(q), -np.inf)
+    most = score.max(1)
+    lse = most + np.log(np.exp(score - most[:, None]).sum(1))
+    return np.exp(score - lse[:, None]), lse
+
+
+def cross_attn(q, k, v, lens):
+    """q [batch, queries, n_q, d], k and v [batch, states, n_kv, d] -> o like q, lse [batch, n_q, queries]"""
+    b, nq, heads, d = q.shape
+    o, lse = np.zeros(q.shape), np.zeros((b, heads, nq))
+    for i in range(b):
+        n = min(max(int(lens[i]), 0), k.shape[1])
+        for a in range(heads):
+            h = a * k.shape[2] // heads
+            p, lse[i, a] = cross_weights(q[i, :, a], k[i, :, h], n)
+            o[i, :, a] = p @ v[i, :n, h]
+    return o, lse
+
+
+def cross_attn_bwd(q, k, v, lens, dout):
+    """-> dq like q, dk and dv like k"""
+    b, nq, heads, d = q.shape
+    dq, dk, dv = np.zeros(q.shape), np.zeros(k.shape), np.zeros(v.shape)
+    for i in range(b):
+        n = min(max(int(lens[i]), 0), k.shape[1])
+        for a in range(heads):
+            h = a * k.shape[2] // heads
+            p, _ = cross_weights(q[i, :, a], k[i, :, h], n)
+            dp = dout[i, :, a] @ v[i, :n, h].T
+            ds = p * (dp - (p * dp).sum(1, keepdims=True))
+            dq[i, :, a] = ds @ k[i, :n, h] / np.sqrt(d)
+            dk[i, :n, h] += ds.T @ q[i, :, a] / np.sqrt(d)
+            dv[i, :n, h] += p.T @ dout[i, :, a]
+    return dq, dk, dv
+
+
+def teacher_weights(ids, teacher, vocab, temperature, log_probs):
+    """-> t and log t of one row's entries; 0 and minus infinity where there is none"""
+    with np.errstate(divide="ignore", invalid="ignore"):
+        given = (ids >= 0) & (ids < vocab)
+        v = np.where(given, np.asarray(teacher, dtype=np.float64), -np.inf)
+        if not log_probs:
+            v = v / temperature
+            most = v.max()
+            if most > -np.inf:
+                v = v - most
+                v = v - np.log(np.exp(v).sum())
+        return np.exp(v), v
+
+
+def distill(z, ids, teacher, temperature, log_probs):
+    """z [rows, vocab] -> loss, lse [rows]"""
+    loss, lse = np.zeros(len(z)), np.zeros(len(z))
+    with np.errstate(invalid="ignore", divide="ignore"):
+        for r, row in enumerate(z / temperature):
+            most = row.max()
+            lse[r] = most + np.log(np.exp(row - most).sum())
+            t, log_t = teacher_weights(ids[r], teacher[r], z.shape[1], temperature, log_probs)
+            for j in np.nonzero(t)[0]:
+                loss[r] += t[j] * (log_t[j] - (row[ids[r, j]] - lse[r]))
+    return loss, lse
+
+
+def distill_bwd(z, ids, teacher, temperature, log_probs, dloss):
+    dz = np.zeros(z.shape)
+    for r, row in enumerate(z / temperature):
+        t, _ = teacher_weights(ids[r], teacher[r], z.shape[1], temperature, log_probs)
+        if dloss[r] == 0 or not t.any():
+            continue
+        e = np.exp(row - row.max())
+        dz[r] = e / e.sum() * t.sum()
+        for j in np.nonzero(t)[0]:
+            dz[r, ids[r, j]] -= t[j]
+        dz[r] *= dloss[r] / temperature
+    return dz

@@ -117,9 +117,16 @@ _SIGS = {
     "optstage_op_qknorm_rope_bwd": [_u32, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _u32, _u32, _u32, _u32, _u32, _vp],
     "optstage_op_embed_fwd": [_u32, _vp, _vp, _vp, _u32, _u32, _u32, _f32, _vp],
     "optstage_op_embed_bwd": [_u32, _vp, _vp, _vp, _vp, _u64, _u32, _u32, _u32, _f32, _vp],
+    "optstage_op_rope_axes": [_u32, _vp, _u32, _vp, _u32, _vp, _u32, _vp, _u32, C.c_char_p, _u32, _u32, _u32, _u32, _u32, _vp],
+    "optstage_op_cross_attn_fwd": [_u32, _vp, _u32, _vp, _vp, _u32, _vp, _vp, _vp, _vp, _u64, _u32, _u32, _u32, _u32, _u32, _u32, _vp],
+    "optstage_op_cross_attn_bwd": [_u32, _vp, _u32, _vp, _vp, _u32, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _u64, _u32, _u32, _u32, _u32, _u32, _u32, _vp],
+    "optstage_op_distill_fwd": [_u32, _vp, _u32, _vp, _vp, _vp, _vp, _vp, _u64, _u32, _u32, _u32, _f32, _u32, _vp],
+    "optstage_op_distill_bwd": [_u32, _vp, _u32, _vp, _vp, _vp, _vp, _vp, _u32, _u32, _u32, _u32, _f32, _u32, _vp],
+    "optstage_op_distill": [_u32, _vp, _u32, _vp, _vp, _vp, _vp, _vp, _vp, _u32, _vp, _u64, _u32, _u32, _u32, _f32, _u32, _vp],
     "optstage_op_checksum": [_vp, _u64, _vp, _vp],
 }
-EXPORTS = tuple(_SIGS) + ("optstage_destroy", "optstage_last_error", "optstage_op_attn_bwd_ws_floats", "optstage_op_embed_bwd_ws_bytes")
+EXPORTS = tuple(_SIGS) + ("optstage_destroy", "optstage_last_error", "optstage_op_attn_bwd_ws_floats", "optstage_op_embed_bwd_ws_bytes",
+                           "optstage_op_cross_attn_ws_bytes", "optstage_op_distill_ws_bytes")
 
 
 def lib():
@@ -148,6 +155,10 @@ def lib():
         L.optstage_op_attn_bwd_ws_floats.restype = _u64
         L.optstage_op_embed_bwd_ws_bytes.argtypes = [_u32] * 2
         L.optstage_op_embed_bwd_ws_bytes.restype = _u64
+        L.optstage_op_cross_attn_ws_bytes.argtypes = [_u32] * 7
+        L.optstage_op_cross_attn_ws_bytes.restype = _u64
+        L.optstage_op_distill_ws_bytes.argtypes = [_u32] * 3
+        L.optstage_op_distill_ws_bytes.restype = _u64
         _lib = L
     return _lib
 

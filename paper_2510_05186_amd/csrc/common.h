@@ -217,3 +217,17 @@ enum { EMBED_FEW = 0, EMBED_PLACED = -1 };
 int embed_bwd_order(int rows, unsigned vocab);
 // the sorted places that a wave of its sums takes
 int embed_bwd_places(int dtype, int rows, unsigned vocab, int h);
+// positions: [axes][rows]; axis: HOST, the axis of each of the d / 2 pairs, 255 for none
+hipError_t launch_rope_axes(int dtype, const void* src, size_t ld_src, void* dst, size_t ld_dst, const float* table, int n_positions, const int* positions,
+                            const uint8_t* axis, int rows, int n_rot, int n_pass, int d, int backward, hipStream_t s);
+// queries [batch seq_q] and states [batch seq_kv], rows ldq and ldkv elements apart
+struct CrossShape { size_t ldq, ldkv; int seq_q, seq_kv, batch, n_q, n_kv, d; };
+hipError_t launch_cross_attn_fwd(int dtype, const CrossShape& c, const void* q, const void* k, const void* v, const int* kv_len, void* o, float* lse, void* ws,
+                                 hipStream_t s);
+hipError_t launch_cross_attn_bwd(int dtype, const CrossShape& c, const void* q, const void* k, const void* v, const int* kv_len, const void* o, const void* dout,
+                                 const float* lse, void* dq, void* dk, void* dv, void* ws, hipStream_t s);
+uint64_t cross_attn_ws_bytes(int dtype, int seq_q, int seq_kv, int batch, int n_q, int n_kv, int d);
+// loss and lse (null: lse is read, the gradient alone), dz (null: no gradient)
+hipError_t launch_distill(int dtype, const void* z, size_t ldz, const int* ids, const float* teacher, const float* dloss, float* loss, float* lse, void* dz, size_t lddz,
+                          void* ws, int rows, int vocab, int k, float temperature, int log_probs, hipStream_t s);
+uint64_t distill_ws_bytes(int rows, int vocab, int k);

@@ -426,4 +426,140 @@ optstage_status optstage_op_embed_bwd(uint32_t dtype, const int32_t* ids, const 
   return wrap(launch_embed_bwd((int)dtype, ids, dy, grad, ws, (int)rows, vocab, (int)hidden, scale, (hipStream_t)stream), "embed_bwd");
 }
 
+// ---- rotary positions with several axes ----------------------------------------------------------------------
+static bool aligned4(const void* p) { return ((uintptr_t)p & 3) == 0; }
+
+optstage_status optstage_op_rope_axes(uint32_t dtype, const void* src, uint32_t ld_src, void* dst, uint32_t ld_dst, const float* table, uint32_t n_positions,
+                                      const int32_t* positions, uint32_t n_axes, const uint8_t* axis, uint32_t rows, uint32_t n_rot, uint32_t n_pass,
+                                      uint32_t head_dim, uint32_t backward, void* stream) {
+  REQ(src && dst && table && positions && axis, "rope_axes: null operand");
+  REQ(aligned16(src) && aligned16(dst) && aligned16(table) && aligned4(positions), "rope_axes: src, dst and table must be 16-byte aligned, positions 4");
+  REQ(dtype <= 1, "rope_axes: bad dtype");
+  const uint32_t vec = dtype == OPTSTAGE_BF16 ? 8 : 4;
+  REQ(head_dim && head_dim <= 256 && head_dim % (2 * vec) == 0, "rope_axes: head_dim must be a multiple of 16 (fp32: 8), at most 256");
+  REQ(rows && rows < (1u << 30) && n_rot && n_rot < 65536 && n_pass < 65536 && n_positions && n_positions < (1u << 30), "rope_axes: bad extent");
+  const uint64_t width = (uint64_t)(n_rot + n_pass) * head_dim;
+  REQ(ld_src >= width && ld_dst >= width && ld_src % vec == 0 && ld_dst % vec == 0, "rope_axes: row distance smaller than a row, or no multiple of 8 (fp32: 4)");
+  REQ(src != dst || ld_src == ld_dst, "rope_axes: in place, ld_dst must be ld_src");
+  REQ(n_axes >= 1 && n_axes <= 4, "rope_axes: 1 to 4 axes");
+  for (uint32_t i = 0; i < head_dim / 2; ++i) REQ(axis[i] < n_axes || axis[i] == 255, "rope_axes: a pair's axis is neither below n_axes nor 255");
+  return wrap(launch_rope_axes((int)dtype, src, ld_src, dst, ld_dst, table, (int)n_positions, positions, axis, (int)rows, (int)n_rot, (int)n_pass, (int)head_dim,
+                               backward ? 1 : 0, (hipStream_t)stream),
+              "rope_axes");
+}
+
+// ---- cross attention ---------------------------------------------------------------------------------------
+static bool cross_shape_ok(uint32_t seq_q, uint32_t seq_kv, uint32_t batch, uint32_t n_q, uint32_t n_kv, uint32_t d) {
+  return seq_q && seq_q < (1u << 24) && seq_kv && seq_kv < (1u << 24) && batch && batch < 65536 && n_kv && n_q < 65536 && n_q % n_kv == 0 && n_q &&
+         (uint64_t)batch * seq_q < (1u << 30) && (uint64_t)batch * seq_kv < (1u << 30) && (uint64_t)n_q / n_kv * seq_q < (1u << 30) && (d == 64 || d == 128);
+}
+
+uint64_t optstage_op_cross_attn_ws_bytes(uint32_t dtype, uint32_t seq_q, uint32_t seq_kv, uint32_t batch, uint32_t n_q, uint32_t n_kv, uint32_t head_dim) {
+  if (dtype > 1 || !cross_shape_ok(seq_q, seq_kv, batch, n_q, n_kv, head_dim)) return 0;
+  return cross_attn_ws_bytes((int)dtype, (int)seq_q, (int)seq_kv, (int)batch, (int)n_q, (int)n_kv, (int)head_dim);
+}
+
+// what both directions ask of their operands
+static const char* cross_attn_wrong(uint32_t dtype, const void* q, uint32_t ldq, const void* k, const void* v, uint32_t ldkv, const int32_t* kv_len, const void* ws,
+                                    uint64_t ws_bytes, uint32_t seq_q, uint32_t seq_kv, uint32_t batch, uint32_t n_q, uint32_t n_kv, uint32_t d) {
+  if (!q || !k || !v || !ws) return "cross_attn: null operand";
+  if (!(aligned16(q) && aligned16(k) && aligned16(v) && aligned16(ws) && aligned4(kv_len))) return "cross_attn: operands must be 16-byte aligned, kv_len 4";
+  if (dtype > 1 || !cross_shape_ok(seq_q, seq_kv, batch, n_q, n_kv, d))
+    return "cross_attn: bad argument (head_dim is 64 or 128, n_q a multiple of n_kv, sequences below 2^24, rows below 2^30)";
+  const uint32_t vec = dtype == OPTSTAGE_BF16 ? 8 : 4;
+  if (ldq < (uint64_t)n_q * d || ldkv < (uint64_t)n_kv * d || ldq % vec || ldkv % vec || ldq >= (1u << 24) || ldkv >= (1u << 24))
+    return "cross_attn: row distance smaller than a row, no multiple of 8 (fp32: 4), or 2^24 and more";
+  if (ws_bytes < cross_attn_ws_bytes((int)dtype, (int)seq_q, (int)seq_kv, (int)batch, (int)n_q, (int)n_kv, (int)d))
+    return "cross_attn: workspace smaller than optstage_op_cross_attn_ws_bytes()";
+  return nullptr;
+}
+
+optstage_status optstage_op_cross_attn_fwd(uint32_t dtype, const void* q, uint32_t ldq, const void* k, const void* v, uint32_t ldkv, const int32_t* kv_len, void* o,
+                                           float* lse, void* ws, uint64_t ws_bytes, uint32_t seq_q, uint32_t seq_kv, uint32_t batch, uint32_t n_q, uint32_t n_kv,
+                                           uint32_t head_dim, void* stream) {
+  const char* wrong = cross_attn_wrong(dtype, q, ldq, k, v, ldkv, kv_len, ws, ws_bytes, seq_q, seq_kv, batch, n_q, n_kv, head_dim);
+  REQ(!wrong, wrong);
+  REQ(o && lse, "cross_attn_fwd: null operand");
+  REQ(aligned16(o) && aligned4(lse), "cross_attn_fwd: o must be 16-byte aligned, lse 4");
+  REQ(o != q && o != k && o != v, "cross_attn_fwd: o must be a buffer of its own");
+  const CrossShape c = {ldq, ldkv, (int)seq_q, (int)seq_kv, (int)batch, (int)n_q, (int)n_kv, (int)head_dim};
+  return wrap(launch_cross_attn_fwd((int)dtype, c, q, k, v, kv_len, o, lse, ws, (hipStream_t)stream), "cross_attn_fwd");
+}
+
+optstage_status optstage_op_cross_attn_bwd(uint32_t dtype, const void* q, uint32_t ldq, const void* k, const void* v, uint32_t ldkv, const int32_t* kv_len, const void* o,
+                                           const void* dout, const float* lse, void* dq, void* dk, void* dv, void* ws, uint64_t ws_bytes, uint32_t seq_q,
+                                           uint32_t seq_kv, uint32_t batch, uint32_t n_q, uint32_t n_kv, uint32_t head_dim, void* stream) {
+  const char* wrong = cross_attn_wrong(dtype, q, ldq, k, v, ldkv, kv_len, ws, ws_bytes, seq_q, seq_kv, batch, n_q, n_kv, head_dim);
+  REQ(!wrong, wrong);
+  REQ(o && dout && lse && dq && dk && dv, "cross_attn_bwd: null operand");
+  REQ(aligned16(o) && aligned16(dout) && aligned4(lse) && aligned16(dq) && aligned16(dk) && aligned16(dv), "cross_attn_bwd: operands must be 16-byte aligned, lse 4");
+  const void* in[] = {q, k, v, o, dout, lse};
+  for (const void* p : in) REQ(dq != p && dk != p && dv != p, "cross_attn_bwd: dq, dk and dv must be buffers of their own");
+  REQ(dq != dk && dq != dv && dk != dv, "cross_attn_bwd: dq, dk and dv must be buffers of their own");
+  const CrossShape c = {ldq, ldkv, (int)seq_q, (int)seq_kv, (int)batch, (int)n_q, (int)n_kv, (int)head_dim};
+  return wrap(launch_cross_attn_bwd((int)dtype, c, q, k, v, kv_len, o, dout, lse, dq, dk, dv, ws, (hipStream_t)stream), "cross_attn_bwd");
+}
+
+// ---- loss against a teacher's top entries ---------------------------------------------------------------------
+static bool distill_shape_ok(uint32_t rows, uint32_t vocab, uint32_t k) { return rows && rows < (1u << 30) && vocab && vocab < (1u << 30) && k && k <= 1024; }
+
+uint64_t optstage_op_distill_ws_bytes(uint32_t rows, uint32_t vocab, uint32_t k) {
+  return distill_shape_ok(rows, vocab, k) ? distill_ws_bytes((int)rows, (int)vocab, (int)k) : 0;
+}
+
+static const char* distill_wrong(uint32_t dtype, const void* z, uint32_t ldz, const int32_t* ids, const float* teacher, uint32_t rows, uint32_t vocab, uint32_t k,
+                                 float temperature, uint32_t log_probs) {
+  if (!z || !ids || !teacher) return "distill: null operand";
+  if (!(aligned16(z) && aligned4(ids) && aligned4(teacher))) return "distill: z must be 16-byte aligned, ids and teacher 4";
+  if (dtype > 1 || log_probs > 1 || !distill_shape_ok(rows, vocab, k) || ldz < vocab) return "distill: bad argument (k is 1 to 1024, ldz at least vocab)";
+  if (!(temperature > 0.f && temperature <= 3.402823466e38f && 1.f / temperature <= 3.402823466e38f)) return "distill: temperature must be positive and finite";
+  return nullptr;
+}
+static const char* distill_dz_wrong(const void* z, uint32_t ldz, const float* dloss, const void* dz, uint32_t lddz, uint32_t vocab) {
+  if (!dloss || !dz) return "distill: null operand";
+  if (!(aligned4(dloss) && aligned16(dz))) return "distill: dz must be 16-byte aligned, dloss 4";
+  if (lddz < vocab || (dz == z && lddz != ldz)) return "distill: lddz smaller than vocab, or in place and not ldz";
+  return nullptr;
+}
+static const char* distill_loss_wrong(const float* loss, const float* lse, const void* ws, uint64_t ws_bytes, uint32_t rows, uint32_t vocab, uint32_t k) {
+  if (!loss || !lse || !ws) return "distill: null operand";
+  if (!(aligned4(loss) && aligned4(lse) && aligned16(ws)) || loss == lse) return "distill: ws must be 16-byte aligned, loss and lse 4 and two buffers";
+  if (ws_bytes < distill_ws_bytes((int)rows, (int)vocab, (int)k)) return "distill: workspace smaller than optstage_op_distill_ws_bytes()";
+  return nullptr;
+}
+
+optstage_status optstage_op_distill_fwd(uint32_t dtype, const void* z, uint32_t ldz, const int32_t* ids, const float* teacher, float* loss, float* lse, void* ws,
+                                        uint64_t ws_bytes, uint32_t rows, uint32_t vocab, uint32_t k, float temperature, uint32_t log_probs, void* stream) {
+  const char* wrong = distill_wrong(dtype, z, ldz, ids, teacher, rows, vocab, k, temperature, log_probs);
+  if (!wrong) wrong = distill_loss_wrong(loss, lse, ws, ws_bytes, rows, vocab, k);
+  REQ(!wrong, wrong);
+  return wrap(launch_distill((int)dtype, z, ldz, ids, teacher, nullptr, loss, lse, nullptr, 0, ws, (int)rows, (int)vocab, (int)k, temperature, (int)log_probs,
+                             (hipStream_t)stream),
+              "distill_fwd");
+}
+
+optstage_status optstage_op_distill_bwd(uint32_t dtype, const void* z, uint32_t ldz, const int32_t* ids, const float* teacher, const float* lse, const float* dloss,
+                                        void* dz, uint32_t lddz, uint32_t rows, uint32_t vocab, uint32_t k, float temperature, uint32_t log_probs, void* stream) {
+  const char* wrong = distill_wrong(dtype, z, ldz, ids, teacher, rows, vocab, k, temperature, log_probs);
+  if (!wrong) wrong = distill_dz_wrong(z, ldz, dloss, dz, lddz, vocab);
+  REQ(!wrong, wrong);
+  REQ(lse && aligned4(lse), "distill_bwd: lse is null or not 4-byte aligned");
+  return wrap(launch_distill((int)dtype, z, ldz, ids, teacher, dloss, nullptr, const_cast<float*>(lse), dz, lddz, nullptr, (int)rows, (int)vocab, (int)k, temperature,
+                             (int)log_probs, (hipStream_t)stream),
+              "distill_bwd");
+}
+
+optstage_status optstage_op_distill(uint32_t dtype, const void* z, uint32_t ldz, const int32_t* ids, const float* teacher, const float* dloss, float* loss, float* lse,
+                                    void* dz, uint32_t lddz, void* ws, uint64_t ws_bytes, uint32_t rows, uint32_t vocab, uint32_t k, float temperature,
+                                    uint32_t log_probs, void* stream) {
+  const char* wrong = distill_wrong(dtype, z, ldz, ids, teacher, rows, vocab, k, temperature, log_probs);
+  if (!wrong) wrong = distill_loss_wrong(loss, lse, ws, ws_bytes, rows, vocab, k);
+  if (!wrong) wrong = distill_dz_wrong(z, ldz, dloss, dz, lddz, vocab);
+  REQ(!wrong, wrong);
+  REQ(dloss != loss && dloss != lse, "distill: dloss must be a buffer of its own");
+  return wrap(launch_distill((int)dtype, z, ldz, ids, teacher, dloss, loss, lse, dz, lddz, ws, (int)rows, (int)vocab, (int)k, temperature, (int)log_probs,
+                             (hipStream_t)stream),
+              "distill");
+}
+
 }  // extern "C"

@@ -1,0 +1,110 @@
+"""What rotary positions with several axes, cross attention and the loss against a teacher's top entries refuse, on the host: nothing is launched, addresses are never read."""
+import pytest
+
+from paper_2510_05186_amd import binding as B
+
+FP32, BF16 = 0, 1
+A = [4096 * (i + 1) for i in range(16)]          # addresses of 16-byte alignment
+
+
+def refused(status):
+    assert status == B.E_ARG, status
+    return B.lib().optstage_last_error().decode()
+
+
+def call(name, args, **change):
+    for k in change:
+        assert k in args, k
+    return refused(getattr(B.lib(), name)(*{**args, **change}.values()))
+
+
+def rope(**change):
+    args = dict(dtype=BF16, src=A[0], ld_src=640, dst=A[1], ld_dst=640, table=A[2], n_positions=10, positions=A[3], n_axes=2, axis=bytes([0, 1] * 32), rows=4, n_rot=4, n_pass=1,
+                head_dim=128, backward=0, stream=0)
+    return call("optstage_op_rope_axes", args, **change)
+
+
+@pytest.mark.parametrize("change", [dict(src=0), dict(dst=0), dict(table=0), dict(positions=0), dict(axis=None), dict(src=A[0] + 8), dict(dst=A[1] + 2), dict(table=A[2] + 8), dict(positions=A[3] + 2),
+                                    dict(dtype=2), dict(head_dim=0), dict(head_dim=120), dict(head_dim=272, ld_src=2000, ld_dst=2000), dict(dtype=FP32, head_dim=132), dict(rows=0), dict(n_rot=0), dict(n_positions=0),
+                                    dict(ld_src=639), dict(ld_src=632), dict(ld_dst=644), dict(n_axes=0), dict(n_axes=5), dict(axis=bytes([0, 2] * 32)), dict(axis=bytes([0] * 63 + [254])),
+                                    dict(dst=A[0], ld_dst=648), dict(rows=1 << 30), dict(n_rot=65536, ld_src=1 << 24, ld_dst=1 << 24)])
+def test_rope_axes_refuses(change):
+    assert "rope_axes" in rope(**change)
+
+
+SHAPE = dict(seq_q=100, seq_kv=50, batch=2, n_q=4, n_kv=2, head_dim=64, stream=0)
+
+
+def cross_fwd(**change):
+    args = dict(dtype=BF16, q=A[0], ldq=256, k=A[1], v=A[2], ldkv=128, kv_len=A[3], o=A[4], lse=A[5], ws=A[6], ws_bytes=1 << 40, **SHAPE)
+    return call("optstage_op_cross_attn_fwd", args, **change)
+
+
+def cross_bwd(**change):
+    args = dict(dtype=BF16, q=A[0], ldq=256, k=A[1], v=A[2], ldkv=128, kv_len=A[3], o=A[4], dout=A[7], lse=A[5], dq=A[8], dk=A[9], dv=A[10], ws=A[6], ws_bytes=1 << 40, **SHAPE)
+    return call("optstage_op_cross_attn_bwd", args, **change)
+
+
+COMMON = [dict(q=0), dict(k=0), dict(v=0), dict(ws=0), dict(o=0), dict(lse=0), dict(q=A[0] + 8), dict(k=A[1] + 2), dict(v=A[2] + 8), dict(ws=A[6] + 4), dict(o=A[4] + 8), dict(lse=A[5] + 2), dict(kv_len=A[3] + 1),
+          dict(dtype=2), dict(head_dim=96), dict(head_dim=32), dict(n_q=5), dict(n_kv=0), dict(n_q=0), dict(n_kv=8), dict(seq_q=0), dict(seq_kv=0), dict(batch=0), dict(seq_q=1 << 24), dict(seq_kv=1 << 24),
+          dict(batch=65536), dict(ldq=255), dict(ldq=248), dict(ldkv=120), dict(ldkv=132), dict(ldq=1 << 24), dict(ldkv=1 << 24), dict(dtype=FP32, ldq=258), dict(ws_bytes=0)]
+
+
+@pytest.mark.parametrize("change", COMMON + [dict(o=A[0]), dict(o=A[1]), dict(o=A[2])])
+def test_cross_attention_refuses(change):
+    assert "cross_attn" in cross_fwd(**change)
+
+
+@pytest.mark.parametrize("change", COMMON + [dict(dout=0), dict(dq=0), dict(dk=0), dict(dv=0), dict(dout=A[7] + 8), dict(dq=A[8] + 8), dict(dk=A[9] + 8), dict(dv=A[10] + 8), dict(dq=A[0]), dict(dq=A[4]),
+                                             dict(dq=A[7]), dict(dk=A[1]), dict(dv=A[2]), dict(dk=A[0]), dict(dk=A[8]), dict(dv=A[9]), dict(dv=A[8])])
+def test_cross_attention_gradient_refuses(change):
+    assert "cross_attn" in cross_bwd(**change)
+
+
+def test_cross_attention_workspace():
+    f = B.lib().optstage_op_cross_attn_ws_bytes
+    need = f(BF16, 100, 50, 2, 4, 2, 64)
+    assert need >= 4 * 2 * 4 * 100
+    assert "workspace" in cross_fwd(ws_bytes=need - 1) and "workspace" in cross_bwd(ws_bytes=need - 1)
+    assert f(2, 100, 50, 2, 4, 2, 64) == 0 and f(BF16, 0, 50, 2, 4, 2, 64) == 0 and f(BF16, 100, 50, 2, 5, 2, 64) == 0 and f(BF16, 100, 50, 2, 4, 2, 80) == 0
+    # what callers may count on: eight bytes per query row and head, and 256 MiB
+    for nq, nk, b, hq, hkv, d in [(1, 1 << 20, 64, 64, 8, 128), (4096, 4096, 1, 64, 8, 128), (8192, 100, 16, 16, 16, 64), (16, 16384, 16, 128, 16, 128), (1 << 16, 1, 1, 8, 1, 64)]:
+        for dt in (BF16, FP32):
+            assert 0 < f(dt, nq, nk, b, hq, hkv, d) <= 8 * b * hq * nq + (257 << 20)
+
+
+D_SHAPE = dict(rows=4, vocab=100, k=5, temperature=1.0, log_probs=0, stream=0)
+
+
+def distill(**change):
+    args = dict(dtype=BF16, z=A[0], ldz=100, ids=A[1], teacher=A[2], dloss=A[3], loss=A[4], lse=A[5], dz=A[6], lddz=104, ws=A[7], ws_bytes=1 << 30, **D_SHAPE)
+    return call("optstage_op_distill", args, **change)
+
+
+def distill_fwd(**change):
+    args = dict(dtype=BF16, z=A[0], ldz=100, ids=A[1], teacher=A[2], loss=A[4], lse=A[5], ws=A[7], ws_bytes=1 << 30, **D_SHAPE)
+    return call("optstage_op_distill_fwd", args, **change)
+
+
+def distill_bwd(**change):
+    args = dict(dtype=BF16, z=A[0], ldz=100, ids=A[1], teacher=A[2], lse=A[5], dloss=A[3], dz=A[6], lddz=104, **D_SHAPE)
+    return call("optstage_op_distill_bwd", args, **change)
+
+
+D_COMMON = [dict(z=0), dict(ids=0), dict(teacher=0), dict(lse=0), dict(z=A[0] + 8), dict(ids=A[1] + 2), dict(teacher=A[2] + 1), dict(lse=A[5] + 2), dict(dtype=2), dict(rows=0), dict(vocab=0), dict(k=0), dict(k=1025),
+            dict(ldz=99), dict(temperature=0.0), dict(temperature=-1.0), dict(temperature=float("nan")), dict(temperature=float("inf")), dict(temperature=1e-42), dict(log_probs=2), dict(rows=1 << 30), dict(vocab=1 << 30, ldz=1 << 30)]
+D_FWD = [dict(loss=0), dict(ws=0), dict(loss=A[4] + 2), dict(ws=A[7] + 4), dict(loss=A[5]), dict(ws_bytes=0)]
+D_BWD = [dict(dloss=0), dict(dz=0), dict(dloss=A[3] + 2), dict(dz=A[6] + 2), dict(lddz=99), dict(dz=A[0], lddz=104)]
+
+
+@pytest.mark.parametrize("f,changes", [(distill_fwd, D_COMMON + D_FWD), (distill_bwd, D_COMMON + D_BWD), (distill, D_COMMON + D_FWD + D_BWD + [dict(dloss=A[4]), dict(dloss=A[5])])])
+def test_distillation_refuses(f, changes):
+    for change in changes:
+        assert "distill" in f(**change), change
+
+
+def test_distillation_workspace():
+    f = B.lib().optstage_op_distill_ws_bytes
+    assert f(0, 10, 1) == 0 and f(4, 0, 1) == 0 and f(4, 10, 0) == 0 and f(4, 10, 1025) == 0
+    assert "workspace" in distill_fwd(ws_bytes=f(4, 100, 5) - 1)
+    assert all(0 < f(rows, vocab, 64) <= 1 << 20 for rows in (1, 7, 200, 5000, 1 << 20) for vocab in (1, 1000, 131072, 1 << 20))
