@@ -1,8 +1,964 @@
-// Attention of queries to the states of another sequence, of which the first kv_len count, with its gradients: a wave per row, fp32 throughout.
-#include "common.h"
+// Attention of queries to the states of another sequence, of which the first kv_len count, with its gradients.
+//
+// bf16: the register and LDS scheme of attention_mfma.hip (every product on v_mfma_f32_32x32x16_bf16 in the orientation whose result is the next one's operand, tiles
+// straight from memory into LDS), without a diagonal.  What differs:
+//  * A kv head's query heads are one run of rows: row R of a group is query R % seq_q of its head R / seq_q, so that states are read once for the group and a
+//    single token of eight heads fills a quarter of a tile instead of eight tiles.
+//  * States beyond kv_len are never read: every block of 64 states has a buffer descriptor of its own that ends with them (so a cache of any length is within 32-bit
+//    offsets), loads past it are zero, and what they score is taken out of the softmax.
+//  * Work is split where rows alone do not fill the chip: forward and dQ over the states, dK / dV over the queries.  Parts leave fp32 sums in the workspace that
+//    a second launch joins in a fixed order.
+// The probabilities and dS enter the second products as one bf16 number (2^-8 of each at most, which adds about as much to the result's error as its own
+// rounding does); sums, softmax and D are fp32.  A single state has no gradient of its score: dS = p (dP - D) is 0 by definition and is not computed, since D
+// comes from the rounded o.
+#include "attention_tiles.h"
 
 namespace {
 
+constexpr float LOWEST = -3.402823466e38f;
+
+struct CrossArgs {
+  const bf16_t *q, *k, *v; const int* kv_len; const bf16_t *o_in, *dout;
+  bf16_t* o; float* lse; bf16_t *dq, *dk, *dv; float *delta, *part;
+  size_t ldq, ldkv;
+  int seq_q, seq_kv, n_q, n_kv, rep, rows, splits;     // rows = rep seq_q, the rows of a kv head; splits: parts of the states (forward, dQ) or of the rows (dK / dV)
+  Divisor by_seq_q;
+};
+
+__device__ __forceinline__ int cross_states(const CrossArgs& p, int b) { return p.kv_len ? min(max(p.kv_len[b], 0), p.seq_kv) : p.seq_kv; }
+
+// descriptor of the first `rows` rows of `width` bytes from p on, `stride` bytes apart: loads beyond read zero.  All of it is the same for the whole wave.
+__device__ __forceinline__ i32x4_t rows_desc(const void* p, int rows, unsigned stride, unsigned width) {
+  const unsigned long long ad = (unsigned long long)p;
+  i32x4_t d;
+  d[0] = __builtin_amdgcn_readfirstlane((int)(unsigned)ad);
+  d[1] = __builtin_amdgcn_readfirstlane((int)(unsigned)(ad >> 32) & 0xffff);
+  d[2] = __builtin_amdgcn_readfirstlane(rows > 0 ? (int)((unsigned)(rows - 1) * stride + width) : 0);
+  d[3] = 0x00020000;
+  return d;
+}
+
+#define OPTSTAGE_SB() __builtin_amdgcn_sched_barrier(0)
+#define OPTSTAGE_TILE_LOAD(dst, voff, desc) \
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" :: "s"(dst), "v"(voff), "s"(desc) : "memory", "m0")
+// this wave's loads have landed (the barrier covers the other waves') and nobody still reads what the next ones overwrite
+#define OPTSTAGE_BLOCK_SYNC() asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory")
+
+// store4, or zeros: what a state that does not count has gathered is another's
+__device__ __forceinline__ void store4_if(bf16_t* at, const f32x16_t& x, int v, float scale, bool on) {
+  bf16x4_t r;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) r[i] = on ? (bf16_t)(x[v + i] * scale) : (bf16_t)0.f;
+  *reinterpret_cast<bf16x4_t*>(at) = r;
+}
+
+typedef short i16x4_t __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) i16x4_t lds_i16x4_t;
+__device__ __forceinline__ bf16x8_t transposed8(int lo_at, int hi_at) {
+  const i16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4_t*)(unsigned)lo_at);
+  const i16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4_t*)(unsigned)hi_at);
+  return __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+}
+
+// the blocks of 64 states of part `part` of `splits`: [first, end)
+struct Blocks { int first, end; };
+__device__ __forceinline__ Blocks blocks_of(int n, int part, int splits) {
+  const int all = (n + 63) / 64, per = (all + splits - 1) / splits;
+  return {min(all, part * per), min(all, part * per + per)};
+}
+
+// ---- forward: grid (n_kv x splits x tiles of 32 NW rows, batch), NW waves of 32 rows ----------------------------------------------------
+// LDS: two stages of K, two of V, 64 states each.  Steps of consecutive tiles of 32 states are interleaved by hand as in attention_mfma.hip: the exponentials of a
+// tile run between the score MFMAs of the next, the maxima of the next between its O^T MFMAs; the softmax reference is raised only when a score lies more
+// than FWD_TAU / c above it.
+constexpr float FWD_TAU = 8.f;
+
+template <int D, int NW>
+__global__ __launch_bounds__(64 * NW) void cross_fwd_mfma(const CrossArgs p) {
+  typedef Head<D> H;
+  constexpr int ROWB = H::ROWB, TILE = H::TILE, NKS = H::NKS, NDT = H::NDT;
+  constexpr int WROWS = 64 / NW, NLD = WROWS / H::RPL;
+  constexpr int V_RING = 2 * TILE;
+  extern __shared__ __attribute__((aligned(16))) char smem[];
+  const int tid = threadIdx.x, lane = tid & 63, g = lane >> 5, c32 = lane & 31;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int kvh = blockIdx.x % p.n_kv, at_x = blockIdx.x / p.n_kv, tile = at_x / p.splits, part = at_x % p.splits, b = blockIdx.y;
+  const int n = __builtin_amdgcn_readfirstlane(cross_states(p, b));
+  const Blocks kb = blocks_of(n, part, p.splits);
+  const int end = min(n, 64 * kb.end);                  // states of this part end here
+  const int row = tile * 32 * NW + 32 * wave + c32;
+  const bool mine = row < p.rows;
+  const int rowc = mine ? row : p.rows - 1, head = p.by_seq_q.quotient(rowc), t = rowc - head * p.seq_q;
+  const size_t stat = ((size_t)b * p.n_kv + kvh) * p.rows + rowc, all_rows = (size_t)gridDim.y * p.n_kv * p.rows;
+  const size_t out_at = (((size_t)b * p.seq_q + t) * p.n_q + kvh * p.rep + head) * D;
+  const float scale = rsqrtf((float)D), c = scale * LOG2E, thr = FWD_TAU / c;
+
+  if (kb.first >= kb.end) {                             // no states
+    if (!mine) return;
+    if (p.splits > 1) {
+      if (g == 0) *reinterpret_cast<float2*>(p.part + (size_t)p.splits * all_rows * D + ((size_t)part * all_rows + stat) * 2) = make_float2(-INFINITY, 0.f);
+      return;
+    }
+    const bf16x8_t zero = {};
+#pragma unroll
+    for (int ks = 0; ks < NKS; ++ks) *reinterpret_cast<bf16x8_t*>(p.o + out_at + 16 * ks + 8 * g) = zero;
+    if (g == 0) p.lse[stat] = -INFINITY;
+    return;
+  }
+
+  bf16x8_t Qf[NKS];
+  {
+    const bf16_t* qp = p.q + ((size_t)b * p.seq_q + t) * p.ldq + (size_t)(kvh * p.rep + head) * D + 8 * g;
+#pragma unroll
+    for (int ks = 0; ks < NKS; ++ks) Qf[ks] = *reinterpret_cast<const bf16x8_t*>(qp + 16 * ks);
+  }
+  f32x16_t acc[NDT];                                    // O^T: lane = row, registers = d
+#pragma unroll
+  for (int dt = 0; dt < NDT; ++dt)
+#pragma unroll
+    for (int v = 0; v < 16; ++v) acc[dt][v] = 0.f;
+  float mref = LOWEST, lsum = 0.f;                      // finite: a score of minus infinity lies below it and weighs nothing
+
+  const int lds0 = (int)(unsigned)(size_t)(lds_void_t*)smem;
+  int rm_addr[NKS], tr_addr[NDT][2];
+  {
+    const int f = H::swz(c32);
+#pragma unroll
+    for (int ks = 0; ks < NKS; ++ks) rm_addr[ks] = c32 * ROWB + (((2 * ks + g) ^ f) << 4);
+    const int cg = (lane >> 4) & 1, e = (lane >> 2) & 3, r = lane & 3;
+#pragma unroll
+    for (int dt = 0; dt < NDT; ++dt)
+#pragma unroll
+      for (int kq = 0; kq < 2; ++kq)
+        tr_addr[dt][kq] = lds0 + V_RING + (4 * g + e) * ROWB + (((4 * dt + 2 * cg + (r >> 1)) ^ H::swz(8 * kq + 4 * g + e)) << 4) + (r & 1) * 8;
+  }
+  const unsigned stride = (unsigned)p.ldkv * 2u;
+  unsigned voff[NLD];
+#pragma unroll
+  for (int j = 0; j < NLD; ++j) {
+    const int lr = WROWS * wave + H::RPL * j + lane / H::CH;
+    voff[j] = (unsigned)lr * stride + (unsigned)((lane % H::CH) ^ H::swz(lr)) * 16u;
+  }
+  const size_t base = ((size_t)b * p.seq_kv) * p.ldkv + (size_t)kvh * D;
+  auto issue_tile = [&](const bf16_t* x, int blk, int lds) {
+    const i32x4_t rs = rows_desc(x + base + (size_t)blk * 64 * p.ldkv, min(n - 64 * blk, 64), stride, ROWB);
+    const unsigned dst = (unsigned)(lds0 + lds) + (WROWS * wave) * ROWB;
+#pragma unroll
+    for (int j = 0; j < NLD; ++j) OPTSTAGE_TILE_LOAD(dst + j * 1024, voff[j], rs);
+  };
+  auto tr_frag = [&](int at, int dt, int tt, int u) {
+    return transposed8(tr_addr[dt][0] + at + (32 * tt + 16 * u) * ROWB, tr_addr[dt][1] + at + (32 * tt + 16 * u + 8) * ROWB);
+  };
+  auto rm_frag = [&](const char* at, int tt, int ks) { return *reinterpret_cast<const bf16x8_t*>(at + tt * 32 * ROWB + rm_addr[ks]); };
+
+  constexpr int PF = 3, PT = 3;
+  bf16x8_t kf[PF], trf[PT];
+  // scores of tile tt of the K stage into nxt, between them the exponentials of cur; the first operand fragments of a step are read during the step before it
+  auto step_scores = [&](bool with_exp, int stage_k, int tt, f32x16_t& cur, f32x16_t& nxt, int stage_v, int tv) __attribute__((always_inline)) {
+    const char* sK = smem + stage_k * TILE;
+    const float mc = mref * c;
+    float ls = 0.f;
+#pragma unroll
+    for (int ks = 0; ks < NKS; ++ks) {
+      OPTSTAGE_SB();
+      if (ks + PF - 1 < NKS) kf[(ks + PF - 1) % PF] = rm_frag(sK, tt, ks + PF - 1);
+      if (stage_v >= 0 && ks + PT - 1 >= NKS) trf[ks + PT - 1 - NKS] = tr_frag(stage_v * TILE, (ks + PT - 1 - NKS) % NDT, tv, (ks + PT - 1 - NKS) / NDT);
+      OPTSTAGE_SB();
+      asm volatile("s_nop 1" :: "v"(kf[ks % PF]));      // the operand has settled before an MFMA that the compiler does not see into
+      if (ks == 0)
+        asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, 0" : "=&v"(nxt) : "v"(kf[0]), "a"(Qf[0]));
+      else
+        asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+v"(nxt) : "v"(kf[ks % PF]), "a"(Qf[ks]));
+      OPTSTAGE_SB();
+      if (with_exp) {
+        constexpr int PV = 16 / NKS;
+#pragma unroll
+        for (int x = 0; x < PV; ++x) {
+          const int v = ks * PV + x;
+          cur[v] = __builtin_amdgcn_exp2f(fmaf(cur[v], c, -mc));
+          ls += cur[v];
+          asm volatile("" : "+v"(cur[v]), "+v"(ls));    // stays between the MFMAs it is written between
+        }
+      }
+      OPTSTAGE_SB();
+    }
+    OPTSTAGE_SB();
+    lsum += ls;
+  };
+  // states past the part's end (a whole tile of them behind the last block) leave the softmax
+  auto mask_tile = [&](int key0, f32x16_t& sc) __attribute__((always_inline)) {
+    if (key0 + 32 <= end) return;                       // the same for the whole workgroup
+    asm volatile("s_nop 7" ::: "memory");               // the scores' last MFMA has written its results
+#pragma unroll
+    for (int v = 0; v < 16; ++v)
+      if (key0 + 8 * (v >> 2) + 4 * g + (v & 3) >= end) sc[v] = -INFINITY;
+  };
+  auto max_part = [&](int i, const f32x16_t& sc, float& mx) __attribute__((always_inline)) {
+#pragma unroll
+    for (int x = 0; x < 4 / NDT; ++x) {
+      const int v = 2 * (i * (4 / NDT) + x);
+      mx = fmaxf(mx, fmaxf(sc[v], sc[v + 1]));
+    }
+    asm volatile("" : "+v"(mx));
+  };
+  auto raise_reference = [&](float mx) __attribute__((always_inline)) {
+    mx = pair_max32(mx);
+    if (__any(mx > mref + thr)) {
+      asm volatile("s_nop 15\n\ts_nop 7" ::: "memory"); // the last O^T MFMAs have left the matrix unit
+      const float mn = fmaxf(mref, mx);
+      const float alpha = mn == mref ? 1.f : __builtin_amdgcn_exp2f((mref - mn) * c);
+      mref = mn;
+      lsum *= alpha;
+#pragma unroll
+      for (int dt = 0; dt < NDT; ++dt) {
+        OPTSTAGE_SB();
+#pragma unroll
+        for (int v = 0; v < 16; ++v) acc[dt][v] *= alpha;
+      }
+      OPTSTAGE_SB();
+    }
+  };
+  // O^T += V^T P^T of the tile in cur, between the MFMAs the maxima of the next tile (scores in nxt, states from key1 on)
+  auto step_output = [&](bool fill, int stage_v, int tt, int key1, f32x16_t& cur, f32x16_t& nxt, int stage_k, int tk) __attribute__((always_inline)) {
+    if (fill) {
+#pragma unroll
+      for (int i = 0; i < PT - 1; ++i) trf[i] = tr_frag(stage_v * TILE, i % NDT, tt, i / NDT);
+    }
+    mask_tile(key1, nxt);
+    float mx = -INFINITY;
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const bf16x8_t pr = pack8(cur, u);
+#pragma unroll
+      for (int dt = 0; dt < NDT; ++dt) {
+        const int i = u * NDT + dt, n2 = i + PT - 1, k2 = i + PF - 1 - 2 * NDT;
+        OPTSTAGE_SB();
+        if (n2 < 2 * NDT) trf[n2 % PT] = tr_frag(stage_v * TILE, n2 % NDT, tt, n2 / NDT);
+        if (stage_k >= 0 && k2 >= 0) kf[k2] = rm_frag(smem + stage_k * TILE, tk, k2);
+        if (dt == 0) asm volatile("s_nop 1" :: "v"(pr) : "memory");
+        OPTSTAGE_SB();
+        asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+a"(acc[dt]) : "v"(trf[i % PT]), "v"(pr));
+        OPTSTAGE_SB();
+        max_part(i, nxt, mx);
+      }
+    }
+    OPTSTAGE_SB();
+    raise_reference(mx);
+  };
+  auto fill_k = [&](int stage, int tt) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < PF - 1; ++i) kf[i] = rm_frag(smem + stage * TILE, tt, i);
+  };
+  f32x16_t sA, sB;
+  issue_tile(p.k, kb.first, 0);
+  OPTSTAGE_BLOCK_SYNC();
+  if (kb.first + 1 < kb.end) issue_tile(p.k, kb.first + 1, TILE);
+  issue_tile(p.v, kb.first, V_RING);
+  fill_k(0, 0);
+  step_scores(false, 0, 0, sB, sA, -1, 0);
+  {
+    asm volatile("s_nop 15\n\ts_nop 7" ::: "memory");
+    mask_tile(64 * kb.first, sA);
+    float mx = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < 2 * NDT; ++i) max_part(i, sA, mx);
+    raise_reference(mx);
+    fill_k(0, 1);
+  }
+  auto block = [&](int blk, int st) __attribute__((always_inline)) {
+    step_scores(true, st, 1, sA, sB, -1, 0);
+    OPTSTAGE_BLOCK_SYNC();                              // K of the next block and V of this one, requested a block ago
+    if (blk + 2 < kb.end) issue_tile(p.k, blk + 2, st * TILE);
+    if (blk + 1 < kb.end) issue_tile(p.v, blk + 1, V_RING + (st ^ 1) * TILE);
+    step_output(true, st, 0, 64 * blk + 32, sA, sB, st ^ 1, 0);
+    // behind the last block these scores are of a stage that holds none of the part's states: masked, never used
+    step_scores(true, st ^ 1, 0, sB, sA, st, 1);
+    step_output(false, st, 1, 64 * blk + 64, sB, sA, st ^ 1, 1);
+  };
+  for (int blk = kb.first; blk < kb.end; blk += 2) {
+    block(blk, 0);
+    if (blk + 1 < kb.end) block(blk + 1, 1);
+  }
+  asm volatile("s_nop 15\n\ts_nop 7" ::: "memory");
+  const float lt = lsum + __shfl_xor(lsum, 32, 64);
+  if (!mine) return;
+  if (p.splits > 1) {
+    float* out = p.part + ((size_t)part * all_rows + stat) * D;
+#pragma unroll
+    for (int dt = 0; dt < NDT; ++dt)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        OPTSTAGE_SB();
+        *reinterpret_cast<f32x4_t*>(out + 32 * dt + 8 * j + 4 * g) = f32x4_t{acc[dt][4 * j], acc[dt][4 * j + 1], acc[dt][4 * j + 2], acc[dt][4 * j + 3]};
+      }
+    if (g == 0) *reinterpret_cast<float2*>(p.part + (size_t)p.splits * all_rows * D + ((size_t)part * all_rows + stat) * 2) = make_float2(mref, lt);
+    return;
+  }
+  const float inv = 1.f / lt;
+  bf16_t* orow = p.o + out_at;
+#pragma unroll
+  for (int dt = 0; dt < NDT; ++dt) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      OPTSTAGE_SB();
+      store4(orow + 32 * dt + 8 * j + 4 * g, acc[dt], 4 * j, inv);
+    }
+  }
+  if (g == 0) p.lse[stat] = mref * scale + logf(lt);
+}
+
+// o and lse of a row from its parts' sums: a thread has 8 columns
+template <int D> __global__ __launch_bounds__(256) void cross_fwd_join(const CrossArgs p, size_t all_rows) {
+  constexpr int Q = D / 8;
+  const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x, stat = i / Q;
+  if (stat >= all_rows) return;
+  const int col = (int)(i % Q) * 8;
+  const float scale = rsqrtf((float)D), c = scale * LOG2E;
+  const float2* ml = reinterpret_cast<const float2*>(p.part + (size_t)p.splits * all_rows * D) + stat;
+  float m = -INFINITY, l = 0.f, x[8] = {};
+  for (int s = 0; s < p.splits; ++s) m = fmaxf(m, ml[s * all_rows].x);
+  for (int s = 0; s < p.splits; ++s) {
+    const float2 w = ml[s * all_rows];
+    if (w.x == -INFINITY) continue;                     // a part without states has left no sums
+    const float f = __builtin_amdgcn_exp2f((w.x - m) * c);
+    l = fmaf(w.y, f, l);
+    const f32x4_t* a = reinterpret_cast<const f32x4_t*>(p.part + (s * all_rows + stat) * D + col);
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[4 * h + e] = fmaf(a[h][e], f, x[4 * h + e]);
+  }
+  const size_t t = stat % p.seq_q, a = stat / p.seq_q % p.n_q, b = stat / p.seq_q / p.n_q;
+  const bool none = m == -INFINITY;
+  const float inv = none ? 0.f : 1.f / l;
+  bf16x8_t out;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) out[e] = (bf16_t)(x[e] * inv);
+  *reinterpret_cast<bf16x8_t*>(p.o + ((b * p.seq_q + t) * p.n_q + a) * D + col) = out;
+  if (col == 0) p.lse[stat] = none ? -INFINITY : m * scale + logf(l);
+}
+
+// ---- backward, dQ: grid as forward ---------------------------------------------------------------------------------------------------
+// The rows' Q and dO fragments and dQ^T stay in registers; blocks of 64 states (K and V rows) stream through two stages.  Stores -D = -<dO, o> of its rows for the
+// dK / dV kernel, which runs after it.
+template <int D, int NW>
+__global__ __launch_bounds__(64 * NW) void cross_dq_mfma(const CrossArgs p) {
+  typedef Head<D> H;
+  constexpr int ROWB = H::ROWB, TILE = H::TILE, NKS = H::NKS, NDT = H::NDT;
+  constexpr int WROWS = 64 / NW, NLD = WROWS / H::RPL;
+  constexpr int STAGE = 2 * TILE;
+  extern __shared__ __attribute__((aligned(16))) char smem[];
+  const int tid = threadIdx.x, lane = tid & 63, g = lane >> 5, c32 = lane & 31;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int kvh = blockIdx.x % p.n_kv, at_x = blockIdx.x / p.n_kv, tile = at_x / p.splits, part = at_x % p.splits, b = blockIdx.y;
+  const int n = __builtin_amdgcn_readfirstlane(cross_states(p, b));
+  const Blocks kb = blocks_of(n == 1 ? 0 : n, part, p.splits);   // one state: no gradient of its score
+  const int row = tile * 32 * NW + 32 * wave + c32;
+  const bool mine = row < p.rows;
+  const int rowc = mine ? row : p.rows - 1, head = p.by_seq_q.quotient(rowc), t = rowc - head * p.seq_q;
+  const size_t stat = ((size_t)b * p.n_kv + kvh) * p.rows + rowc;
+  const float scale = rsqrtf((float)D), c = scale * LOG2E;
+  bf16x8_t Qf[NKS], dOf[NKS];
+  float Lc, Dq;
+  {
+    const size_t at = (size_t)(kvh * p.rep + head) * D + 8 * g, tok = (size_t)b * p.seq_q + t;
+    const bf16_t *qp = p.q + tok * p.ldq + at, *dop = p.dout + tok * p.n_q * D + at, *op = p.o_in + tok * p.n_q * D + at;
+    float dsum = 0.f;
+#pragma unroll
+    for (int ks = 0; ks < NKS; ++ks) {
+      Qf[ks] = *reinterpret_cast<const bf16x8_t*>(qp + 16 * ks);
+      dOf[ks] = *reinterpret_cast<const bf16x8_t*>(dop + 16 * ks);
+      const bf16x8_t of = *reinterpret_cast<const bf16x8_t*>(op + 16 * ks);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) dsum = fmaf((float)dOf[ks][e], (float)of[e], dsum);
+    }
+    Lc = -p.lse[stat] * LOG2E;
+    Dq = dsum + __shfl_xor(dsum, 32, 64);
+    if (part == 0 && g == 0 && mine) p.delta[stat] = -Dq;
+  }
+  f32x16_t negD;                                        // the initial value of the dP^T MFMAs, which then deliver dP^T - D
+#pragma unroll
+  for (int v = 0; v < 16; ++v) negD[v] = -Dq;
+#pragma unroll
+  for (int ks = 0; ks < NKS; ++ks) asm volatile("" : "+a"(Qf[ks]), "+a"(dOf[ks]));
+  f32x16_t acc[NDT];
+#pragma unroll
+  for (int dt = 0; dt < NDT; ++dt)
+#pragma unroll
+    for (int v = 0; v < 16; ++v) acc[dt][v] = 0.f;
+  const int lds0 = (int)(unsigned)(size_t)(lds_void_t*)smem;
+  int rm_addr[NKS], tr_addr[NDT][2];
+  {
+    const int f = H::swz(c32);
+#pragma unroll
+    for (int ks = 0; ks < NKS; ++ks) {
+      rm_addr[ks] = lds0 + c32 * ROWB + (((2 * ks + g) ^ f) << 4);
+      asm volatile("" : "+v"(rm_addr[ks]));             // one number per read, not the terms of a sum
+    }
+    const int cg = (lane >> 4) & 1, e = (lane >> 2) & 3, r = lane & 3;
+#pragma unroll
+    for (int dt = 0; dt < NDT; ++dt)
+#pragma unroll
+      for (int kq = 0; kq < 2; ++kq) {
+        tr_addr[dt][kq] = lds0 + (4 * g + e) * ROWB + (((4 * dt + 2 * cg + (r >> 1)) ^ H::swz(8 * kq + 4 * g + e)) << 4) + (r & 1) * 8;
+        asm volatile("" : "+v"(tr_addr[dt][kq]));
+      }
+  }
+  const unsigned stride = (unsigned)p.ldkv * 2u;
+  unsigned voff[NLD];
+#pragma unroll
+  for (int j = 0; j < NLD; ++j) {
+    const int lr = WROWS * wave + H::RPL * j + lane / H::CH;
+    voff[j] = (unsigned)lr * stride + (unsigned)((lane % H::CH) ^ H::swz(lr)) * 16u;
+  }
+  const size_t base = ((size_t)b * p.seq_kv) * p.ldkv + (size_t)kvh * D;
+  auto issue_block = [&](int blk, int stage) {
+    const int rows = min(n - 64 * blk, 64);
+    const size_t at = base + (size_t)blk * 64 * p.ldkv;
+    const i32x4_t rk = rows_desc(p.k + at, rows, stride, ROWB), rv = rows_desc(p.v + at, rows, stride, ROWB);
+    const unsigned dst = (unsigned)lds0 + stage * STAGE + (WROWS * wave) * ROWB;
+#pragma unroll
+    for (int j = 0; j < NLD; ++j) {
+      OPTSTAGE_TILE_LOAD(dst + j * 1024, voff[j], rk);
+      OPTSTAGE_TILE_LOAD(dst + TILE + j * 1024, voff[j], rv);
+    }
+  };
+  auto tr_frag = [&](int at, int dt, int tt, int u) {
+    return transposed8(tr_addr[dt][0] + at + (32 * tt + 16 * u) * ROWB, tr_addr[dt][1] + at + (32 * tt + 16 * u + 8) * ROWB);
+  };
+  auto rm_frag = [&](int at, int tt, int ks) { return *(const lds_bf16x8_t*)(unsigned)(rm_addr[ks] + at + tt * 32 * ROWB); };
+#define OPTSTAGE_MFMA_V(acc, a, b) asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+v"(acc) : "v"(a), "a"(b))
+#define OPTSTAGE_MFMA_0(acc, a, b) asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, 0" : "=&v"(acc) : "v"(a), "a"(b))
+  auto block = [&](int blk, int stage) __attribute__((always_inline)) {
+    const int sK = stage * STAGE, sV = sK + TILE;
+#pragma unroll
+    for (int tt = 0; tt < 2; ++tt) {
+      const int key0 = 64 * blk + 32 * tt;
+      if (key0 >= n) continue;                          // the same for the whole workgroup
+      const bool edge = key0 + 32 > n;
+      f32x16_t s, dp;                                   // lane = row, registers = states key0 + 8 (v / 4) + 4 g + v % 4
+      bf16x8_t kf[2], vf[2];
+      kf[0] = rm_frag(sK, tt, 0);
+#pragma unroll
+      for (int ks = 0; ks < NKS; ++ks) {                // S^T = K Q^T
+        OPTSTAGE_SB();
+        if (ks < NKS - 1) kf[(ks + 1) & 1] = rm_frag(sK, tt, ks + 1);
+        else vf[0] = rm_frag(sV, tt, 0);
+        OPTSTAGE_SB();
+        if (ks == 0) OPTSTAGE_MFMA_0(s, kf[0], Qf[0]);
+        else OPTSTAGE_MFMA_V(s, kf[ks & 1], Qf[ks]);
+      }
+#pragma unroll
+      for (int ks = 0; ks < NKS; ++ks) {                // dP^T = V dO^T, the exponentials of S^T under its MFMAs
+        OPTSTAGE_SB();
+        if (ks < NKS - 1) vf[(ks + 1) & 1] = rm_frag(sV, tt, ks + 1);
+        OPTSTAGE_SB();
+        if (ks == 0) {
+          asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %3" : "=&v"(dp) : "v"(vf[0]), "a"(dOf[0]), "v"(negD));
+          asm volatile("s_nop 7" ::: "memory");         // the exponentials read S^T a few cycles after the matrix unit has written it
+        } else {
+          OPTSTAGE_MFMA_V(dp, vf[ks & 1], dOf[ks]);
+        }
+        OPTSTAGE_SB();
+#pragma unroll
+        for (int e = 0; e < 16 / NKS; ++e) {
+          const int v = (16 / NKS) * ks + e;
+          s[v] = __builtin_amdgcn_exp2f(fmaf(s[v], c, Lc));
+        }
+      }
+      OPTSTAGE_SB();
+      if (edge) {
+        asm volatile("" ::: "memory");                  // a real branch: only the last tile pays for the mask
+#pragma unroll
+        for (int v = 0; v < 16; ++v)
+          if (key0 + 8 * (v >> 2) + 4 * g + (v & 3) >= n) s[v] = 0.f;
+      }
+      asm volatile("s_nop 15\n\ts_nop 7" ::: "memory"); // dP^T has left the matrix unit
+      OPTSTAGE_SB();
+      bf16x8_t trf[2];                                  // dQ^T += K^T dS^T; dS^T of the second half under the MFMAs of the first
+      trf[0] = tr_frag(sK, 0, tt, 0);
+#pragma unroll
+      for (int v = 0; v < 8; ++v) dp[v] = s[v] * dp[v];
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const bf16x8_t d = pack8(dp, u);
+#pragma unroll
+        for (int dt = 0; dt < NDT; ++dt) {
+          const int i = u * NDT + dt;
+          OPTSTAGE_SB();
+          if (i < 2 * NDT - 1) trf[(i + 1) & 1] = tr_frag(sK, (dt + 1) % NDT, tt, dt == NDT - 1 ? 1 : u);
+          OPTSTAGE_SB();
+          acc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(trf[i & 1], d, acc[dt], 0, 0, 0);
+          OPTSTAGE_SB();
+          if (u == 0) {
+#pragma unroll
+            for (int e = 0; e < 8 / NDT; ++e) {
+              const int v = 8 + (8 / NDT) * dt + e;
+              dp[v] = s[v] * dp[v];
+            }
+          }
+        }
+      }
+      OPTSTAGE_SB();
+    }
+  };
+#undef OPTSTAGE_MFMA_V
+#undef OPTSTAGE_MFMA_0
+  if (kb.first < kb.end) issue_block(kb.first, 0);
+  for (int blk = kb.first; blk < kb.end; blk += 2) {
+    OPTSTAGE_BLOCK_SYNC();
+    if (blk + 1 < kb.end) issue_block(blk + 1, 1);
+    block(blk, 0);
+    if (blk + 1 < kb.end) {
+      OPTSTAGE_BLOCK_SYNC();
+      if (blk + 2 < kb.end) issue_block(blk + 2, 0);
+      block(blk + 1, 1);
+    }
+  }
+  if (!mine) return;
+  if (p.splits > 1) {
+    if (kb.first >= kb.end) return;                     // the join counts the parts that have states
+    float* out = p.part + ((size_t)part * gridDim.y * p.n_kv * p.rows + stat) * D;
+#pragma unroll
+    for (int dt = 0; dt < NDT; ++dt)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        OPTSTAGE_SB();
+        *reinterpret_cast<f32x4_t*>(out + 32 * dt + 8 * j + 4 * g) = f32x4_t{acc[dt][4 * j], acc[dt][4 * j + 1], acc[dt][4 * j + 2], acc[dt][4 * j + 3]};
+      }
+    return;
+  }
+  bf16_t* dq = p.dq + ((size_t)b * p.seq_q + t) * p.ldq + (size_t)(kvh * p.rep + head) * D;
+#pragma unroll
+  for (int dt = 0; dt < NDT; ++dt)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      OPTSTAGE_SB();
+      store4(dq + 32 * dt + 8 * j + 4 * g, acc[dt], 4 * j, scale);
+    }
+}
+
+template <int D> __global__ __launch_bounds__(256) void cross_dq_join(const CrossArgs p, size_t all_rows) {
+  constexpr int Q = D / 8;
+  const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x, stat = i / Q;
+  if (stat >= all_rows) return;
+  const int col = (int)(i % Q) * 8;
+  const size_t t = stat % p.seq_q, a = stat / p.seq_q % p.n_q, b = stat / p.seq_q / p.n_q;
+  const int n = cross_states(p, (int)b), all = n == 1 ? 0 : (n + 63) / 64, per = (all + p.splits - 1) / p.splits;
+  float x[8] = {};
+  for (int s = 0; s * per < all; ++s) {
+    const f32x4_t* f = reinterpret_cast<const f32x4_t*>(p.part + (s * all_rows + stat) * D + col);
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[4 * h + e] += f[h][e];
+  }
+  bf16x8_t out;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) out[e] = (bf16_t)(x[e] * rsqrtf((float)D));
+  *reinterpret_cast<bf16x8_t*>(p.dq + (b * p.seq_q + t) * p.ldq + a * D + col) = out;
+}
+
+// ---- backward, dK / dV: grid (n_kv x splits x tiles of 128 KT states, batch), 4 NG waves --------------------------------------------------
+// A wave owns 32 KT states: K fragments, dK^T and dV^T in registers, the V rows of the workgroup's states in LDS.  Blocks of 64 rows (Q and dO, lse and -D) stream through
+// two stages; rows past the last one read as zeros and add nothing.  NG = 2: a second group of waves takes the other 32 rows of every block, and the first adds its sums.
+template <int D, int KT, int NG>
+__global__ __launch_bounds__(256 * NG) void cross_dkv_mfma(const CrossArgs p) {
+  typedef Head<D> H;
+  constexpr int ROWB = H::ROWB, TILE = H::TILE, NKS = H::NKS, NDT = H::NDT;
+  constexpr int WROWS = 16 / NG, NLD = WROWS / H::RPL;
+  constexpr int STAGE = 2 * TILE + 512;                 // Q tile, dO tile, 64 lse, 64 -D
+  extern __shared__ __attribute__((aligned(16))) char smem[];
+  const int tid = threadIdx.x, lane = tid & 63, g = lane >> 5, c32 = lane & 31;
+  const int id = __builtin_amdgcn_readfirstlane(tid >> 6), wave = id & 3, grp = NG == 1 ? 0 : id >> 2;
+  constexpr int WK = 32 * KT, GK = 4 * WK;
+  const int kvh = blockIdx.x % p.n_kv, at_x = blockIdx.x / p.n_kv, k0 = at_x / p.splits * GK, part = at_x % p.splits, b = blockIdx.y;
+  const int n = __builtin_amdgcn_readfirstlane(cross_states(p, b));
+  const int first_k = k0 + WK * wave;
+  const float scale = rsqrtf((float)D), c = scale * LOG2E;
+  const size_t base = ((size_t)b * p.seq_kv) * p.ldkv + (size_t)kvh * D;
+  if (k0 >= n) {                                        // states that do not count have no gradient
+    if (p.splits > 1) return;                           // the join writes their zeros
+    const bf16x8_t zero = {};
+    for (int i = tid; i < GK * (D / 8); i += 256 * NG) {
+      const int s = k0 + i / (D / 8), col = i % (D / 8) * 8;
+      if (s >= p.seq_kv) break;
+      *reinterpret_cast<bf16x8_t*>(p.dk + base + (size_t)s * p.ldkv + col) = zero;
+      *reinterpret_cast<bf16x8_t*>(p.dv + base + (size_t)s * p.ldkv + col) = zero;
+    }
+    return;
+  }
+  bf16x8_t Kf[KT][NKS];
+#pragma unroll
+  for (int kk = 0; kk < KT; ++kk) {
+    const bf16_t* kp = p.k + base + (size_t)min(first_k + 32 * kk + c32, n - 1) * p.ldkv + 8 * g;
+#pragma unroll
+    for (int ks = 0; ks < NKS; ++ks) Kf[kk][ks] = *reinterpret_cast<const bf16x8_t*>(kp + 16 * ks);
+  }
+  f32x16_t accK[KT][NDT], accV[KT][NDT];                // lane = state, registers = d
+#pragma unroll
+  for (int kk = 0; kk < KT; ++kk)
+#pragma unroll
+    for (int dt = 0; dt < NDT; ++dt)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) { accK[kk][dt][v] = 0.f; accV[kk][dt][v] = 0.f; }
+  const int lds0 = (int)(unsigned)(size_t)(lds_void_t*)smem;
+  const int half = grp * 32, row4 = lds0 + 16 * g + half * 4;
+  int rm_addr[NKS], tr_addr[NDT][2];
+  {
+    const int f = H::swz(c32);
+#pragma unroll
+    for (int ks = 0; ks < NKS; ++ks) {
+      rm_addr[ks] = lds0 + half * ROWB + c32 * ROWB + (((2 * ks + g) ^ f) << 4);
+      asm volatile("" : "+v"(rm_addr[ks]));
+    }
+    const int cg = (lane >> 4) & 1, e = (lane >> 2) & 3, r = lane & 3;
+#pragma unroll
+    for (int dt = 0; dt < NDT; ++dt)
+#pragma unroll
+      for (int kq = 0; kq < 2; ++kq) {
+        tr_addr[dt][kq] = lds0 + half * ROWB + (4 * g + e) * ROWB + (((4 * dt + 2 * cg + (r >> 1)) ^ H::swz(8 * kq + 4 * g + e)) << 4) + (r & 1) * 8;
+        asm volatile("" : "+v"(tr_addr[dt][kq]));
+      }
+  }
+  const size_t head0 = (size_t)kvh * p.rep * D;
+  const i32x4_t rs_q = rows_desc(p.q + (size_t)b * p.seq_q * p.ldq + head0, p.seq_q, (unsigned)p.ldq * 2u, (unsigned)p.rep * ROWB);
+  const i32x4_t rs_do = rows_desc(p.dout + (size_t)b * p.seq_q * p.n_q * D + head0, p.seq_q, (unsigned)p.n_q * ROWB, (unsigned)p.rep * ROWB);
+  const size_t stat0 = ((size_t)b * p.n_kv + kvh) * p.rows;
+  const i32x4_t rs_l = rows_desc(p.lse + stat0, p.rows, 4u, 4u), rs_d = rows_desc(p.delta + stat0, p.rows, 4u, 4u);
+  const int sV = 2 * STAGE + wave * WK * ROWB - half * ROWB;
+  {
+    const i32x4_t rs_v = rows_desc(p.v + base + (size_t)first_k * p.ldkv, min(n - first_k, WK), (unsigned)p.ldkv * 2u, ROWB);
+#pragma unroll
+    for (int j0 = 0; j0 < 2 * KT * NLD; ++j0) {         // both groups read them: each loads its share
+      const int j = j0 + grp * 2 * KT * NLD, lr = H::RPL * j + lane / H::CH;
+      OPTSTAGE_TILE_LOAD((unsigned)(lds0 + 2 * STAGE + wave * WK * ROWB + j * 1024), (unsigned)lr * (unsigned)p.ldkv * 2u + (unsigned)((lane % H::CH) ^ H::swz(lr)) * 16u, rs_v);
+    }
+  }
+  const int blocks = (p.rows + 63) / 64, per = (blocks + p.splits - 1) / p.splits, it0 = min(blocks, part * per), it1 = min(blocks, it0 + per);
+  auto issue_block = [&](int it, int stage) {
+    const unsigned dst = (unsigned)lds0 + stage * STAGE + (WROWS * id) * ROWB;
+#pragma unroll
+    for (int j = 0; j < NLD; ++j) {
+      const int lr = WROWS * id + H::RPL * j + lane / H::CH, row = 64 * it + lr;
+      const unsigned chunk = (unsigned)((lane % H::CH) ^ H::swz(lr)) * 16u;
+      const unsigned head = p.by_seq_q.quotient(row), t = row - head * p.seq_q;
+      // a row past the last one: an offset past any end
+      const unsigned oq = row < p.rows ? t * ((unsigned)p.ldq * 2u) + head * ROWB + chunk : 0xFFFFFFF0u;
+      const unsigned od = row < p.rows ? t * ((unsigned)p.n_q * ROWB) + head * ROWB + chunk : 0xFFFFFFF0u;
+      OPTSTAGE_TILE_LOAD(dst + j * 1024, oq, rs_q);
+      OPTSTAGE_TILE_LOAD(dst + TILE + j * 1024, od, rs_do);
+    }
+    if (id < 2)                                         // wave 0: lse of the 64 rows, wave 1: -D
+      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds"
+                   :: "s"((unsigned)lds0 + stage * STAGE + 2 * TILE + id * 256), "v"((unsigned)(64 * it + lane) * 4u), "s"(id == 0 ? rs_l : rs_d) : "memory", "m0");
+  };
+  auto tr_frag = [&](int at, int dt, int tt, int u) {
+    return transposed8(tr_addr[dt][0] + at + (32 * tt + 16 * u) * ROWB, tr_addr[dt][1] + at + (32 * tt + 16 * u + 8) * ROWB);
+  };
+  auto rm_frag = [&](int at, int tt, int ks) { return *(const lds_bf16x8_t*)(unsigned)(rm_addr[ks] + at + tt * 32 * ROWB); };
+#define OPTSTAGE_MFMA_V(acc, a, b) asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+v"(acc) : "v"(a), "v"(b))
+#define OPTSTAGE_MFMA_0(acc, a, b) asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, 0" : "=&v"(acc) : "v"(a), "v"(b))
+  auto block = [&](int stage) __attribute__((always_inline)) {
+    const int sQ = stage * STAGE, sDO = sQ + TILE, sL = sQ + 2 * TILE, sD = sL + 256;
+#pragma unroll
+    for (int tt = 0; tt < 2 / NG; ++tt) {
+      f32x16_t s[KT], dp[KT];                           // lane = state, registers = rows 32 tt + 8 (v / 4) + 4 g + v % 4 of the block
+      f32x4_t nL[4];
+      f32x16_t negD;
+      bf16x8_t qf[2], df[2], vf[2][KT];
+      qf[0] = rm_frag(sQ, tt, 0);
+#pragma unroll
+      for (int ks = 0; ks < NKS; ++ks) {                // S = Q K^T
+        OPTSTAGE_SB();
+        if (ks < NKS - 1) {
+          qf[(ks + 1) & 1] = rm_frag(sQ, tt, ks + 1);
+        } else {
+          df[0] = rm_frag(sDO, tt, 0);
+#pragma unroll
+          for (int kk = 0; kk < KT; ++kk) vf[0][kk] = rm_frag(sV, kk, 0);
+        }
+        if (KT == 2 ? ks < 4 : ks == NKS - 1) nL[KT == 2 ? ks : 0] = *(const lds_f32x4_t*)(unsigned)(row4 + sL + (32 * tt + 8 * (KT == 2 ? ks : 0)) * 4);
+        if (ks >= NKS - 4) {
+          const f32x4_t d4 = *(const lds_f32x4_t*)(unsigned)(row4 + sD + (32 * tt + 8 * (ks - (NKS - 4))) * 4);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) (KT == 2 ? negD : dp[0])[4 * (ks - (NKS - 4)) + i] = d4[i];
+        }
+        OPTSTAGE_SB();
+        if (ks == 0) {
+#pragma unroll
+          for (int kk = 0; kk < KT; ++kk) OPTSTAGE_MFMA_0(s[kk], qf[0], Kf[kk][0]);
+        } else {
+#pragma unroll
+          for (int kk = 0; kk < KT; ++kk) OPTSTAGE_MFMA_V(s[kk], qf[ks & 1], Kf[kk][ks]);
+        }
+        OPTSTAGE_SB();
+        if (KT == 2 && ks >= NKS - 4) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) nL[ks - (NKS - 4)][i] *= -LOG2E;
+        }
+      }
+#pragma unroll
+      for (int ks = 0; ks < NKS; ++ks) {                // dP - D = dO V^T - D, the exponentials of S under its MFMAs
+        OPTSTAGE_SB();
+        if (ks < NKS - 1) {
+          df[(ks + 1) & 1] = rm_frag(sDO, tt, ks + 1);
+#pragma unroll
+          for (int kk = 0; kk < KT; ++kk) vf[(ks + 1) & 1][kk] = rm_frag(sV, kk, ks + 1);
+        }
+        constexpr int KL = NKS / 4;
+        if (KT == 1 && ks % KL == KL - 1 && ks / KL < 3)
+          nL[ks / KL + 1] = *(const lds_f32x4_t*)(unsigned)(row4 + sL + (32 * tt + 8 * (ks / KL + 1)) * 4);
+        OPTSTAGE_SB();
+        if (ks == 0) {
+#pragma unroll
+          for (int kk = 0; kk < KT; ++kk) {
+            if constexpr (KT == 2) asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %3" : "=&v"(dp[kk]) : "v"(df[0]), "v"(vf[0][kk]), "v"(negD));
+            else OPTSTAGE_MFMA_V(dp[kk], df[0], vf[0][kk]);
+          }
+          if (KT == 1) asm volatile("s_nop 7" ::: "memory");
+        } else {
+#pragma unroll
+          for (int kk = 0; kk < KT; ++kk) OPTSTAGE_MFMA_V(dp[kk], df[ks & 1], vf[ks & 1][kk]);
+        }
+        OPTSTAGE_SB();
+#pragma unroll
+        for (int e = 0; e < 16 / NKS; ++e) {
+          const int v = (16 / NKS) * ks + e;
+#pragma unroll
+          for (int kk = 0; kk < KT; ++kk) s[kk][v] = __builtin_amdgcn_exp2f(fmaf(s[kk][v], c, KT == 2 ? nL[v >> 2][v & 3] : nL[v >> 2][v & 3] * -LOG2E));
+        }
+      }
+      OPTSTAGE_SB();
+      bf16x8_t trf[2];                                  // dV^T += dO^T P, dS = P (dP - D) under its MFMAs (the first two cover dP's latency)
+      trf[0] = tr_frag(sDO, 0, tt, 0);
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        bf16x8_t pr[KT];
+#pragma unroll
+        for (int kk = 0; kk < KT; ++kk) pr[kk] = pack8(s[kk], u);
+#pragma unroll
+        for (int dt = 0; dt < NDT; ++dt) {
+          const int i = u * NDT + dt;
+          OPTSTAGE_SB();
+          if (i < 2 * NDT - 1) trf[(i + 1) & 1] = tr_frag(sDO, (dt + 1) % NDT, tt, dt == NDT - 1 ? 1 : u);
+          else trf[0] = tr_frag(sQ, 0, tt, 0);
+          OPTSTAGE_SB();
+#pragma unroll
+          for (int kk = 0; kk < KT; ++kk) accV[kk][dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(trf[i & 1], pr[kk], accV[kk][dt], 0, 0, 0);
+          OPTSTAGE_SB();
+          if (KT == 1 && i == 0) asm volatile("s_nop 15" ::: "memory");   // dP has left the matrix unit
+#pragma unroll
+          for (int e = 0; e < 8 / NDT; ++e) {
+            const int v = (8 / NDT) * i + e;
+#pragma unroll
+            for (int kk = 0; kk < KT; ++kk) dp[kk][v] = s[kk][v] * dp[kk][v];
+          }
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {                     // dK^T += Q^T dS
+        bf16x8_t d[KT];
+#pragma unroll
+        for (int kk = 0; kk < KT; ++kk) d[kk] = pack8(dp[kk], u);
+#pragma unroll
+        for (int dt = 0; dt < NDT; ++dt) {
+          const int i = u * NDT + dt;
+          OPTSTAGE_SB();
+          if (i < 2 * NDT - 1) trf[(i + 1) & 1] = tr_frag(sQ, (dt + 1) % NDT, tt, dt == NDT - 1 ? 1 : u);
+          OPTSTAGE_SB();
+#pragma unroll
+          for (int kk = 0; kk < KT; ++kk) accK[kk][dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(trf[i & 1], d[kk], accK[kk][dt], 0, 0, 0);
+        }
+      }
+      OPTSTAGE_SB();
+    }
+  };
+#undef OPTSTAGE_MFMA_V
+#undef OPTSTAGE_MFMA_0
+  if (it0 < it1) issue_block(it0, 0);
+  for (int it = it0; it < it1; it += 2) {
+    OPTSTAGE_BLOCK_SYNC();
+    if (it + 1 < it1) issue_block(it + 1, 1);
+    block(0);
+    if (it + 1 < it1) {
+      OPTSTAGE_BLOCK_SYNC();
+      if (it + 2 < it1) issue_block(it + 2, 0);
+      block(1);
+    }
+  }
+  if constexpr (NG == 2) {
+    __syncthreads();
+    if (grp == 1) meet_give<KT, NDT>(smem, wave, lane, accV);
+    __syncthreads();
+    if (grp == 0) meet_take<KT, NDT>(smem, wave, lane, accV);
+    __syncthreads();
+    if (grp == 1) meet_give<KT, NDT>(smem, wave, lane, accK);
+    __syncthreads();
+    if (grp == 1) return;
+    meet_take<KT, NDT>(smem, wave, lane, accK);
+  }
+  if (p.splits > 1 && it0 >= it1) return;               // the join counts the parts that have rows
+#pragma unroll
+  for (int kk = 0; kk < KT; ++kk) {
+    const int s = first_k + 32 * kk + c32;
+    if (s >= p.seq_kv) continue;
+    if (p.splits > 1) {
+      if (s >= n) continue;
+      float* out = p.part + (((size_t)part * gridDim.y + b) * p.seq_kv + s) * p.n_kv * 2 * D + (size_t)kvh * 2 * D;
+#pragma unroll
+      for (int dt = 0; dt < NDT; ++dt)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          f32x4_t rk, rv;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) { rk[i] = accK[kk][dt][4 * j + i]; rv[i] = accV[kk][dt][4 * j + i]; }
+          *reinterpret_cast<f32x4_t*>(out + 32 * dt + 8 * j + 4 * g) = rk;
+          *reinterpret_cast<f32x4_t*>(out + D + 32 * dt + 8 * j + 4 * g) = rv;
+        }
+      continue;
+    }
+    bf16_t *krow = p.dk + base + (size_t)s * p.ldkv, *vrow = p.dv + base + (size_t)s * p.ldkv;
+#pragma unroll
+    for (int dt = 0; dt < NDT; ++dt)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        OPTSTAGE_SB();
+        store4_if(krow + 32 * dt + 8 * j + 4 * g, accK[kk][dt], 4 * j, scale, s < n && n > 1);
+        store4_if(vrow + 32 * dt + 8 * j + 4 * g, accV[kk][dt], 4 * j, 1.f, s < n);
+      }
+  }
+}
+
+// dk and dv of a state and kv head from the parts' sums; a thread has 8 columns of one of them
+template <int D> __global__ __launch_bounds__(256) void cross_dkv_join(const CrossArgs p, size_t batch) {
+  constexpr int Q = 2 * D / 8;
+  const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x, per_part = batch * p.seq_kv * p.n_kv;
+  if (i / Q >= per_part) return;
+  const int col = (int)(i % Q) * 8 % D, is_v = (int)(i % Q) * 8 / D;
+  const int h = i / Q % p.n_kv;
+  const size_t row = i / Q / p.n_kv;
+  const int s = row % p.seq_kv, n = cross_states(p, (int)(row / p.seq_kv));
+  const int blocks = (p.rows + 63) / 64, per = (blocks + p.splits - 1) / p.splits;
+  float x[8] = {};
+  if (s < n && (is_v || n > 1)) {
+    for (int q = 0; q * per < blocks; ++q) {
+      const f32x4_t* f = reinterpret_cast<const f32x4_t*>(p.part + q * per_part * 2 * D + i * 8);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[e] += f[e / 4][e % 4];
+    }
+  }
+  bf16x8_t out;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) out[e] = (bf16_t)(is_v ? x[e] : x[e] * rsqrtf((float)D));
+  *reinterpret_cast<bf16x8_t*>((is_v ? p.dv : p.dk) + row * p.ldkv + (size_t)h * D + col) = out;
+}
+#undef OPTSTAGE_SB
+#undef OPTSTAGE_TILE_LOAD
+#undef OPTSTAGE_BLOCK_SYNC
+
+// ---- how a call is divided -------------------------------------------------------------------------------------------------------------
+struct CrossPlan { int waves, tiles, splits; };
+
+// forward and dQ: rows of 32 to a wave; parts of the states where the workgroups are fewer than the chip holds
+CrossPlan plan_rows(const CrossShape& c) {
+  const long rows = (long)(c.n_q / c.n_kv) * c.seq_q, groups = (long)c.n_kv * c.batch;
+  CrossPlan p;
+  p.waves = rows <= 32 ? 1 : rows <= 64 ? 2 : 4;
+  if (rows > 128 && groups * ((rows + 255) / 256) >= 448) p.waves = 8;
+  p.tiles = (int)((rows + 32 * p.waves - 1) / (32 * p.waves));
+  const long wgs = groups * p.tiles, blocks = (c.seq_kv + 63) / 64, want = p.waves == 8 ? 256 : p.waves == 4 ? 512 : 1024;
+  long splits = wgs >= want / 2 ? 1 : want / wgs;
+  splits = splits < blocks / 4 ? splits : blocks / 4;
+  p.splits = splits < 1 ? 1 : (int)splits;
+  return p;
+}
+// dK / dV: 256 states to a workgroup (heads of 128), parts of the rows
+CrossPlan plan_states(const CrossShape& c) {
+  const long rows = (long)(c.n_q / c.n_kv) * c.seq_q, groups = (long)c.n_kv * c.batch;
+  CrossPlan p;
+  p.waves = c.d == 128 && c.seq_kv > 128 ? 2 : 1;       // states of 128 a workgroup
+  const int gk = 128 * p.waves;
+  p.tiles = (c.seq_kv + gk - 1) / gk;
+  const long wgs = groups * p.tiles, blocks = (rows + 63) / 64;
+  long splits = wgs >= 192 ? 1 : 256 / wgs;
+  splits = splits < blocks / 2 ? splits : blocks / 2;
+  p.splits = splits < 1 ? 1 : (int)splits;
+  return p;
+}
+
+// the parts' sums stay below 256 MiB
+constexpr uint64_t MOST_PARTS = 256ull << 20;
+uint64_t rows_part_bytes(const CrossShape& c, int splits) { return splits > 1 ? 4ull * splits * c.batch * c.n_q * c.seq_q * (c.d + 2) : 0; }
+uint64_t states_part_bytes(const CrossShape& c, int splits) { return splits > 1 ? 4ull * splits * c.batch * c.n_kv * c.seq_kv * 2 * c.d : 0; }
+CrossPlan bounded(CrossPlan p, const CrossShape& c, uint64_t (*bytes)(const CrossShape&, int)) {
+  while (p.splits > 1 && bytes(c, p.splits) > MOST_PARTS) --p.splits;
+  return p;
+}
+
+size_t delta_floats(const CrossShape& c) { return ((size_t)c.batch * c.n_q * c.seq_q + 3) / 4 * 4; }
+
+template <int D, int NW> hipError_t run_fwd(const CrossArgs& a, const CrossPlan& pl, int batch, hipStream_t s) {
+  constexpr int smem = 4 * Head<D>::TILE;
+  static LdsAttrOnce once;
+  auto kern = cross_fwd_mfma<D, NW>;
+  if (hipError_t e = once.ensure(reinterpret_cast<const void*>(kern), smem); e != hipSuccess) return e;
+  hipLaunchKernelGGL(kern, dim3((unsigned)a.n_kv * pl.tiles * pl.splits, batch), dim3(64 * NW), smem, s, a);
+  return hipGetLastError();
+}
+template <int D, int NW> hipError_t run_dq(const CrossArgs& a, const CrossPlan& pl, int batch, hipStream_t s) {
+  constexpr int smem = 4 * Head<D>::TILE;
+  static LdsAttrOnce once;
+  auto kern = cross_dq_mfma<D, NW>;
+  if (hipError_t e = once.ensure(reinterpret_cast<const void*>(kern), smem); e != hipSuccess) return e;
+  hipLaunchKernelGGL(kern, dim3((unsigned)a.n_kv * pl.tiles * pl.splits, batch), dim3(64 * NW), smem, s, a);
+  return hipGetLastError();
+}
+template <int D, int KT, int NG> hipError_t run_dkv(const CrossArgs& a, const CrossPlan& pl, int batch, hipStream_t s) {
+  constexpr int smem = 2 * (2 * Head<D>::TILE + 512) + 2 * KT * Head<D>::TILE;
+  static LdsAttrOnce once;
+  auto kern = cross_dkv_mfma<D, KT, NG>;
+  if (hipError_t e = once.ensure(reinterpret_cast<const void*>(kern), smem); e != hipSuccess) return e;
+  hipLaunchKernelGGL(kern, dim3((unsigned)a.n_kv * pl.tiles * pl.splits, batch), dim3(256 * NG), smem, s, a);
+  return hipGetLastError();
+}
+unsigned joins(size_t items) { return (unsigned)((items + 255) / 256); }
+
+template <int D> hipError_t cross_fwd_bf16(CrossArgs a, const CrossShape& c, hipStream_t s) {
+  const CrossPlan pl = bounded(plan_rows(c), c, rows_part_bytes);
+  a.splits = pl.splits;
+  hipError_t e = pl.waves == 1   ? run_fwd<D, 1>(a, pl, c.batch, s)
+                 : pl.waves == 2 ? run_fwd<D, 2>(a, pl, c.batch, s)
+                 : pl.waves == 4 ? run_fwd<D, 4>(a, pl, c.batch, s)
+                                 : run_fwd<D, 8>(a, pl, c.batch, s);
+  if (e != hipSuccess || pl.splits == 1) return e;
+  const size_t all = (size_t)c.batch * c.n_q * c.seq_q;
+  hipLaunchKernelGGL(cross_fwd_join<D>, dim3(joins(all * (D / 8))), dim3(256), 0, s, a, all);
+  return hipGetLastError();
+}
+template <int D> hipError_t cross_bwd_bf16(CrossArgs a, const CrossShape& c, hipStream_t s) {
+  CrossPlan pl = bounded(plan_rows(c), c, rows_part_bytes);
+  a.splits = pl.splits;
+  hipError_t e = pl.waves == 1   ? run_dq<D, 1>(a, pl, c.batch, s)
+                 : pl.waves == 2 ? run_dq<D, 2>(a, pl, c.batch, s)
+                 : pl.waves == 4 ? run_dq<D, 4>(a, pl, c.batch, s)
+                                 : run_dq<D, 8>(a, pl, c.batch, s);
+  if (e != hipSuccess) return e;
+  if (pl.splits > 1) {
+    const size_t all = (size_t)c.batch * c.n_q * c.seq_q;
+    hipLaunchKernelGGL(cross_dq_join<D>, dim3(joins(all * (D / 8))), dim3(256), 0, s, a, all);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+  }
+  pl = bounded(plan_states(c), c, states_part_bytes);
+  a.splits = pl.splits;
+  if constexpr (D == 128) e = pl.waves == 2 ? run_dkv<D, 2, 1>(a, pl, c.batch, s) : run_dkv<D, 1, 2>(a, pl, c.batch, s);
+  else e = run_dkv<D, 1, 2>(a, pl, c.batch, s);
+  if (e != hipSuccess || pl.splits == 1) return e;
+  hipLaunchKernelGGL(cross_dkv_join<D>, dim3(joins((size_t)c.batch * c.seq_kv * c.n_kv * (2 * D / 8))), dim3(256), 0, s, a, (size_t)c.batch);
+  return hipGetLastError();
+}
+
+// ---- fp32 ------------------------------------------------------------------------------------------------------------------------------
 struct Cross {
   const void *q, *k, *v; const int* kv_len; const void *o_in, *dout;
   void* o; float* lse; void *dq, *dk, *dv; float* delta;
@@ -10,7 +966,7 @@ struct Cross {
   int seq_q, seq_kv, batch, n_q, n_kv;
 };
 
-__device__ __forceinline__ int states(const Cross& p, int b) { return p.kv_len ? min(max(p.kv_len[b], 0), p.seq_kv) : p.seq_kv; }
+__device__ __forceinline__ int states_f32(const Cross& p, int b) { return p.kv_len ? min(max(p.kv_len[b], 0), p.seq_kv) : p.seq_kv; }
 
 template <typename T, int D, bool BWD> __global__ __launch_bounds__(256) void cross_rows(const Cross p) {
   constexpr int E = D / 64;
@@ -19,7 +975,7 @@ template <typename T, int D, bool BWD> __global__ __launch_bounds__(256) void cr
   if (item >= (size_t)p.batch * p.n_q * p.seq_q) return;
   const int t = item % p.seq_q, a = item / p.seq_q % p.n_q, b = item / p.seq_q / p.n_q, h = a / (p.n_q / p.n_kv);
   const size_t row = (size_t)b * p.seq_q + t;
-  const int n = states(p, b);
+  const int n = states_f32(p, b);
   const float scale = rsqrtf((float)D);
   const T* q = (const T*)p.q + row * p.ldq + (size_t)a * D;
   float x[E], acc[E] = {}, g[E], m = -INFINITY, l = 0.f, dd = 0.f, L = 0.f;
@@ -57,14 +1013,14 @@ template <typename T, int D, bool BWD> __global__ __launch_bounds__(256) void cr
   if (!BWD && lane == 0) p.lse[item] = n == 0 ? -INFINITY : m + logf(l);
 }
 
-template <typename T, int D> __global__ __launch_bounds__(256) void cross_states(const Cross p) {
+template <typename T, int D> __global__ __launch_bounds__(256) void cross_state_rows(const Cross p) {
   constexpr int E = D / 64;
   const int lane = threadIdx.x & 63;
   const size_t item = (size_t)blockIdx.x * 4 + (threadIdx.x >> 6);            // (sequence, head, state)
   if (item >= (size_t)p.batch * p.n_kv * p.seq_kv) return;
   const int j = item % p.seq_kv, h = item / p.seq_kv % p.n_kv, b = item / p.seq_kv / p.n_kv;
   const size_t at = ((size_t)b * p.seq_kv + j) * p.ldkv + (size_t)h * D + lane;
-  const int n = states(p, b);
+  const int n = states_f32(p, b);
   const float scale = rsqrtf((float)D);
   float k[E], v[E], ak[E] = {}, av[E] = {};
   if (j < n) {
@@ -97,24 +1053,49 @@ template <typename T, int D> hipError_t run(const Cross& p, bool bwd, hipStream_
     return hipGetLastError();
   }
   hipLaunchKernelGGL((cross_rows<T, D, true>), dim3(g), dim3(256), 0, s, p);
-  hipLaunchKernelGGL((cross_states<T, D>), dim3(waves4((size_t)p.batch * p.n_kv * p.seq_kv)), dim3(256), 0, s, p);
+  hipLaunchKernelGGL((cross_state_rows<T, D>), dim3(waves4((size_t)p.batch * p.n_kv * p.seq_kv)), dim3(256), 0, s, p);
   return hipGetLastError();
 }
-hipError_t run_any(int dtype, int d, const Cross& p, bool bwd, hipStream_t s) {
-  if (dtype == DT_BF16) return d == 64 ? run<bf16_t, 64>(p, bwd, s) : run<bf16_t, 128>(p, bwd, s);
-  return d == 64 ? run<float, 64>(p, bwd, s) : run<float, 128>(p, bwd, s);
+
+CrossArgs cross_args(const CrossShape& c, const void* q, const void* k, const void* v, const int* kv_len, float* ws) {
+  CrossArgs a = {};
+  a.q = (const bf16_t*)q; a.k = (const bf16_t*)k; a.v = (const bf16_t*)v; a.kv_len = kv_len;
+  a.delta = ws; a.part = ws + delta_floats(c);
+  a.ldq = c.ldq; a.ldkv = c.ldkv;
+  a.seq_q = c.seq_q; a.seq_kv = c.seq_kv; a.n_q = c.n_q; a.n_kv = c.n_kv; a.rep = c.n_q / c.n_kv; a.rows = a.rep * c.seq_q; a.splits = 1;
+  a.by_seq_q = Divisor((unsigned)c.seq_q);
+  return a;
 }
 
 }  // namespace
 
-uint64_t cross_attn_ws_bytes(int, int seq_q, int, int batch, int n_q, int, int) { return 4ull * batch * n_q * seq_q; }
+uint64_t cross_attn_ws_bytes(int dtype, int seq_q, int seq_kv, int batch, int n_q, int n_kv, int d) {
+  const CrossShape c = {0, 0, seq_q, seq_kv, batch, n_q, n_kv, d};
+  uint64_t part = 0;
+  if (dtype == DT_BF16) {
+    const uint64_t r = rows_part_bytes(c, bounded(plan_rows(c), c, rows_part_bytes).splits), s = states_part_bytes(c, bounded(plan_states(c), c, states_part_bytes).splits);
+    part = r > s ? r : s;
+  }
+  return 4ull * delta_floats(c) + part;
+}
 
-hipError_t launch_cross_attn_fwd(int dtype, const CrossShape& c, const void* q, const void* k, const void* v, const int* kv_len, void* o, float* lse, void*, hipStream_t s) {
+hipError_t launch_cross_attn_fwd(int dtype, const CrossShape& c, const void* q, const void* k, const void* v, const int* kv_len, void* o, float* lse, void* ws, hipStream_t s) {
+  if (dtype == DT_BF16) {
+    CrossArgs a = cross_args(c, q, k, v, kv_len, (float*)ws);
+    a.o = (bf16_t*)o; a.lse = lse;
+    return c.d == 64 ? cross_fwd_bf16<64>(a, c, s) : cross_fwd_bf16<128>(a, c, s);
+  }
   Cross p = {q, k, v, kv_len, nullptr, nullptr, o, lse, nullptr, nullptr, nullptr, nullptr, c.ldq, c.ldkv, c.seq_q, c.seq_kv, c.batch, c.n_q, c.n_kv};
-  return run_any(dtype, c.d, p, false, s);
+  return c.d == 64 ? run<float, 64>(p, false, s) : run<float, 128>(p, false, s);
 }
 hipError_t launch_cross_attn_bwd(int dtype, const CrossShape& c, const void* q, const void* k, const void* v, const int* kv_len, const void* o, const void* dout,
                                  const float* lse, void* dq, void* dk, void* dv, void* ws, hipStream_t s) {
+  if (dtype == DT_BF16) {
+    CrossArgs a = cross_args(c, q, k, v, kv_len, (float*)ws);
+    a.o_in = (const bf16_t*)o; a.dout = (const bf16_t*)dout; a.lse = const_cast<float*>(lse);
+    a.dq = (bf16_t*)dq; a.dk = (bf16_t*)dk; a.dv = (bf16_t*)dv;
+    return c.d == 64 ? cross_bwd_bf16<64>(a, c, s) : cross_bwd_bf16<128>(a, c, s);
+  }
   Cross p = {q, k, v, kv_len, o, dout, nullptr, const_cast<float*>(lse), dq, dk, dv, (float*)ws, c.ldq, c.ldkv, c.seq_q, c.seq_kv, c.batch, c.n_q, c.n_kv};
-  return run_any(dtype, c.d, p, true, s);
+  return c.d == 64 ? run<float, 64>(p, true, s) : run<float, 128>(p, true, s);
 }

@@ -451,7 +451,7 @@ optstage_status optstage_op_rope_axes(uint32_t dtype, const void* src, uint32_t 
 // ---- cross attention ---------------------------------------------------------------------------------------
 static bool cross_shape_ok(uint32_t seq_q, uint32_t seq_kv, uint32_t batch, uint32_t n_q, uint32_t n_kv, uint32_t d) {
   return seq_q && seq_q < (1u << 24) && seq_kv && seq_kv < (1u << 24) && batch && batch < 65536 && n_kv && n_q < 65536 && n_q % n_kv == 0 && n_q &&
-         (uint64_t)batch * seq_q < (1u << 30) && (uint64_t)batch * seq_kv < (1u << 30) && (uint64_t)n_q / n_kv * seq_q < (1u << 30) && (d == 64 || d == 128);
+         (uint64_t)batch * seq_q < (1u << 30) && (uint64_t)batch * seq_kv < (1u << 30) && (uint64_t)n_q * seq_q < (1u << 29) && (uint64_t)n_kv * seq_kv < (1u << 29) && (d == 64 || d == 128);
 }
 
 uint64_t optstage_op_cross_attn_ws_bytes(uint32_t dtype, uint32_t seq_q, uint32_t seq_kv, uint32_t batch, uint32_t n_q, uint32_t n_kv, uint32_t head_dim) {
@@ -465,7 +465,7 @@ static const char* cross_attn_wrong(uint32_t dtype, const void* q, uint32_t ldq,
   if (!q || !k || !v || !ws) return "cross_attn: null operand";
   if (!(aligned16(q) && aligned16(k) && aligned16(v) && aligned16(ws) && aligned4(kv_len))) return "cross_attn: operands must be 16-byte aligned, kv_len 4";
   if (dtype > 1 || !cross_shape_ok(seq_q, seq_kv, batch, n_q, n_kv, d))
-    return "cross_attn: bad argument (head_dim is 64 or 128, n_q a multiple of n_kv, sequences below 2^24, rows below 2^30)";
+    return "cross_attn: bad argument (head_dim is 64 or 128, n_q a multiple of n_kv, sequences below 2^24, rows below 2^30, of a sequence times heads below 2^29)";
   const uint32_t vec = dtype == OPTSTAGE_BF16 ? 8 : 4;
   if (ldq < (uint64_t)n_q * d || ldkv < (uint64_t)n_kv * d || ldq % vec || ldkv % vec || ldq >= (1u << 24) || ldkv >= (1u << 24))
     return "cross_attn: row distance smaller than a row, no multiple of 8 (fp32: 4), or 2^24 and more";
@@ -493,6 +493,8 @@ optstage_status optstage_op_cross_attn_bwd(uint32_t dtype, const void* q, uint32
   REQ(!wrong, wrong);
   REQ(o && dout && lse && dq && dk && dv, "cross_attn_bwd: null operand");
   REQ(aligned16(o) && aligned16(dout) && aligned4(lse) && aligned16(dq) && aligned16(dk) && aligned16(dv), "cross_attn_bwd: operands must be 16-byte aligned, lse 4");
+  REQ(dtype != OPTSTAGE_BF16 || ((uint64_t)seq_q * ldq < (15ull << 27) && (uint64_t)seq_q * n_q * head_dim < (15ull << 27)),
+      "cross_attn_bwd: a sequence's rows of q and of dout must span less than 15 * 2^28 bytes");
   const void* in[] = {q, k, v, o, dout, lse};
   for (const void* p : in) REQ(dq != p && dk != p && dv != p, "cross_attn_bwd: dq, dk and dv must be buffers of their own");
   REQ(dq != dk && dq != dv && dk != dv, "cross_attn_bwd: dq, dk and dv must be buffers of their own");
