@@ -205,7 +205,7 @@ optstage_status optstage_op_cross_attn_fwd(uint32_t dtype, const void* q, uint32
                                            float* lse, void* ws, uint64_t ws_bytes, uint32_t seq_q, uint32_t seq_kv, uint32_t batch, uint32_t n_q, uint32_t n_kv,
                                            uint32_t head_dim, void* stream);
 /* dq like q (rows ldq apart), dk and dv like k and v (rows ldkv apart), every row written, buffers of their own.  o and lse are the forward pass's.  bf16: a sequence's rows
- * of q, and of dout, span less than 15 * 2^28 bytes.  A sequence of one state has no gradient of its scores: dq and dk are 0. */
+ * of q, and of dout, and 64 more span less than 15 * 2^28 bytes.  A sequence of one state has no gradient of its scores: dq and dk are 0. */
 optstage_status optstage_op_cross_attn_bwd(uint32_t dtype, const void* q, uint32_t ldq, const void* k, const void* v, uint32_t ldkv, const int32_t* kv_len, const void* o,
                                            const void* dout, const float* lse, void* dq, void* dk, void* dv, void* ws, uint64_t ws_bytes, uint32_t seq_q,
                                            uint32_t seq_kv, uint32_t batch, uint32_t n_q, uint32_t n_kv, uint32_t head_dim, void* stream);

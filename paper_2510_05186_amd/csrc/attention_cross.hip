@@ -22,6 +22,7 @@ struct CrossArgs {
   bf16_t* o; float* lse; bf16_t *dq, *dk, *dv; float *delta, *part;
   size_t ldq, ldkv;
   int seq_q, seq_kv, n_q, n_kv, rep, rows, splits;     // rows = rep seq_q, the rows of a kv head; splits: parts of the states (forward, dQ) or of the rows (dK / dV)
+  int block_heads, blocks_per_head, row_blocks;         // of the rows, in the dK / dV kernel
   Divisor by_seq_q;
 };
 
@@ -559,6 +560,19 @@ template <int D> __global__ __launch_bounds__(256) void cross_dq_join(const Cros
   *reinterpret_cast<bf16x8_t*>(p.dq + (b * p.seq_q + t) * p.ldq + a * D + col) = out;
 }
 
+// Blocks of up to 64 rows of a kv head: 64 queries of one head, or, of shorter sequences, as many whole heads (a divisor of theirs) as fit: then a
+// block's lanes differ from the next one's by one distance, and no block holds rows of a third kind.
+struct RowBlocks { int heads, per_head, all; };
+__host__ __device__ __forceinline__ RowBlocks row_blocks(int seq_q, int rep) {
+  if (seq_q >= 64) return {1, (seq_q + 63) / 64, rep * ((seq_q + 63) / 64)};
+  int heads = 64 / seq_q < rep ? 64 / seq_q : rep;
+  while (rep % heads) --heads;
+  return {heads, 1, rep / heads};
+}
+__device__ __forceinline__ RowBlocks row_blocks(const CrossArgs& p) { return {p.block_heads, p.blocks_per_head, p.row_blocks}; }
+// an offset past every descriptor's end, whatever is added to it for a block: rows span less than 15 * 2^28 bytes
+constexpr unsigned PAST = 0xF0000000u;
+
 // ---- backward, dK / dV: grid (n_kv x splits x tiles of 128 KT states, batch), 4 NG waves --------------------------------------------------
 // A wave owns 32 KT states: K fragments, dK^T and dV^T in registers, the V rows of the workgroup's states in LDS.  Blocks of 64 rows (Q and dO, lse and -D) stream through
 // two stages; rows past the last one read as zeros and add nothing.  NG = 2: a second group of waves takes the other 32 rows of every block, and the first adds its sums.
@@ -635,23 +649,32 @@ __global__ __launch_bounds__(256 * NG) void cross_dkv_mfma(const CrossArgs p) {
       OPTSTAGE_TILE_LOAD((unsigned)(lds0 + 2 * STAGE + wave * WK * ROWB + j * 1024), (unsigned)lr * (unsigned)p.ldkv * 2u + (unsigned)((lane % H::CH) ^ H::swz(lr)) * 16u, rs_v);
     }
   }
-  const int blocks = (p.rows + 63) / 64, per = (blocks + p.splits - 1) / p.splits, it0 = min(blocks, part * per), it1 = min(blocks, it0 + per);
+  // what a lane loads of a block lies where it lay in the block before, but for the same distance for all
+  const RowBlocks rb = row_blocks(p);
+  unsigned voff_q[NLD], voff_do[NLD];
+#pragma unroll
+  for (int j = 0; j < NLD; ++j) {
+    const int lr = WROWS * id + H::RPL * j + lane / H::CH, hl = p.seq_q < 64 ? lr / p.seq_q : 0, t = lr - hl * p.seq_q;
+    const unsigned at = (unsigned)hl * ROWB + (unsigned)((lane % H::CH) ^ H::swz(lr)) * 16u;
+    voff_q[j] = hl < rb.heads ? (unsigned)t * (unsigned)p.ldq * 2u + at : PAST;
+    voff_do[j] = hl < rb.heads ? (unsigned)t * (unsigned)p.n_q * ROWB + at : PAST;
+  }
+  const int per = (rb.all + p.splits - 1) / p.splits, it0 = min(rb.all, part * per), it1 = min(rb.all, it0 + per);
   auto issue_block = [&](int it, int stage) {
+    const int head = p.seq_q < 64 ? it * rb.heads : it / rb.per_head, r0 = p.seq_q < 64 ? 0 : 64 * (it - head * rb.per_head);
+    const unsigned oq = (unsigned)r0 * (unsigned)p.ldq * 2u + (unsigned)head * ROWB, od = ((unsigned)r0 * (unsigned)p.n_q + (unsigned)head) * ROWB;
     const unsigned dst = (unsigned)lds0 + stage * STAGE + (WROWS * id) * ROWB;
 #pragma unroll
     for (int j = 0; j < NLD; ++j) {
-      const int lr = WROWS * id + H::RPL * j + lane / H::CH, row = 64 * it + lr;
-      const unsigned chunk = (unsigned)((lane % H::CH) ^ H::swz(lr)) * 16u;
-      const unsigned head = p.by_seq_q.quotient(row), t = row - head * p.seq_q;
-      // a row past the last one: an offset past any end
-      const unsigned oq = row < p.rows ? t * ((unsigned)p.ldq * 2u) + head * ROWB + chunk : 0xFFFFFFF0u;
-      const unsigned od = row < p.rows ? t * ((unsigned)p.n_q * ROWB) + head * ROWB + chunk : 0xFFFFFFF0u;
-      OPTSTAGE_TILE_LOAD(dst + j * 1024, oq, rs_q);
-      OPTSTAGE_TILE_LOAD(dst + TILE + j * 1024, od, rs_do);
+      OPTSTAGE_TILE_LOAD(dst + j * 1024, voff_q[j] + oq, rs_q);
+      OPTSTAGE_TILE_LOAD(dst + TILE + j * 1024, voff_do[j] + od, rs_do);
     }
-    if (id < 2)                                         // wave 0: lse of the 64 rows, wave 1: -D
+    if (id < 2) {                                       // wave 0: lse of the block's rows, wave 1: -D; 0 where there is no row
+      const bool on = p.seq_q < 64 ? lane < rb.heads * p.seq_q : r0 + lane < p.seq_q;
+      const unsigned vo = on ? ((unsigned)head * (unsigned)p.seq_q + (unsigned)(r0 + lane)) * 4u : 0xFFFFFFF0u;
       asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds"
-                   :: "s"((unsigned)lds0 + stage * STAGE + 2 * TILE + id * 256), "v"((unsigned)(64 * it + lane) * 4u), "s"(id == 0 ? rs_l : rs_d) : "memory", "m0");
+                   :: "s"((unsigned)lds0 + stage * STAGE + 2 * TILE + id * 256), "v"(vo), "s"(id == 0 ? rs_l : rs_d) : "memory", "m0");
+    }
   };
   auto tr_frag = [&](int at, int dt, int tt, int u) {
     return transposed8(tr_addr[dt][0] + at + (32 * tt + 16 * u) * ROWB, tr_addr[dt][1] + at + (32 * tt + 16 * u + 8) * ROWB);
@@ -659,10 +682,12 @@ __global__ __launch_bounds__(256 * NG) void cross_dkv_mfma(const CrossArgs p) {
   auto rm_frag = [&](int at, int tt, int ks) { return *(const lds_bf16x8_t*)(unsigned)(rm_addr[ks] + at + tt * 32 * ROWB); };
 #define OPTSTAGE_MFMA_V(acc, a, b) asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+v"(acc) : "v"(a), "v"(b))
 #define OPTSTAGE_MFMA_0(acc, a, b) asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, 0" : "=&v"(acc) : "v"(a), "v"(b))
-  auto block = [&](int stage) __attribute__((always_inline)) {
+  auto block = [&](int it, int stage) __attribute__((always_inline)) {
+    const int rows = p.seq_q < 64 ? rb.heads * p.seq_q : p.seq_q - 64 * (it % rb.per_head);
     const int sQ = stage * STAGE, sDO = sQ + TILE, sL = sQ + 2 * TILE, sD = sL + 256;
 #pragma unroll
     for (int tt = 0; tt < 2 / NG; ++tt) {
+      if (half + 32 * tt >= rows) continue;             // the same for the whole wave: no rows in this half of the block
       f32x16_t s[KT], dp[KT];                           // lane = state, registers = rows 32 tt + 8 (v / 4) + 4 g + v % 4 of the block
       f32x4_t nL[4];
       f32x16_t negD;
@@ -780,11 +805,11 @@ __global__ __launch_bounds__(256 * NG) void cross_dkv_mfma(const CrossArgs p) {
   for (int it = it0; it < it1; it += 2) {
     OPTSTAGE_BLOCK_SYNC();
     if (it + 1 < it1) issue_block(it + 1, 1);
-    block(0);
+    block(it, 0);
     if (it + 1 < it1) {
       OPTSTAGE_BLOCK_SYNC();
       if (it + 2 < it1) issue_block(it + 2, 0);
-      block(1);
+      block(it + 1, 1);
     }
   }
   if constexpr (NG == 2) {
@@ -839,7 +864,7 @@ template <int D> __global__ __launch_bounds__(256) void cross_dkv_join(const Cro
   const int h = i / Q % p.n_kv;
   const size_t row = i / Q / p.n_kv;
   const int s = row % p.seq_kv, n = cross_states(p, (int)(row / p.seq_kv));
-  const int blocks = (p.rows + 63) / 64, per = (blocks + p.splits - 1) / p.splits;
+  const int blocks = p.row_blocks, per = (blocks + p.splits - 1) / p.splits;
   float x[8] = {};
   if (s < n && (is_v || n > 1)) {
     for (int q = 0; q * per < blocks; ++q) {
@@ -875,12 +900,12 @@ CrossPlan plan_rows(const CrossShape& c) {
 }
 // dK / dV: 256 states to a workgroup (heads of 128), parts of the rows
 CrossPlan plan_states(const CrossShape& c) {
-  const long rows = (long)(c.n_q / c.n_kv) * c.seq_q, groups = (long)c.n_kv * c.batch;
+  const long groups = (long)c.n_kv * c.batch;
   CrossPlan p;
   p.waves = c.d == 128 && c.seq_kv > 128 ? 2 : 1;       // states of 128 a workgroup
   const int gk = 128 * p.waves;
   p.tiles = (c.seq_kv + gk - 1) / gk;
-  const long wgs = groups * p.tiles, blocks = (rows + 63) / 64;
+  const long wgs = groups * p.tiles, blocks = row_blocks(c.seq_q, c.n_q / c.n_kv).all;
   long splits = wgs >= 192 ? 1 : 256 / wgs;
   splits = splits < blocks / 2 ? splits : blocks / 2;
   p.splits = splits < 1 ? 1 : (int)splits;
@@ -1063,6 +1088,8 @@ CrossArgs cross_args(const CrossShape& c, const void* q, const void* k, const vo
   a.delta = ws; a.part = ws + delta_floats(c);
   a.ldq = c.ldq; a.ldkv = c.ldkv;
   a.seq_q = c.seq_q; a.seq_kv = c.seq_kv; a.n_q = c.n_q; a.n_kv = c.n_kv; a.rep = c.n_q / c.n_kv; a.rows = a.rep * c.seq_q; a.splits = 1;
+  const RowBlocks rb = row_blocks(c.seq_q, a.rep);
+  a.block_heads = rb.heads; a.blocks_per_head = rb.per_head; a.row_blocks = rb.all;
   a.by_seq_q = Divisor((unsigned)c.seq_q);
   return a;
 }

@@ -493,8 +493,8 @@ optstage_status optstage_op_cross_attn_bwd(uint32_t dtype, const void* q, uint32
   REQ(!wrong, wrong);
   REQ(o && dout && lse && dq && dk && dv, "cross_attn_bwd: null operand");
   REQ(aligned16(o) && aligned16(dout) && aligned4(lse) && aligned16(dq) && aligned16(dk) && aligned16(dv), "cross_attn_bwd: operands must be 16-byte aligned, lse 4");
-  REQ(dtype != OPTSTAGE_BF16 || ((uint64_t)seq_q * ldq < (15ull << 27) && (uint64_t)seq_q * n_q * head_dim < (15ull << 27)),
-      "cross_attn_bwd: a sequence's rows of q and of dout must span less than 15 * 2^28 bytes");
+  REQ(dtype != OPTSTAGE_BF16 || ((seq_q + 64ull) * ldq < (15ull << 27) && (seq_q + 64ull) * n_q * head_dim < (15ull << 27)),
+      "cross_attn_bwd: a sequence's rows of q and of dout, and 64 more, must span less than 15 * 2^28 bytes");
   const void* in[] = {q, k, v, o, dout, lse};
   for (const void* p : in) REQ(dq != p && dk != p && dv != p, "cross_attn_bwd: dq, dk and dv must be buffers of their own");
   REQ(dq != dk && dq != dv && dk != dv, "cross_attn_bwd: dq, dk and dv must be buffers of their own");
