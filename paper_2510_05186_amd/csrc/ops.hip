@@ -514,7 +514,7 @@ static const char* distill_wrong(uint32_t dtype, const void* z, uint32_t ldz, co
   if (!z || !ids || !teacher) return "distill: null operand";
   if (!(aligned16(z) && aligned4(ids) && aligned4(teacher))) return "distill: z must be 16-byte aligned, ids and teacher 4";
   if (dtype > 1 || log_probs > 1 || !distill_shape_ok(rows, vocab, k) || ldz < vocab) return "distill: bad argument (k is 1 to 1024, ldz at least vocab)";
-  if (!(temperature > 0.f && temperature <= 3.402823466e38f && 1.f / temperature <= 3.402823466e38f)) return "distill: temperature must be positive and finite";
+  if (!(temperature >= 1e-30f && temperature <= 1e30f)) return "distill: temperature must lie between 1e-30 and 1e30";
   return nullptr;
 }
 static const char* distill_dz_wrong(const void* z, uint32_t ldz, const float* dloss, const void* dz, uint32_t lddz, uint32_t vocab) {
