@@ -3,7 +3,10 @@
 // for the gradient g of the row's loss.  Bound by memory: a row of logits in, a row of their gradient out; what is done with a teacher's entries (64 bits,
 // one wave) runs while the row's loads are in flight.
 //
-// A row's maximum and sum are one pass: every thread keeps m and s = sum of exp((z - m) / T) of what it has seen, 16 bytes of the row at a time.
+// A row's reference and sum are one pass: every wave keeps m, the largest of its first 16 bytes a lane, and s = sum of exp((z - m) / T).  Where a later logit lies so far
+// above m that s overflows, or nothing but the lowest values is left of a row, the row (its piece) is summed again with the running maximum.
+// A logit costs a conversion, a multiply-add, an exponential and an addition in each direction, half of what the running maximum would: at 4096 rows of 131072 words
+// the vector units are busy half of the time that memory takes.
 //  * Both directions, rows enough for the chip: a workgroup has a row in its registers from the maximum to the gradient (up to 128K words of bf16; of longer
 //    ones the rest is read a second time).
 //  * Rows too few for that: a row in pieces, a launch for their m and s, a second one that joins them and writes the gradient.
@@ -21,6 +24,10 @@ template <typename T> struct Any16;
 template <> struct Any16<bf16_t> { typedef bf16_t t __attribute__((ext_vector_type(8), aligned(2))); };
 template <> struct Any16<float> { typedef float t __attribute__((ext_vector_type(4), aligned(4))); };
 
+// what a row's entries make of its loss: sum + mass (log of the sum of exp(z / T) - z0 / T), with sum = sum of t (log t - (z - z0) / T), mass = sum of t and z0 one of
+// their own logits, so that nothing large cancels
+struct Teacher { double sum, mass, z0; };
+
 struct Distill {
   const void* z; const int* ids; const float* teacher; const float* dloss;
   float* loss; float* lse; void* dz;
@@ -29,10 +36,10 @@ struct Distill {
   float inv_t, c;                                       // 1 / T, log2(e) / T
   int log_probs;
   int pieces, piece;                                    // of a row, and elements of one (a multiple of a chunk)
-  float2* stats; double2* parts;                        // [rows][pieces]: m, s; [rows]: sum of t (log t - z / T), sum of t
+  float2* stats; Teacher* parts;                        // [rows][pieces]: m, s; [rows]
 };
 
-// m and s of what a thread has seen.  m starts at a finite number: minus infinity (a masked word) lies below it and adds nothing.
+// m and s of what a thread has seen, m a running maximum.  It starts at a finite number: minus infinity (a masked word) lies below it and adds nothing.
 struct Running {
   float m = LOWEST, s = 0.f;
   template <int N> __device__ __forceinline__ void add(const float (&x)[N], float c) {
@@ -55,13 +62,41 @@ struct Running {
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) join(__shfl_xor(m, o, 64), __shfl_xor(s, o, 64), c);
   }
+  // m c as one number, and what that rounding left out: exp2((x - m) c) = exp2(x c - reference) * rest
+  __device__ __forceinline__ float reference(float c) const { return m * c; }
+  __device__ __forceinline__ float rest(float c) const { return __builtin_amdgcn_exp2f(fmaf(-m, c, m * c)); }
+  // whether the sum holds, and x c stays finite
+  __device__ __forceinline__ bool sound(float c) const { return s > 0.f && s < INFINITY && fabsf(m * c) < 1e38f; }
 };
+// The same against a reference that a wave has taken from its first chunks.
+struct Quick {
+  float m, mc, s;
+  __device__ __forceinline__ Quick(float reference, float c) : m(reference), mc(reference * c), s(0.f) {}
+  template <int N> __device__ __forceinline__ void add(const float (&x)[N], float c) {
+    float t = 0.f;
+#pragma unroll
+    for (int e = 0; e < N; ++e) t += __builtin_amdgcn_exp2f(fmaf(x[e], c, -mc));
+    s += t;
+  }
+  __device__ __forceinline__ Running end(float c) const {
+    Running r;
+    r.m = m;
+    r.s = s * __builtin_amdgcn_exp2f(fmaf(-m, c, mc));
+    return r;
+  }
+};
+template <int N> __device__ __forceinline__ float wave_reference(const float (&x)[N]) {
+  float most = x[0];
+#pragma unroll
+  for (int e = 1; e < N; ++e) most = fmaxf(most, x[e]);
+  return wave_max(most);
+}
 
 // the row's entries, for the whole workgroup
 struct Entries {
   int id[MAX_K];
   float t[MAX_K], z[MAX_K];
-  double sum, mass;                                     // sum of t (log t - z / T), sum of t
+  Teacher all;
 };
 struct Shared {
   Entries e;
@@ -80,41 +115,49 @@ template <typename T> __device__ __forceinline__ void read_entries(const Distill
   const int* ids = p.ids + row * p.k;
   const float* teacher = p.teacher + row * p.k;
   const T* z = (const T*)p.z + row * p.ldz;
-  float most = -INFINITY;
+  float most = -INFINITY, z0 = -INFINITY;
+#pragma unroll 1
   for (int j = lane; j < p.k; j += 64) {
     const int id = ids[j];
     const bool on = (unsigned)id < (unsigned)p.vocab;
     const float a = on ? (p.log_probs ? teacher[j] : teacher[j] * p.inv_t) : -INFINITY;
     e.id[j] = on ? id : -1;
     e.t[j] = a;
-    e.z[j] = on ? (float)z[id] : 0.f;
+    const float x = on ? (float)z[id] : -INFINITY;
+    e.z[j] = x;
     most = fmaxf(most, a);
+    z0 = fmaxf(z0, x);
   }
   most = wave_max(most);
+  z0 = wave_max(z0);
+  if (!(fabsf(z0) < INFINITY)) z0 = 0.f;
   const double shift = p.log_probs || most == -INFINITY ? 0.0 : (double)most;
   double norm = 1.0;
   if (!p.log_probs) {
     norm = 0.0;
+#pragma unroll 1
     for (int j = lane; j < p.k; j += 64) norm += exp((double)e.t[j] - shift);
     norm = wave_sum64(norm);
     if (norm == 0.0) norm = 1.0;                        // no entries
   }
   const double log_norm = shift + log(norm);
   double sum = 0.0, mass = 0.0;
+#pragma unroll 1
   for (int j = lane; j < p.k; j += 64) {
     const double lt = (double)e.t[j] - log_norm, t = exp(lt);
-    if (t != 0.0) sum += t * (lt - (double)e.z[j] * (double)p.inv_t);
+    if (t != 0.0) sum += t * (lt - ((double)e.z[j] - (double)z0) * (double)p.inv_t);
     mass += t;
     e.t[j] = (float)t;
   }
   sum = wave_sum64(sum);
   mass = wave_sum64(mass);
-  if (lane == 0) { e.sum = sum; e.mass = mass; }
+  if (lane == 0) e.all = {sum, mass, z0};
 }
 
 // the gradient at entry j's word, t being all that the row's entries give it
 __device__ __forceinline__ float teacher_at(const Entries& e, int k, int id) {
   float t = 0.f;
+#pragma unroll 4
   for (int i = 0; i < k; ++i) t += e.id[i] == id ? e.t[i] : 0.f;
   return t;
 }
@@ -154,73 +197,132 @@ template <int NT> __device__ __forceinline__ Running join_group(Running r, Share
   for (int w = 0; w < NT / 64; ++w) all.join(sh.m[w], sh.s[w], c);
   return all;
 }
-__device__ __forceinline__ double log_total(const Distill& p, const Running& r) { return (double)r.m * (double)p.inv_t + log((double)r.s); }
+// loss and lse of a row
+__device__ __forceinline__ void finish(const Distill& p, size_t row, const Running& r, const Teacher& t) {
+  const double log_s = log((double)r.s);
+  p.lse[row] = (float)((double)r.m * (double)p.inv_t + log_s);
+  p.loss[row] = (float)(t.mass == 0.0 ? 0.0 : t.sum + t.mass * (((double)r.m - t.z0) * (double)p.inv_t + log_s));
+}
 
-// ---- a row in a workgroup's registers: R chunks a thread
-template <typename T, int NT, int R> __global__ __launch_bounds__(NT) void distill_row(const Distill p) {
-  constexpr int N = Vec16<T>::N, STEP = NT * N, HELD = R * STEP;
-  __shared__ Shared sh;
-  const size_t row = blockIdx.x;
-  const T* z = (const T*)p.z + row * p.ldz;
-  T* dz = (T*)p.dz + row * p.lddz;
-  const int first = threadIdx.x * N;
-  typename Any16<T>::t held[R];
-#pragma unroll
-  for (int r = 0; r < R; ++r) {
-    const int at = first + r * STEP;
-    if (at + N <= p.vocab) held[r] = *reinterpret_cast<const typename Any16<T>::t*>(z + at);
-    else
-#pragma unroll
-      for (int e = 0; e < N; ++e) held[r][e] = at + e < p.vocab ? z[at + e] : (T)-INFINITY;
-  }
-  if (threadIdx.x < 64) read_entries<T>(p, row, sh.e);
-  Running run;
-#pragma unroll
-  for (int r = 0; r < R; ++r) {
-    if (r * STEP >= p.vocab) break;
-    float x[N];
-#pragma unroll
-    for (int e = 0; e < N; ++e) x[e] = (float)held[r][e];
-    run.add(x, p.c);
-  }
-  for (int at = HELD + first; at < p.vocab; at += STEP) {
-    float x[N];
-    load_chunk(z, at, p.vocab, x);
-    run.add(x, p.c);
-  }
-  const Running all = join_group<NT>(run, sh, p.c);
-  const double mass = sh.e.mass;
-  if (threadIdx.x == 0) {
-    const double lse = log_total(p, all);
-    p.lse[row] = (float)lse;
-    p.loss[row] = (float)(mass == 0.0 ? 0.0 : sh.e.sum + mass * lse);
-  }
-  const float w = p.dloss[row] * p.inv_t;
-  const bool none = w == 0.f || mass == 0.0;
-  const float f = none ? 0.f : w * (float)mass / all.s;
-  auto give = [&](int at, float (&x)[N]) {
-#pragma unroll
-    for (int e = 0; e < N; ++e) x[e] = none ? 0.f : f * __builtin_amdgcn_exp2f((x[e] - all.m) * p.c);
-    store_chunk(dz, at, p.vocab, x);
-  };
-#pragma unroll
-  for (int r = 0; r < R; ++r) {
-    if (r * STEP >= p.vocab) break;
-    float x[N];
-#pragma unroll
-    for (int e = 0; e < N; ++e) x[e] = (float)held[r][e];
-    give(first + r * STEP, x);
-  }
-  for (int at = HELD + first; at < p.vocab; at += STEP) {
-    float x[N];
-    load_chunk(z, at, p.vocab, x);
-    give(at, x);
-  }
-  if (none) return;
+// a piece of a row summed again by the running maximum
+template <typename T, int NT> __device__ __forceinline__ Running sum_again(const Distill& p, const T* z, int begin, int end, Shared& sh) {
   __syncthreads();
-  for (int j = threadIdx.x; j < p.k; j += NT) {
-    const int id = sh.e.id[j];
-    if (id >= 0) dz[id] = (T)(f * __builtin_amdgcn_exp2f((sh.e.z[j] - all.m) * p.c) - w * teacher_at(sh.e, p.k, id));
+  Running run;
+#pragma unroll 1
+  for (int at = begin + (int)threadIdx.x * Vec16<T>::N; at < end; at += NT * Vec16<T>::N) {
+    float x[Vec16<T>::N];
+    load_chunk(z, at, end, x);
+    run.add(x, p.c);
+  }
+  return join_group<NT>(run, sh, p.c);
+}
+
+// ---- rows in a workgroup's registers, R chunks a thread, one row after the other: a chunk that has been written makes room for the next row's, so that the memory
+// system has that row's loads while it takes this row's gradient (one workgroup of 16 waves fills a compute unit: nothing else would).
+// (R - 2) NT chunks are less than a row: all steps but the last two are whole, and no step is behind a branch (held would be copied around it).  Chunks of those two
+// that would cross the row's end start N before it: their elements below `at` are another chunk's and are masked.  vocab >= N.
+template <typename T, int NT, int R> __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(4))) void distill_rows(const Distill p) {
+  constexpr int N = Vec16<T>::N, STEP = NT * N, HELD = R * STEP;
+  typedef typename Any16<T>::t chunk_t;
+  typedef unsigned u32x4_t __attribute__((ext_vector_type(4)));
+  __shared__ Entries entries[2];
+  __shared__ Shared sh;
+  const int first = threadIdx.x * N, last = p.vocab - N;
+  auto fetch = [&](const T* z, int step) {
+    const unsigned at = step < R - 2 ? (unsigned)first : (unsigned)min(first + step * STEP, last);
+    return *reinterpret_cast<const chunk_t*>(z + (step < R - 2 ? step * STEP : 0) + at);
+  };
+  auto values = [&](const chunk_t& v, int step, float (&x)[N]) {
+#pragma unroll
+    for (int e = 0; e < N; ++e) x[e] = (float)v[e];
+    if (step >= R - 2) {
+      const int over = first + step * STEP - last;      // elements that are another chunk's
+#pragma unroll
+      for (int e = 0; e < N; ++e) x[e] = e < over ? -INFINITY : x[e];
+    }
+  };
+  u32x4_t held[R];
+#pragma unroll
+  for (int r = 0; r < R; ++r) held[r] = __builtin_bit_cast(u32x4_t, fetch((const T*)p.z + blockIdx.x * p.ldz, r));
+  int turn = 0;
+#pragma unroll 1
+  for (size_t row = blockIdx.x; row < (size_t)p.rows; row += gridDim.x, turn ^= 1) {
+    const T* z = (const T*)p.z + row * p.ldz;
+    T* dz = (T*)p.dz + row * p.lddz;
+    const T* zn = (const T*)p.z + (row + gridDim.x < (size_t)p.rows ? row + gridDim.x : row) * p.ldz;
+    Entries& en = entries[turn];
+    if (threadIdx.x < 64) read_entries<T>(p, row, en);
+    Running part;
+    {
+      float x[N];
+      values(__builtin_bit_cast(chunk_t, held[0]), 0, x);
+      const float m = wave_reference(x);
+      if (m > LOWEST) {
+        Quick run(m, p.c);
+        run.add(x, p.c);
+#pragma unroll
+        for (int r = 1; r < R; ++r) {
+          values(__builtin_bit_cast(chunk_t, held[r]), r, x);
+          run.add(x, p.c);
+        }
+#pragma unroll 1
+        for (int step = R; step * STEP < p.vocab; ++step) {
+          values(fetch(z, step), step, x);
+          run.add(x, p.c);
+        }
+        part = run.end(p.c);
+      } else {                                          // nothing to refer to: the running maximum, over the wave's chunks
+#pragma unroll 1
+        for (int at = first; at < p.vocab; at += STEP) {
+          load_chunk(z, at, p.vocab, x);
+          part.add(x, p.c);
+        }
+      }
+    }
+#pragma unroll
+    for (int r = 0; r < R; ++r) asm volatile("" : "+v"(held[r]));   // kept as they came: their values in 32 bits would take twice the registers
+    Running all = join_group<NT>(part, sh, p.c);
+    if (!all.sound(p.c)) all = sum_again<T, NT>(p, z, 0, p.vocab, sh);
+    const double mass = en.all.mass;
+    if (threadIdx.x == 0) finish(p, row, all, en.all);
+    const float w = p.dloss[row] * p.inv_t;
+    const bool none = w == 0.f || mass == 0.0;
+    const bool sound = all.sound(p.c);
+    const float f = none ? 0.f : w * (float)mass / all.s, fr = sound ? f * all.rest(p.c) : f, mc = all.reference(p.c);
+    if (!sound) {
+#pragma unroll 1
+      for (int at = first; at < p.vocab; at += STEP) {
+        float x[N];
+        load_chunk(z, at, p.vocab, x);
+#pragma unroll
+        for (int e = 0; e < N; ++e) x[e] = none ? 0.f : f * __builtin_amdgcn_exp2f((x[e] - all.m) * p.c);
+        store_chunk(dz, at, p.vocab, x);
+      }
+    }
+    auto give = [&](chunk_t v, int step) {
+#pragma unroll
+      for (int e = 0; e < N; ++e) v[e] = (T)(fr * __builtin_amdgcn_exp2f(fmaf((float)v[e], p.c, -mc)));
+      const int over = step < R - 2 ? 0 : first + step * STEP - last;
+      if (!sound || over >= N) return;
+      if (over <= 0) *reinterpret_cast<chunk_t*>(dz + step * STEP + (unsigned)first) = v;
+      else
+#pragma unroll
+        for (int e = 0; e < N; ++e)
+          if (e >= over) dz[last + e] = v[e];
+    };
+#pragma unroll 1
+    for (int step = R; step * STEP < p.vocab; ++step) give(fetch(z, step), step);
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      give(__builtin_bit_cast(chunk_t, held[r]), r);
+      held[r] = __builtin_bit_cast(u32x4_t, fetch(zn, r));
+    }
+    __syncthreads();
+    if (!none)
+      for (int j = threadIdx.x; j < p.k; j += NT) {
+        const int id = en.id[j];
+        if (id >= 0) dz[id] = (T)(f * __builtin_amdgcn_exp2f((en.z[j] - all.m) * p.c) - w * teacher_at(en, p.k, id));
+      }
   }
 }
 
@@ -232,35 +334,44 @@ template <typename T, int NT> __global__ __launch_bounds__(NT) void distill_stat
   const int piece = blockIdx.x % p.pieces, begin = piece * p.piece, end = min(p.vocab, begin + p.piece);
   const T* z = (const T*)p.z + row * p.ldz;
   if (piece == 0 && threadIdx.x < 64) read_entries<T>(p, row, sh.e);
-  Running run;
   int at = begin + threadIdx.x * N;
-  for (; at + (U - 1) * STEP + N <= end; at += U * STEP) {
-    typename Any16<T>::t v[U];
+  float x[N];
+  load_chunk(z, at, end, x);
+  const float m = wave_reference(x);
+  Running part;
+  if (m > LOWEST) {
+    Quick run(m, p.c);
+    for (; at + (U - 1) * STEP + N <= end; at += U * STEP) {
+      typename Any16<T>::t v[U];
 #pragma unroll
-    for (int u = 0; u < U; ++u) v[u] = *reinterpret_cast<const typename Any16<T>::t*>(z + at + u * STEP);
+      for (int u = 0; u < U; ++u) v[u] = *reinterpret_cast<const typename Any16<T>::t*>(z + at + u * STEP);
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      float x[N];
+      for (int u = 0; u < U; ++u) {
 #pragma unroll
-      for (int e = 0; e < N; ++e) x[e] = (float)v[u][e];
+        for (int e = 0; e < N; ++e) x[e] = (float)v[u][e];
+        run.add(x, p.c);
+      }
+    }
+    for (; at < end; at += STEP) {
+      load_chunk(z, at, end, x);
       run.add(x, p.c);
     }
+    part = run.end(p.c);
+  } else {
+    for (; at < end; at += STEP) {
+      load_chunk(z, at, end, x);
+      part.add(x, p.c);
+    }
   }
-  for (; at < end; at += STEP) {
-    float x[N];
-    load_chunk(z, at, end, x);
-    run.add(x, p.c);
-  }
-  const Running all = join_group<NT>(run, sh, p.c);
+  Running all = join_group<NT>(part, sh, p.c);
+  if (!all.sound(p.c)) all = sum_again<T, NT>(p, z, begin, end, sh);
   if (threadIdx.x) return;
   if (p.dz || p.pieces > 1) {                            // joined by the next launch
     p.stats[blockIdx.x] = make_float2(all.m, all.s);
-    if (piece == 0) p.parts[row] = make_double2(sh.e.sum, sh.e.mass);
+    if (piece == 0) p.parts[row] = sh.e.all;
     return;
   }
-  const double lse = log_total(p, all);
-  p.lse[row] = (float)lse;
-  p.loss[row] = (float)(sh.e.mass == 0.0 ? 0.0 : sh.e.sum + sh.e.mass * lse);
+  finish(p, row, all, sh.e.all);
 }
 
 // m and s of a row from its pieces, in the same order for every reader: one wave
@@ -273,17 +384,11 @@ __device__ __forceinline__ Running join_pieces(const Distill& p, size_t row) {
   r.join_wave(p.c);
   return r;
 }
-__device__ __forceinline__ void finish(const Distill& p, size_t row, const Running& r) {
-  const double2 part = p.parts[row];
-  const double lse = log_total(p, r);
-  p.lse[row] = (float)lse;
-  p.loss[row] = (float)(part.y == 0.0 ? 0.0 : part.x + part.y * lse);
-}
 __global__ __launch_bounds__(256) void distill_finish(const Distill p) {
   const size_t row = (size_t)blockIdx.x * 4 + (threadIdx.x >> 6);
   if (row >= (size_t)p.rows) return;
   const Running r = join_pieces(p, row);
-  if ((threadIdx.x & 63) == 0) finish(p, row, r);
+  if ((threadIdx.x & 63) == 0) finish(p, row, r, p.parts[row]);
 }
 
 // ---- the gradient of a row's piece, from lse (JOIN: from the pieces' m and s, the first piece writes loss and lse).  Grid rows x pieces.
@@ -300,24 +405,46 @@ template <typename T, int NT, bool JOIN> __global__ __launch_bounds__(NT) void d
       if (threadIdx.x == 0) {
         sh.m[0] = r.m;
         sh.s[0] = r.s;
-        if (piece == 0) finish(p, row, r);
+        if (piece == 0) finish(p, row, r, p.parts[row]);
       }
     }
     read_entries<T>(p, row, sh.e);
   }
   __syncthreads();
   const float w = p.dloss[row] * p.inv_t;
-  const double mass = sh.e.mass;
+  const double mass = sh.e.all.mass;
   const bool none = w == 0.f || mass == 0.0;
-  // p = exp((z - m) / T) / s, or exp(z / T - lse): f exp2(z c - shift)
-  const float m = JOIN ? sh.m[0] : 0.f, l = JOIN ? 0.f : p.lse[row] * LOG2E;
-  const float f = none ? 0.f : JOIN ? w * (float)mass / sh.s[0] : w * (float)mass;
-  auto prob = [&](float x) { return f * __builtin_amdgcn_exp2f(JOIN ? (x - m) * p.c : fmaf(x, p.c, -l)); };
+  // p = exp((z - m) / T) / s, or, from lse, exp(z / T - lse): f exp2(z c - shift), with what the shift's rounding leaves out in f
+  Running r;
+  float f = w * (float)mass, shift;
+  bool sound = true;
+  if (JOIN) {
+    r.m = sh.m[0];
+    r.s = sh.s[0];
+    f /= r.s;
+    sound = r.sound(p.c);
+    shift = r.reference(p.c);
+    if (sound) f *= r.rest(p.c);
+  } else {
+    const double exact = (double)p.lse[row] / (double)p.inv_t * (double)p.c;
+    shift = (float)exact;
+    f *= __builtin_amdgcn_exp2f((float)((double)shift - exact));
+  }
+  auto prob = [&](float x) { return f * __builtin_amdgcn_exp2f(fmaf(x, p.c, -shift)); };
   int at = begin + threadIdx.x * N;
   if (none) {
     const float x[N] = {};
     for (; at < end; at += STEP) store_chunk(dz, at, end, x);
     return;
+  }
+  if (JOIN && !sound) {
+    for (; at < end; at += STEP) {
+      float x[N];
+      load_chunk(z, at, end, x);
+#pragma unroll
+      for (int e = 0; e < N; ++e) x[e] = f * __builtin_amdgcn_exp2f((x[e] - r.m) * p.c);
+      store_chunk(dz, at, end, x);
+    }
   }
   for (; at + (U - 1) * STEP + N <= end; at += U * STEP) {
     typename Any16<T>::t v[U];
@@ -340,7 +467,7 @@ template <typename T, int NT, bool JOIN> __global__ __launch_bounds__(NT) void d
   __syncthreads();
   for (int j = threadIdx.x; j < p.k; j += NT) {
     const int id = sh.e.id[j];
-    if (id >= begin && id < end) dz[id] = (T)(prob(sh.e.z[j]) - w * teacher_at(sh.e, p.k, id));
+    if (id >= begin && id < end) dz[id] = (T)((sound ? prob(sh.e.z[j]) : f * __builtin_amdgcn_exp2f((sh.e.z[j] - r.m) * p.c)) - w * teacher_at(sh.e, p.k, id));
   }
 }
 
@@ -356,19 +483,30 @@ void divide(Distill& p, int pieces) {
   p.pieces = (p.vocab + p.piece - 1) / p.piece;
 }
 
+template <typename T, int NT, int R> hipError_t run_rows(const Distill& p, int per_unit, hipStream_t s) {
+  const int most = 256 * per_unit;
+  hipLaunchKernelGGL((distill_rows<T, NT, R>), dim3(p.rows < most ? p.rows : most), dim3(NT), 0, s, p);
+  return hipGetLastError();
+}
+// the fewest steps that hold a row, in twos; workgroups that fill a compute unit
 template <typename T> hipError_t run_both(const Distill& p, hipStream_t s) {
   const int chunks = (p.vocab + Vec16<T>::N - 1) / Vec16<T>::N;
-  const dim3 grid(p.rows);
-  if (chunks <= 256 * 2) hipLaunchKernelGGL((distill_row<T, 256, 2>), grid, dim3(256), 0, s, p);
-  else if (chunks <= 256 * 8) hipLaunchKernelGGL((distill_row<T, 256, 8>), grid, dim3(256), 0, s, p);
-  else if (chunks <= 512 * 8) hipLaunchKernelGGL((distill_row<T, 512, 8>), grid, dim3(512), 0, s, p);
-  else if (chunks <= 1024 * 8) hipLaunchKernelGGL((distill_row<T, 1024, 8>), grid, dim3(1024), 0, s, p);
-  else hipLaunchKernelGGL((distill_row<T, 1024, 16>), grid, dim3(1024), 0, s, p);
-  return hipGetLastError();
+  if (chunks <= 256 * 2) return run_rows<T, 256, 2>(p, 4, s);
+  if (chunks <= 256 * 4) return run_rows<T, 256, 4>(p, 4, s);
+  if (chunks <= 256 * 6) return run_rows<T, 256, 6>(p, 4, s);
+  if (chunks <= 256 * 8) return run_rows<T, 256, 8>(p, 4, s);
+  if (chunks <= 512 * 6) return run_rows<T, 512, 6>(p, 2, s);
+  if (chunks <= 512 * 8) return run_rows<T, 512, 8>(p, 2, s);
+  if (chunks <= 1024 * 6) return run_rows<T, 1024, 6>(p, 1, s);
+  if (chunks <= 1024 * 8) return run_rows<T, 1024, 8>(p, 1, s);
+  if (chunks <= 1024 * 10) return run_rows<T, 1024, 10>(p, 1, s);
+  if (chunks <= 1024 * 12) return run_rows<T, 1024, 12>(p, 1, s);
+  if (chunks <= 1024 * 14) return run_rows<T, 1024, 14>(p, 1, s);
+  return run_rows<T, 1024, 16>(p, 1, s);
 }
 
 template <typename T> hipError_t run(Distill p, hipStream_t s) {
-  if (p.loss && p.dz && p.rows >= FEW_ROWS) return run_both<T>(p, s);
+  if (p.loss && p.dz && p.rows >= FEW_ROWS && p.vocab >= Vec16<T>::N) return run_both<T>(p, s);
   if (p.loss) {
     divide(p, p.rows >= FEW_ROWS ? 1 : pieces_of(p.rows, p.vocab));
     hipLaunchKernelGGL((distill_stats<T, 256>), dim3((unsigned)p.rows * p.pieces), dim3(256), 0, s, p);
@@ -385,13 +523,13 @@ template <typename T> hipError_t run(Distill p, hipStream_t s) {
 }  // namespace
 
 uint64_t distill_ws_bytes(int rows, int vocab, int) {
-  return 16 + (rows < FEW_ROWS ? 16ull * rows + 8ull * rows * pieces_of(rows, vocab) : 0);
+  return 16 + (rows < FEW_ROWS ? sizeof(Teacher) * rows + 8ull * rows * pieces_of(rows, vocab) : 0);
 }
 
 hipError_t launch_distill(int dtype, const void* z, size_t ldz, const int* ids, const float* teacher, const float* dloss, float* loss, float* lse, void* dz, size_t lddz,
                           void* ws, int rows, int vocab, int k, float temperature, int log_probs, hipStream_t s) {
   Distill p = {z, ids, teacher, dloss, loss, lse, dz, ldz, lddz, rows, vocab, k, 1.f / temperature, LOG2E / temperature, log_probs, 1, vocab, nullptr, nullptr};
-  p.parts = (double2*)ws;
+  p.parts = (Teacher*)ws;
   p.stats = (float2*)(p.parts + rows);
   return dtype == DT_BF16 ? run<bf16_t>(p, s) : run<float>(p, s);
 }

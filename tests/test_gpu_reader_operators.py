@@ -35,6 +35,7 @@ def zone(shape, dtype, fill=9.0):
 
 def within(got, ref, bound, what=""):
     got = host(got) if isinstance(got, torch.Tensor) else got
+    ref = np.where(np.abs(ref) > 2.0 ** 128 - 2.0 ** 103, np.sign(ref) * np.inf, ref)      # past the range of either type: rounds to infinity
     same = (got == ref) | (np.isnan(got) & np.isnan(ref))
     with np.errstate(invalid="ignore"):
         d = np.where(same, 0.0, np.abs(got - ref))
@@ -555,6 +556,59 @@ def test_distillation_of_rows_that_are_not_finite(how, dtype, rows, vocab):
         setattr(c, a, getattr(c, a)[fine])
     c.shape = (len(fine),) + c.shape[1:]
     c.loss, c.lse = torch.from_numpy(loss[fine]), torch.from_numpy(lse[fine])
+    c.check(torch.from_numpy(dz[fine]))
+
+
+@pytest.mark.parametrize("how", ["both", "apart"])
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+@pytest.mark.parametrize("rows,vocab", [(9, 700), (9, 40009), (9, 131200), (170, 9001), (170, 70003)])
+@pytest.mark.parametrize("temperature", [1.0, 0.125])
+def test_distillation_of_rows_of_every_range(how, dtype, rows, vocab, temperature):
+    """Logits that rise by hundreds behind the first words, fall behind them, lie far from zero, are masked by minus infinity or by the type's lowest value in front, behind or nearly everywhere,
+    are all alike, or all the lowest value."""
+    c = Distill(dtype, rows, vocab, 6, temperature, bare=True, seed=8)
+    low = float(torch.finfo(TDT[dtype]).min)
+    base = c.Z[:9].copy()
+    half = vocab // 2
+    c.Z[0, half:] += 300.0
+    c.Z[1, :half] += 300.0
+    c.Z[2] += 4096.0
+    c.Z[3, :half] = -np.inf
+    c.Z[4, half:] = low
+    c.Z[5] = np.where(np.arange(vocab) == vocab - 2, base[5], low)
+    c.Z[6] = 3.0
+    c.Z[7, :min(600, half)] = low
+    c.Z[8] -= 2048.0
+    c.ids[3] = half + np.arange(6)
+    c.Z = q(c.Z, dtype)
+    c.Z[3, :half] = -np.inf
+    c.upload()
+    dz = c.call(how)
+    torch.cuda.synchronize()
+    c.check(dz)                                         # (what lse's rounding takes from the gradient of a far row is in the bound: 2 e_lse)
+    c.untouched()
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+@pytest.mark.parametrize("rows,vocab", [(3, 900), (3, 50000), (170, 9001), (170, 131073)])
+def test_distillation_of_a_row_of_lowest_values(dtype, rows, vocab):
+    """All words masked by the type's lowest value: the distribution is even."""
+    c = Distill(dtype, rows, vocab, 4, bare=True)
+    low = float(torch.finfo(TDT[dtype]).min)
+    c.Z[1], c.ids[1], c.T[1] = low, [0, 1, vocab // 2, vocab - 1], 0.0
+    c.upload()
+    dz = host(c.call("both"))
+    torch.cuda.synchronize()
+    w = float(c.w[1])
+    want = np.full(vocab, w / vocab)
+    want[c.ids[1]] -= w / 4
+    within(dz[1], want, np.abs(want) * (HALF[dtype] + 16 * EPS) + 16 * EPS * abs(w) / vocab, "even")
+    within(host(c.loss)[1:2], np.array([np.log(vocab / 4)]), 1e-5)
+    fine = [0] + list(range(2, rows))
+    for a in ("Z", "ids", "T", "w"):
+        setattr(c, a, getattr(c, a)[fine])
+    c.shape = (len(fine),) + c.shape[1:]
+    c.loss, c.lse = c.loss[fine], c.lse[fine]
     c.check(torch.from_numpy(dz[fine]))
 
 
