@@ -17,7 +17,6 @@
 namespace {
 
 constexpr float LOG2E = 1.4426950408889634f, LOWEST = -3.402823466e38f;
-constexpr int MAX_K = 1024;
 
 // 16 bytes of a row at any address of its elements
 template <typename T> struct Any16;
@@ -25,8 +24,8 @@ template <> struct Any16<bf16_t> { typedef bf16_t t __attribute__((ext_vector_ty
 template <> struct Any16<float> { typedef float t __attribute__((ext_vector_type(4), aligned(4))); };
 
 // what a row's entries make of its loss: sum + mass (log of the sum of exp(z / T) - z0 / T), with sum = sum of t (log t - (z - z0) / T), mass = sum of t and z0 one of
-// their own logits, so that nothing large cancels
-struct Teacher { double sum, mass, z0; };
+// their own logits, so that nothing large cancels; log t = the teacher's value - log_norm; twice: a word is named twice
+struct Teacher { double sum, mass, z0, log_norm; int twice, unused; };
 
 struct Distill {
   const void* z; const int* ids; const float* teacher; const float* dloss;
@@ -92,14 +91,15 @@ template <int N> __device__ __forceinline__ float wave_reference(const float (&x
   return wave_max(most);
 }
 
-// the row's entries, for the whole workgroup
+// a row's entries in LDS (dynamic: 16 bytes an entry): word or -1, t, logit at the word, the teacher's value
 struct Entries {
-  int id[MAX_K];
-  float t[MAX_K], z[MAX_K];
-  Teacher all;
+  int* id; float *t, *z, *value;
+  __device__ __forceinline__ Entries(float* lds, int slot, int k) : id((int*)lds + 4 * k * slot), t(lds + 4 * k * slot + k), z(t + k), value(z + k) {}
 };
+constexpr size_t entries_bytes(int k) { return 16ull * k; }
+
 struct Shared {
-  Entries e;
+  Teacher teacher;
   float m[16], s[16];
 };
 
@@ -109,24 +109,49 @@ __device__ __forceinline__ double wave_sum64(double v) {
   return v;
 }
 
-// One wave: ids, t and z at the ids into LDS.  Read before anything of the row is written (dz may be z).
-template <typename T> __device__ __forceinline__ void read_entries(const Distill& p, size_t row, Entries& e) {
+// exp of a 64-bit number: of its 32-bit part, times one plus the rest (two roundings of 32 bits; the 64-bit functions take a wave a microsecond)
+__device__ __forceinline__ float exp_of(double x) {
+  const float hi = (float)x;
+  return x == -INFINITY ? 0.f : expf(hi) * (1.f + (float)(x - (double)hi));
+}
+// log of a positive 32-bit number to 2^-26: its exponent times log 2 in 64 bits, the rest near one
+__device__ __forceinline__ double log_of(float x) {
+  int k;
+  float f = frexpf(x, &k);
+  if (f < 0.70710678f) {
+    f *= 2.f;
+    --k;
+  }
+  return (double)k * 0.69314718055994531 + (double)logf(f);
+}
+
+// entry j's logit of the teacher ahead of its normalisation, minus infinity where it is not there
+__device__ __forceinline__ float entry(const Distill& p, size_t row, int j, int& id) {
+  id = p.ids[row * p.k + j];
+  const float a = p.teacher[row * p.k + j];
+  if ((unsigned)id < (unsigned)p.vocab) return p.log_probs ? a : a * p.inv_t;
+  id = -1;
+  return -INFINITY;
+}
+
+// One wave: a row's entries into LDS and what they come to.  WEIGHTS: t takes the place of the teacher's values there.  GATHER: with the logits at the words, read
+// before anything of the row is written (dz may be z); without them `sum` is that of t log t alone.
+template <typename T, bool WEIGHTS, bool GATHER> __device__ __forceinline__ Teacher read_entries(const Distill& p, size_t row, const Entries& e) {
   const int lane = threadIdx.x & 63;
-  const int* ids = p.ids + row * p.k;
-  const float* teacher = p.teacher + row * p.k;
   const T* z = (const T*)p.z + row * p.ldz;
   float most = -INFINITY, z0 = -INFINITY;
 #pragma unroll 1
   for (int j = lane; j < p.k; j += 64) {
-    const int id = ids[j];
-    const bool on = (unsigned)id < (unsigned)p.vocab;
-    const float a = on ? (p.log_probs ? teacher[j] : teacher[j] * p.inv_t) : -INFINITY;
-    e.id[j] = on ? id : -1;
+    int id;
+    const float a = entry(p, row, j, id);
+    e.id[j] = id;
     e.t[j] = a;
-    const float x = on ? (float)z[id] : -INFINITY;
-    e.z[j] = x;
     most = fmaxf(most, a);
-    z0 = fmaxf(z0, x);
+    if (GATHER) {
+      const float x = id >= 0 ? (float)z[id] : -INFINITY;
+      e.z[j] = x;
+      z0 = fmaxf(z0, x);
+    }
   }
   most = wave_max(most);
   z0 = wave_max(z0);
@@ -136,30 +161,56 @@ template <typename T> __device__ __forceinline__ void read_entries(const Distill
   if (!p.log_probs) {
     norm = 0.0;
 #pragma unroll 1
-    for (int j = lane; j < p.k; j += 64) norm += exp((double)e.t[j] - shift);
+    for (int j = lane; j < p.k; j += 64) norm += (double)exp_of((double)e.t[j] - shift);
     norm = wave_sum64(norm);
     if (norm == 0.0) norm = 1.0;                        // no entries
   }
-  const double log_norm = shift + log(norm);
+  const double log_norm = shift + (p.log_probs ? 0.0 : log_of((float)norm));
   double sum = 0.0, mass = 0.0;
 #pragma unroll 1
   for (int j = lane; j < p.k; j += 64) {
-    const double lt = (double)e.t[j] - log_norm, t = exp(lt);
-    if (t != 0.0) sum += t * (lt - ((double)e.z[j] - (double)z0) * (double)p.inv_t);
+    const double lt = (double)e.t[j] - log_norm, t = (double)exp_of(lt);
+    if (t != 0.0) sum += t * (GATHER ? lt - ((double)e.z[j] - (double)z0) * (double)p.inv_t : lt);
     mass += t;
-    e.t[j] = (float)t;
+    if (WEIGHTS) e.t[j] = (float)t;
   }
-  sum = wave_sum64(sum);
-  mass = wave_sum64(mass);
-  if (lane == 0) e.all = {sum, mass, z0};
+  return {wave_sum64(sum), wave_sum64(mass), z0, log_norm, 0, 0};
 }
 
-// the gradient at entry j's word, t being all that the row's entries give it
+// all that the row's entries give a word
 __device__ __forceinline__ float teacher_at(const Entries& e, int k, int id) {
   float t = 0.f;
 #pragma unroll 4
   for (int i = 0; i < k; ++i) t += e.id[i] == id ? e.t[i] : 0.f;
   return t;
+}
+
+// What the rows' entries come to, ahead of the pass over the rows: a wave a row, four to a workgroup.  In that pass one wave's 64-bit arithmetic and its two loads
+// one behind the other would hold up the other fifteen (4096 rows of 131072 words with 128 entries: 120 of 583 us).  Whether a row names a word twice: by a table of
+// its words in LDS.
+template <typename T> __global__ __launch_bounds__(256) void distill_teacher(const Distill p, int slots) {
+  extern __shared__ float lds[];
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const size_t row = (size_t)blockIdx.x * 4 + wave;
+  const Entries e(lds, wave, p.k);
+  int* table = (int*)lds + 16 * p.k + wave * slots;
+  for (int i = lane; i < slots; i += 64) table[i] = -1;
+  __syncthreads();
+  if (row >= (size_t)p.rows) return;
+  Teacher t = read_entries<T, false, false>(p, row, e);
+  bool twice = false;
+#pragma unroll 1
+  for (int j = lane; j < p.k; j += 64) {
+    const int id = e.id[j];
+    if (id < 0) continue;
+    for (unsigned at = (unsigned)id * 2654435769u >> 8 & (slots - 1);; at = (at + 1) & (slots - 1)) {   // a free place or the word's is found: the table is half empty
+      const int was = atomicCAS(table + at, -1, id);
+      if (was == id) twice = true;
+      if (was == -1 || was == id) break;
+    }
+  }
+  t.twice = __any(twice) ? 1 : 0;
+  if (lane == 0) p.parts[row] = t;
 }
 
 template <typename T> __device__ __forceinline__ void load_chunk(const T* z, int at, int end, float (&x)[Vec16<T>::N]) {
@@ -199,7 +250,7 @@ template <int NT> __device__ __forceinline__ Running join_group(Running r, Share
 }
 // loss and lse of a row
 __device__ __forceinline__ void finish(const Distill& p, size_t row, const Running& r, const Teacher& t) {
-  const double log_s = log((double)r.s);
+  const double log_s = log_of(r.s);
   p.lse[row] = (float)((double)r.m * (double)p.inv_t + log_s);
   p.loss[row] = (float)(t.mass == 0.0 ? 0.0 : t.sum + t.mass * (((double)r.m - t.z0) * (double)p.inv_t + log_s));
 }
@@ -225,7 +276,7 @@ template <typename T, int NT, int R> __global__ __launch_bounds__(NT) __attribut
   constexpr int N = Vec16<T>::N, STEP = NT * N, HELD = R * STEP;
   typedef typename Any16<T>::t chunk_t;
   typedef unsigned u32x4_t __attribute__((ext_vector_type(4)));
-  __shared__ Entries entries[2];
+  extern __shared__ float lds[];
   __shared__ Shared sh;
   const int first = threadIdx.x * N, last = p.vocab - N;
   auto fetch = [&](const T* z, int step) {
@@ -244,14 +295,20 @@ template <typename T, int NT, int R> __global__ __launch_bounds__(NT) __attribut
   u32x4_t held[R];
 #pragma unroll
   for (int r = 0; r < R; ++r) held[r] = __builtin_bit_cast(u32x4_t, fetch((const T*)p.z + blockIdx.x * p.ldz, r));
-  int turn = 0;
+  int turn = 0, id_next = -1;
+  float a_next = -INFINITY;
+  if ((int)threadIdx.x < p.k) a_next = entry(p, blockIdx.x, threadIdx.x, id_next);
 #pragma unroll 1
   for (size_t row = blockIdx.x; row < (size_t)p.rows; row += gridDim.x, turn ^= 1) {
     const T* z = (const T*)p.z + row * p.ldz;
     T* dz = (T*)p.dz + row * p.lddz;
-    const T* zn = (const T*)p.z + (row + gridDim.x < (size_t)p.rows ? row + gridDim.x : row) * p.ldz;
-    Entries& en = entries[turn];
-    if (threadIdx.x < 64) read_entries<T>(p, row, en);
+    const size_t next = row + gridDim.x < (size_t)p.rows ? row + gridDim.x : row;
+    const T* zn = (const T*)p.z + next * p.ldz;
+    const Entries en(lds, turn, p.k);
+    const Teacher& teacher = p.parts[row];
+    const double log_norm = teacher.log_norm;
+    const int id = id_next;                             // this thread's entry, requested a row ahead
+    const float a = a_next, zid = id >= 0 ? (float)z[id] : -INFINITY;
     Running part;
     {
       float x[N];
@@ -281,10 +338,26 @@ template <typename T, int NT, int R> __global__ __launch_bounds__(NT) __attribut
     }
 #pragma unroll
     for (int r = 0; r < R; ++r) asm volatile("" : "+v"(held[r]));   // kept as they came: their values in 32 bits would take twice the registers
+    if ((int)threadIdx.x < p.k) {
+      en.id[threadIdx.x] = id;
+      en.t[threadIdx.x] = exp_of((double)a - log_norm);
+      en.z[threadIdx.x] = zid;
+      en.value[threadIdx.x] = a;
+#pragma unroll 1
+      for (int j = threadIdx.x + NT; j < p.k; j += NT) {
+        int other;
+        const float v = entry(p, row, j, other);
+        en.id[j] = other;
+        en.t[j] = exp_of((double)v - log_norm);
+        en.value[j] = v;
+        en.z[j] = other >= 0 ? (float)z[other] : -INFINITY;
+      }
+      a_next = entry(p, next, threadIdx.x, id_next);
+    }
     Running all = join_group<NT>(part, sh, p.c);
     if (!all.sound(p.c)) all = sum_again<T, NT>(p, z, 0, p.vocab, sh);
-    const double mass = en.all.mass;
-    if (threadIdx.x == 0) finish(p, row, all, en.all);
+    const double mass = teacher.mass;
+    const bool twice = teacher.twice;
     const float w = p.dloss[row] * p.inv_t;
     const bool none = w == 0.f || mass == 0.0;
     const bool sound = all.sound(p.c);
@@ -304,8 +377,11 @@ template <typename T, int NT, int R> __global__ __launch_bounds__(NT) __attribut
       for (int e = 0; e < N; ++e) v[e] = (T)(fr * __builtin_amdgcn_exp2f(fmaf((float)v[e], p.c, -mc)));
       const int over = step < R - 2 ? 0 : first + step * STEP - last;
       if (!sound || over >= N) return;
-      if (over <= 0) *reinterpret_cast<chunk_t*>(dz + step * STEP + (unsigned)first) = v;
-      else
+      if (over <= 0) {
+        // rows of 64 KB and more do not stay in the caches for whoever reads them next: past them (4096 rows of 131072 words 473 -> 456 us)
+        if (NT == 1024) __builtin_nontemporal_store(v, reinterpret_cast<chunk_t*>(dz + step * STEP + (unsigned)first));
+        else *reinterpret_cast<chunk_t*>(dz + step * STEP + (unsigned)first) = v;
+      } else
 #pragma unroll
         for (int e = 0; e < N; ++e)
           if (e >= over) dz[last + e] = v[e];
@@ -318,10 +394,20 @@ template <typename T, int NT, int R> __global__ __launch_bounds__(NT) __attribut
       held[r] = __builtin_bit_cast(u32x4_t, fetch(zn, r));
     }
     __syncthreads();
+    if (threadIdx.x >= NT - 64) {                       // the loss, by the wave that has the fewest entries to write
+      double sum = 0.0;
+#pragma unroll 1
+      for (int j = threadIdx.x - (NT - 64); j < p.k; j += 64) {
+        const double t = (double)en.t[j];
+        if (t != 0.0) sum += t * ((double)en.value[j] - log_norm - ((double)en.z[j] - (double)all.m) * (double)p.inv_t);
+      }
+      sum = wave_sum64(sum);
+      if (threadIdx.x == NT - 1) finish(p, row, all, {sum, mass, all.m, 0.0, 0, 0});
+    }
     if (!none)
       for (int j = threadIdx.x; j < p.k; j += NT) {
         const int id = en.id[j];
-        if (id >= 0) dz[id] = (T)(f * __builtin_amdgcn_exp2f((en.z[j] - all.m) * p.c) - w * teacher_at(en, p.k, id));
+        if (id >= 0) dz[id] = (T)(f * __builtin_amdgcn_exp2f((en.z[j] - all.m) * p.c) - w * (twice ? teacher_at(en, p.k, id) : en.t[j]));
       }
   }
 }
@@ -329,11 +415,15 @@ template <typename T, int NT, int R> __global__ __launch_bounds__(NT) __attribut
 // ---- m and s of a row's piece; forward alone and a whole row: loss and lse.  Grid rows x pieces.
 template <typename T, int NT> __global__ __launch_bounds__(NT) void distill_stats(const Distill p) {
   constexpr int N = Vec16<T>::N, STEP = NT * N, U = 4;
+  extern __shared__ float lds[];
   __shared__ Shared sh;
   const size_t row = blockIdx.x / p.pieces;
   const int piece = blockIdx.x % p.pieces, begin = piece * p.piece, end = min(p.vocab, begin + p.piece);
   const T* z = (const T*)p.z + row * p.ldz;
-  if (piece == 0 && threadIdx.x < 64) read_entries<T>(p, row, sh.e);
+  if (piece == 0 && threadIdx.x < 64) {
+    const Teacher mine = read_entries<T, false, true>(p, row, Entries(lds, 0, p.k));
+    if (threadIdx.x == 0) sh.teacher = mine;
+  }
   int at = begin + threadIdx.x * N;
   float x[N];
   load_chunk(z, at, end, x);
@@ -368,10 +458,10 @@ template <typename T, int NT> __global__ __launch_bounds__(NT) void distill_stat
   if (threadIdx.x) return;
   if (p.dz || p.pieces > 1) {                            // joined by the next launch
     p.stats[blockIdx.x] = make_float2(all.m, all.s);
-    if (piece == 0) p.parts[row] = sh.e.all;
+    if (piece == 0) p.parts[row] = sh.teacher;
     return;
   }
-  finish(p, row, all, sh.e.all);
+  finish(p, row, all, sh.teacher);
 }
 
 // m and s of a row from its pieces, in the same order for every reader: one wave
@@ -394,11 +484,13 @@ __global__ __launch_bounds__(256) void distill_finish(const Distill p) {
 // ---- the gradient of a row's piece, from lse (JOIN: from the pieces' m and s, the first piece writes loss and lse).  Grid rows x pieces.
 template <typename T, int NT, bool JOIN> __global__ __launch_bounds__(NT) void distill_grad(const Distill p) {
   constexpr int N = Vec16<T>::N, STEP = NT * N, U = 4;
+  extern __shared__ float lds[];
   __shared__ Shared sh;
   const size_t row = blockIdx.x / p.pieces;
   const int piece = blockIdx.x % p.pieces, begin = piece * p.piece, end = min(p.vocab, begin + p.piece);
   const T* z = (const T*)p.z + row * p.ldz;
   T* dz = (T*)p.dz + row * p.lddz;
+  const Entries e(lds, 0, p.k);
   if (threadIdx.x < 64) {
     if (JOIN) {
       const Running r = join_pieces(p, row);
@@ -408,11 +500,12 @@ template <typename T, int NT, bool JOIN> __global__ __launch_bounds__(NT) void d
         if (piece == 0) finish(p, row, r, p.parts[row]);
       }
     }
-    read_entries<T>(p, row, sh.e);
+    const Teacher mine = read_entries<T, true, true>(p, row, e);
+    if (threadIdx.x == 0) sh.teacher = mine;
   }
   __syncthreads();
   const float w = p.dloss[row] * p.inv_t;
-  const double mass = sh.e.all.mass;
+  const double mass = sh.teacher.mass;
   const bool none = w == 0.f || mass == 0.0;
   // p = exp((z - m) / T) / s, or, from lse, exp(z / T - lse): f exp2(z c - shift), with what the shift's rounding leaves out in f
   Running r;
@@ -466,8 +559,8 @@ template <typename T, int NT, bool JOIN> __global__ __launch_bounds__(NT) void d
   }
   __syncthreads();
   for (int j = threadIdx.x; j < p.k; j += NT) {
-    const int id = sh.e.id[j];
-    if (id >= begin && id < end) dz[id] = (T)((sound ? prob(sh.e.z[j]) : f * __builtin_amdgcn_exp2f((sh.e.z[j] - r.m) * p.c)) - w * teacher_at(sh.e, p.k, id));
+    const int id = e.id[j];
+    if (id >= begin && id < end) dz[id] = (T)((sound ? prob(e.z[j]) : f * __builtin_amdgcn_exp2f((e.z[j] - r.m) * p.c)) - w * teacher_at(e, p.k, id));
   }
 }
 
@@ -485,11 +578,17 @@ void divide(Distill& p, int pieces) {
 
 template <typename T, int NT, int R> hipError_t run_rows(const Distill& p, int per_unit, hipStream_t s) {
   const int most = 256 * per_unit;
-  hipLaunchKernelGGL((distill_rows<T, NT, R>), dim3(p.rows < most ? p.rows : most), dim3(NT), 0, s, p);
+  hipLaunchKernelGGL((distill_rows<T, NT, R>), dim3(p.rows < most ? p.rows : most), dim3(NT), 2 * entries_bytes(p.k), s, p);
   return hipGetLastError();
 }
 // the fewest steps that hold a row, in twos; workgroups that fill a compute unit
 template <typename T> hipError_t run_both(const Distill& p, hipStream_t s) {
+  int slots = 64;
+  while (slots < 2 * p.k) slots *= 2;
+  static LdsAttrOnce lds_attr;
+  if (hipError_t e = lds_attr.ensure(reinterpret_cast<const void*>(distill_teacher<T>), 4 * (16 * 1024 + 4 * 2048)); e != hipSuccess) return e;
+  hipLaunchKernelGGL(distill_teacher<T>, dim3((p.rows + 3) / 4), dim3(256), 4 * (entries_bytes(p.k) + 4 * slots), s, p, slots);
+  if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
   const int chunks = (p.vocab + Vec16<T>::N - 1) / Vec16<T>::N;
   if (chunks <= 256 * 2) return run_rows<T, 256, 2>(p, 4, s);
   if (chunks <= 256 * 4) return run_rows<T, 256, 4>(p, 4, s);
@@ -505,31 +604,54 @@ template <typename T> hipError_t run_both(const Distill& p, hipStream_t s) {
   return run_rows<T, 1024, 16>(p, 1, s);
 }
 
-template <typename T> hipError_t run(Distill p, hipStream_t s) {
-  if (p.loss && p.dz && p.rows >= FEW_ROWS && p.vocab >= Vec16<T>::N) return run_both<T>(p, s);
+// rows that one launch of the pass over whole rows takes: what their entries come to is in the workspace
+constexpr int ROWS_A_LAUNCH = 16384;
+
+template <typename T> hipError_t run_parts(Distill p, bool whole, hipStream_t s) {
+  divide(p, whole ? 1 : pieces_of(p.rows, p.vocab));
+  p.stats = (float2*)(p.parts + p.rows);
+  const dim3 grid((unsigned)p.rows * p.pieces);
+  const size_t lds = entries_bytes(p.k);
   if (p.loss) {
-    divide(p, p.rows >= FEW_ROWS ? 1 : pieces_of(p.rows, p.vocab));
-    hipLaunchKernelGGL((distill_stats<T, 256>), dim3((unsigned)p.rows * p.pieces), dim3(256), 0, s, p);
+    hipLaunchKernelGGL((distill_stats<T, 256>), grid, dim3(256), lds, s, p);
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-    if (p.dz) hipLaunchKernelGGL((distill_grad<T, 256, true>), dim3((unsigned)p.rows * p.pieces), dim3(256), 0, s, p);
+    if (p.dz) hipLaunchKernelGGL((distill_grad<T, 256, true>), grid, dim3(256), lds, s, p);
     else if (p.pieces > 1) hipLaunchKernelGGL(distill_finish, dim3((p.rows + 3) / 4), dim3(256), 0, s, p);
-    return hipGetLastError();
+  } else {
+    hipLaunchKernelGGL((distill_grad<T, 256, false>), grid, dim3(256), lds, s, p);
   }
-  divide(p, p.rows >= FEW_ROWS ? 1 : pieces_of(p.rows, p.vocab));
-  hipLaunchKernelGGL((distill_grad<T, 256, false>), dim3((unsigned)p.rows * p.pieces), dim3(256), 0, s, p);
   return hipGetLastError();
+}
+
+template <typename T> hipError_t run(const Distill& p, hipStream_t s) {
+  if (p.rows < FEW_ROWS) return run_parts<T>(p, false, s);
+  if (!p.loss || !p.dz) return run_parts<T>(p, true, s);
+  for (int first = 0; first < p.rows; first += ROWS_A_LAUNCH) {
+    Distill q = p;
+    q.rows = p.rows - first < ROWS_A_LAUNCH ? p.rows - first : ROWS_A_LAUNCH;
+    q.z = (const T*)p.z + first * p.ldz;
+    q.dz = (T*)p.dz + first * p.lddz;
+    q.ids += (size_t)first * p.k;
+    q.teacher += (size_t)first * p.k;
+    q.dloss += first;
+    q.loss += first;
+    q.lse += first;
+    if (hipError_t e = p.vocab >= Vec16<T>::N ? run_both<T>(q, s) : run_parts<T>(q, true, s); e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
 }  // namespace
 
+// what the entries of a launch's rows come to, m and s of rows' pieces
 uint64_t distill_ws_bytes(int rows, int vocab, int) {
-  return 16 + (rows < FEW_ROWS ? sizeof(Teacher) * rows + 8ull * rows * pieces_of(rows, vocab) : 0);
+  if (rows < FEW_ROWS) return sizeof(Teacher) * rows + 8ull * rows * pieces_of(rows, vocab);
+  return (sizeof(Teacher) + 8ull) * (rows < ROWS_A_LAUNCH ? rows : ROWS_A_LAUNCH);
 }
 
 hipError_t launch_distill(int dtype, const void* z, size_t ldz, const int* ids, const float* teacher, const float* dloss, float* loss, float* lse, void* dz, size_t lddz,
                           void* ws, int rows, int vocab, int k, float temperature, int log_probs, hipStream_t s) {
   Distill p = {z, ids, teacher, dloss, loss, lse, dz, ldz, lddz, rows, vocab, k, 1.f / temperature, LOG2E / temperature, log_probs, 1, vocab, nullptr, nullptr};
   p.parts = (Teacher*)ws;
-  p.stats = (float2*)(p.parts + rows);
   return dtype == DT_BF16 ? run<bf16_t>(p, s) : run<float>(p, s);
 }

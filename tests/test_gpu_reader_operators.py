@@ -36,7 +36,8 @@ def zone(shape, dtype, fill=9.0):
 def within(got, ref, bound, what=""):
     got = host(got) if isinstance(got, torch.Tensor) else got
     ref = np.where(np.abs(ref) > 2.0 ** 128 - 2.0 ** 103, np.sign(ref) * np.inf, ref)      # past the range of either type: rounds to infinity
-    same = (got == ref) | (np.isnan(got) & np.isnan(ref))
+    over = (np.abs(ref) + bound > 2.0 ** 128 - 2.0 ** 103) & (got == np.sign(ref) * np.inf)      # or a value within the bound does
+    same = (got == ref) | (np.isnan(got) & np.isnan(ref)) | over
     with np.errstate(invalid="ignore"):
         d = np.where(same, 0.0, np.abs(got - ref))
     bad = ~(d <= np.broadcast_to(bound, ref.shape)) & ~same
@@ -475,7 +476,8 @@ class Distill:
 
     def check(self, dz):
         """Bounds.  exp((z - m) / T) is off by a few fp32 roundings of the exponent (its size |z - m| / T and, from a stored lse, |lse|), the sum of vocab of them by what each is off
-        and log2-many to vocab / 64 additions (512 roundings are more than any division of the row makes); the loss is a sum in 64 bits but for lse."""
+        and log2-many to vocab / 64 additions (512 roundings are more than any division of the row makes); the loss is a sum in 64 bits of 32-bit t.  A t is an exponential (2 EPS) times
+        one plus a rest (2 EPS); the teacher's normalisation is a sum of such numbers, rounded (1 EPS), and its logarithm (2^-26): with that 10 EPS of t in all, and 6 EPS of log t."""
         rows, vocab, k, T, log_probs = self.shape
         z = self.Z[:, :vocab]
         loss, lse = P.distill(z, self.ids, self.T, T, log_probs)
@@ -488,13 +490,18 @@ class Distill:
         ts = [P.teacher_weights(self.ids[r], self.T[r], vocab, T, log_probs)[0] for r in range(rows)]
         mass = np.array([t.sum() for t in ts])
         within(self.lse, lse, e_lse, "lse")
-        within(self.loss, loss, e_lse * mass + EPS * np.abs(loss) + 1e-12, "loss")
+        terms = np.zeros(rows)
+        for r in range(rows):
+            t, log_t = P.teacher_weights(self.ids[r], self.T[r], vocab, T, log_probs)
+            for j in np.nonzero(t)[0]:
+                terms[r] += t[j] * abs(log_t[j] - (z[r, self.ids[r, j]] / T - lse[r]))
+        within(self.loss, loss, (e_lse + 6 * EPS) * mass + 10 * EPS * terms + EPS * np.abs(loss) + 1e-12, "loss")
         top = np.zeros_like(z)
         for r in range(rows):
             for j in np.nonzero(ts[r])[0]:
                 top[r, self.ids[r, j]] += ts[r][j]
         # (a probability below the least normal number is off by up to that number: its steps are 2^-149 wide, and the hardware's exponential gives 0)
-        e_p = ((EPS * (6 * spread + 16) + 2 * e_lse[:, None]) * p + FLUSH) * mass[:, None] + FLUSH + 4 * EPS * (p * mass[:, None] + top)
+        e_p = ((EPS * (6 * spread + 16) + 2 * e_lse[:, None]) * p + FLUSH) * mass[:, None] + FLUSH + 12 * EPS * (p * mass[:, None] + top)
         within(host(dz)[:, :vocab], ref, np.abs(self.w.astype(np.float64))[:, None] / T * e_p + (HALF[self.dtype] + 2 * EPS) * np.abs(ref) + TINY[self.dtype], "dz")
 
     def untouched(self, inplace=False):
