@@ -11,22 +11,24 @@
 // The probabilities and dS enter the second products as one bf16 number (2^-8 of each at most, which adds about as much to the result's error as its own
 // rounding does); sums, softmax and D are fp32.  A single state has no gradient of its score: dS = p (dP - D) is 0 by definition and is not computed, since D
 // comes from the rounded o.
+#include "attention_f32_tiles.h"
 #include "attention_tiles.h"
 
 namespace {
 
 constexpr float LOWEST = -3.402823466e38f;
 
-struct CrossArgs {
-  const bf16_t *q, *k, *v; const int* kv_len; const bf16_t *o_in, *dout;
-  bf16_t* o; float* lse; bf16_t *dq, *dk, *dv; float *delta, *part;
+template <typename T> struct CrossArgsOf {
+  const T *q, *k, *v; const int* kv_len; const T *o_in, *dout;
+  T* o; float* lse; T *dq, *dk, *dv; float *delta, *part;
   size_t ldq, ldkv;
   int seq_q, seq_kv, n_q, n_kv, rep, rows, splits;     // rows = rep seq_q, the rows of a kv head; splits: parts of the states (forward, dQ) or of the rows (dK / dV)
   int block_heads, blocks_per_head, row_blocks;         // of the rows, in the dK / dV kernel
   Divisor by_seq_q;
 };
+typedef CrossArgsOf<bf16_t> CrossArgs;
 
-__device__ __forceinline__ int cross_states(const CrossArgs& p, int b) { return p.kv_len ? min(max(p.kv_len[b], 0), p.seq_kv) : p.seq_kv; }
+template <typename T> __device__ __forceinline__ int cross_states(const CrossArgsOf<T>& p, int b) { return p.kv_len ? min(max(p.kv_len[b], 0), p.seq_kv) : p.seq_kv; }
 
 // descriptor of the first `rows` rows of `width` bytes from p on, `stride` bytes apart: loads beyond read zero.  All of it is the same for the whole wave.
 __device__ __forceinline__ i32x4_t rows_desc(const void* p, int rows, unsigned stride, unsigned width) {
@@ -308,13 +310,23 @@ __global__ __launch_bounds__(64 * NW) void cross_fwd_mfma(const CrossArgs p) {
   if (g == 0) p.lse[stat] = mref * scale + logf(lt);
 }
 
-// o and lse of a row from its parts' sums: a thread has 8 columns
-template <int D> __global__ __launch_bounds__(256) void cross_fwd_join(const CrossArgs p, size_t all_rows) {
+template <typename T> __device__ __forceinline__ void store8(T* at, const float (&x)[8], float scale) {
+  Vec16<T> v;
+#pragma unroll
+  for (int h = 0; h < 8; h += Vec16<T>::N) {
+#pragma unroll
+    for (int e = 0; e < Vec16<T>::N; ++e) v.set(e, x[h + e] * scale);
+    *reinterpret_cast<Vec16<T>*>(at + h) = v;
+  }
+}
+
+// o and lse of a row from its parts' sums, whose references are in units of `unit`: a thread has 8 columns
+template <typename T, int D> __global__ __launch_bounds__(256) void cross_fwd_join(const CrossArgsOf<T> p, size_t all_rows, float unit) {
   constexpr int Q = D / 8;
   const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x, stat = i / Q;
   if (stat >= all_rows) return;
   const int col = (int)(i % Q) * 8;
-  const float scale = rsqrtf((float)D), c = scale * LOG2E;
+  const float c = unit * LOG2E;
   const float2* ml = reinterpret_cast<const float2*>(p.part + (size_t)p.splits * all_rows * D) + stat;
   float m = -INFINITY, l = 0.f, x[8] = {};
   for (int s = 0; s < p.splits; ++s) m = fmaxf(m, ml[s * all_rows].x);
@@ -332,11 +344,8 @@ template <int D> __global__ __launch_bounds__(256) void cross_fwd_join(const Cro
   const size_t t = stat % p.seq_q, a = stat / p.seq_q % p.n_q, b = stat / p.seq_q / p.n_q;
   const bool none = m == -INFINITY;
   const float inv = none ? 0.f : 1.f / l;
-  bf16x8_t out;
-#pragma unroll
-  for (int e = 0; e < 8; ++e) out[e] = (bf16_t)(x[e] * inv);
-  *reinterpret_cast<bf16x8_t*>(p.o + ((b * p.seq_q + t) * p.n_q + a) * D + col) = out;
-  if (col == 0) p.lse[stat] = none ? -INFINITY : m * scale + logf(l);
+  store8(p.o + ((b * p.seq_q + t) * p.n_q + a) * D + col, x, inv);
+  if (col == 0) p.lse[stat] = none ? -INFINITY : m * unit + logf(l);
 }
 
 // ---- backward, dQ: grid as forward ---------------------------------------------------------------------------------------------------
@@ -539,13 +548,14 @@ __global__ __launch_bounds__(64 * NW) void cross_dq_mfma(const CrossArgs p) {
     }
 }
 
-template <int D> __global__ __launch_bounds__(256) void cross_dq_join(const CrossArgs p, size_t all_rows) {
+// BLOCK: states to a block of the division into parts
+template <typename T, int D, int BLOCK> __global__ __launch_bounds__(256) void cross_dq_join(const CrossArgsOf<T> p, size_t all_rows) {
   constexpr int Q = D / 8;
   const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x, stat = i / Q;
   if (stat >= all_rows) return;
   const int col = (int)(i % Q) * 8;
   const size_t t = stat % p.seq_q, a = stat / p.seq_q % p.n_q, b = stat / p.seq_q / p.n_q;
-  const int n = cross_states(p, (int)b), all = n == 1 ? 0 : (n + 63) / 64, per = (all + p.splits - 1) / p.splits;
+  const int n = cross_states(p, (int)b), all = n == 1 ? 0 : (n + BLOCK - 1) / BLOCK, per = (all + p.splits - 1) / p.splits;
   float x[8] = {};
   for (int s = 0; s * per < all; ++s) {
     const f32x4_t* f = reinterpret_cast<const f32x4_t*>(p.part + (s * all_rows + stat) * D + col);
@@ -554,10 +564,7 @@ template <int D> __global__ __launch_bounds__(256) void cross_dq_join(const Cros
 #pragma unroll
       for (int e = 0; e < 4; ++e) x[4 * h + e] += f[h][e];
   }
-  bf16x8_t out;
-#pragma unroll
-  for (int e = 0; e < 8; ++e) out[e] = (bf16_t)(x[e] * rsqrtf((float)D));
-  *reinterpret_cast<bf16x8_t*>(p.dq + (b * p.seq_q + t) * p.ldq + a * D + col) = out;
+  store8(p.dq + (b * p.seq_q + t) * p.ldq + a * D + col, x, rsqrtf((float)D));
 }
 
 // Blocks of up to 64 rows of a kv head: 64 queries of one head, or, of shorter sequences, as many whole heads (a divisor of theirs) as fit: then a
@@ -856,7 +863,7 @@ __global__ __launch_bounds__(256 * NG) void cross_dkv_mfma(const CrossArgs p) {
 }
 
 // dk and dv of a state and kv head from the parts' sums; a thread has 8 columns of one of them
-template <int D> __global__ __launch_bounds__(256) void cross_dkv_join(const CrossArgs p, size_t batch) {
+template <typename T, int D> __global__ __launch_bounds__(256) void cross_dkv_join(const CrossArgsOf<T> p, size_t batch) {
   constexpr int Q = 2 * D / 8;
   const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x, per_part = batch * p.seq_kv * p.n_kv;
   if (i / Q >= per_part) return;
@@ -873,10 +880,7 @@ template <int D> __global__ __launch_bounds__(256) void cross_dkv_join(const Cro
       for (int e = 0; e < 8; ++e) x[e] += f[e / 4][e % 4];
     }
   }
-  bf16x8_t out;
-#pragma unroll
-  for (int e = 0; e < 8; ++e) out[e] = (bf16_t)(is_v ? x[e] : x[e] * rsqrtf((float)D));
-  *reinterpret_cast<bf16x8_t*>((is_v ? p.dv : p.dk) + row * p.ldkv + (size_t)h * D + col) = out;
+  store8((is_v ? p.dv : p.dk) + row * p.ldkv + (size_t)h * D + col, x, is_v ? 1.f : rsqrtf((float)D));
 }
 #undef OPTSTAGE_SB
 #undef OPTSTAGE_TILE_LOAD
@@ -958,7 +962,7 @@ template <int D> hipError_t cross_fwd_bf16(CrossArgs a, const CrossShape& c, hip
                                  : run_fwd<D, 8>(a, pl, c.batch, s);
   if (e != hipSuccess || pl.splits == 1) return e;
   const size_t all = (size_t)c.batch * c.n_q * c.seq_q;
-  hipLaunchKernelGGL(cross_fwd_join<D>, dim3(joins(all * (D / 8))), dim3(256), 0, s, a, all);
+  hipLaunchKernelGGL((cross_fwd_join<bf16_t, D>), dim3(joins(all * (D / 8))), dim3(256), 0, s, a, all, 1.f / sqrtf((float)D));
   return hipGetLastError();
 }
 template <int D> hipError_t cross_bwd_bf16(CrossArgs a, const CrossShape& c, hipStream_t s) {
@@ -971,7 +975,7 @@ template <int D> hipError_t cross_bwd_bf16(CrossArgs a, const CrossShape& c, hip
   if (e != hipSuccess) return e;
   if (pl.splits > 1) {
     const size_t all = (size_t)c.batch * c.n_q * c.seq_q;
-    hipLaunchKernelGGL(cross_dq_join<D>, dim3(joins(all * (D / 8))), dim3(256), 0, s, a, all);
+    hipLaunchKernelGGL((cross_dq_join<bf16_t, D, 64>), dim3(joins(all * (D / 8))), dim3(256), 0, s, a, all);
     if ((e = hipGetLastError()) != hipSuccess) return e;
   }
   pl = bounded(plan_states(c), c, states_part_bytes);
@@ -979,113 +983,287 @@ template <int D> hipError_t cross_bwd_bf16(CrossArgs a, const CrossShape& c, hip
   if constexpr (D == 128) e = pl.waves == 2 ? run_dkv<D, 2, 1>(a, pl, c.batch, s) : run_dkv<D, 1, 2>(a, pl, c.batch, s);
   else e = run_dkv<D, 1, 2>(a, pl, c.batch, s);
   if (e != hipSuccess || pl.splits == 1) return e;
-  hipLaunchKernelGGL(cross_dkv_join<D>, dim3(joins((size_t)c.batch * c.seq_kv * c.n_kv * (2 * D / 8))), dim3(256), 0, s, a, (size_t)c.batch);
+  hipLaunchKernelGGL((cross_dkv_join<bf16_t, D>), dim3(joins((size_t)c.batch * c.seq_kv * c.n_kv * (2 * D / 8))), dim3(256), 0, s, a, (size_t)c.batch);
   return hipGetLastError();
 }
 
 // ---- fp32 ------------------------------------------------------------------------------------------------------------------------------
-struct Cross {
-  const void *q, *k, *v; const int* kv_len; const void *o_in, *dout;
-  void* o; float* lse; void *dq, *dk, *dv; float* delta;
-  size_t ldq, ldkv;
-  int seq_q, seq_kv, batch, n_q, n_kv;
+// Scheme of attention_f32.hip: a workgroup has 16 rows (states, for dK / dV), its four waves take the other side's tiles of 16 in turn, and their sums meet
+// in LDS.  Rows of a kv head and parts as above; states past the last one repeat it as keys, weigh nothing, and are zeros as values.
+template <int D> struct Fp32 : F32<D> {
+  typedef F32<D> F;
+  // columns() of rows that end at `last`: zeros behind it
+  static __device__ __forceinline__ void columns0(f32x4_t (&v)[4][F::H], const float* base, size_t ld, int first, int last, int g, int r) {
+    F::columns(v, base, ld, first, last, g, r);
+    if (first + 15 <= last) return;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (first + 4 * g + e > last)
+#pragma unroll
+        for (int h = 0; h < F::H; ++h) v[e][h] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  }
 };
-
-__device__ __forceinline__ int states_f32(const Cross& p, int b) { return p.kv_len ? min(max(p.kv_len[b], 0), p.seq_kv) : p.seq_kv; }
-
-template <typename T, int D, bool BWD> __global__ __launch_bounds__(256) void cross_rows(const Cross p) {
-  constexpr int E = D / 64;
-  const int lane = threadIdx.x & 63;
-  const size_t item = (size_t)blockIdx.x * 4 + (threadIdx.x >> 6);            // (sequence, head, query)
-  if (item >= (size_t)p.batch * p.n_q * p.seq_q) return;
-  const int t = item % p.seq_q, a = item / p.seq_q % p.n_q, b = item / p.seq_q / p.n_q, h = a / (p.n_q / p.n_kv);
-  const size_t row = (size_t)b * p.seq_q + t;
-  const int n = states_f32(p, b);
-  const float scale = rsqrtf((float)D);
-  const T* q = (const T*)p.q + row * p.ldq + (size_t)a * D;
-  float x[E], acc[E] = {}, g[E], m = -INFINITY, l = 0.f, dd = 0.f, L = 0.f;
-  for (int e = 0; e < E; ++e) x[e] = (float)q[lane + 64 * e] * scale;
-  if (BWD) {
-    const size_t at = row * p.n_q * D + (size_t)a * D + lane;
-    for (int e = 0; e < E; ++e) {
-      g[e] = (float)((const T*)p.dout)[at + 64 * e];
-      dd += g[e] * (float)((const T*)p.o_in)[at + 64 * e];
-    }
-    dd = wave_sum(dd);
-    L = p.lse[item];
-    if (lane == 0) p.delta[item] = dd;
-  }
-  for (int j = 0; j < n; ++j) {
-    const T* k = (const T*)p.k + ((size_t)b * p.seq_kv + j) * p.ldkv + (size_t)h * D + lane;
-    const T* v = (const T*)p.v + ((size_t)b * p.seq_kv + j) * p.ldkv + (size_t)h * D + lane;
-    float s = 0.f, dp = 0.f;
-    for (int e = 0; e < E; ++e) s += x[e] * (float)k[64 * e];
-    s = wave_sum(s);
-    if (BWD) {
-      for (int e = 0; e < E; ++e) dp += g[e] * (float)v[64 * e];
-      dp = wave_sum(dp);
-      const float ds = n == 1 ? 0.f : expf(s - L) * (dp - dd) * scale;
-      for (int e = 0; e < E; ++e) acc[e] += ds * (float)k[64 * e];
-    } else {
-      const float mn = s > m || s != s ? s : m, f = expf(m - mn), w = expf(s - mn);
-      l = l * f + w;
-      for (int e = 0; e < E; ++e) acc[e] = acc[e] * f + w * (float)v[64 * e];
-      m = mn;
-    }
-  }
-  T* out = BWD ? (T*)p.dq + row * p.ldq + (size_t)a * D + lane : (T*)p.o + row * p.n_q * D + (size_t)a * D + lane;
-  for (int e = 0; e < E; ++e) out[64 * e] = (T)(BWD || n == 0 ? acc[e] : acc[e] / l);
-  if (!BWD && lane == 0) p.lse[item] = n == 0 ? -INFINITY : m + logf(l);
+struct RowAt { int head; size_t token; };              // of a kv head's heads; in all sequences
+template <typename T> __device__ __forceinline__ RowAt row_at(const CrossArgsOf<T>& p, int b, int row) {
+  const int head = p.by_seq_q.quotient(row);
+  return {head, (size_t)b * p.seq_q + (row - head * p.seq_q)};
 }
 
-template <typename T, int D> __global__ __launch_bounds__(256) void cross_state_rows(const Cross p) {
-  constexpr int E = D / 64;
-  const int lane = threadIdx.x & 63;
-  const size_t item = (size_t)blockIdx.x * 4 + (threadIdx.x >> 6);            // (sequence, head, state)
-  if (item >= (size_t)p.batch * p.n_kv * p.seq_kv) return;
-  const int j = item % p.seq_kv, h = item / p.seq_kv % p.n_kv, b = item / p.seq_kv / p.n_kv;
-  const size_t at = ((size_t)b * p.seq_kv + j) * p.ldkv + (size_t)h * D + lane;
-  const int n = states_f32(p, b);
-  const float scale = rsqrtf((float)D);
-  float k[E], v[E], ak[E] = {}, av[E] = {};
-  if (j < n) {
-    for (int e = 0; e < E; ++e) {
-      k[e] = (float)((const T*)p.k)[at + 64 * e] * scale;
-      v[e] = (float)((const T*)p.v)[at + 64 * e];
-    }
-    const int rep = p.n_q / p.n_kv;
-    for (int i = 0; i < rep * p.seq_q; ++i) {
-      const int a = h * rep + i / p.seq_q, t = i % p.seq_q;
-      const T* q = (const T*)p.q + ((size_t)b * p.seq_q + t) * p.ldq + (size_t)a * D + lane;
-      const T* g = (const T*)p.dout + (((size_t)b * p.seq_q + t) * p.n_q + a) * D + lane;
-      const size_t st = ((size_t)b * p.n_q + a) * p.seq_q + t;
-      float s = 0.f, dp = 0.f;
-      for (int e = 0; e < E; ++e) { s += (float)q[64 * e] * k[e]; dp += (float)g[64 * e] * v[e]; }
-      s = wave_sum(s);
-      dp = wave_sum(dp);
-      const float w = expf(s - p.lse[st]), ds = n == 1 ? 0.f : w * (dp - p.delta[st]) * scale;
-      for (int e = 0; e < E; ++e) { av[e] += w * (float)g[64 * e]; ak[e] += ds * (float)q[64 * e]; }
-    }
+template <int D> __global__ __launch_bounds__(256) void cross_fwd_f32(const CrossArgsOf<float> p) {
+  typedef Fp32<D> F;
+  __shared__ __attribute__((aligned(16))) float part_sums[4][ROWS][D + 4];
+  __shared__ float pm[4][ROWS], pl[4][ROWS];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, g = lane >> 4;
+  const int kvh = blockIdx.x % p.n_kv, at_x = blockIdx.x / p.n_kv, tile = at_x / p.splits, part = at_x % p.splits, b = blockIdx.y;
+  const int n = cross_states(p, b), tiles = (n + ROWS - 1) / ROWS, per = (tiles + p.splits - 1) / p.splits, t0 = min(tiles, part * per), t1 = min(tiles, t0 + per);
+  const size_t all_rows = (size_t)gridDim.y * p.n_kv * p.rows, stat0 = ((size_t)b * p.n_kv + kvh) * p.rows;
+  const size_t base = (size_t)b * p.seq_kv * p.ldkv + (size_t)kvh * D;
+  f32x4_t q[F::S], acc[F::NT];
+  {
+    const RowAt at = row_at(p, b, min(tile * ROWS + r, p.rows - 1));
+    F::rows(q, p.q + at.token * p.ldq + (size_t)(kvh * p.rep + at.head) * D, g);
   }
-  for (int e = 0; e < E; ++e) { ((T*)p.dk)[at + 64 * e] = (T)ak[e]; ((T*)p.dv)[at + 64 * e] = (T)av[e]; }
+  F::scaled(q, rsqrtf((float)D));
+  F::clear(acc);
+  float m = LOWEST, l = 0.f;
+  for (int t = t0 + wave; t < t1; t += 4) {
+    f32x4_t k[F::S], v[4][F::H];
+    F::rows(k, p.k + base + (size_t)min(ROWS * t + r, n - 1) * p.ldkv, g);
+    F::columns0(v, p.v + base, p.ldkv, ROWS * t, n - 1, g, r);
+    f32x4_t s = F::product(k, q);                       // s[e]: state 16 t + 4 g + e, row r
+    if (ROWS * t + ROWS > n) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (ROWS * t + 4 * g + e >= n) s[e] = -INFINITY;
+    }
+    const float mn = fmaxf(m, max_g(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3]))));
+    const float alpha = expf(m - mn);
+    f32x4_t w;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) w[e] = expf(s[e] - mn);
+    l = l * alpha + (w[0] + w[1]) + (w[2] + w[3]);      // this lane's states; summed over the four lanes at the end
+#pragma unroll
+    for (int i = 0; i < F::NT; ++i)
+#pragma unroll
+      for (int x = 0; x < 4; ++x) acc[i][x] *= alpha;
+    F::accumulate(acc, v, w);
+    m = mn;
+  }
+  l = sum_g(l);
+  F::put(part_sums[wave], acc, g, r);
+  if (g == 0) { pm[wave][r] = m; pl[wave][r] = l; }
+  __syncthreads();
+#pragma unroll
+  for (int h = 0; h < F::H; ++h) {
+    const int i = threadIdx.x + 256 * h, lr = i / (D / 4), c = (i % (D / 4)) * 4, row = tile * ROWS + lr;
+    if (row >= p.rows) continue;
+    const float M = fmaxf(fmaxf(pm[0][lr], pm[1][lr]), fmaxf(pm[2][lr], pm[3][lr]));
+    float L = 0.f;
+    f32x4_t v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      const float f = expf(pm[w][lr] - M);
+      L += pl[w][lr] * f;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] += part_sums[w][lr][c + e] * f;
+    }
+    const size_t stat = stat0 + row;
+    if (p.splits > 1) {
+      if (t0 < t1) *reinterpret_cast<f32x4_t*>(p.part + ((size_t)part * all_rows + stat) * D + c) = v;
+      if (c == 0) *reinterpret_cast<float2*>(p.part + (size_t)p.splits * all_rows * D + ((size_t)part * all_rows + stat) * 2) = t0 < t1 ? make_float2(M, L) : make_float2(-INFINITY, 0.f);
+      continue;
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = n ? v[e] / L : 0.f;
+    const RowAt at = row_at(p, b, row);
+    *reinterpret_cast<f32x4_t*>(p.o + (at.token * p.n_q + kvh * p.rep + at.head) * D + c) = v;
+    if (c == 0) p.lse[stat] = n ? M + logf(L) : -INFINITY;
+  }
 }
 
-unsigned waves4(size_t items) { return (unsigned)((items + 3) / 4); }
-template <typename T, int D> hipError_t run(const Cross& p, bool bwd, hipStream_t s) {
-  const unsigned g = waves4((size_t)p.batch * p.n_q * p.seq_q);
-  if (!bwd) {
-    hipLaunchKernelGGL((cross_rows<T, D, false>), dim3(g), dim3(256), 0, s, p);
-    return hipGetLastError();
+template <int D> __global__ __launch_bounds__(256) void cross_dq_f32(const CrossArgsOf<float> p) {
+  typedef Fp32<D> F;
+  __shared__ __attribute__((aligned(16))) float part_sums[4][ROWS][D + 4];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, g = lane >> 4;
+  const int kvh = blockIdx.x % p.n_kv, at_x = blockIdx.x / p.n_kv, tile = at_x / p.splits, part = at_x % p.splits, b = blockIdx.y;
+  const int n = cross_states(p, b), tiles = n == 1 ? 0 : (n + ROWS - 1) / ROWS, per = (tiles + p.splits - 1) / p.splits, t0 = min(tiles, part * per), t1 = min(tiles, t0 + per);
+  const size_t base = (size_t)b * p.seq_kv * p.ldkv + (size_t)kvh * D, stat0 = ((size_t)b * p.n_kv + kvh) * p.rows;
+  const float scale = rsqrtf((float)D);
+  const int row_r = min(tile * ROWS + r, p.rows - 1);
+  f32x4_t q[F::S], dO[F::S], acc[F::NT];
+  float dsum = 0.f;
+  {
+    const RowAt at = row_at(p, b, row_r);
+    const size_t col = (size_t)(kvh * p.rep + at.head) * D, o_at = at.token * p.n_q * D + col;
+    f32x4_t x[F::S];
+    F::rows(q, p.q + at.token * p.ldq + col, g);
+    F::rows(dO, p.dout + o_at, g);
+    F::rows(x, p.o_in + o_at, g);
+#pragma unroll
+    for (int s = 0; s < F::S; ++s)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) dsum = fmaf(dO[s][e], x[s][e], dsum);
   }
-  hipLaunchKernelGGL((cross_rows<T, D, true>), dim3(g), dim3(256), 0, s, p);
-  hipLaunchKernelGGL((cross_state_rows<T, D>), dim3(waves4((size_t)p.batch * p.n_kv * p.seq_kv)), dim3(256), 0, s, p);
+  F::scaled(q, scale);
+  F::clear(acc);
+  dsum = sum_g(dsum);
+  const float L = p.lse[stat0 + row_r];
+  if (part == 0 && wave == 0 && g == 0 && tile * ROWS + r < p.rows) p.delta[stat0 + row_r] = dsum;
+  for (int t = t0 + wave; t < t1; t += 4) {
+    f32x4_t k[F::S], v[F::S], kc[4][F::H];
+    const size_t at = base + (size_t)min(ROWS * t + r, n - 1) * p.ldkv;
+    F::rows(k, p.k + at, g);
+    F::rows(v, p.v + at, g);
+    F::columns0(kc, p.k + base, p.ldkv, ROWS * t, n - 1, g, r);
+    const f32x4_t s = F::product(k, q), dp = F::product(v, dO);
+    f32x4_t ds;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) ds[e] = ROWS * t + 4 * g + e >= n ? 0.f : expf(s[e] - L) * (dp[e] - dsum);
+    F::accumulate(acc, kc, ds);
+  }
+  F::put(part_sums[wave], acc, g, r);
+  __syncthreads();
+  if (p.splits > 1 && t0 >= t1) return;
+#pragma unroll
+  for (int h = 0; h < F::H; ++h) {
+    const int i = threadIdx.x + 256 * h, lr = i / (D / 4), c = (i % (D / 4)) * 4, row = tile * ROWS + lr;
+    if (row >= p.rows) continue;
+    f32x4_t v;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = ((part_sums[0][lr][c + e] + part_sums[1][lr][c + e]) + part_sums[2][lr][c + e]) + part_sums[3][lr][c + e];
+    if (p.splits > 1) {
+      *reinterpret_cast<f32x4_t*>(p.part + ((size_t)part * gridDim.y * p.n_kv * p.rows + stat0 + row) * D + c) = v;
+      continue;
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] *= scale;
+    const RowAt at = row_at(p, b, row);
+    *reinterpret_cast<f32x4_t*>(p.dq + at.token * p.ldq + (size_t)(kvh * p.rep + at.head) * D + c) = v;
+  }
+}
+
+// rows past the last one repeat it, weigh nothing and are zeros in the second products
+template <int D> __global__ __launch_bounds__(256) void cross_dkv_f32(const CrossArgsOf<float> p) {
+  typedef Fp32<D> F;
+  __shared__ __attribute__((aligned(16))) float part_sums[4][ROWS][D + 4];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, g = lane >> 4;
+  const int kvh = blockIdx.x % p.n_kv, at_x = blockIdx.x / p.n_kv, k0 = at_x / p.splits * ROWS, part = at_x % p.splits, b = blockIdx.y;
+  const int n = cross_states(p, b), tiles = (p.rows + ROWS - 1) / ROWS, per = (tiles + p.splits - 1) / p.splits, t0 = min(tiles, part * per), t1 = min(tiles, t0 + per);
+  const size_t base = (size_t)b * p.seq_kv * p.ldkv + (size_t)kvh * D, stat0 = ((size_t)b * p.n_kv + kvh) * p.rows;
+  const float scale = rsqrtf((float)D);
+  if (p.splits > 1 && (k0 >= n || t0 >= t1)) return;    // the join counts the parts that have rows, and writes zeros
+  f32x4_t ak[F::NT], av[F::NT];
+  F::clear(ak);
+  F::clear(av);
+  if (k0 < n) {
+    f32x4_t k[F::S], v[F::S];
+    const size_t at = base + (size_t)min(k0 + r, n - 1) * p.ldkv;
+    F::rows(k, p.k + at, g);
+    F::rows(v, p.v + at, g);
+    F::scaled(k, scale);
+    for (int t = t0 + wave; t < t1; t += 4) {
+      const RowAt mine = row_at(p, b, min(ROWS * t + r, p.rows - 1));
+      const size_t col = (size_t)(kvh * p.rep + mine.head) * D;
+      f32x4_t q[F::S], dO[F::S], c[4][F::H], w, ds;
+      F::rows(q, p.q + mine.token * p.ldq + col, g);
+      F::rows(dO, p.dout + mine.token * p.n_q * D + col, g);
+      const f32x4_t s = F::product(q, k), dp = F::product(dO, v);   // [e]: row 16 t + 4 g + e, state k0 + r
+      const float *qc[4], *gc[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int row = ROWS * t + 4 * g + e, rowc = min(row, p.rows - 1);
+        const RowAt a = row_at(p, b, rowc);
+        const size_t acol = (size_t)(kvh * p.rep + a.head) * D + 4 * r;
+        qc[e] = p.q + a.token * p.ldq + acol;
+        gc[e] = p.dout + a.token * p.n_q * D + acol;
+        w[e] = row < p.rows ? expf(s[e] - p.lse[stat0 + rowc]) : 0.f;
+        ds[e] = row < p.rows && n > 1 ? w[e] * (dp[e] - p.delta[stat0 + rowc]) : 0.f;   // one state has no gradient of its score
+      }
+      const f32x4_t zero = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+#pragma unroll
+        for (int h = 0; h < F::H; ++h) c[e][h] = ROWS * t + 4 * g + e < p.rows ? *reinterpret_cast<const f32x4_t*>(gc[e] + 64 * h) : zero;
+      F::accumulate(av, c, w);
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+#pragma unroll
+        for (int h = 0; h < F::H; ++h) c[e][h] = ROWS * t + 4 * g + e < p.rows ? *reinterpret_cast<const f32x4_t*>(qc[e] + 64 * h) : zero;
+      F::accumulate(ak, c, ds);
+    }
+  }
+#pragma unroll
+  for (int which = 0; which < 2; ++which) {
+    if (which) __syncthreads();
+    F::put(part_sums[wave], which ? av : ak, g, r);
+    __syncthreads();
+#pragma unroll
+    for (int h = 0; h < F::H; ++h) {
+      const int i = threadIdx.x + 256 * h, lr = i / (D / 4), c = (i % (D / 4)) * 4, s = k0 + lr;
+      if (s >= p.seq_kv) continue;
+      f32x4_t v;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] = ((part_sums[0][lr][c + e] + part_sums[1][lr][c + e]) + part_sums[2][lr][c + e]) + part_sums[3][lr][c + e];
+      if (p.splits > 1) {
+        if (s < n) *reinterpret_cast<f32x4_t*>(p.part + ((((size_t)part * gridDim.y + b) * p.seq_kv + s) * p.n_kv + kvh) * 2 * D + which * D + c) = v;
+        continue;
+      }
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] = s >= n || (!which && n == 1) ? 0.f : which ? v[e] : v[e] * scale;
+      *reinterpret_cast<f32x4_t*>((which ? p.dv : p.dk) + base + (size_t)s * p.ldkv + c) = v;
+    }
+  }
+}
+
+// parts where tiles of 16 rows are fewer than two to a compute unit: at least eight of the other side's to a part
+CrossPlan plan_f32(const CrossShape& c, bool states) {
+  const long rows = ((long)(c.n_q / c.n_kv) * c.seq_q + ROWS - 1) / ROWS, keys = (c.seq_kv + ROWS - 1) / ROWS;
+  CrossPlan p;
+  p.waves = 4;
+  p.tiles = (int)(states ? keys : rows);
+  const long wgs = (long)c.n_kv * c.batch * p.tiles, other = states ? rows : keys;
+  long splits = wgs >= 512 ? 1 : 1024 / wgs;
+  splits = splits < other / 8 ? splits : other / 8;
+  p.splits = splits < 1 ? 1 : (int)splits;
+  return bounded(p, c, states ? states_part_bytes : rows_part_bytes);
+}
+
+template <int D> hipError_t cross_fwd_fp32(CrossArgsOf<float> a, const CrossShape& c, hipStream_t s) {
+  const CrossPlan pl = plan_f32(c, false);
+  a.splits = pl.splits;
+  hipLaunchKernelGGL(cross_fwd_f32<D>, dim3((unsigned)a.n_kv * pl.tiles * pl.splits, c.batch), dim3(256), 0, s, a);
+  if (pl.splits > 1) {
+    if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+    const size_t all = (size_t)c.batch * c.n_q * c.seq_q;
+    hipLaunchKernelGGL((cross_fwd_join<float, D>), dim3(joins(all * (D / 8))), dim3(256), 0, s, a, all, 1.f);
+  }
+  return hipGetLastError();
+}
+template <int D> hipError_t cross_bwd_fp32(CrossArgsOf<float> a, const CrossShape& c, hipStream_t s) {
+  CrossPlan pl = plan_f32(c, false);
+  a.splits = pl.splits;
+  hipLaunchKernelGGL(cross_dq_f32<D>, dim3((unsigned)a.n_kv * pl.tiles * pl.splits, c.batch), dim3(256), 0, s, a);
+  if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+  if (pl.splits > 1) {
+    const size_t all = (size_t)c.batch * c.n_q * c.seq_q;
+    hipLaunchKernelGGL((cross_dq_join<float, D, ROWS>), dim3(joins(all * (D / 8))), dim3(256), 0, s, a, all);
+    if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+  }
+  pl = plan_f32(c, true);
+  a.splits = pl.splits;
+  a.row_blocks = (a.rows + ROWS - 1) / ROWS;
+  hipLaunchKernelGGL(cross_dkv_f32<D>, dim3((unsigned)a.n_kv * pl.tiles * pl.splits, c.batch), dim3(256), 0, s, a);
+  if (pl.splits > 1) {
+    if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+    hipLaunchKernelGGL((cross_dkv_join<float, D>), dim3(joins((size_t)c.batch * c.seq_kv * c.n_kv * (2 * D / 8))), dim3(256), 0, s, a, (size_t)c.batch);
+  }
   return hipGetLastError();
 }
 
-CrossArgs cross_args(const CrossShape& c, const void* q, const void* k, const void* v, const int* kv_len, float* ws) {
-  CrossArgs a = {};
-  a.q = (const bf16_t*)q; a.k = (const bf16_t*)k; a.v = (const bf16_t*)v; a.kv_len = kv_len;
-  a.delta = ws; a.part = ws + delta_floats(c);
+template <typename T> CrossArgsOf<T> cross_args(const CrossShape& c, const void* q, const void* k, const void* v, const int* kv_len, void* ws) {
+  CrossArgsOf<T> a = {};
+  a.q = (const T*)q; a.k = (const T*)k; a.v = (const T*)v; a.kv_len = kv_len;
+  a.delta = (float*)ws; a.part = (float*)ws + delta_floats(c);
   a.ldq = c.ldq; a.ldkv = c.ldkv;
   a.seq_q = c.seq_q; a.seq_kv = c.seq_kv; a.n_q = c.n_q; a.n_kv = c.n_kv; a.rep = c.n_q / c.n_kv; a.rows = a.rep * c.seq_q; a.splits = 1;
   const RowBlocks rb = row_blocks(c.seq_q, a.rep);
@@ -1093,36 +1271,44 @@ CrossArgs cross_args(const CrossShape& c, const void* q, const void* k, const vo
   a.by_seq_q = Divisor((unsigned)c.seq_q);
   return a;
 }
+template <typename T> CrossArgsOf<T> fwd_args(const CrossShape& c, const void* q, const void* k, const void* v, const int* kv_len, void* o, float* lse, void* ws) {
+  CrossArgsOf<T> a = cross_args<T>(c, q, k, v, kv_len, ws);
+  a.o = (T*)o; a.lse = lse;
+  return a;
+}
+template <typename T> CrossArgsOf<T> bwd_args(const CrossShape& c, const void* q, const void* k, const void* v, const int* kv_len, const void* o, const void* dout,
+                                              const float* lse, void* dq, void* dk, void* dv, void* ws) {
+  CrossArgsOf<T> a = cross_args<T>(c, q, k, v, kv_len, ws);
+  a.o_in = (const T*)o; a.dout = (const T*)dout; a.lse = const_cast<float*>(lse);
+  a.dq = (T*)dq; a.dk = (T*)dk; a.dv = (T*)dv;
+  return a;
+}
 
 }  // namespace
 
+// D of every row, and the parts' sums of whichever launch needs most
 uint64_t cross_attn_ws_bytes(int dtype, int seq_q, int seq_kv, int batch, int n_q, int n_kv, int d) {
   const CrossShape c = {0, 0, seq_q, seq_kv, batch, n_q, n_kv, d};
-  uint64_t part = 0;
-  if (dtype == DT_BF16) {
-    const uint64_t r = rows_part_bytes(c, bounded(plan_rows(c), c, rows_part_bytes).splits), s = states_part_bytes(c, bounded(plan_states(c), c, states_part_bytes).splits);
-    part = r > s ? r : s;
-  }
-  return 4ull * delta_floats(c) + part;
+  const CrossPlan by_rows = dtype == DT_BF16 ? bounded(plan_rows(c), c, rows_part_bytes) : plan_f32(c, false);
+  const CrossPlan by_states = dtype == DT_BF16 ? bounded(plan_states(c), c, states_part_bytes) : plan_f32(c, true);
+  const uint64_t r = rows_part_bytes(c, by_rows.splits), s = states_part_bytes(c, by_states.splits);
+  return 4ull * delta_floats(c) + (r > s ? r : s);
 }
 
 hipError_t launch_cross_attn_fwd(int dtype, const CrossShape& c, const void* q, const void* k, const void* v, const int* kv_len, void* o, float* lse, void* ws, hipStream_t s) {
   if (dtype == DT_BF16) {
-    CrossArgs a = cross_args(c, q, k, v, kv_len, (float*)ws);
-    a.o = (bf16_t*)o; a.lse = lse;
+    const CrossArgs a = fwd_args<bf16_t>(c, q, k, v, kv_len, o, lse, ws);
     return c.d == 64 ? cross_fwd_bf16<64>(a, c, s) : cross_fwd_bf16<128>(a, c, s);
   }
-  Cross p = {q, k, v, kv_len, nullptr, nullptr, o, lse, nullptr, nullptr, nullptr, nullptr, c.ldq, c.ldkv, c.seq_q, c.seq_kv, c.batch, c.n_q, c.n_kv};
-  return c.d == 64 ? run<float, 64>(p, false, s) : run<float, 128>(p, false, s);
+  const CrossArgsOf<float> a = fwd_args<float>(c, q, k, v, kv_len, o, lse, ws);
+  return c.d == 64 ? cross_fwd_fp32<64>(a, c, s) : cross_fwd_fp32<128>(a, c, s);
 }
 hipError_t launch_cross_attn_bwd(int dtype, const CrossShape& c, const void* q, const void* k, const void* v, const int* kv_len, const void* o, const void* dout,
                                  const float* lse, void* dq, void* dk, void* dv, void* ws, hipStream_t s) {
   if (dtype == DT_BF16) {
-    CrossArgs a = cross_args(c, q, k, v, kv_len, (float*)ws);
-    a.o_in = (const bf16_t*)o; a.dout = (const bf16_t*)dout; a.lse = const_cast<float*>(lse);
-    a.dq = (bf16_t*)dq; a.dk = (bf16_t*)dk; a.dv = (bf16_t*)dv;
+    const CrossArgs a = bwd_args<bf16_t>(c, q, k, v, kv_len, o, dout, lse, dq, dk, dv, ws);
     return c.d == 64 ? cross_bwd_bf16<64>(a, c, s) : cross_bwd_bf16<128>(a, c, s);
   }
-  Cross p = {q, k, v, kv_len, o, dout, nullptr, const_cast<float*>(lse), dq, dk, dv, (float*)ws, c.ldq, c.ldkv, c.seq_q, c.seq_kv, c.batch, c.n_q, c.n_kv};
-  return c.d == 64 ? run<float, 64>(p, true, s) : run<float, 128>(p, true, s);
+  const CrossArgsOf<float> a = bwd_args<float>(c, q, k, v, kv_len, o, dout, lse, dq, dk, dv, ws);
+  return c.d == 64 ? cross_bwd_fp32<64>(a, c, s) : cross_bwd_fp32<128>(a, c, s);
 }
