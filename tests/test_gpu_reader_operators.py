@@ -88,6 +88,12 @@ def test_rope_axes(dtype, rows, n_rot, n_pass, d, inplace, back):
     rope_case(dtype, rows, n_rot, n_pass, d, AXES[d], 4, 50, (24, 8) if rows % 2 else (0, 0), inplace, back)
 
 
+@pytest.mark.parametrize("dtype,rows,n_rot,n_pass,d", [(BF16, 2900, 40, 4, 128), (FP32, 1001, 21, 11, 256), (BF16, 16001, 6, 6, 96)])
+@pytest.mark.parametrize("inplace,back", [(False, 0), (True, 1)])
+def test_rope_axes_of_rows_that_go_past_the_caches(dtype, rows, n_rot, n_pass, d, inplace, back):
+    rope_case(dtype, rows, n_rot, n_pass, d, AXES[d], 4, 300, (0, 0), inplace, back)
+
+
 @pytest.mark.parametrize("n_rot,n_pass", [(1, 0), (3, 2)])
 def test_rope_axes_narrow_fp32_heads(n_rot, n_pass):
     rope_case(FP32, 77, n_rot, n_pass, 8, AXES[8], 2, 9, (4, 0))
