@@ -14,6 +14,8 @@
 #include "attention_f32_tiles.h"
 #include "attention_tiles.h"
 
+#include <math.h>
+
 namespace {
 
 constexpr float LOWEST = -3.402823466e38f;
@@ -320,32 +322,43 @@ template <typename T> __device__ __forceinline__ void store8(T* at, const float 
   }
 }
 
-// o and lse of a row from its parts' sums, whose references are in units of `unit`: a thread has 8 columns
+// o and lse of a row from its parts' sums, whose references are in units of `unit`: a wave a row, a lane a part for its weight, then D / 64 columns
 template <typename T, int D> __global__ __launch_bounds__(256) void cross_fwd_join(const CrossArgsOf<T> p, size_t all_rows, float unit) {
-  constexpr int Q = D / 8;
-  const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x, stat = i / Q;
+  constexpr int E = D / 64, U = 8;
+  typedef float sums_t __attribute__((ext_vector_type(E)));
+  const size_t stat = (size_t)blockIdx.x * 4 + (threadIdx.x >> 6);
   if (stat >= all_rows) return;
-  const int col = (int)(i % Q) * 8;
+  const int lane = threadIdx.x & 63;
   const float c = unit * LOG2E;
   const float2* ml = reinterpret_cast<const float2*>(p.part + (size_t)p.splits * all_rows * D) + stat;
-  float m = -INFINITY, l = 0.f, x[8] = {};
-  for (int s = 0; s < p.splits; ++s) m = fmaxf(m, ml[s * all_rows].x);
-  for (int s = 0; s < p.splits; ++s) {
-    const float2 w = ml[s * all_rows];
-    if (w.x == -INFINITY) continue;                     // a part without states has left no sums
-    const float f = __builtin_amdgcn_exp2f((w.x - m) * c);
-    l = fmaf(w.y, f, l);
-    const f32x4_t* a = reinterpret_cast<const f32x4_t*>(p.part + (s * all_rows + stat) * D + col);
+  const float2 mine = lane < p.splits ? ml[lane * all_rows] : make_float2(-INFINITY, 0.f);
+  const float m = wave_max(mine.x);
+  const float f = mine.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((mine.x - m) * c), l = wave_sum(mine.y * f);
+  float x[E] = {};
+  const float* sums = p.part + stat * D + lane * E;
+  for (int s0 = 0; s0 < p.splits; s0 += U) {
+    sums_t v[U];
 #pragma unroll
-    for (int h = 0; h < 2; ++h)
+    for (int u = 0; u < U; ++u) {
+      // a part without states has left no sums; they come last
+      const bool on = s0 + u < p.splits && __shfl(mine.x, s0 + u, 64) != -INFINITY;
+      v[u] = sums_t(0.f);
+      if (on) v[u] = *reinterpret_cast<const sums_t*>(sums + (size_t)(s0 + u) * all_rows * D);
+    }
 #pragma unroll
-      for (int e = 0; e < 4; ++e) x[4 * h + e] = fmaf(a[h][e], f, x[4 * h + e]);
+    for (int u = 0; u < U; ++u) {
+      const float w = __shfl(f, (s0 + u) & 63, 64);
+#pragma unroll
+      for (int e = 0; e < E; ++e) x[e] = fmaf(v[u][e], w, x[e]);
+    }
   }
   const size_t t = stat % p.seq_q, a = stat / p.seq_q % p.n_q, b = stat / p.seq_q / p.n_q;
   const bool none = m == -INFINITY;
   const float inv = none ? 0.f : 1.f / l;
-  store8(p.o + ((b * p.seq_q + t) * p.n_q + a) * D + col, x, inv);
-  if (col == 0) p.lse[stat] = none ? -INFINITY : m * unit + logf(l);
+  T* o = p.o + ((b * p.seq_q + t) * p.n_q + a) * D + lane * E;
+#pragma unroll
+  for (int e = 0; e < E; ++e) o[e] = (T)(x[e] * inv);
+  if (lane == 0) p.lse[stat] = none ? -INFINITY : m * unit + logf(l);
 }
 
 // ---- backward, dQ: grid as forward ---------------------------------------------------------------------------------------------------
@@ -580,19 +593,21 @@ __device__ __forceinline__ RowBlocks row_blocks(const CrossArgs& p) { return {p.
 // an offset past every descriptor's end, whatever is added to it for a block: rows span less than 15 * 2^28 bytes
 constexpr unsigned PAST = 0xF0000000u;
 
-// ---- backward, dK / dV: grid (n_kv x splits x tiles of 128 KT states, batch), 4 NG waves --------------------------------------------------
-// A wave owns 32 KT states: K fragments, dK^T and dV^T in registers, the V rows of the workgroup's states in LDS.  Blocks of 64 rows (Q and dO, lse and -D) stream through
-// two stages; rows past the last one read as zeros and add nothing.  NG = 2: a second group of waves takes the other 32 rows of every block, and the first adds its sums.
-template <int D, int KT, int NG>
-__global__ __launch_bounds__(256 * NG) void cross_dkv_mfma(const CrossArgs p) {
+// ---- backward, dK / dV: grid (n_kv x splits x tiles of 128 states, batch), 8 waves --------------------------------------------------
+// A wave owns 32 states: K fragments, dK^T and dV^T in registers, the V rows of the workgroup's states in LDS.  Blocks of 64 rows (Q and dO, lse and -D) stream through
+// two stages; rows past the last one read as zeros and add nothing.  Two groups of four waves have the same states and 32 rows of every block each; the first
+// adds the second's sums at the end.  (64 states to a wave, one wave to a SIMD: 1629 us against 1650 for 64 / 8 heads x 4096 queries and states, forward's
+// dQ included, but 582 / 561 for 32 heads x 4096 x 2305 and 70 / 55 for 16 heads x 2 x 1024 x 577, by its fewer workgroups.)
+template <int D>
+__global__ __launch_bounds__(512) void cross_dkv_mfma(const CrossArgs p) {
   typedef Head<D> H;
   constexpr int ROWB = H::ROWB, TILE = H::TILE, NKS = H::NKS, NDT = H::NDT;
-  constexpr int WROWS = 16 / NG, NLD = WROWS / H::RPL;
+  constexpr int WROWS = 8, NLD = WROWS / H::RPL;
   constexpr int STAGE = 2 * TILE + 512;                 // Q tile, dO tile, 64 lse, 64 -D
   extern __shared__ __attribute__((aligned(16))) char smem[];
   const int tid = threadIdx.x, lane = tid & 63, g = lane >> 5, c32 = lane & 31;
-  const int id = __builtin_amdgcn_readfirstlane(tid >> 6), wave = id & 3, grp = NG == 1 ? 0 : id >> 2;
-  constexpr int WK = 32 * KT, GK = 4 * WK;
+  const int id = __builtin_amdgcn_readfirstlane(tid >> 6), wave = id & 3, grp = id >> 2;
+  constexpr int WK = 32, GK = 4 * WK;
   const int kvh = blockIdx.x % p.n_kv, at_x = blockIdx.x / p.n_kv, k0 = at_x / p.splits * GK, part = at_x % p.splits, b = blockIdx.y;
   const int n = __builtin_amdgcn_readfirstlane(cross_states(p, b));
   const int first_k = k0 + WK * wave;
@@ -601,7 +616,7 @@ __global__ __launch_bounds__(256 * NG) void cross_dkv_mfma(const CrossArgs p) {
   if (k0 >= n) {                                        // states that do not count have no gradient
     if (p.splits > 1) return;                           // the join writes their zeros
     const bf16x8_t zero = {};
-    for (int i = tid; i < GK * (D / 8); i += 256 * NG) {
+    for (int i = tid; i < GK * (D / 8); i += 512) {
       const int s = k0 + i / (D / 8), col = i % (D / 8) * 8;
       if (s >= p.seq_kv) break;
       *reinterpret_cast<bf16x8_t*>(p.dk + base + (size_t)s * p.ldkv + col) = zero;
@@ -609,20 +624,17 @@ __global__ __launch_bounds__(256 * NG) void cross_dkv_mfma(const CrossArgs p) {
     }
     return;
   }
-  bf16x8_t Kf[KT][NKS];
+  bf16x8_t Kf[NKS];
+  {
+    const bf16_t* kp = p.k + base + (size_t)min(first_k + c32, n - 1) * p.ldkv + 8 * g;
 #pragma unroll
-  for (int kk = 0; kk < KT; ++kk) {
-    const bf16_t* kp = p.k + base + (size_t)min(first_k + 32 * kk + c32, n - 1) * p.ldkv + 8 * g;
-#pragma unroll
-    for (int ks = 0; ks < NKS; ++ks) Kf[kk][ks] = *reinterpret_cast<const bf16x8_t*>(kp + 16 * ks);
+    for (int ks = 0; ks < NKS; ++ks) Kf[ks] = *reinterpret_cast<const bf16x8_t*>(kp + 16 * ks);
   }
-  f32x16_t accK[KT][NDT], accV[KT][NDT];                // lane = state, registers = d
+  f32x16_t accK[1][NDT], accV[1][NDT];                  // lane = state, registers = d
 #pragma unroll
-  for (int kk = 0; kk < KT; ++kk)
+  for (int dt = 0; dt < NDT; ++dt)
 #pragma unroll
-    for (int dt = 0; dt < NDT; ++dt)
-#pragma unroll
-      for (int v = 0; v < 16; ++v) { accK[kk][dt][v] = 0.f; accV[kk][dt][v] = 0.f; }
+    for (int v = 0; v < 16; ++v) { accK[0][dt][v] = 0.f; accV[0][dt][v] = 0.f; }
   const int lds0 = (int)(unsigned)(size_t)(lds_void_t*)smem;
   const int half = grp * 32, row4 = lds0 + 16 * g + half * 4;
   int rm_addr[NKS], tr_addr[NDT][2];
@@ -651,8 +663,8 @@ __global__ __launch_bounds__(256 * NG) void cross_dkv_mfma(const CrossArgs p) {
   {
     const i32x4_t rs_v = rows_desc(p.v + base + (size_t)first_k * p.ldkv, min(n - first_k, WK), (unsigned)p.ldkv * 2u, ROWB);
 #pragma unroll
-    for (int j0 = 0; j0 < 2 * KT * NLD; ++j0) {         // both groups read them: each loads its share
-      const int j = j0 + grp * 2 * KT * NLD, lr = H::RPL * j + lane / H::CH;
+    for (int j0 = 0; j0 < 2 * NLD; ++j0) {              // both groups read them: each loads its share
+      const int j = j0 + grp * 2 * NLD, lr = H::RPL * j + lane / H::CH;
       OPTSTAGE_TILE_LOAD((unsigned)(lds0 + 2 * STAGE + wave * WK * ROWB + j * 1024), (unsigned)lr * (unsigned)p.ldkv * 2u + (unsigned)((lane % H::CH) ^ H::swz(lr)) * 16u, rs_v);
     }
   }
@@ -683,128 +695,93 @@ __global__ __launch_bounds__(256 * NG) void cross_dkv_mfma(const CrossArgs p) {
                    :: "s"((unsigned)lds0 + stage * STAGE + 2 * TILE + id * 256), "v"(vo), "s"(id == 0 ? rs_l : rs_d) : "memory", "m0");
     }
   };
-  auto tr_frag = [&](int at, int dt, int tt, int u) {
-    return transposed8(tr_addr[dt][0] + at + (32 * tt + 16 * u) * ROWB, tr_addr[dt][1] + at + (32 * tt + 16 * u + 8) * ROWB);
-  };
-  auto rm_frag = [&](int at, int tt, int ks) { return *(const lds_bf16x8_t*)(unsigned)(rm_addr[ks] + at + tt * 32 * ROWB); };
+  auto tr_frag = [&](int at, int dt, int u) { return transposed8(tr_addr[dt][0] + at + 16 * u * ROWB, tr_addr[dt][1] + at + (16 * u + 8) * ROWB); };
+  auto rm_frag = [&](int at, int ks) { return *(const lds_bf16x8_t*)(unsigned)(rm_addr[ks] + at); };
 #define OPTSTAGE_MFMA_V(acc, a, b) asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+v"(acc) : "v"(a), "v"(b))
 #define OPTSTAGE_MFMA_0(acc, a, b) asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, 0" : "=&v"(acc) : "v"(a), "v"(b))
   auto block = [&](int it, int stage) __attribute__((always_inline)) {
     const int rows = p.seq_q < 64 ? rb.heads * p.seq_q : p.seq_q - 64 * (it % rb.per_head);
+    if (half >= rows) return;                           // the same for the whole wave: no rows in this half of the block
     const int sQ = stage * STAGE, sDO = sQ + TILE, sL = sQ + 2 * TILE, sD = sL + 256;
+    f32x16_t s, dp;                                     // lane = state, registers = rows half + 8 (v / 4) + 4 g + v % 4 of the block
+    f32x4_t nL[4];
+    bf16x8_t qf[2], df[2], vf[2];
+    qf[0] = rm_frag(sQ, 0);
 #pragma unroll
-    for (int tt = 0; tt < 2 / NG; ++tt) {
-      if (half + 32 * tt >= rows) continue;             // the same for the whole wave: no rows in this half of the block
-      f32x16_t s[KT], dp[KT];                           // lane = state, registers = rows 32 tt + 8 (v / 4) + 4 g + v % 4 of the block
-      f32x4_t nL[4];
-      f32x16_t negD;
-      bf16x8_t qf[2], df[2], vf[2][KT];
-      qf[0] = rm_frag(sQ, tt, 0);
-#pragma unroll
-      for (int ks = 0; ks < NKS; ++ks) {                // S = Q K^T
-        OPTSTAGE_SB();
-        if (ks < NKS - 1) {
-          qf[(ks + 1) & 1] = rm_frag(sQ, tt, ks + 1);
-        } else {
-          df[0] = rm_frag(sDO, tt, 0);
-#pragma unroll
-          for (int kk = 0; kk < KT; ++kk) vf[0][kk] = rm_frag(sV, kk, 0);
-        }
-        if (KT == 2 ? ks < 4 : ks == NKS - 1) nL[KT == 2 ? ks : 0] = *(const lds_f32x4_t*)(unsigned)(row4 + sL + (32 * tt + 8 * (KT == 2 ? ks : 0)) * 4);
-        if (ks >= NKS - 4) {
-          const f32x4_t d4 = *(const lds_f32x4_t*)(unsigned)(row4 + sD + (32 * tt + 8 * (ks - (NKS - 4))) * 4);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) (KT == 2 ? negD : dp[0])[4 * (ks - (NKS - 4)) + i] = d4[i];
-        }
-        OPTSTAGE_SB();
-        if (ks == 0) {
-#pragma unroll
-          for (int kk = 0; kk < KT; ++kk) OPTSTAGE_MFMA_0(s[kk], qf[0], Kf[kk][0]);
-        } else {
-#pragma unroll
-          for (int kk = 0; kk < KT; ++kk) OPTSTAGE_MFMA_V(s[kk], qf[ks & 1], Kf[kk][ks]);
-        }
-        OPTSTAGE_SB();
-        if (KT == 2 && ks >= NKS - 4) {
-#pragma unroll
-          for (int i = 0; i < 4; ++i) nL[ks - (NKS - 4)][i] *= -LOG2E;
-        }
+    for (int ks = 0; ks < NKS; ++ks) {                  // S = Q K^T
+      OPTSTAGE_SB();
+      if (ks < NKS - 1) {
+        qf[(ks + 1) & 1] = rm_frag(sQ, ks + 1);
+      } else {
+        df[0] = rm_frag(sDO, 0);
+        vf[0] = rm_frag(sV, 0);
+        nL[0] = *(const lds_f32x4_t*)(unsigned)(row4 + sL);
       }
+      if (ks >= NKS - 4) {                              // -D: the initial value of dP's accumulator
+        const f32x4_t d4 = *(const lds_f32x4_t*)(unsigned)(row4 + sD + 8 * (ks - (NKS - 4)) * 4);
 #pragma unroll
-      for (int ks = 0; ks < NKS; ++ks) {                // dP - D = dO V^T - D, the exponentials of S under its MFMAs
-        OPTSTAGE_SB();
-        if (ks < NKS - 1) {
-          df[(ks + 1) & 1] = rm_frag(sDO, tt, ks + 1);
-#pragma unroll
-          for (int kk = 0; kk < KT; ++kk) vf[(ks + 1) & 1][kk] = rm_frag(sV, kk, ks + 1);
-        }
-        constexpr int KL = NKS / 4;
-        if (KT == 1 && ks % KL == KL - 1 && ks / KL < 3)
-          nL[ks / KL + 1] = *(const lds_f32x4_t*)(unsigned)(row4 + sL + (32 * tt + 8 * (ks / KL + 1)) * 4);
-        OPTSTAGE_SB();
-        if (ks == 0) {
-#pragma unroll
-          for (int kk = 0; kk < KT; ++kk) {
-            if constexpr (KT == 2) asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %3" : "=&v"(dp[kk]) : "v"(df[0]), "v"(vf[0][kk]), "v"(negD));
-            else OPTSTAGE_MFMA_V(dp[kk], df[0], vf[0][kk]);
-          }
-          if (KT == 1) asm volatile("s_nop 7" ::: "memory");
-        } else {
-#pragma unroll
-          for (int kk = 0; kk < KT; ++kk) OPTSTAGE_MFMA_V(dp[kk], df[ks & 1], vf[ks & 1][kk]);
-        }
-        OPTSTAGE_SB();
-#pragma unroll
-        for (int e = 0; e < 16 / NKS; ++e) {
-          const int v = (16 / NKS) * ks + e;
-#pragma unroll
-          for (int kk = 0; kk < KT; ++kk) s[kk][v] = __builtin_amdgcn_exp2f(fmaf(s[kk][v], c, KT == 2 ? nL[v >> 2][v & 3] : nL[v >> 2][v & 3] * -LOG2E));
-        }
+        for (int i = 0; i < 4; ++i) dp[4 * (ks - (NKS - 4)) + i] = d4[i];
       }
       OPTSTAGE_SB();
-      bf16x8_t trf[2];                                  // dV^T += dO^T P, dS = P (dP - D) under its MFMAs (the first two cover dP's latency)
-      trf[0] = tr_frag(sDO, 0, tt, 0);
-#pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        bf16x8_t pr[KT];
-#pragma unroll
-        for (int kk = 0; kk < KT; ++kk) pr[kk] = pack8(s[kk], u);
-#pragma unroll
-        for (int dt = 0; dt < NDT; ++dt) {
-          const int i = u * NDT + dt;
-          OPTSTAGE_SB();
-          if (i < 2 * NDT - 1) trf[(i + 1) & 1] = tr_frag(sDO, (dt + 1) % NDT, tt, dt == NDT - 1 ? 1 : u);
-          else trf[0] = tr_frag(sQ, 0, tt, 0);
-          OPTSTAGE_SB();
-#pragma unroll
-          for (int kk = 0; kk < KT; ++kk) accV[kk][dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(trf[i & 1], pr[kk], accV[kk][dt], 0, 0, 0);
-          OPTSTAGE_SB();
-          if (KT == 1 && i == 0) asm volatile("s_nop 15" ::: "memory");   // dP has left the matrix unit
-#pragma unroll
-          for (int e = 0; e < 8 / NDT; ++e) {
-            const int v = (8 / NDT) * i + e;
-#pragma unroll
-            for (int kk = 0; kk < KT; ++kk) dp[kk][v] = s[kk][v] * dp[kk][v];
-          }
-        }
-      }
-#pragma unroll
-      for (int u = 0; u < 2; ++u) {                     // dK^T += Q^T dS
-        bf16x8_t d[KT];
-#pragma unroll
-        for (int kk = 0; kk < KT; ++kk) d[kk] = pack8(dp[kk], u);
-#pragma unroll
-        for (int dt = 0; dt < NDT; ++dt) {
-          const int i = u * NDT + dt;
-          OPTSTAGE_SB();
-          if (i < 2 * NDT - 1) trf[(i + 1) & 1] = tr_frag(sQ, (dt + 1) % NDT, tt, dt == NDT - 1 ? 1 : u);
-          OPTSTAGE_SB();
-#pragma unroll
-          for (int kk = 0; kk < KT; ++kk) accK[kk][dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(trf[i & 1], d[kk], accK[kk][dt], 0, 0, 0);
-        }
-      }
+      if (ks == 0) OPTSTAGE_MFMA_0(s, qf[0], Kf[0]);
+      else OPTSTAGE_MFMA_V(s, qf[ks & 1], Kf[ks]);
       OPTSTAGE_SB();
     }
+#pragma unroll
+    for (int ks = 0; ks < NKS; ++ks) {                  // dP - D = dO V^T - D, the exponentials of S under its MFMAs
+      OPTSTAGE_SB();
+      if (ks < NKS - 1) {
+        df[(ks + 1) & 1] = rm_frag(sDO, ks + 1);
+        vf[(ks + 1) & 1] = rm_frag(sV, ks + 1);
+      }
+      constexpr int KL = NKS / 4;                       // lse of the next four rows one step ahead of its exponentials
+      if (ks % KL == KL - 1 && ks / KL < 3) nL[ks / KL + 1] = *(const lds_f32x4_t*)(unsigned)(row4 + sL + 8 * (ks / KL + 1) * 4);
+      OPTSTAGE_SB();
+      OPTSTAGE_MFMA_V(dp, df[ks & 1], vf[ks & 1]);
+      if (ks == 0) asm volatile("s_nop 7" ::: "memory"); // the exponentials read S a few cycles after the matrix unit has written it
+      OPTSTAGE_SB();
+#pragma unroll
+      for (int e = 0; e < 16 / NKS; ++e) {
+        const int v = (16 / NKS) * ks + e;
+        s[v] = __builtin_amdgcn_exp2f(fmaf(s[v], c, nL[v >> 2][v & 3] * -LOG2E));
+      }
+    }
+    OPTSTAGE_SB();
+    bf16x8_t trf[2];                                    // dV^T += dO^T P, dS = P (dP - D) under its MFMAs
+    trf[0] = tr_frag(sDO, 0, 0);
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const bf16x8_t pr = pack8(s, u);
+#pragma unroll
+      for (int dt = 0; dt < NDT; ++dt) {
+        const int i = u * NDT + dt;
+        OPTSTAGE_SB();
+        if (i < 2 * NDT - 1) trf[(i + 1) & 1] = tr_frag(sDO, (dt + 1) % NDT, dt == NDT - 1 ? 1 : u);
+        else trf[0] = tr_frag(sQ, 0, 0);
+        OPTSTAGE_SB();
+        accV[0][dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(trf[i & 1], pr, accV[0][dt], 0, 0, 0);
+        OPTSTAGE_SB();
+        if (i == 0) asm volatile("s_nop 15" ::: "memory");   // dP has left the matrix unit
+#pragma unroll
+        for (int e = 0; e < 8 / NDT; ++e) {
+          const int v = (8 / NDT) * i + e;
+          dp[v] = s[v] * dp[v];
+        }
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {                       // dK^T += Q^T dS
+      const bf16x8_t d = pack8(dp, u);
+#pragma unroll
+      for (int dt = 0; dt < NDT; ++dt) {
+        const int i = u * NDT + dt;
+        OPTSTAGE_SB();
+        if (i < 2 * NDT - 1) trf[(i + 1) & 1] = tr_frag(sQ, (dt + 1) % NDT, dt == NDT - 1 ? 1 : u);
+        OPTSTAGE_SB();
+        accK[0][dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(trf[i & 1], d, accK[0][dt], 0, 0, 0);
+      }
+    }
+    OPTSTAGE_SB();
   };
 #undef OPTSTAGE_MFMA_V
 #undef OPTSTAGE_MFMA_0
@@ -819,47 +796,41 @@ __global__ __launch_bounds__(256 * NG) void cross_dkv_mfma(const CrossArgs p) {
       block(it + 1, 1);
     }
   }
-  if constexpr (NG == 2) {
-    __syncthreads();
-    if (grp == 1) meet_give<KT, NDT>(smem, wave, lane, accV);
-    __syncthreads();
-    if (grp == 0) meet_take<KT, NDT>(smem, wave, lane, accV);
-    __syncthreads();
-    if (grp == 1) meet_give<KT, NDT>(smem, wave, lane, accK);
-    __syncthreads();
-    if (grp == 1) return;
-    meet_take<KT, NDT>(smem, wave, lane, accK);
-  }
+  __syncthreads();
+  if (grp == 1) meet_give<1, NDT>(smem, wave, lane, accV);
+  __syncthreads();
+  if (grp == 0) meet_take<1, NDT>(smem, wave, lane, accV);
+  __syncthreads();
+  if (grp == 1) meet_give<1, NDT>(smem, wave, lane, accK);
+  __syncthreads();
+  if (grp == 1) return;
+  meet_take<1, NDT>(smem, wave, lane, accK);
   if (p.splits > 1 && it0 >= it1) return;               // the join counts the parts that have rows
-#pragma unroll
-  for (int kk = 0; kk < KT; ++kk) {
-    const int s = first_k + 32 * kk + c32;
-    if (s >= p.seq_kv) continue;
-    if (p.splits > 1) {
-      if (s >= n) continue;
-      float* out = p.part + (((size_t)part * gridDim.y + b) * p.seq_kv + s) * p.n_kv * 2 * D + (size_t)kvh * 2 * D;
-#pragma unroll
-      for (int dt = 0; dt < NDT; ++dt)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          f32x4_t rk, rv;
-#pragma unroll
-          for (int i = 0; i < 4; ++i) { rk[i] = accK[kk][dt][4 * j + i]; rv[i] = accV[kk][dt][4 * j + i]; }
-          *reinterpret_cast<f32x4_t*>(out + 32 * dt + 8 * j + 4 * g) = rk;
-          *reinterpret_cast<f32x4_t*>(out + D + 32 * dt + 8 * j + 4 * g) = rv;
-        }
-      continue;
-    }
-    bf16_t *krow = p.dk + base + (size_t)s * p.ldkv, *vrow = p.dv + base + (size_t)s * p.ldkv;
+  const int s = first_k + c32;
+  if (s >= p.seq_kv) return;
+  if (p.splits > 1) {
+    if (s >= n) return;
+    float* out = p.part + (((size_t)part * gridDim.y + b) * p.seq_kv + s) * p.n_kv * 2 * D + (size_t)kvh * 2 * D;
 #pragma unroll
     for (int dt = 0; dt < NDT; ++dt)
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        OPTSTAGE_SB();
-        store4_if(krow + 32 * dt + 8 * j + 4 * g, accK[kk][dt], 4 * j, scale, s < n && n > 1);
-        store4_if(vrow + 32 * dt + 8 * j + 4 * g, accV[kk][dt], 4 * j, 1.f, s < n);
+        f32x4_t rk, rv;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { rk[i] = accK[0][dt][4 * j + i]; rv[i] = accV[0][dt][4 * j + i]; }
+        *reinterpret_cast<f32x4_t*>(out + 32 * dt + 8 * j + 4 * g) = rk;
+        *reinterpret_cast<f32x4_t*>(out + D + 32 * dt + 8 * j + 4 * g) = rv;
       }
+    return;
   }
+  bf16_t *krow = p.dk + base + (size_t)s * p.ldkv, *vrow = p.dv + base + (size_t)s * p.ldkv;
+#pragma unroll
+  for (int dt = 0; dt < NDT; ++dt)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      store4_if(krow + 32 * dt + 8 * j + 4 * g, accK[0][dt], 4 * j, scale, s < n && n > 1);
+      store4_if(vrow + 32 * dt + 8 * j + 4 * g, accV[0][dt], 4 * j, 1.f, s < n);
+    }
 }
 
 // dk and dv of a state and kv head from the parts' sums; a thread has 8 columns of one of them
@@ -888,30 +859,41 @@ template <typename T, int D> __global__ __launch_bounds__(256) void cross_dkv_jo
 
 // ---- how a call is divided -------------------------------------------------------------------------------------------------------------
 struct CrossPlan { int waves, tiles, splits; };
+constexpr int MOST_SPLITS = 64;                         // the join's lanes
 
-// forward and dQ: rows of 32 to a wave; parts of the states where the workgroups are fewer than the chip holds
+// Forward and dQ: 32 rows to a wave; parts of the states where the workgroups are fewer than the chip holds.
+//  * Two waves to a workgroup where that many tiles of 128 rows would be few: 8 heads x 300 queries and states 9.8 us, four waves 11.1; 8 x 512 x 4096 29.6 / 27.4;
+//    one token of 32 / 8 heads over 16384 states 21.0 / 21.6 (one wave 22.4, eight 24).
+//  * Up to 64 rows a workgroup waits for its blocks (1.1 us each) and the join costs 5 us and some 0.2 a part: about the root of twice the blocks.  One token of 32 / 8
+//    heads, 16384 states (256 blocks): 1 part 272 us, 8 42, 16 26, 32 21, 64 27; 4 sequences of 16, 16 / 4 heads, 2000 states (32): 38, 8 14.4, 16 15.5.  Many sequences
+//    need fewer, but of unequal length more than two workgroups to a compute unit: 16 x 8 heads, up to 16384 states 2 parts 155, 4 103, 8 83, 16 82 us.
+//  * More rows are bound by the matrix unit: one workgroup per compute unit.  8 heads x 700 queries x 2000 states (48 tiles): 1 part 40, 4 24.3, 8 26.5.
 CrossPlan plan_rows(const CrossShape& c) {
   const long rows = (long)(c.n_q / c.n_kv) * c.seq_q, groups = (long)c.n_kv * c.batch;
   CrossPlan p;
-  p.waves = rows <= 32 ? 1 : rows <= 64 ? 2 : 4;
-  if (rows > 128 && groups * ((rows + 255) / 256) >= 448) p.waves = 8;
+  p.waves = rows <= 64 || groups * ((rows + 127) / 128) <= 24 ? 2 : 4;
   p.tiles = (int)((rows + 32 * p.waves - 1) / (32 * p.waves));
-  const long wgs = groups * p.tiles, blocks = (c.seq_kv + 63) / 64, want = p.waves == 8 ? 256 : p.waves == 4 ? 512 : 1024;
-  long splits = wgs >= want / 2 ? 1 : want / wgs;
-  splits = splits < blocks / 4 ? splits : blocks / 4;
+  const long wgs = groups * p.tiles, blocks = (c.seq_kv + 63) / 64;
+  long splits = 1;
+  if (blocks >= 8 && wgs <= (rows <= 64 ? 384 : 128)) {
+    splits = (rows <= 64 ? 1024 : 256) / wgs;
+    const long root = (long)ceil(sqrt(2.0 * (double)blocks));
+    splits = splits < root ? splits : root;
+    splits = splits < MOST_SPLITS ? splits : MOST_SPLITS;
+  }
   p.splits = splits < 1 ? 1 : (int)splits;
   return p;
 }
-// dK / dV: 256 states to a workgroup (heads of 128), parts of the rows
+// dK / dV: 128 states to a workgroup, one to a compute unit; parts of the rows, of eight blocks at least (both kernels and the joins, us: 32 / 8 heads x 4096 x 1024, 64
+// workgroups: 1 part 488, 2 318, 4 257; 16 heads x 2 x 1024 x 577, 160: 55, 2 parts 76; 8 x 512 x 4096, 256: 58 / 83)
 CrossPlan plan_states(const CrossShape& c) {
   const long groups = (long)c.n_kv * c.batch;
   CrossPlan p;
-  p.waves = c.d == 128 && c.seq_kv > 128 ? 2 : 1;       // states of 128 a workgroup
-  const int gk = 128 * p.waves;
-  p.tiles = (c.seq_kv + gk - 1) / gk;
+  p.waves = 8;
+  p.tiles = (c.seq_kv + 127) / 128;
   const long wgs = groups * p.tiles, blocks = row_blocks(c.seq_q, c.n_q / c.n_kv).all;
-  long splits = wgs >= 192 ? 1 : 256 / wgs;
-  splits = splits < blocks / 2 ? splits : blocks / 2;
+  long splits = wgs >= 160 ? 1 : 256 / wgs;
+  splits = splits < blocks / 8 ? splits : blocks / 8;
   p.splits = splits < 1 ? 1 : (int)splits;
   return p;
 }
@@ -943,12 +925,12 @@ template <int D, int NW> hipError_t run_dq(const CrossArgs& a, const CrossPlan& 
   hipLaunchKernelGGL(kern, dim3((unsigned)a.n_kv * pl.tiles * pl.splits, batch), dim3(64 * NW), smem, s, a);
   return hipGetLastError();
 }
-template <int D, int KT, int NG> hipError_t run_dkv(const CrossArgs& a, const CrossPlan& pl, int batch, hipStream_t s) {
-  constexpr int smem = 2 * (2 * Head<D>::TILE + 512) + 2 * KT * Head<D>::TILE;
+template <int D> hipError_t run_dkv(const CrossArgs& a, const CrossPlan& pl, int batch, hipStream_t s) {
+  constexpr int smem = 2 * (2 * Head<D>::TILE + 512) + 2 * Head<D>::TILE;
   static LdsAttrOnce once;
-  auto kern = cross_dkv_mfma<D, KT, NG>;
+  auto kern = cross_dkv_mfma<D>;
   if (hipError_t e = once.ensure(reinterpret_cast<const void*>(kern), smem); e != hipSuccess) return e;
-  hipLaunchKernelGGL(kern, dim3((unsigned)a.n_kv * pl.tiles * pl.splits, batch), dim3(256 * NG), smem, s, a);
+  hipLaunchKernelGGL(kern, dim3((unsigned)a.n_kv * pl.tiles * pl.splits, batch), dim3(512), smem, s, a);
   return hipGetLastError();
 }
 unsigned joins(size_t items) { return (unsigned)((items + 255) / 256); }
@@ -956,22 +938,16 @@ unsigned joins(size_t items) { return (unsigned)((items + 255) / 256); }
 template <int D> hipError_t cross_fwd_bf16(CrossArgs a, const CrossShape& c, hipStream_t s) {
   const CrossPlan pl = bounded(plan_rows(c), c, rows_part_bytes);
   a.splits = pl.splits;
-  hipError_t e = pl.waves == 1   ? run_fwd<D, 1>(a, pl, c.batch, s)
-                 : pl.waves == 2 ? run_fwd<D, 2>(a, pl, c.batch, s)
-                 : pl.waves == 4 ? run_fwd<D, 4>(a, pl, c.batch, s)
-                                 : run_fwd<D, 8>(a, pl, c.batch, s);
+  hipError_t e = pl.waves == 2 ? run_fwd<D, 2>(a, pl, c.batch, s) : run_fwd<D, 4>(a, pl, c.batch, s);
   if (e != hipSuccess || pl.splits == 1) return e;
   const size_t all = (size_t)c.batch * c.n_q * c.seq_q;
-  hipLaunchKernelGGL((cross_fwd_join<bf16_t, D>), dim3(joins(all * (D / 8))), dim3(256), 0, s, a, all, 1.f / sqrtf((float)D));
+  hipLaunchKernelGGL((cross_fwd_join<bf16_t, D>), dim3((unsigned)((all + 3) / 4)), dim3(256), 0, s, a, all, 1.f / sqrtf((float)D));
   return hipGetLastError();
 }
 template <int D> hipError_t cross_bwd_bf16(CrossArgs a, const CrossShape& c, hipStream_t s) {
   CrossPlan pl = bounded(plan_rows(c), c, rows_part_bytes);
   a.splits = pl.splits;
-  hipError_t e = pl.waves == 1   ? run_dq<D, 1>(a, pl, c.batch, s)
-                 : pl.waves == 2 ? run_dq<D, 2>(a, pl, c.batch, s)
-                 : pl.waves == 4 ? run_dq<D, 4>(a, pl, c.batch, s)
-                                 : run_dq<D, 8>(a, pl, c.batch, s);
+  hipError_t e = pl.waves == 2 ? run_dq<D, 2>(a, pl, c.batch, s) : run_dq<D, 4>(a, pl, c.batch, s);
   if (e != hipSuccess) return e;
   if (pl.splits > 1) {
     const size_t all = (size_t)c.batch * c.n_q * c.seq_q;
@@ -980,8 +956,7 @@ template <int D> hipError_t cross_bwd_bf16(CrossArgs a, const CrossShape& c, hip
   }
   pl = bounded(plan_states(c), c, states_part_bytes);
   a.splits = pl.splits;
-  if constexpr (D == 128) e = pl.waves == 2 ? run_dkv<D, 2, 1>(a, pl, c.batch, s) : run_dkv<D, 1, 2>(a, pl, c.batch, s);
-  else e = run_dkv<D, 1, 2>(a, pl, c.batch, s);
+  e = run_dkv<D>(a, pl, c.batch, s);
   if (e != hipSuccess || pl.splits == 1) return e;
   hipLaunchKernelGGL((cross_dkv_join<bf16_t, D>), dim3(joins((size_t)c.batch * c.seq_kv * c.n_kv * (2 * D / 8))), dim3(256), 0, s, a, (size_t)c.batch);
   return hipGetLastError();
@@ -1224,6 +1199,7 @@ CrossPlan plan_f32(const CrossShape& c, bool states) {
   const long wgs = (long)c.n_kv * c.batch * p.tiles, other = states ? rows : keys;
   long splits = wgs >= 512 ? 1 : 1024 / wgs;
   splits = splits < other / 8 ? splits : other / 8;
+  splits = splits < MOST_SPLITS ? splits : MOST_SPLITS;
   p.splits = splits < 1 ? 1 : (int)splits;
   return bounded(p, c, states ? states_part_bytes : rows_part_bytes);
 }
@@ -1235,7 +1211,7 @@ template <int D> hipError_t cross_fwd_fp32(CrossArgsOf<float> a, const CrossShap
   if (pl.splits > 1) {
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     const size_t all = (size_t)c.batch * c.n_q * c.seq_q;
-    hipLaunchKernelGGL((cross_fwd_join<float, D>), dim3(joins(all * (D / 8))), dim3(256), 0, s, a, all, 1.f);
+    hipLaunchKernelGGL((cross_fwd_join<float, D>), dim3((unsigned)((all + 3) / 4)), dim3(256), 0, s, a, all, 1.f);
   }
   return hipGetLastError();
 }
