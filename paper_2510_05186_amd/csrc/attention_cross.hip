@@ -397,11 +397,8 @@ __global__ __launch_bounds__(64 * NW) void cross_dq_mfma(const CrossArgs p) {
     }
     Lc = -p.lse[stat] * LOG2E;
     Dq = dsum + __shfl_xor(dsum, 32, 64);
-    if (part == 0 && g == 0 && mine) p.delta[stat] = -Dq;
   }
   f32x16_t negD;                                        // the initial value of the dP^T MFMAs, which then deliver dP^T - D
-#pragma unroll
-  for (int v = 0; v < 16; ++v) negD[v] = -Dq;
 #pragma unroll
   for (int ks = 0; ks < NKS; ++ks) asm volatile("" : "+a"(Qf[ks]), "+a"(dOf[ks]));
   f32x16_t acc[NDT];
@@ -452,52 +449,56 @@ __global__ __launch_bounds__(64 * NW) void cross_dq_mfma(const CrossArgs p) {
   auto rm_frag = [&](int at, int tt, int ks) { return *(const lds_bf16x8_t*)(unsigned)(rm_addr[ks] + at + tt * 32 * ROWB); };
 #define OPTSTAGE_MFMA_V(acc, a, b) asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+v"(acc) : "v"(a), "a"(b))
 #define OPTSTAGE_MFMA_0(acc, a, b) asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, 0" : "=&v"(acc) : "v"(a), "a"(b))
+  // P^T and dP^T - D of the tile of 32 states from key0 on, half tt of a stage; P is 0 behind the last state
+  auto weights = [&](int sK, int tt, int key0, f32x16_t& s, f32x16_t& dp) __attribute__((always_inline)) {
+    const int sV = sK + TILE;
+    bf16x8_t kf[2], vf[2];
+    kf[0] = rm_frag(sK, tt, 0);
+#pragma unroll
+    for (int ks = 0; ks < NKS; ++ks) {                  // S^T = K Q^T
+      OPTSTAGE_SB();
+      if (ks < NKS - 1) kf[(ks + 1) & 1] = rm_frag(sK, tt, ks + 1);
+      else vf[0] = rm_frag(sV, tt, 0);
+      OPTSTAGE_SB();
+      if (ks == 0) OPTSTAGE_MFMA_0(s, kf[0], Qf[0]);
+      else OPTSTAGE_MFMA_V(s, kf[ks & 1], Qf[ks]);
+    }
+#pragma unroll
+    for (int ks = 0; ks < NKS; ++ks) {                  // dP^T = V dO^T, the exponentials of S^T under its MFMAs
+      OPTSTAGE_SB();
+      if (ks < NKS - 1) vf[(ks + 1) & 1] = rm_frag(sV, tt, ks + 1);
+      OPTSTAGE_SB();
+      if (ks == 0) {
+        asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %3" : "=&v"(dp) : "v"(vf[0]), "a"(dOf[0]), "v"(negD));
+        asm volatile("s_nop 7" ::: "memory");           // the exponentials read S^T a few cycles after the matrix unit has written it
+      } else {
+        OPTSTAGE_MFMA_V(dp, vf[ks & 1], dOf[ks]);
+      }
+      OPTSTAGE_SB();
+#pragma unroll
+      for (int e = 0; e < 16 / NKS; ++e) {
+        const int v = (16 / NKS) * ks + e;
+        s[v] = __builtin_amdgcn_exp2f(fmaf(s[v], c, Lc));
+      }
+    }
+    OPTSTAGE_SB();
+    if (key0 + 32 > n) {
+      asm volatile("" ::: "memory");                    // a real branch: only the last tile pays for the mask
+#pragma unroll
+      for (int v = 0; v < 16; ++v)
+        if (key0 + 8 * (v >> 2) + 4 * g + (v & 3) >= n) s[v] = 0.f;
+    }
+    asm volatile("s_nop 15\n\ts_nop 7" ::: "memory");   // dP^T has left the matrix unit
+    OPTSTAGE_SB();
+  };
   auto block = [&](int blk, int stage) __attribute__((always_inline)) {
-    const int sK = stage * STAGE, sV = sK + TILE;
+    const int sK = stage * STAGE;
 #pragma unroll
     for (int tt = 0; tt < 2; ++tt) {
       const int key0 = 64 * blk + 32 * tt;
       if (key0 >= n) continue;                          // the same for the whole workgroup
-      const bool edge = key0 + 32 > n;
       f32x16_t s, dp;                                   // lane = row, registers = states key0 + 8 (v / 4) + 4 g + v % 4
-      bf16x8_t kf[2], vf[2];
-      kf[0] = rm_frag(sK, tt, 0);
-#pragma unroll
-      for (int ks = 0; ks < NKS; ++ks) {                // S^T = K Q^T
-        OPTSTAGE_SB();
-        if (ks < NKS - 1) kf[(ks + 1) & 1] = rm_frag(sK, tt, ks + 1);
-        else vf[0] = rm_frag(sV, tt, 0);
-        OPTSTAGE_SB();
-        if (ks == 0) OPTSTAGE_MFMA_0(s, kf[0], Qf[0]);
-        else OPTSTAGE_MFMA_V(s, kf[ks & 1], Qf[ks]);
-      }
-#pragma unroll
-      for (int ks = 0; ks < NKS; ++ks) {                // dP^T = V dO^T, the exponentials of S^T under its MFMAs
-        OPTSTAGE_SB();
-        if (ks < NKS - 1) vf[(ks + 1) & 1] = rm_frag(sV, tt, ks + 1);
-        OPTSTAGE_SB();
-        if (ks == 0) {
-          asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %3" : "=&v"(dp) : "v"(vf[0]), "a"(dOf[0]), "v"(negD));
-          asm volatile("s_nop 7" ::: "memory");         // the exponentials read S^T a few cycles after the matrix unit has written it
-        } else {
-          OPTSTAGE_MFMA_V(dp, vf[ks & 1], dOf[ks]);
-        }
-        OPTSTAGE_SB();
-#pragma unroll
-        for (int e = 0; e < 16 / NKS; ++e) {
-          const int v = (16 / NKS) * ks + e;
-          s[v] = __builtin_amdgcn_exp2f(fmaf(s[v], c, Lc));
-        }
-      }
-      OPTSTAGE_SB();
-      if (edge) {
-        asm volatile("" ::: "memory");                  // a real branch: only the last tile pays for the mask
-#pragma unroll
-        for (int v = 0; v < 16; ++v)
-          if (key0 + 8 * (v >> 2) + 4 * g + (v & 3) >= n) s[v] = 0.f;
-      }
-      asm volatile("s_nop 15\n\ts_nop 7" ::: "memory"); // dP^T has left the matrix unit
-      OPTSTAGE_SB();
+      weights(sK, tt, key0, s, dp);
       bf16x8_t trf[2];                                  // dQ^T += K^T dS^T; dS^T of the second half under the MFMAs of the first
       trf[0] = tr_frag(sK, 0, tt, 0);
 #pragma unroll
@@ -525,9 +526,27 @@ __global__ __launch_bounds__(64 * NW) void cross_dq_mfma(const CrossArgs p) {
       OPTSTAGE_SB();
     }
   };
-#undef OPTSTAGE_MFMA_V
-#undef OPTSTAGE_MFMA_0
   if (kb.first < kb.end) issue_block(kb.first, 0);
+#pragma unroll
+  for (int v = 0; v < 16; ++v) negD[v] = -Dq;
+  if (n <= 64 && kb.first < kb.end) {
+    // Few states: what o's rounding leaves in D is large against dP - D (2 states: dq 2.2 times as far from 64 bits as one rounding, 16 states 1.5; from some 64 on
+    // 1.45, dS's own rounding).  All of them are in this block: D is corrected by the sum of P (dP - D), which has to be 0.
+    OPTSTAGE_BLOCK_SYNC();
+    float sum = 0.f;
+#pragma unroll
+    for (int tt = 0; tt < 2; ++tt) {
+      if (32 * tt >= n) continue;
+      f32x16_t s, dp;
+      weights(0, tt, 32 * tt, s, dp);
+#pragma unroll
+      for (int v = 0; v < 16; ++v) sum = fmaf(s[v], dp[v], sum);
+    }
+    Dq += sum + __shfl_xor(sum, 32, 64);
+#pragma unroll
+    for (int v = 0; v < 16; ++v) negD[v] = -Dq;
+  }
+  if (part == 0 && g == 0 && mine) p.delta[stat] = -Dq;
   for (int blk = kb.first; blk < kb.end; blk += 2) {
     OPTSTAGE_BLOCK_SYNC();
     if (blk + 1 < kb.end) issue_block(blk + 1, 1);
@@ -538,6 +557,8 @@ __global__ __launch_bounds__(64 * NW) void cross_dq_mfma(const CrossArgs p) {
       block(blk + 1, 1);
     }
   }
+#undef OPTSTAGE_MFMA_V
+#undef OPTSTAGE_MFMA_0
   if (!mine) return;
   if (p.splits > 1) {
     if (kb.first >= kb.end) return;                     // the join counts the parts that have states

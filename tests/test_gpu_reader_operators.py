@@ -235,6 +235,12 @@ class Cross:
                     D = (p * dp).sum(1, keepdims=True)
                     ds = p * (dp - D)
                     e_D = np.abs((g * o[i, :, a]).sum(1, keepdims=True) - D) + (d + 4) * EPS * (np.abs(g) * np.abs(o[i, :, a])).sum(1, keepdims=True)
+                    if self.dtype == BF16 and n <= 64:
+                        # few states: D0 = <dout, o> is corrected by the sum of p (dp - D0), off by what its terms and their sum are, and by what the sum of p lacks of one
+                        D0 = (g * o[i, :, a]).sum(1, keepdims=True)
+                        off = (e_p + (n + d + 16) * EPS) * p
+                        e_D = (off * (np.abs(dp - D0) + np.abs(D0))).sum(1, keepdims=True) + (d + 4) * EPS * (p * (np.abs(g) @ np.abs(v).T)).sum(1, keepdims=True) + FLUSH
+                        e_D = e_D + (d + 8) * EPS * (np.abs(g) * np.abs(o[i, :, a])).sum(1, keepdims=True)
                     e_ds = np.abs(ds) * (e_p + low + 4 * EPS) + p * (1 + e_p) * (e_D + (d + 4) * EPS * (np.abs(g) @ np.abs(v).T))
                     e_ds = e_ds + FLUSH * (2 + np.abs(dp - D))
                     if n == 1:
