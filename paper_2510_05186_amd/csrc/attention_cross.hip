@@ -1211,15 +1211,281 @@ template <int D> __global__ __launch_bounds__(256) void cross_dkv_f32(const Cros
   }
 }
 
-// parts where tiles of 16 rows are fewer than two to a compute unit: at least eight of the other side's to a part
+// Many rows (states): 16 to a wave, 64 to a workgroup, which read every tile of the other side from LDS, where its threads have put it (the next tile's loads
+// are in flight meanwhile, two buffers); the kernels above read theirs from the caches, once per wave.  Which pays: wide_pays.
+template <int D> struct Staged {
+  static constexpr int LD = D + 4, H = D / 64;          // floats to a row in LDS: 16 rows' chunks fall on all banks
+  f32x4_t v[H];
+  // this thread's pieces of 16 rows: at(row) is where row 0 <= row < 16 starts, null for zeros
+  template <typename F> __device__ __forceinline__ void load(F at) {
+#pragma unroll
+    for (int h = 0; h < H; ++h) {
+      const int i = threadIdx.x + 256 * h, row = i / (D / 4), c = (i % (D / 4)) * 4;
+      const float* p = at(row);
+      v[h] = p ? *reinterpret_cast<const f32x4_t*>(p + c) : f32x4_t{0.f, 0.f, 0.f, 0.f};
+    }
+  }
+  __device__ __forceinline__ void put(float (*lds)[LD]) const {
+#pragma unroll
+    for (int h = 0; h < H; ++h) {
+      const int i = threadIdx.x + 256 * h;
+      *reinterpret_cast<f32x4_t*>(&lds[i / (D / 4)][(i % (D / 4)) * 4]) = v[h];
+    }
+  }
+};
+// four columns of a result row: 64 h + 16 g + 4 v
+template <int NT> __device__ __forceinline__ f32x4_t result4(const f32x4_t (&acc)[NT], int h, int v) {
+  return f32x4_t{acc[4 * h][v], acc[4 * h + 1][v], acc[4 * h + 2][v], acc[4 * h + 3][v]};
+}
+
+template <int D> __global__ __launch_bounds__(256) void cross_fwd_f32_wide(const CrossArgsOf<float> p) {
+  typedef F32<D> F;
+  constexpr int LD = Staged<D>::LD;
+  __shared__ __attribute__((aligned(16))) float sK[2][ROWS][LD], sV[2][ROWS][LD];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, g = lane >> 4;
+  const int kvh = blockIdx.x % p.n_kv, at_x = blockIdx.x / p.n_kv, tile = at_x / p.splits, part = at_x % p.splits, b = blockIdx.y;
+  const int n = cross_states(p, b), tiles = (n + ROWS - 1) / ROWS, per = (tiles + p.splits - 1) / p.splits, t0 = min(tiles, part * per), t1 = min(tiles, t0 + per);
+  const size_t all_rows = (size_t)gridDim.y * p.n_kv * p.rows, stat0 = ((size_t)b * p.n_kv + kvh) * p.rows;
+  const size_t base = (size_t)b * p.seq_kv * p.ldkv + (size_t)kvh * D;
+  const int row = 4 * ROWS * tile + ROWS * wave + r;
+  const RowAt at = row_at(p, b, min(row, p.rows - 1));
+  f32x4_t q[F::S], acc[F::NT];
+  F::rows(q, p.q + at.token * p.ldq + (size_t)(kvh * p.rep + at.head) * D, g);
+  F::scaled(q, rsqrtf((float)D));
+  F::clear(acc);
+  float m = LOWEST, l = 0.f;
+  Staged<D> kn, vn;
+  auto fetch = [&](int t) {
+    kn.load([&](int i) { return ROWS * t + i < n ? p.k + base + (size_t)(ROWS * t + i) * p.ldkv : nullptr; });
+    vn.load([&](int i) { return ROWS * t + i < n ? p.v + base + (size_t)(ROWS * t + i) * p.ldkv : nullptr; });
+  };
+  if (t0 < t1) {
+    fetch(t0);
+    kn.put(sK[0]);
+    vn.put(sV[0]);
+  }
+  __syncthreads();
+  for (int t = t0, buf = 0; t < t1; ++t, buf ^= 1) {
+    if (t + 1 < t1) fetch(t + 1);
+    f32x4_t k[F::S], v[4][F::H];
+    F::rows(k, sK[buf][r], g);
+    f32x4_t s = F::product(k, q);                       // s[e]: state 16 t + 4 g + e, row r
+    F::columns(v, sV[buf][0], LD, 0, ROWS - 1, g, r);
+    if (ROWS * t + ROWS > n) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (ROWS * t + 4 * g + e >= n) s[e] = -INFINITY;
+    }
+    const float mn = fmaxf(m, max_g(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3]))));
+    const float alpha = expf(m - mn);
+    f32x4_t w;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) w[e] = expf(s[e] - mn);
+    l = l * alpha + (w[0] + w[1]) + (w[2] + w[3]);
+#pragma unroll
+    for (int i = 0; i < F::NT; ++i)
+#pragma unroll
+      for (int x = 0; x < 4; ++x) acc[i][x] *= alpha;
+    F::accumulate(acc, v, w);
+    m = mn;
+    if (t + 1 < t1) {
+      kn.put(sK[buf ^ 1]);
+      vn.put(sV[buf ^ 1]);
+    }
+    __syncthreads();
+  }
+  l = sum_g(l);
+  if (row >= p.rows) return;
+  const size_t stat = stat0 + row;
+  if (p.splits > 1) {
+    if (g == 0) *reinterpret_cast<float2*>(p.part + (size_t)p.splits * all_rows * D + ((size_t)part * all_rows + stat) * 2) = t0 < t1 ? make_float2(m, l) : make_float2(-INFINITY, 0.f);
+    if (t0 >= t1) return;
+  }
+  float* out = p.splits > 1 ? p.part + ((size_t)part * all_rows + stat) * D : p.o + (at.token * p.n_q + kvh * p.rep + at.head) * D;
+  const float inv = p.splits > 1 ? 1.f : n ? 1.f / l : 0.f;
+#pragma unroll
+  for (int h = 0; h < F::H; ++h)
+#pragma unroll
+    for (int v = 0; v < 4; ++v) {
+      f32x4_t x = result4(acc, h, v);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[e] *= inv;
+      *reinterpret_cast<f32x4_t*>(out + 64 * h + 16 * g + 4 * v) = x;
+    }
+  if (p.splits == 1 && g == 0) p.lse[stat] = n ? m + logf(l) : -INFINITY;
+}
+
+template <int D> __global__ __launch_bounds__(256) void cross_dq_f32_wide(const CrossArgsOf<float> p) {
+  typedef F32<D> F;
+  constexpr int LD = Staged<D>::LD;
+  __shared__ __attribute__((aligned(16))) float sK[2][ROWS][LD], sV[2][ROWS][LD];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, g = lane >> 4;
+  const int kvh = blockIdx.x % p.n_kv, at_x = blockIdx.x / p.n_kv, tile = at_x / p.splits, part = at_x % p.splits, b = blockIdx.y;
+  const int n = cross_states(p, b), tiles = n == 1 ? 0 : (n + ROWS - 1) / ROWS, per = (tiles + p.splits - 1) / p.splits, t0 = min(tiles, part * per), t1 = min(tiles, t0 + per);
+  const size_t base = (size_t)b * p.seq_kv * p.ldkv + (size_t)kvh * D, stat0 = ((size_t)b * p.n_kv + kvh) * p.rows;
+  const float scale = rsqrtf((float)D);
+  const int row = 4 * ROWS * tile + ROWS * wave + r, rowc = min(row, p.rows - 1);
+  const RowAt at = row_at(p, b, rowc);
+  const size_t col = (size_t)(kvh * p.rep + at.head) * D;
+  f32x4_t q[F::S], dO[F::S], acc[F::NT];
+  float dsum = 0.f;
+  {
+    f32x4_t x[F::S];
+    F::rows(q, p.q + at.token * p.ldq + col, g);
+    F::rows(dO, p.dout + at.token * p.n_q * D + col, g);
+    F::rows(x, p.o_in + at.token * p.n_q * D + col, g);
+#pragma unroll
+    for (int s = 0; s < F::S; ++s)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) dsum = fmaf(dO[s][e], x[s][e], dsum);
+  }
+  F::scaled(q, scale);
+  F::clear(acc);
+  dsum = sum_g(dsum);
+  const float L = p.lse[stat0 + rowc];
+  if (part == 0 && g == 0 && row < p.rows) p.delta[stat0 + row] = dsum;
+  Staged<D> kn, vn;
+  auto fetch = [&](int t) {
+    kn.load([&](int i) { return ROWS * t + i < n ? p.k + base + (size_t)(ROWS * t + i) * p.ldkv : nullptr; });
+    vn.load([&](int i) { return ROWS * t + i < n ? p.v + base + (size_t)(ROWS * t + i) * p.ldkv : nullptr; });
+  };
+  if (t0 < t1) {
+    fetch(t0);
+    kn.put(sK[0]);
+    vn.put(sV[0]);
+  }
+  __syncthreads();
+  for (int t = t0, buf = 0; t < t1; ++t, buf ^= 1) {
+    if (t + 1 < t1) fetch(t + 1);
+    f32x4_t x[F::S], kc[4][F::H], ds;
+    F::rows(x, sK[buf][r], g);
+    const f32x4_t s = F::product(x, q);
+    F::rows(x, sV[buf][r], g);
+    const f32x4_t dp = F::product(x, dO);
+    F::columns(kc, sK[buf][0], LD, 0, ROWS - 1, g, r);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) ds[e] = ROWS * t + 4 * g + e >= n ? 0.f : expf(s[e] - L) * (dp[e] - dsum);
+    F::accumulate(acc, kc, ds);
+    if (t + 1 < t1) {
+      kn.put(sK[buf ^ 1]);
+      vn.put(sV[buf ^ 1]);
+    }
+    __syncthreads();
+  }
+  if (row >= p.rows || (p.splits > 1 && t0 >= t1)) return;
+  float* out = p.splits > 1 ? p.part + ((size_t)part * gridDim.y * p.n_kv * p.rows + stat0 + row) * D : p.dq + at.token * p.ldq + col;
+  const float f = p.splits > 1 ? 1.f : scale;
+#pragma unroll
+  for (int h = 0; h < F::H; ++h)
+#pragma unroll
+    for (int v = 0; v < 4; ++v) {
+      f32x4_t x = result4(acc, h, v);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[e] *= f;
+      *reinterpret_cast<f32x4_t*>(out + 64 * h + 16 * g + 4 * v) = x;
+    }
+}
+
+// rows past the last one are zeros with lse and D zero: a weight of one times nothing
+template <int D> __global__ __launch_bounds__(256) void cross_dkv_f32_wide(const CrossArgsOf<float> p) {
+  typedef F32<D> F;
+  constexpr int LD = Staged<D>::LD;
+  __shared__ __attribute__((aligned(16))) float sQ[2][ROWS][LD], sG[2][ROWS][LD], sL[2][ROWS], sD[2][ROWS];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, g = lane >> 4;
+  const int kvh = blockIdx.x % p.n_kv, at_x = blockIdx.x / p.n_kv, k0 = at_x / p.splits * 4 * ROWS, part = at_x % p.splits, b = blockIdx.y;
+  const int n = cross_states(p, b), tiles = (p.rows + ROWS - 1) / ROWS, per = (tiles + p.splits - 1) / p.splits, t0 = min(tiles, part * per), t1 = min(tiles, t0 + per);
+  const size_t base = (size_t)b * p.seq_kv * p.ldkv + (size_t)kvh * D, stat0 = ((size_t)b * p.n_kv + kvh) * p.rows;
+  const float scale = rsqrtf((float)D);
+  if (p.splits > 1 && (k0 >= n || t0 >= t1)) return;    // the join counts the parts that have rows, and writes zeros
+  const int state = k0 + ROWS * wave + r;
+  f32x4_t ak[F::NT], av[F::NT];
+  F::clear(ak);
+  F::clear(av);
+  if (k0 < n) {
+    f32x4_t k[F::S], v[F::S];
+    const size_t at = base + (size_t)min(state, n - 1) * p.ldkv;
+    F::rows(k, p.k + at, g);
+    F::rows(v, p.v + at, g);
+    F::scaled(k, scale);
+    Staged<D> qn, gn;
+    float ln = 0.f;
+    auto fetch = [&](int t) {
+      auto place = [&](int i, const float* x, size_t ld) {
+        const int row = ROWS * t + i;
+        if (row >= p.rows) return (const float*)nullptr;
+        const RowAt a = row_at(p, b, row);
+        return x + a.token * ld + (size_t)(kvh * p.rep + a.head) * D;
+      };
+      qn.load([&](int i) { return place(i, p.q, p.ldq); });
+      gn.load([&](int i) { return place(i, p.dout, (size_t)p.n_q * D); });
+      if (threadIdx.x < 2 * ROWS) {
+        const int row = ROWS * t + (threadIdx.x & (ROWS - 1));
+        ln = row < p.rows ? (threadIdx.x < ROWS ? p.lse : p.delta)[stat0 + row] : 0.f;
+      }
+    };
+    auto put = [&](int buf) {
+      qn.put(sQ[buf]);
+      gn.put(sG[buf]);
+      if (threadIdx.x < 2 * ROWS) (threadIdx.x < ROWS ? sL : sD)[buf][threadIdx.x & (ROWS - 1)] = ln;
+    };
+    if (t0 < t1) {
+      fetch(t0);
+      put(0);
+    }
+    __syncthreads();
+    for (int t = t0, buf = 0; t < t1; ++t, buf ^= 1) {
+      if (t + 1 < t1) fetch(t + 1);
+      f32x4_t x[F::S], c[4][F::H], w, ds;
+      F::rows(x, sQ[buf][r], g);
+      const f32x4_t s = F::product(x, k);               // [e]: row 16 t + 4 g + e, state r
+      F::rows(x, sG[buf][r], g);
+      const f32x4_t dp = F::product(x, v);
+      const f32x4_t L = *reinterpret_cast<const f32x4_t*>(&sL[buf][4 * g]), Dr = *reinterpret_cast<const f32x4_t*>(&sD[buf][4 * g]);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        w[e] = expf(s[e] - L[e]);
+        ds[e] = n > 1 ? w[e] * (dp[e] - Dr[e]) : 0.f;   // one state has no gradient of its score
+      }
+      F::columns(c, sG[buf][0], LD, 0, ROWS - 1, g, r);
+      F::accumulate(av, c, w);
+      F::columns(c, sQ[buf][0], LD, 0, ROWS - 1, g, r);
+      F::accumulate(ak, c, ds);
+      if (t + 1 < t1) put(buf ^ 1);
+      __syncthreads();
+    }
+  }
+  if (state >= p.seq_kv || (p.splits > 1 && state >= n)) return;
+#pragma unroll
+  for (int which = 0; which < 2; ++which) {
+    float* out = p.splits > 1 ? p.part + ((((size_t)part * gridDim.y + b) * p.seq_kv + state) * p.n_kv + kvh) * 2 * D + which * D
+                              : (which ? p.dv : p.dk) + base + (size_t)state * p.ldkv;
+    const bool on = state < n && (which || n > 1);
+    const float f = p.splits > 1 || which ? 1.f : scale;
+#pragma unroll
+    for (int h = 0; h < F::H; ++h)
+#pragma unroll
+      for (int v = 0; v < 4; ++v) {
+        f32x4_t x = which ? result4(av, h, v) : result4(ak, h, v);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[e] = on ? x[e] * f : 0.f;
+        *reinterpret_cast<f32x4_t*>(out + 64 * h + 16 * g + 4 * v) = x;
+      }
+  }
+}
+
+// 64 rows (states) to a workgroup (`waves` 4), or 16 whose waves divide the other side (1).  Forward and backward, us, 16 / 64: 16 heads of 64 x 512 x 512 (128 workgroups of 64)
+// 84 / 97, 4 x 16 heads x 512 x 1024 508 / 411, 8 heads of 128 x 2048 x 2048 1017 / 773, 4 heads x 4096 x 4096 1984 / 1486; fewer workgroups but a long other side, 8 / 2
+// heads x 2048 x 2048 (64 of states, 512 tiles of rows) 1022 / 801.
+bool wide_pays(long wide_wgs, long others) { return wide_wgs > 128 || (wide_wgs >= 48 && others >= 128); }
 CrossPlan plan_f32(const CrossShape& c, bool states) {
-  const long rows = ((long)(c.n_q / c.n_kv) * c.seq_q + ROWS - 1) / ROWS, keys = (c.seq_kv + ROWS - 1) / ROWS;
+  const long mine = states ? c.seq_kv : (long)(c.n_q / c.n_kv) * c.seq_q, others = ((states ? (long)(c.n_q / c.n_kv) * c.seq_q : c.seq_kv) + ROWS - 1) / ROWS;
+  const long groups = (long)c.n_kv * c.batch;
   CrossPlan p;
-  p.waves = 4;
-  p.tiles = (int)(states ? keys : rows);
-  const long wgs = (long)c.n_kv * c.batch * p.tiles, other = states ? rows : keys;
-  long splits = wgs >= 512 ? 1 : 1024 / wgs;
-  splits = splits < other / 8 ? splits : other / 8;
+  p.waves = wide_pays(groups * ((mine + 63) / 64), others) ? 4 : 1;
+  p.tiles = (int)((mine + ROWS * p.waves - 1) / (ROWS * p.waves));
+  const long wgs = groups * p.tiles;
+  long splits = p.waves == 4 ? (wgs >= 384 ? 1 : 512 / wgs) : (wgs >= 512 ? 1 : 1024 / wgs);
+  splits = splits < others / 8 ? splits : others / 8;
   splits = splits < MOST_SPLITS ? splits : MOST_SPLITS;
   p.splits = splits < 1 ? 1 : (int)splits;
   return bounded(p, c, states ? states_part_bytes : rows_part_bytes);
@@ -1228,7 +1494,9 @@ CrossPlan plan_f32(const CrossShape& c, bool states) {
 template <int D> hipError_t cross_fwd_fp32(CrossArgsOf<float> a, const CrossShape& c, hipStream_t s) {
   const CrossPlan pl = plan_f32(c, false);
   a.splits = pl.splits;
-  hipLaunchKernelGGL(cross_fwd_f32<D>, dim3((unsigned)a.n_kv * pl.tiles * pl.splits, c.batch), dim3(256), 0, s, a);
+  const dim3 grid((unsigned)a.n_kv * pl.tiles * pl.splits, c.batch);
+  if (pl.waves == 4) hipLaunchKernelGGL(cross_fwd_f32_wide<D>, grid, dim3(256), 0, s, a);
+  else hipLaunchKernelGGL(cross_fwd_f32<D>, grid, dim3(256), 0, s, a);
   if (pl.splits > 1) {
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     const size_t all = (size_t)c.batch * c.n_q * c.seq_q;
@@ -1239,7 +1507,9 @@ template <int D> hipError_t cross_fwd_fp32(CrossArgsOf<float> a, const CrossShap
 template <int D> hipError_t cross_bwd_fp32(CrossArgsOf<float> a, const CrossShape& c, hipStream_t s) {
   CrossPlan pl = plan_f32(c, false);
   a.splits = pl.splits;
-  hipLaunchKernelGGL(cross_dq_f32<D>, dim3((unsigned)a.n_kv * pl.tiles * pl.splits, c.batch), dim3(256), 0, s, a);
+  dim3 grid((unsigned)a.n_kv * pl.tiles * pl.splits, c.batch);
+  if (pl.waves == 4) hipLaunchKernelGGL(cross_dq_f32_wide<D>, grid, dim3(256), 0, s, a);
+  else hipLaunchKernelGGL(cross_dq_f32<D>, grid, dim3(256), 0, s, a);
   if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
   if (pl.splits > 1) {
     const size_t all = (size_t)c.batch * c.n_q * c.seq_q;
@@ -1249,7 +1519,9 @@ template <int D> hipError_t cross_bwd_fp32(CrossArgsOf<float> a, const CrossShap
   pl = plan_f32(c, true);
   a.splits = pl.splits;
   a.row_blocks = (a.rows + ROWS - 1) / ROWS;
-  hipLaunchKernelGGL(cross_dkv_f32<D>, dim3((unsigned)a.n_kv * pl.tiles * pl.splits, c.batch), dim3(256), 0, s, a);
+  grid.x = (unsigned)a.n_kv * pl.tiles * pl.splits;
+  if (pl.waves == 4) hipLaunchKernelGGL(cross_dkv_f32_wide<D>, grid, dim3(256), 0, s, a);
+  else hipLaunchKernelGGL(cross_dkv_f32<D>, grid, dim3(256), 0, s, a);
   if (pl.splits > 1) {
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     hipLaunchKernelGGL((cross_dkv_join<float, D>), dim3(joins((size_t)c.batch * c.seq_kv * c.n_kv * (2 * D / 8))), dim3(256), 0, s, a, (size_t)c.batch);
@@ -1282,6 +1554,12 @@ template <typename T> CrossArgsOf<T> bwd_args(const CrossShape& c, const void* q
 }
 
 }  // namespace
+
+int cross_attn_form(int dtype, int states, int seq_q, int seq_kv, int batch, int n_q, int n_kv, int d) {
+  const CrossShape c = {0, 0, seq_q, seq_kv, batch, n_q, n_kv, d};
+  const CrossPlan p = dtype != DT_BF16 ? plan_f32(c, states != 0) : states ? bounded(plan_states(c), c, states_part_bytes) : bounded(plan_rows(c), c, rows_part_bytes);
+  return 1000 * p.waves + p.splits;
+}
 
 // D of every row, and the parts' sums of whichever launch needs most
 uint64_t cross_attn_ws_bytes(int dtype, int seq_q, int seq_kv, int batch, int n_q, int n_kv, int d) {

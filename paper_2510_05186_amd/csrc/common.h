@@ -226,6 +226,9 @@ hipError_t launch_cross_attn_fwd(int dtype, const CrossShape& c, const void* q, 
                                  hipStream_t s);
 hipError_t launch_cross_attn_bwd(int dtype, const CrossShape& c, const void* q, const void* k, const void* v, const int* kv_len, const void* o, const void* dout,
                                  const float* lse, void* dq, void* dk, void* dv, void* ws, hipStream_t s);
+// the form that a call's forward and dQ launches (states = 0) or its dK / dV launch take by its sizes: 1000 times the waves that have rows (states) of their own, plus
+// the parts of the other side
+int cross_attn_form(int dtype, int states, int seq_q, int seq_kv, int batch, int n_q, int n_kv, int d);
 uint64_t cross_attn_ws_bytes(int dtype, int seq_q, int seq_kv, int batch, int n_q, int n_kv, int d);
 // loss and lse (null: lse is read, the gradient alone), dz (null: no gradient)
 hipError_t launch_distill(int dtype, const void* z, size_t ldz, const int* ids, const float* teacher, const float* dloss, float* loss, float* lse, void* dz, size_t lddz,

@@ -302,6 +302,17 @@ def test_cross_attention_of_many_queries_over_a_few_states(dtype, b, nq, nk, hq,
     cross_both(Cross(dtype, b, nq, nk, hq, hkv, d))
 
 
+# (batch, queries, states, heads, kv heads, head size) -> the forms that they take: test_reader_operators_refusals.py holds them to that
+FORMS = {(4, 520, 100, 4, 4, 64): None, (4, 520, 400, 4, 4, 64): [400, 77, 0, 399], (4, 520, 600, 4, 4, 128): [1, 600, 130, 64], (4, 100, 600, 8, 4, 64): [600, 599, 2, 31], (4, 300, 600, 4, 4, 64): None,
+         (2, 1100, 700, 4, 2, 64): [700, 65], (1, 1100, 2300, 4, 1, 128): None}
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+@pytest.mark.parametrize("shape", FORMS)
+def test_cross_attention_of_every_division(dtype, shape):
+    cross_both(Cross(dtype, *shape, FORMS[shape]))
+
+
 @pytest.mark.parametrize("dtype", [BF16, FP32])
 @pytest.mark.parametrize("d", [64, 128])
 @pytest.mark.parametrize("size", [8.0, 60.0])

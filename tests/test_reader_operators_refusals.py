@@ -1,4 +1,6 @@
 """What rotary positions with several axes, cross attention and the loss against a teacher's top entries refuse, on the host: nothing is launched, addresses are never read."""
+import ctypes
+
 import pytest
 
 from paper_2510_05186_amd import binding as B
@@ -108,3 +110,18 @@ def test_distillation_workspace():
     assert f(0, 10, 1) == 0 and f(4, 0, 1) == 0 and f(4, 10, 0) == 0 and f(4, 10, 1025) == 0
     assert "workspace" in distill_fwd(ws_bytes=f(4, 100, 5) - 1)
     assert all(0 < f(rows, vocab, 64) <= 1 << 20 for rows in (1, 7, 200, 5000, 1 << 20) for vocab in (1, 1000, 131072, 1 << 20))
+
+
+def test_the_sizes_tested_take_every_form():
+    """cross_attn_form(dtype, states, seq_q, seq_kv, batch, n_q, n_kv, d): waves with rows of their own * 1000 + parts of the other side."""
+    f = ctypes.CDLL(B.LIB_PATH)["_Z15cross_attn_formiiiiiiii"]
+    form = lambda dt, states, b, nq, nk, hq, hkv, d: divmod(f(dt, states, nq, nk, b, hq, hkv, d), 1000)  # noqa: E731
+    shapes = [(4, 520, 100, 4, 4, 64), (4, 520, 400, 4, 4, 64), (4, 520, 600, 4, 4, 128), (4, 100, 600, 8, 4, 64), (4, 300, 600, 4, 4, 64), (2, 1100, 700, 4, 2, 64), (1, 1100, 2300, 4, 1, 128),
+              (1, 300, 1, 2, 1, 128), (1, 1, 4099, 8, 1, 128), (1, 3000, 50, 2, 1, 128), (1, 257, 16, 2, 2, 64), (2, 300, 900, 8, 2, 128)]
+    seen = {(dt, states, form(dt, states, *s)[0], form(dt, states, *s)[1] > 1) for s in shapes for dt in (FP32, BF16) for states in (0, 1)}
+    assert seen == {(BF16, 0, w, s) for w in (2, 4) for s in (False, True)} | {(BF16, 1, 8, s) for s in (False, True)} | {(FP32, st, w, s) for st in (0, 1) for w in (1, 4) for s in (False, True)}, seen
+    # never more parts than the join's lanes, or than 256 MiB of sums
+    for b, nq, nk, hq, hkv, d in shapes + [(1, 1, 1 << 22, 64, 1, 128), (1, 16, 1 << 20, 128, 16, 128), (16, 64, 60000, 64, 8, 128)]:
+        for dt in (FP32, BF16):
+            assert 1 <= form(dt, 0, b, nq, nk, hq, hkv, d)[1] <= 64
+            assert 1 <= form(dt, 1, b, nq, nk, hq, hkv, d)[1] <= 256
