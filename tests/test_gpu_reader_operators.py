@@ -701,6 +701,21 @@ def test_distillation_offsets_beyond_32_bits():
     assert torch.allclose(loss[-5:], c.loss.repeat(2)[rows % 5:rows % 5 + 5], rtol=1e-5)
 
 
+@pytest.mark.parametrize("dtype,rows,vocab", [(BF16, 640, 131080), (FP32, 330, 131075), (BF16, 300, 66001)])
+def test_distillation_gradient_of_logits_that_go_past_the_caches(dtype, rows, vocab):
+    """Rows of a few patterns: from lse, a row's gradient is the same bits however many rows there are."""
+    c = Distill(dtype, 5, vocab, 7, bare=True)
+    want = c.call("apart").clone()
+    torch.cuda.synchronize()
+    c.check(want)
+    rep = lambda t: t.view(5, -1).repeat(rows // 5, 1).contiguous()  # noqa: E731
+    z, i, t, g, lse = (rep(x) for x in (c.z, c.i, c.t, c.g, c.lse))
+    for dz in (torch.empty_like(z), z):
+        ok(lib().optstage_op_distill_bwd(dtype, z.data_ptr(), vocab, i.data_ptr(), t.data_ptr(), lse.data_ptr(), g.data_ptr(), dz.data_ptr(), vocab, rows, vocab, 7, 1.0, 0, stream()))
+        torch.cuda.synchronize()
+        assert torch.equal(dz.view(-1, 5, vocab), want.view(1, 5, vocab).expand(rows // 5, 5, vocab))
+
+
 # ------------------------------------------------------------------ together
 @pytest.mark.parametrize("dtype", [BF16, FP32])
 def test_a_training_step_of_a_reading_layer_with_a_teacher(dtype):
