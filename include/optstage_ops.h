@@ -188,7 +188,7 @@ uint64_t optstage_op_embed_bwd_ws_bytes(uint32_t rows, uint32_t hidden);
  * ld_dst: n_rot heads of head_dim that are rotated, then n_pass (may be 0) that are not (copied where dst is not src).  Pair i of a head, elements i and
  * i + head_dim / 2, turns by table[p][i] (optstage_op_rope_table's entries, or the caller's own frequencies) with p = positions[axis[i]][row]; backward != 0 turns
  * back (gradients).  positions: DEVICE int32 [n_axes][rows] (any address of an int32); axis: HOST, head_dim / 2 bytes, read before the call returns, each below
- * n_axes, or 255 for a pair that does not turn.  Nor does one whose position is negative or >= n_positions (padding).  head_dim is a multiple of 16 (fp32:
+ * n_axes, or 255 for a pair that does not turn.  Nor does one whose position is negative or >= n_positions (padding): it stays as it is, whatever it holds.  head_dim is a multiple of 16 (fp32:
  * 8), at most 256; ld_src and ld_dst are multiples of 8 (fp32: 4).  dst may be src (with ld_dst = ld_src). */
 optstage_status optstage_op_rope_axes(uint32_t dtype, const void* src, uint32_t ld_src, void* dst, uint32_t ld_dst, const float* table, uint32_t n_positions,
                                       const int32_t* positions, uint32_t n_axes, const uint8_t* axis, uint32_t rows, uint32_t n_rot, uint32_t n_pass,
@@ -218,7 +218,8 @@ uint64_t optstage_op_cross_attn_ws_bytes(uint32_t dtype, uint32_t seq_q, uint32_
  *   loss[r] = sum over j of t_j (log t_j - log p[ids_j]),  lse[r] = log of the sum of exp(z / temperature)                         (fp32 [rows])
  *   dz[r][v] = dloss[r] / temperature * (p_v * sum of all t_j - sum of t_j with ids_j = v)
  * A teacher's entry of minus infinity has t = 0 and adds nothing.  A row without entries has loss 0 and gradient 0, and so has the gradient of a row whose
- * dloss is 0 (padding), whatever its logits are.  dz rows lie lddz apart; columns past vocab are neither read nor written; dz may be z (with lddz = ldz).
+ * dloss is 0 (padding), whatever its logits are.  From lse (distill_bwd) a gradient is off by up to 2^-24 |lse| of p more, which rows of logits in the thousands feel;
+ * optstage_op_distill has the row's own sum.  dz rows lie lddz apart; columns past vocab are neither read nor written; dz may be z (with lddz = ldz).
  * k is at most 1024, temperature from 1e-30 to 1e30.  z and dz: 16-byte aligned, any ldz and lddz >= vocab.  ws: DEVICE scratch of
  * at least optstage_op_distill_ws_bytes() bytes, belonging to a call until its work has run. */
 optstage_status optstage_op_distill_fwd(uint32_t dtype, const void* z, uint32_t ldz, const int32_t* ids, const float* teacher, float* loss, float* lse, void* ws,

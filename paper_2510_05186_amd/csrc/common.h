@@ -219,7 +219,7 @@ int embed_bwd_order(int rows, unsigned vocab);
 int embed_bwd_places(int dtype, int rows, unsigned vocab, int h);
 // positions: [axes][rows]; axis: HOST, the axis of each of the d / 2 pairs, 255 for none
 hipError_t launch_rope_axes(int dtype, const void* src, size_t ld_src, void* dst, size_t ld_dst, const float* table, int n_positions, const int* positions,
-                            const uint8_t* axis, int rows, int n_rot, int n_pass, int d, int backward, hipStream_t s);
+                            int n_axes, const uint8_t* axis, int rows, int n_rot, int n_pass, int d, int backward, hipStream_t s);
 // queries [batch seq_q] and states [batch seq_kv], rows ldq and ldkv elements apart
 struct CrossShape { size_t ldq, ldkv; int seq_q, seq_kv, batch, n_q, n_kv, d; };
 hipError_t launch_cross_attn_fwd(int dtype, const CrossShape& c, const void* q, const void* k, const void* v, const int* kv_len, void* o, float* lse, void* ws,

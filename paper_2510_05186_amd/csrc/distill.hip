@@ -393,6 +393,7 @@ template <typename T, int NT, int R> __global__ __launch_bounds__(NT) __attribut
       give(__builtin_bit_cast(chunk_t, held[r]), r);
       held[r] = __builtin_bit_cast(u32x4_t, fetch(zn, r));
     }
+    // (stores of one workgroup's waves to a place arrive there in the order that the barrier gives them: the entries' values come to stay)
     __syncthreads();
     if (threadIdx.x >= NT - 64) {                       // the loss, by the wave that has the fewest entries to write
       double sum = 0.0;
@@ -637,18 +638,22 @@ template <typename T> hipError_t run_parts(Distill p, bool whole, hipStream_t s)
 
 template <typename T> hipError_t run(const Distill& p, hipStream_t s) {
   if (p.rows < FEW_ROWS) return run_parts<T>(p, false, s);
-  if (!p.loss || !p.dz) return run_parts<T>(p, true, s);
-  for (int first = 0; first < p.rows; first += ROWS_A_LAUNCH) {
+  const bool both = p.loss && p.dz;
+  const int most = both ? ROWS_A_LAUNCH : 1 << 22;      // one direction: a launch's 2^30 threads
+  for (int first = 0; first < p.rows; first += most) {
     Distill q = p;
-    q.rows = p.rows - first < ROWS_A_LAUNCH ? p.rows - first : ROWS_A_LAUNCH;
+    q.rows = p.rows - first < most ? p.rows - first : most;
     q.z = (const T*)p.z + first * p.ldz;
-    q.dz = (T*)p.dz + first * p.lddz;
     q.ids += (size_t)first * p.k;
     q.teacher += (size_t)first * p.k;
-    q.dloss += first;
-    q.loss += first;
     q.lse += first;
-    if (hipError_t e = p.vocab >= Vec16<T>::N ? run_both<T>(q, s) : run_parts<T>(q, true, s); e != hipSuccess) return e;
+    if (p.dz) {
+      q.dz = (T*)p.dz + first * p.lddz;
+      q.dloss += first;
+    }
+    if (p.loss) q.loss += first;
+    if (hipError_t e = both && p.vocab >= Vec16<T>::N ? run_both<T>(q, s) : run_parts<T>(q, true, s); e != hipSuccess) return e;
+    if (p.rows - first <= most) break;
   }
   return hipSuccess;
 }

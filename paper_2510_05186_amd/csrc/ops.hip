@@ -443,7 +443,7 @@ optstage_status optstage_op_rope_axes(uint32_t dtype, const void* src, uint32_t 
   REQ(src != dst || ld_src == ld_dst, "rope_axes: in place, ld_dst must be ld_src");
   REQ(n_axes >= 1 && n_axes <= 4, "rope_axes: 1 to 4 axes");
   for (uint32_t i = 0; i < head_dim / 2; ++i) REQ(axis[i] < n_axes || axis[i] == 255, "rope_axes: a pair's axis is neither below n_axes nor 255");
-  return wrap(launch_rope_axes((int)dtype, src, ld_src, dst, ld_dst, table, (int)n_positions, positions, axis, (int)rows, (int)n_rot, (int)n_pass, (int)head_dim,
+  return wrap(launch_rope_axes((int)dtype, src, ld_src, dst, ld_dst, table, (int)n_positions, positions, (int)n_axes, axis, (int)rows, (int)n_rot, (int)n_pass, (int)head_dim,
                                backward ? 1 : 0, (hipStream_t)stream),
               "rope_axes");
 }

@@ -15,10 +15,10 @@ constexpr int NT = 256, MAX_PAIRS = 128, MOST_HEADS = 6;
 struct RopeAxes {
   const void* src; void* dst; const float2* table; const int* positions;
   size_t ld_src, ld_dst;
-  int rows, n_positions, n_rot, n_heads, d;
-  int rows_per_group, head_step;
+  int first, rows, n_positions, n_rot, n_heads, d;                     // a launch's rows: first .. rows - 1
+  int rows_per_group, head_step, n_axes;
   float sign;
-  uint8_t axis[MAX_PAIRS];
+  alignas(8) uint8_t axis[MAX_PAIRS];
 };
 
 // TWOS: pairs 2 i and 2 i + 1 share an axis, 16 bytes of the table at a time.  PAST: rows go past the caches in both directions.
@@ -27,7 +27,7 @@ template <typename T, int U, bool TWOS, bool PAST> __global__ __launch_bounds__(
   constexpr int N = V::N;
   const int half = p.d / 2, vph = half / N, c = (int)(threadIdx.x % vph) * N, slot = threadIdx.x / vph;
   const int r_in = slot / p.head_step, h0 = slot % p.head_step;
-  const size_t row = (size_t)blockIdx.x * p.rows_per_group + r_in;
+  const size_t row = p.first + (size_t)blockIdx.x * p.rows_per_group + r_in;
   if (r_in >= p.rows_per_group || row >= (size_t)p.rows) return;
   const T* src = (const T*)p.src + row * p.ld_src + c;
   T* dst = (T*)p.dst + row * p.ld_dst + c;
@@ -52,14 +52,27 @@ template <typename T, int U, bool TWOS, bool PAST> __global__ __launch_bounds__(
       }
     }
   };
+  typedef unsigned axes_t __attribute__((ext_vector_type(N / 4)));
+  const axes_t axes = *reinterpret_cast<const axes_t*>(p.axis + c);  // of this thread's pairs, a byte each
+  int pos[4];                                                        // requested ahead of the heads: what is asked for first arrives first
+#pragma unroll
+  for (int a = 0; a < 4; ++a) pos[a] = p.positions[(size_t)min(a, p.n_axes - 1) * p.rows + row];
+  __builtin_amdgcn_sched_barrier(0);
   load(h0);
+  __builtin_amdgcn_sched_barrier(0);
   float co[N], si[N];
+  unsigned still = 0;                                                // pairs that do not turn stay as they are, whatever they hold
 #pragma unroll
   for (int e = 0; e < N; e += TWOS ? 2 : 1) {
-    const int a = p.axis[c + e];
-    const int pos = a != 255 ? p.positions[(size_t)a * p.rows + row] : -1;
-    const bool on = (unsigned)pos < (unsigned)p.n_positions;         // outside the table, and for axis 255: not turned
-    const float2* at = p.table + (size_t)(on ? pos : 0) * half + c + e;
+    const unsigned a = axes[e / 4] >> 8 * (e % 4) & 255u;
+    int at_a = pos[0];
+    at_a = a == 1 ? pos[1] : at_a;
+    at_a = a == 2 ? pos[2] : at_a;
+    at_a = a == 3 ? pos[3] : at_a;
+    at_a = a == 255 ? -1 : at_a;
+    const bool on = (unsigned)at_a < (unsigned)p.n_positions;        // outside the table, and for axis 255: not turned
+    if (!on) still |= (TWOS ? 3u : 1u) << e;
+    const float2* at = p.table + (size_t)(on ? at_a : 0) * half + c + e;
     if constexpr (TWOS) {
       const f32x4_t t = *reinterpret_cast<const f32x4_t*>(at);
       co[e] = on ? t[0] : 1.f;
@@ -71,6 +84,23 @@ template <typename T, int U, bool TWOS, bool PAST> __global__ __launch_bounds__(
       co[e] = on ? t.x : 1.f;
       si[e] = on ? t.y * p.sign : 0.f;
     }
+  }
+  if (__any(still != 0)) {                                           // a loop of its own: the other one's is 9 % slower with the choice in it
+    for (int h = h0; h < p.n_heads; h += p.head_step) {
+      V x = in(src + (size_t)h * p.d), y = in(src + (size_t)h * p.d + half);
+      if (h < p.n_rot) {
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+          if (still >> e & 1) continue;
+          const float a = x.get(e), b = y.get(e);
+          x.set(e, a * co[e] - b * si[e]);
+          y.set(e, b * co[e] + a * si[e]);
+        }
+      }
+      out(dst + (size_t)h * p.d, x);
+      out(dst + (size_t)h * p.d + half, y);
+    }
+    return;
   }
   for (int first = h0;;) {
 #pragma unroll
@@ -97,15 +127,15 @@ template <typename T, int U, bool TWOS, bool PAST> __global__ __launch_bounds__(
 // Rows of 32 MB and more in all go past the caches (8192 rows of 80 heads of 128, both directions: 166 -> 140 us; 16384 of 12 57 -> 45), fewer do not: 1000
 // rows of 48 heads 19.1 -> 19.6, and whoever reads them next finds them there.
 constexpr double PAST_BYTES = 32e6;
-template <typename T, int U> void run(const RopeAxes& p, bool twos, hipStream_t s) {
-  const dim3 grid((p.rows + p.rows_per_group - 1) / p.rows_per_group);
+constexpr int MOST_GROUPS = 1 << 23;                    // 2^31 threads a launch
+template <typename T, int U> void run(RopeAxes p, bool twos, hipStream_t s) {
   const bool past = (double)p.rows * p.n_heads * p.d * sizeof(T) >= PAST_BYTES;
-  if (past) {
-    if (twos) hipLaunchKernelGGL((rope_axes_kernel<T, U, true, true>), grid, dim3(NT), 0, s, p);
-    else hipLaunchKernelGGL((rope_axes_kernel<T, U, false, true>), grid, dim3(NT), 0, s, p);
-  } else {
-    if (twos) hipLaunchKernelGGL((rope_axes_kernel<T, U, true, false>), grid, dim3(NT), 0, s, p);
-    else hipLaunchKernelGGL((rope_axes_kernel<T, U, false, false>), grid, dim3(NT), 0, s, p);
+  auto* kern = past ? (twos ? rope_axes_kernel<T, U, true, true> : rope_axes_kernel<T, U, false, true>)
+                    : (twos ? rope_axes_kernel<T, U, true, false> : rope_axes_kernel<T, U, false, false>);
+  for (long first = 0; first < p.rows; first += (long)MOST_GROUPS * p.rows_per_group) {
+    const long groups = (p.rows - first + p.rows_per_group - 1) / p.rows_per_group;
+    p.first = (int)first;
+    hipLaunchKernelGGL(kern, dim3((unsigned)(groups < MOST_GROUPS ? groups : MOST_GROUPS)), dim3(NT), 0, s, p);
   }
 }
 template <typename T> hipError_t run_any(RopeAxes p, bool twos, hipStream_t s) {
@@ -141,8 +171,8 @@ template <typename T> hipError_t run_any(RopeAxes p, bool twos, hipStream_t s) {
 }  // namespace
 
 hipError_t launch_rope_axes(int dtype, const void* src, size_t ld_src, void* dst, size_t ld_dst, const float* table, int n_positions, const int* positions,
-                            const uint8_t* axis, int rows, int n_rot, int n_pass, int d, int backward, hipStream_t s) {
-  RopeAxes p = {src, dst, (const float2*)table, positions, ld_src, ld_dst, rows, n_positions, n_rot, src == dst ? n_rot : n_rot + n_pass, d, 0, 0, backward ? -1.f : 1.f, {}};
+                            int n_axes, const uint8_t* axis, int rows, int n_rot, int n_pass, int d, int backward, hipStream_t s) {
+  RopeAxes p = {src, dst, (const float2*)table, positions, ld_src, ld_dst, 0, rows, n_positions, n_rot, src == dst ? n_rot : n_rot + n_pass, d, 0, 0, n_axes, backward ? -1.f : 1.f, {}};
   memcpy(p.axis, axis, d / 2);
   bool twos = true;
   for (int k = 0; k < d / 2; k += 2) twos = twos && axis[k] == axis[k + 1];

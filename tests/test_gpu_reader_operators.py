@@ -99,6 +99,35 @@ def test_rope_axes_narrow_fp32_heads(n_rot, n_pass):
     rope_case(FP32, 77, n_rot, n_pass, 8, AXES[8], 2, 9, (4, 0))
 
 
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+@pytest.mark.parametrize("axis", [[0, 255, 1, 1] * 16, [0, 0, 255, 255] * 16])
+@pytest.mark.parametrize("back", [0, 1])
+def test_rope_axes_leaves_what_does_not_turn_whatever_it_holds(dtype, axis, back):
+    """NaN, infinities and zeros of both signs in pairs without an axis and in rows whose position lies outside the table; none reaches a pair that turns."""
+    rows, heads, d = 60, 5, 128
+    r = rng(7, dtype)
+    x = torch.from_numpy(r.standard_normal((rows, heads, d))).to(TDT[dtype]).cuda()
+    pos = r.integers(0, 9, (2, rows)).astype(np.int32)
+    pos[0, ::3], pos[1, 1::4] = -1, 9
+    ax = np.array(axis)
+    still = np.array([[a == 255 or not 0 <= pos[a][t] < 9 for a in ax] for t in range(rows)])
+    mask = torch.from_numpy(np.concatenate([still, still], 1)).cuda()[:, None, :].expand(rows, heads, d)
+    odd = torch.tensor([float("nan"), float("inf"), -float("inf"), -0.0, 0.0], dtype=TDT[dtype], device="cuda").repeat(rows * heads * d // 5 + 1)[:rows * heads * d].view(rows, heads, d)
+    clean = x.clone()
+    x = torch.where(mask, odd, x)
+    table = torch.zeros((9, d // 2, 2), device="cuda")
+    ok(lib().optstage_op_rope_table(table.data_ptr(), 9, d, 10000.0, stream()))
+    P0 = torch.from_numpy(pos).cuda()
+    outs = []
+    for v in (x, clean):
+        y = torch.empty_like(v)
+        ok(lib().optstage_op_rope_axes(dtype, v.data_ptr(), heads * d, y.data_ptr(), heads * d, table.data_ptr(), 9, P0.data_ptr(), 2, bytes(axis), rows, heads, 0, d, back, stream()))
+        outs.append(y)
+    torch.cuda.synchronize()
+    bits = torch.int16 if dtype == BF16 else torch.int32
+    assert torch.equal(outs[0].view(bits)[mask], x.view(bits)[mask]) and torch.equal(outs[0][~mask], outs[1][~mask]) and bool(outs[0][~mask].isfinite().all())
+
+
 def test_rope_axes_far_positions_and_one_axis():
     rope_case(BF16, 40, 4, 4, 128, [0] * 64, 1, 200_000)
     rope_case(FP32, 40, 4, 0, 64, [0] * 32, 1, 1)
