@@ -35,8 +35,9 @@ def zone(shape, dtype, fill=9.0):
 
 def within(got, ref, bound, what=""):
     got = host(got) if isinstance(got, torch.Tensor) else got
-    ref = np.where(np.abs(ref) > 2.0 ** 128 - 2.0 ** 103, np.sign(ref) * np.inf, ref)      # past the range of either type: rounds to infinity
-    over = (np.abs(ref) + bound > 2.0 ** 128 - 2.0 ** 103) & (got == np.sign(ref) * np.inf)      # or a value within the bound does
+    end = np.where(ref < 0, -np.inf, np.inf)
+    ref = np.where(np.abs(ref) > 2.0 ** 128 - 2.0 ** 103, end, ref)      # past the range of either type: rounds to infinity
+    over = (np.abs(ref) + bound > 2.0 ** 128 - 2.0 ** 103) & (got == end)      # or a value within the bound does
     same = (got == ref) | (np.isnan(got) & np.isnan(ref)) | over
     with np.errstate(invalid="ignore"):
         d = np.where(same, 0.0, np.abs(got - ref))
