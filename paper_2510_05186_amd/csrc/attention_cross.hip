@@ -1077,11 +1077,23 @@ template <int D> __global__ __launch_bounds__(256) void cross_fwd_f32(const Cros
   }
 }
 
-template <int D> __global__ __launch_bounds__(256) void cross_dq_f32(const CrossArgsOf<float> p) {
+// D of the row whose dO is in `dO`, o at `o`
+template <int D> __device__ __forceinline__ float d_of_row(const f32x4_t (&dO)[Fp32<D>::S], const float* o, int g) {
+  f32x4_t x[Fp32<D>::S];
+  Fp32<D>::rows(x, o, g);
+  float sum = 0.f;
+#pragma unroll
+  for (int s = 0; s < Fp32<D>::S; ++s)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) sum = fmaf(dO[s][e], x[s][e], sum);
+  return sum_g(sum);
+}
+
+template <int D> using PartSums = float[4][ROWS][D + 4];   // of a workgroup's waves
+template <int D> __device__ __forceinline__ void dq_of_rows(const CrossArgsOf<float>& p, int at, PartSums<D>& part_sums) {
   typedef Fp32<D> F;
-  __shared__ __attribute__((aligned(16))) float part_sums[4][ROWS][D + 4];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, g = lane >> 4;
-  const int kvh = blockIdx.x % p.n_kv, at_x = blockIdx.x / p.n_kv, tile = at_x / p.splits, part = at_x % p.splits, b = blockIdx.y;
+  const int kvh = at % p.n_kv, at_x = at / p.n_kv, tile = at_x / p.splits, part = at_x % p.splits, b = blockIdx.y;
   const int n = cross_states(p, b), tiles = n == 1 ? 0 : (n + ROWS - 1) / ROWS, per = (tiles + p.splits - 1) / p.splits, t0 = min(tiles, part * per), t1 = min(tiles, t0 + per);
   const size_t base = (size_t)b * p.seq_kv * p.ldkv + (size_t)kvh * D, stat0 = ((size_t)b * p.n_kv + kvh) * p.rows;
   const float scale = rsqrtf((float)D);
@@ -1091,18 +1103,12 @@ template <int D> __global__ __launch_bounds__(256) void cross_dq_f32(const Cross
   {
     const RowAt at = row_at(p, b, row_r);
     const size_t col = (size_t)(kvh * p.rep + at.head) * D, o_at = at.token * p.n_q * D + col;
-    f32x4_t x[F::S];
     F::rows(q, p.q + at.token * p.ldq + col, g);
     F::rows(dO, p.dout + o_at, g);
-    F::rows(x, p.o_in + o_at, g);
-#pragma unroll
-    for (int s = 0; s < F::S; ++s)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) dsum = fmaf(dO[s][e], x[s][e], dsum);
+    dsum = d_of_row<D>(dO, p.o_in + o_at, g);
   }
   F::scaled(q, scale);
   F::clear(acc);
-  dsum = sum_g(dsum);
   const float L = p.lse[stat0 + row_r];
   if (part == 0 && wave == 0 && g == 0 && tile * ROWS + r < p.rows) p.delta[stat0 + row_r] = dsum;
   for (int t = t0 + wave; t < t1; t += 4) {
@@ -1138,12 +1144,11 @@ template <int D> __global__ __launch_bounds__(256) void cross_dq_f32(const Cross
   }
 }
 
-// rows past the last one repeat it, weigh nothing and are zeros in the second products
-template <int D> __global__ __launch_bounds__(256) void cross_dkv_f32(const CrossArgsOf<float> p) {
+// rows past the last one repeat it, weigh nothing and are zeros in the second products.  OWN_D: D of the rows is formed here, as dq_of_rows() does, instead of read
+template <int D, bool OWN_D> __device__ __forceinline__ void dkv_of_states(const CrossArgsOf<float>& p, int at, PartSums<D>& part_sums) {
   typedef Fp32<D> F;
-  __shared__ __attribute__((aligned(16))) float part_sums[4][ROWS][D + 4];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, g = lane >> 4;
-  const int kvh = blockIdx.x % p.n_kv, at_x = blockIdx.x / p.n_kv, k0 = at_x / p.splits * ROWS, part = at_x % p.splits, b = blockIdx.y;
+  const int kvh = at % p.n_kv, at_x = at / p.n_kv, k0 = at_x / p.splits * ROWS, part = at_x % p.splits, b = blockIdx.y;
   const int n = cross_states(p, b), tiles = (p.rows + ROWS - 1) / ROWS, per = (tiles + p.splits - 1) / p.splits, t0 = min(tiles, part * per), t1 = min(tiles, t0 + per);
   const size_t base = (size_t)b * p.seq_kv * p.ldkv + (size_t)kvh * D, stat0 = ((size_t)b * p.n_kv + kvh) * p.rows;
   const float scale = rsqrtf((float)D);
@@ -1163,6 +1168,8 @@ template <int D> __global__ __launch_bounds__(256) void cross_dkv_f32(const Cros
       f32x4_t q[F::S], dO[F::S], c[4][F::H], w, ds;
       F::rows(q, p.q + mine.token * p.ldq + col, g);
       F::rows(dO, p.dout + mine.token * p.n_q * D + col, g);
+      float d_r = 0.f;
+      if (OWN_D) d_r = d_of_row<D>(dO, p.o_in + mine.token * p.n_q * D + col, g);
       const f32x4_t s = F::product(q, k), dp = F::product(dO, v);   // [e]: row 16 t + 4 g + e, state k0 + r
       const float *qc[4], *gc[4];
 #pragma unroll
@@ -1173,7 +1180,8 @@ template <int D> __global__ __launch_bounds__(256) void cross_dkv_f32(const Cros
         qc[e] = p.q + a.token * p.ldq + acol;
         gc[e] = p.dout + a.token * p.n_q * D + acol;
         w[e] = row < p.rows ? expf(s[e] - p.lse[stat0 + rowc]) : 0.f;
-        ds[e] = row < p.rows && n > 1 ? w[e] * (dp[e] - p.delta[stat0 + rowc]) : 0.f;   // one state has no gradient of its score
+        const float d = OWN_D ? __shfl(d_r, 4 * g + e, 64) : p.delta[stat0 + rowc];
+        ds[e] = row < p.rows && n > 1 ? w[e] * (dp[e] - d) : 0.f;   // one state has no gradient of its score
       }
       const f32x4_t zero = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -1209,6 +1217,22 @@ template <int D> __global__ __launch_bounds__(256) void cross_dkv_f32(const Cros
       *reinterpret_cast<f32x4_t*>((which ? p.dv : p.dk) + base + (size_t)s * p.ldkv + c) = v;
     }
   }
+}
+
+template <int D> __global__ __launch_bounds__(256) void cross_dq_f32(const CrossArgsOf<float> p) {
+  __shared__ __attribute__((aligned(16))) PartSums<D> part_sums;
+  dq_of_rows<D>(p, blockIdx.x, part_sums);
+}
+template <int D> __global__ __launch_bounds__(256) void cross_dkv_f32(const CrossArgsOf<float> p) {
+  __shared__ __attribute__((aligned(16))) PartSums<D> part_sums;
+  dkv_of_states<D, false>(p, blockIdx.x, part_sums);
+}
+// Both side by side in one launch, where neither is in parts: they are few workgroups then, and what a second launch costs is more than D twice (forward and backward,
+// us: 4 heads of 64 x 128 x 77 20.7 -> 14.9, 8 of 128 x 200 x 200 47.5 -> 34.6, 2 x 16 of 64 x 240 x 240 46.5 -> 43.5, 4 x 8 of 64 x 100 x 250 38.5 either way)
+template <int D> __global__ __launch_bounds__(256) void cross_bwd_f32(const CrossArgsOf<float> p, int dkv_groups) {
+  __shared__ __attribute__((aligned(16))) PartSums<D> part_sums;
+  if ((int)blockIdx.x < dkv_groups) dkv_of_states<D, true>(p, blockIdx.x, part_sums);
+  else dq_of_rows<D>(p, blockIdx.x - dkv_groups, part_sums);
 }
 
 // Many rows (states): 16 to a wave, 64 to a workgroup, which read every tile of the other side from LDS, where its threads have put it (the next tile's loads
@@ -1506,8 +1530,15 @@ template <int D> hipError_t cross_fwd_fp32(CrossArgsOf<float> a, const CrossShap
 }
 template <int D> hipError_t cross_bwd_fp32(CrossArgsOf<float> a, const CrossShape& c, hipStream_t s) {
   CrossPlan pl = plan_f32(c, false);
+  const CrossPlan of_states = plan_f32(c, true);
   a.splits = pl.splits;
   dim3 grid((unsigned)a.n_kv * pl.tiles * pl.splits, c.batch);
+  if (pl.waves == 1 && of_states.waves == 1 && pl.splits == 1 && of_states.splits == 1) {
+    const int dkv_groups = a.n_kv * of_states.tiles;
+    grid.x += (unsigned)dkv_groups;
+    hipLaunchKernelGGL(cross_bwd_f32<D>, grid, dim3(256), 0, s, a, dkv_groups);
+    return hipGetLastError();
+  }
   if (pl.waves == 4) hipLaunchKernelGGL(cross_dq_f32_wide<D>, grid, dim3(256), 0, s, a);
   else hipLaunchKernelGGL(cross_dq_f32<D>, grid, dim3(256), 0, s, a);
   if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
@@ -1516,7 +1547,7 @@ template <int D> hipError_t cross_bwd_fp32(CrossArgsOf<float> a, const CrossShap
     hipLaunchKernelGGL((cross_dq_join<float, D, ROWS>), dim3(joins(all * (D / 8))), dim3(256), 0, s, a, all);
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
   }
-  pl = plan_f32(c, true);
+  pl = of_states;
   a.splits = pl.splits;
   a.row_blocks = (a.rows + ROWS - 1) / ROWS;
   grid.x = (unsigned)a.n_kv * pl.tiles * pl.splits;
