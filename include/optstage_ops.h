@@ -4,8 +4,9 @@
  * non-linear part the paper folds into sigma).  They exist so that every kernel can be checked against
  * the CPU oracle and timed on its own; the stage calls in optstage.h launch exactly these kernels.  Beside them stand operators that a
  * training step needs and a stage's op graph does not have, and that no stage call launches: the embedding, which goes around a stage (its input, its
- * input's gradient), and, for layers that their caller writes from single calls as these, activations kept in 8 bits and norms of queries and keys.  A
- * stage keeps its activations in its own arena, in its storage type.
+ * input's gradient), and, for layers that their caller writes from single calls as these, activations kept in 8 bits, norms of queries and keys, rotary positions with
+ * several axes, attention to another sequence's states and the last stage's loss against a teacher's top entries.  A stage keeps its activations in its own arena, in
+ * its storage type.
  *
  * All tensor pointers are DEVICE memory, caller-owned, 16-byte aligned, row-major with tokens as rows.
  * dtype is optstage_dtype (storage type; arithmetic is fp32 / bf16 MFMA with fp32 accumulation).
@@ -199,7 +200,7 @@ optstage_status optstage_op_rope_axes(uint32_t dtype, const void* src, uint32_t 
  * q [batch*seq_q, n_q*d], rows ldq elements apart; k and v [batch*seq_kv, n_kv*d], rows ldkv apart (two column ranges of one packed projection, or two buffers).
  * o, dout [batch*seq_q, n_q*d]; lse fp32 [batch][n_q][seq_q] (natural log).  kv_len: DEVICE int32 [batch] (any address of an int32), or null for all states; below 0
  * counts as 0, above seq_kv as seq_kv.  States past it are not read: they may hold anything.  A sequence without states has o = 0, lse = -infinity and
- * no gradients (0).  A padded query computes as any other; with dout = 0 it adds nothing to dk and dv.  head_dim 64 or 128.  ws: DEVICE scratch of at
+ * no gradients (0).  A padded query computes as any other; finite and with dout = 0 it adds nothing to dk and dv.  head_dim 64 or 128.  ws: DEVICE scratch of at
  * least optstage_op_cross_attn_ws_bytes() bytes for either direction, belonging to a call until its work has run.  bf16: products on the matrix units, sums and softmax in fp32. */
 optstage_status optstage_op_cross_attn_fwd(uint32_t dtype, const void* q, uint32_t ldq, const void* k, const void* v, uint32_t ldkv, const int32_t* kv_len, void* o,
                                            float* lse, void* ws, uint64_t ws_bytes, uint32_t seq_q, uint32_t seq_kv, uint32_t batch, uint32_t n_q, uint32_t n_kv,
