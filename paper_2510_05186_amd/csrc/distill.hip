@@ -64,8 +64,8 @@ struct Running {
   // m c as one number, and what that rounding left out: exp2((x - m) c) = exp2(x c - reference) * rest
   __device__ __forceinline__ float reference(float c) const { return m * c; }
   __device__ __forceinline__ float rest(float c) const { return __builtin_amdgcn_exp2f(fmaf(-m, c, m * c)); }
-  // whether the sum holds, and x c stays finite
-  __device__ __forceinline__ bool sound(float c) const { return s > 0.f && s < INFINITY && fabsf(m * c) < 1e38f; }
+  // whether the sum holds, and rest is some 2^16 at most
+  __device__ __forceinline__ bool sound(float c) const { return s > 0.f && s < INFINITY && fabsf(m * c) < 0x1p28f; }
 };
 // The same against a reference that a wave has taken from its first chunks.
 struct Quick {
@@ -413,18 +413,9 @@ template <typename T, int NT, int R> __global__ __launch_bounds__(NT) __attribut
   }
 }
 
-// ---- m and s of a row's piece; forward alone and a whole row: loss and lse.  Grid rows x pieces.
-template <typename T, int NT> __global__ __launch_bounds__(NT) void distill_stats(const Distill p) {
+// m and s of a row or a piece of it, in all threads
+template <typename T, int NT> __device__ __forceinline__ Running sum_of(const Distill& p, const T* z, int begin, int end, Shared& sh) {
   constexpr int N = Vec16<T>::N, STEP = NT * N, U = 4;
-  extern __shared__ float lds[];
-  __shared__ Shared sh;
-  const size_t row = blockIdx.x / p.pieces;
-  const int piece = blockIdx.x % p.pieces, begin = piece * p.piece, end = min(p.vocab, begin + p.piece);
-  const T* z = (const T*)p.z + row * p.ldz;
-  if (piece == 0 && threadIdx.x < 64) {
-    const Teacher mine = read_entries<T, false, true>(p, row, Entries(lds, 0, p.k));
-    if (threadIdx.x == 0) sh.teacher = mine;
-  }
   int at = begin + threadIdx.x * N;
   float x[N];
   load_chunk(z, at, end, x);
@@ -456,6 +447,21 @@ template <typename T, int NT> __global__ __launch_bounds__(NT) void distill_stat
   }
   Running all = join_group<NT>(part, sh, p.c);
   if (!all.sound(p.c)) all = sum_again<T, NT>(p, z, begin, end, sh);
+  return all;
+}
+
+// ---- m and s of a row's piece; forward alone and a whole row: loss and lse.  Grid rows x pieces.
+template <typename T, int NT> __global__ __launch_bounds__(NT) void distill_stats(const Distill p) {
+  extern __shared__ float lds[];
+  __shared__ Shared sh;
+  const size_t row = blockIdx.x / p.pieces;
+  const int piece = blockIdx.x % p.pieces, begin = piece * p.piece, end = min(p.vocab, begin + p.piece);
+  const T* z = (const T*)p.z + row * p.ldz;
+  if (piece == 0 && threadIdx.x < 64) {
+    const Teacher mine = read_entries<T, false, true>(p, row, Entries(lds, 0, p.k));
+    if (threadIdx.x == 0) sh.teacher = mine;
+  }
+  const Running all = sum_of<T, NT>(p, z, begin, end, sh);
   if (threadIdx.x) return;
   if (p.dz || p.pieces > 1) {                            // joined by the next launch
     p.stats[blockIdx.x] = make_float2(all.m, all.s);
@@ -482,14 +488,22 @@ __global__ __launch_bounds__(256) void distill_finish(const Distill p) {
   if ((threadIdx.x & 63) == 0) finish(p, row, r, p.parts[row]);
 }
 
+// An lse of this size and more is a number of 32 bits whose rounding the gradient's type would show: up to 2^-20 of p for fp32 (20000 words at T 0.7: 9.7e-7 of the gradient's
+// norm in all, 4.8e-7 from the row's own sum), 2^-12 for bf16.  One more read: fp32, forward and backward, 4096 rows of 32000 words 300 -> 340 us, 20 of 100000, a workgroup each, 17 -> 36.
+template <typename T> constexpr float FAR_LSE = sizeof(T) == 4 ? 16.f : 4096.f;
+
 // ---- the gradient of a row's piece, from lse (JOIN: from the pieces' m and s, the first piece writes loss and lse).  Grid rows x pieces.
+// Without JOIN a row of FAR_LSE is summed again, by the workgroup of its first piece, which has the whole row then: dz may be z, so nobody else may write before.
 // PAST: stores (1), loads too (2) past the caches.
 template <typename T, int NT, bool JOIN, int PAST> __global__ __launch_bounds__(NT) void distill_grad(const Distill p) {
   constexpr int N = Vec16<T>::N, STEP = NT * N, U = 4;
   extern __shared__ float lds[];
   __shared__ Shared sh;
   const size_t row = blockIdx.x / p.pieces;
-  const int piece = blockIdx.x % p.pieces, begin = piece * p.piece, end = min(p.vocab, begin + p.piece);
+  const int piece = blockIdx.x % p.pieces;
+  const bool again = !JOIN && fabsf(p.lse[row]) >= FAR_LSE<T>;
+  if (again && piece) return;
+  const int begin = piece * p.piece, end = again ? p.vocab : min(p.vocab, begin + p.piece);
   const T* z = (const T*)p.z + row * p.ldz;
   T* dz = (T*)p.dz + row * p.lddz;
   const Entries e(lds, 0, p.k);
@@ -516,6 +530,10 @@ template <typename T, int NT, bool JOIN, int PAST> __global__ __launch_bounds__(
   if (JOIN) {
     r.m = sh.m[0];
     r.s = sh.s[0];
+  } else if (again && !none) {
+    r = sum_of<T, NT>(p, z, 0, p.vocab, sh);
+  }
+  if (JOIN || again) {
     f /= r.s;
     sound = r.sound(p.c);
     shift = r.reference(p.c);
@@ -532,7 +550,7 @@ template <typename T, int NT, bool JOIN, int PAST> __global__ __launch_bounds__(
     for (; at < end; at += STEP) store_chunk(dz, at, end, x);
     return;
   }
-  if (JOIN && !sound) {
+  if (!sound) {
     for (; at < end; at += STEP) {
       float x[N];
       load_chunk(z, at, end, x);

@@ -554,7 +554,9 @@ class Distill:
             for j in np.nonzero(ts[r])[0]:
                 top[r, self.ids[r, j]] += ts[r][j]
         # (a probability below the least normal number is off by up to that number: its steps are 2^-149 wide, and the hardware's exponential gives 0)
-        e_p = ((EPS * (6 * spread + 16) + 2 * e_lse[:, None]) * p + FLUSH) * mass[:, None] + FLUSH + 12 * EPS * (p * mass[:, None] + top)
+        # (from an lse of up to 16, or 4096 in bf16, its rounding comes in; rows beyond have their own sum)
+        near = e_sum + 2 * EPS * np.minimum(np.abs(lse), 16.0 if self.dtype == FP32 else 4096.0)
+        e_p = ((EPS * (6 * spread + 16) + 2 * near[:, None]) * p + FLUSH) * mass[:, None] + FLUSH + 12 * EPS * (p * mass[:, None] + top)
         within(host(dz)[:, :vocab], ref, np.abs(self.w.astype(np.float64))[:, None] / T * e_p + (HALF[self.dtype] + 2 * EPS) * np.abs(ref) + TINY[self.dtype], "dz")
 
     def untouched(self, inplace=False):
@@ -645,19 +647,20 @@ def test_distillation_of_rows_of_every_range(how, dtype, rows, vocab, temperatur
     c.upload()
     dz = c.call(how)
     torch.cuda.synchronize()
-    c.check(dz)                                         # (what lse's rounding takes from the gradient of a far row is in the bound: 2 e_lse)
+    c.check(dz)                                         # (the rows far from zero have no rounding of lse in their bounds)
     c.untouched()
 
 
+@pytest.mark.parametrize("how", ["both", "apart"])
 @pytest.mark.parametrize("dtype", [BF16, FP32])
+@pytest.mark.parametrize("size", ["lowest", 2.0 ** 35, -(2.0 ** 40), 2.0 ** 90])
 @pytest.mark.parametrize("rows,vocab", [(3, 900), (3, 50000), (170, 9001), (170, 131073)])
-def test_distillation_of_a_row_of_lowest_values(dtype, rows, vocab):
-    """All words masked by the type's lowest value: the distribution is even."""
+def test_distillation_of_a_row_of_alike_values(how, dtype, rows, vocab, size):
+    """All words masked by the type's lowest value, or as far from zero as only sums of differences bear: the distribution is even."""
     c = Distill(dtype, rows, vocab, 4, bare=True)
-    low = float(torch.finfo(TDT[dtype]).min)
-    c.Z[1], c.ids[1], c.T[1] = low, [0, 1, vocab // 2, vocab - 1], 0.0
+    c.Z[1], c.ids[1], c.T[1] = float(torch.finfo(TDT[dtype]).min) if size == "lowest" else size, [0, 1, vocab // 2, vocab - 1], 0.0
     c.upload()
-    dz = host(c.call("both"))
+    dz = host(c.call(how))
     torch.cuda.synchronize()
     w = float(c.w[1])
     want = np.full(vocab, w / vocab)
