@@ -905,8 +905,9 @@ CrossPlan plan_rows(const CrossShape& c) {
   p.splits = splits < 1 ? 1 : (int)splits;
   return p;
 }
-// dK / dV: 128 states to a workgroup, one to a compute unit; parts of the rows, of eight blocks at least (both kernels and the joins, us: 32 / 8 heads x 4096 x 1024, 64
-// workgroups: 1 part 488, 2 318, 4 257; 16 heads x 2 x 1024 x 577, 160: 55, 2 parts 76; 8 x 512 x 4096, 256: 58 / 83)
+// dK / dV: 128 states to a workgroup, one to a compute unit; parts of the rows (both kernels and the joins, us: 32 / 8 heads x 4096 x 1024, 64 workgroups: 1 part 488, 2 318,
+// 4 257; 16 heads x 2 x 1024 x 577, 160: 55, 2 parts 76; 8 x 512 x 4096, 256: 58 / 83), of four blocks at least (forward and backward, of eight / four / two: 4 x 8 heads of 128
+// x 1024 x 64 42.4 / 37.9 / 37.9, 8 x 3085 x 174 49.5 / 46.5 / 46.3, 8 x 300 x 2000 54.2 / 54.2 / 61.5, 16 of 64 x 700 x 700 51.2 / 52.8 / 52.8)
 CrossPlan plan_states(const CrossShape& c) {
   const long groups = (long)c.n_kv * c.batch;
   CrossPlan p;
@@ -914,7 +915,7 @@ CrossPlan plan_states(const CrossShape& c) {
   p.tiles = (c.seq_kv + 127) / 128;
   const long wgs = groups * p.tiles, blocks = row_blocks(c.seq_q, c.n_q / c.n_kv).all;
   long splits = wgs >= 160 ? 1 : 256 / wgs;
-  splits = splits < blocks / 8 ? splits : blocks / 8;
+  splits = splits < blocks / 4 ? splits : blocks / 4;
   p.splits = splits < 1 ? 1 : (int)splits;
   return p;
 }
