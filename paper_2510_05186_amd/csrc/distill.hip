@@ -7,6 +7,7 @@
 // above m that s overflows, or nothing but the lowest values is left of a row, the row (its piece) is summed again with the running maximum.
 // A logit costs a conversion, a multiply-add, an exponential and an addition in each direction, half of what the running maximum would: at 4096 rows of 131072 words
 // the vector units are busy half of the time that memory takes.
+//  * Rows of a few words: a wave has one in its registers, in every direction.
 //  * Both directions, rows enough for the chip: a workgroup has a row in its registers from the maximum to the gradient (up to 128K words of bf16; of longer
 //    ones the rest is read a second time).
 //  * Rows too few for that: a row in pieces, a launch for their m and s, a second one that joins them and writes the gradient.
@@ -185,22 +186,14 @@ __device__ __forceinline__ float teacher_at(const Entries& e, int k, int id) {
   return t;
 }
 
-// What the rows' entries come to, ahead of the pass over the rows: a wave a row, four to a workgroup.  In that pass one wave's 64-bit arithmetic and its two loads
-// one behind the other would hold up the other fifteen (4096 rows of 131072 words with 128 entries: 120 of 583 us).  Whether a row names a word twice: by a table of
-// its words in LDS.
-template <typename T> __global__ __launch_bounds__(256) void distill_teacher(const Distill p, int slots) {
-  extern __shared__ float lds[];
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  const size_t row = (size_t)blockIdx.x * 4 + wave;
-  const Entries e(lds, wave, p.k);
-  int* table = (int*)lds + 16 * p.k + wave * slots;
+// Whether the row whose entries a wave has read names a word twice: by a table of its words in LDS, `slots` (a power of two, twice k at least) of the wave's own.
+__device__ __forceinline__ bool names_twice(const Entries& e, int k, int* table, int slots) {
+  const int lane = threadIdx.x & 63;
   for (int i = lane; i < slots; i += 64) table[i] = -1;
-  __syncthreads();
-  if (row >= (size_t)p.rows) return;
-  Teacher t = read_entries<T, false, false>(p, row, e);
+  __threadfence_block();
   bool twice = false;
 #pragma unroll 1
-  for (int j = lane; j < p.k; j += 64) {
+  for (int j = lane; j < k; j += 64) {
     const int id = e.id[j];
     if (id < 0) continue;
     for (unsigned at = (unsigned)id * 2654435769u >> 8 & (slots - 1);; at = (at + 1) & (slots - 1)) {   // a free place or the word's is found: the table is half empty
@@ -209,8 +202,27 @@ template <typename T> __global__ __launch_bounds__(256) void distill_teacher(con
       if (was == -1 || was == id) break;
     }
   }
-  t.twice = __any(twice) ? 1 : 0;
-  if (lane == 0) p.parts[row] = t;
+  return __any(twice);
+}
+int table_slots(int k) {
+  int slots = 64;
+  while (slots < 2 * k) slots *= 2;
+  return slots;
+}
+// of four rows
+size_t entries_and_table_bytes(int k) { return 4 * (entries_bytes(k) + sizeof(int) * table_slots(k)); }
+
+// What the rows' entries come to, ahead of the pass over the rows: a wave a row, four to a workgroup.  In that pass one wave's 64-bit arithmetic and its two loads
+// one behind the other would hold up the other fifteen (4096 rows of 131072 words with 128 entries: 120 of 583 us).
+template <typename T> __global__ __launch_bounds__(256) void distill_teacher(const Distill p, int slots) {
+  extern __shared__ float lds[];
+  const int wave = threadIdx.x >> 6;
+  const size_t row = (size_t)blockIdx.x * 4 + wave;
+  if (row >= (size_t)p.rows) return;
+  const Entries e(lds, wave, p.k);
+  Teacher t = read_entries<T, false, false>(p, row, e);
+  t.twice = names_twice(e, p.k, (int*)lds + 16 * p.k + wave * slots, slots) ? 1 : 0;
+  if ((threadIdx.x & 63) == 0) p.parts[row] = t;
 }
 
 template <typename T> __device__ __forceinline__ void load_chunk(const T* z, int at, int end, float (&x)[Vec16<T>::N]) {
@@ -463,7 +475,7 @@ template <typename T, int NT> __global__ __launch_bounds__(NT) void distill_stat
   }
   const Running all = sum_of<T, NT>(p, z, begin, end, sh);
   if (threadIdx.x) return;
-  if (p.dz || p.pieces > 1) {                            // joined by the next launch
+  if (p.pieces > 1) {                                    // joined by the next launch
     p.stats[blockIdx.x] = make_float2(all.m, all.s);
     if (piece == 0) p.parts[row] = sh.teacher;
     return;
@@ -590,8 +602,60 @@ template <typename T, int NT, bool JOIN, int PAST> __global__ __launch_bounds__(
   }
 }
 
+// ---- rows of a few words: a wave has one in its registers, four to a workgroup, in every direction; the gradient has the row's own sum.  R chunks a lane.
+template <typename T, int R> __global__ __launch_bounds__(256) void distill_short(const Distill p, int slots) {
+  constexpr int N = Vec16<T>::N;
+  extern __shared__ float lds[];
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const size_t row = (size_t)blockIdx.x * 4 + wave;
+  if (row >= (size_t)p.rows) return;
+  const T* z = (const T*)p.z + row * p.ldz;
+  float x[R][N];
+#pragma unroll
+  for (int r = 0; r < R; ++r) load_chunk(z, (64 * r + lane) * N, p.vocab, x[r]);
+  const Entries e(lds, wave, p.k);
+  const Teacher teacher = read_entries<T, true, true>(p, row, e);
+  const bool twice = p.dz && names_twice(e, p.k, (int*)lds + 16 * p.k + wave * slots, slots);
+  Running all;
+#pragma unroll
+  for (int r = 0; r < R; ++r)
+#pragma unroll
+    for (int i = 0; i < N; ++i) all.m = fmaxf(all.m, x[r][i]);
+  all.m = wave_max(all.m);
+  float sum = 0.f;
+#pragma unroll
+  for (int r = 0; r < R; ++r)
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      x[r][i] = __builtin_amdgcn_exp2f((x[r][i] - all.m) * p.c);
+      sum += x[r][i];
+    }
+  all.s = wave_sum(sum);
+  if (p.loss && lane == 0) finish(p, row, all, teacher);
+  if (!p.dz) return;
+  T* dz = (T*)p.dz + row * p.lddz;
+  const float w = p.dloss[row] * p.inv_t;
+  const bool none = w == 0.f || teacher.mass == 0.0;
+  const float f = none ? 0.f : w * (float)teacher.mass / all.s;
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) x[r][i] = none ? 0.f : f * x[r][i];
+    store_chunk(dz, (64 * r + lane) * N, p.vocab, x[r]);
+  }
+  if (none) return;
+  __threadfence_block();                                // the row ahead of its entries; their words and weights are there for all lanes
+  for (int j = lane; j < p.k; j += 64) {
+    const int id = e.id[j];
+    if (id >= 0) dz[id] = (T)(f * __builtin_amdgcn_exp2f((e.z[j] - all.m) * p.c) - w * (twice ? teacher_at(e, p.k, id) : e.t[j]));
+  }
+}
+
 // Rows below this many leave compute units idle with a workgroup each: they go in pieces.
 constexpr int FEW_ROWS = 160;
+// Rows of up to this many words go a wave each, of twice as many in both directions at once (against a workgroup a row or pieces, us: bf16, both, 16384 rows of 200 words 68 -> 17,
+// of 1000 75 -> 23, of 4000 102 -> 88, 100 of 4000 10.6 -> 8.4; each by itself 16384 of 1000 81 -> 38, of 2048 94 -> 55, but 4096 of 3096 29.4 -> 34.5).
+constexpr int SHORT = 2048;
 // A row's pieces: some 1024 workgroups in all, pieces of 2048 elements and more
 int pieces_of(int rows, int vocab) {
   const int most = (vocab + 2047) / 2048, want = (1024 + rows - 1) / rows;
@@ -609,15 +673,13 @@ template <typename T, int NT, int R> hipError_t run_rows(const Distill& p, int p
 }
 // the fewest steps that hold a row, in twos; workgroups that fill a compute unit
 template <typename T> hipError_t run_both(const Distill& p, hipStream_t s) {
-  int slots = 64;
-  while (slots < 2 * p.k) slots *= 2;
   static LdsAttrOnce lds_attr;
-  if (hipError_t e = lds_attr.ensure(reinterpret_cast<const void*>(distill_teacher<T>), 4 * (16 * 1024 + 4 * 2048)); e != hipSuccess) return e;
-  hipLaunchKernelGGL(distill_teacher<T>, dim3((p.rows + 3) / 4), dim3(256), 4 * (entries_bytes(p.k) + 4 * slots), s, p, slots);
+  if (hipError_t e = lds_attr.ensure(reinterpret_cast<const void*>(distill_teacher<T>), (int)entries_and_table_bytes(1024)); e != hipSuccess) return e;
+  hipLaunchKernelGGL(distill_teacher<T>, dim3((p.rows + 3) / 4), dim3(256), entries_and_table_bytes(p.k), s, p, table_slots(p.k));
   if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
   const int chunks = (p.vocab + Vec16<T>::N - 1) / Vec16<T>::N;
-  if (chunks <= 256 * 2) return run_rows<T, 256, 2>(p, 4, s);
-  if (chunks <= 256 * 4) return run_rows<T, 256, 4>(p, 4, s);
+  if constexpr (256 * 4 * Vec16<T>::N > 2 * SHORT)      // fewer words are short rows
+    if (chunks <= 256 * 4) return run_rows<T, 256, 4>(p, 4, s);
   if (chunks <= 256 * 6) return run_rows<T, 256, 6>(p, 4, s);
   if (chunks <= 256 * 8) return run_rows<T, 256, 8>(p, 4, s);
   if (chunks <= 512 * 6) return run_rows<T, 512, 6>(p, 2, s);
@@ -654,10 +716,23 @@ template <typename T> hipError_t run_parts(Distill p, bool whole, hipStream_t s)
   return hipGetLastError();
 }
 
+template <typename T, int R> hipError_t run_short(const Distill& p, hipStream_t s) {
+  static LdsAttrOnce lds_attr;
+  if (hipError_t e = lds_attr.ensure(reinterpret_cast<const void*>(distill_short<T, R>), (int)entries_and_table_bytes(1024)); e != hipSuccess) return e;
+  hipLaunchKernelGGL((distill_short<T, R>), dim3((p.rows + 3) / 4), dim3(256), entries_and_table_bytes(p.k), s, p, table_slots(p.k));
+  return hipGetLastError();
+}
+template <typename T> hipError_t run_short(const Distill& p, hipStream_t s) {
+  constexpr int R = SHORT / (64 * Vec16<T>::N);
+  if (p.vocab <= SHORT / 4) return run_short<T, R / 4>(p, s);
+  if (p.vocab <= SHORT / 2) return run_short<T, R / 2>(p, s);
+  return p.vocab <= SHORT ? run_short<T, R>(p, s) : run_short<T, 2 * R>(p, s);
+}
+
 template <typename T> hipError_t run(const Distill& p, hipStream_t s) {
-  if (p.rows < FEW_ROWS) return run_parts<T>(p, false, s);
-  const bool both = p.loss && p.dz;
-  const int most = both ? ROWS_A_LAUNCH : 1 << 22;      // one direction: a launch's 2^30 threads
+  const bool both = p.loss && p.dz, is_short = p.vocab <= (both ? 2 * SHORT : SHORT);
+  if (p.rows < FEW_ROWS && !is_short) return run_parts<T>(p, false, s);
+  const int most = both && !is_short ? ROWS_A_LAUNCH : 1 << 22;   // a launch's 2^30 threads
   for (int first = 0; first < p.rows; first += most) {
     Distill q = p;
     q.rows = p.rows - first < most ? p.rows - first : most;
@@ -670,7 +745,7 @@ template <typename T> hipError_t run(const Distill& p, hipStream_t s) {
       q.dloss += first;
     }
     if (p.loss) q.loss += first;
-    if (hipError_t e = both && p.vocab >= Vec16<T>::N ? run_both<T>(q, s) : run_parts<T>(q, true, s); e != hipSuccess) return e;
+    if (hipError_t e = is_short ? run_short<T>(q, s) : both ? run_both<T>(q, s) : run_parts<T>(q, true, s); e != hipSuccess) return e;
     if (p.rows - first <= most) break;
   }
   return hipSuccess;

@@ -2,8 +2,9 @@
 //   lo' = lo cos - hi sin,  hi' = hi cos + lo sin,  (cos, sin) = table[positions[axis[k]][row]][k]
 // and its gradient turns back.
 //
-// Bound by memory: every element in and out once (8192 rows of 80 heads of 128, bf16, both directions: 115 us, 5.8 TB/s).  A thread has one 16-byte chunk of both halves of a head, so that the pairs are its own, and keeps that chunk's
-// cos and sin for several heads of one row; the heads' loads are in flight while the positions lead to the angles.
+// Bound by memory: every element in and out once (8192 rows of 80 heads of 128, bf16, both directions: 115 us, 5.8 TB/s).  A thread has one 16-byte chunk of both
+// halves of a head, so that the pairs are its own, and keeps that chunk's cos and sin for several heads of one row; the heads' loads are in flight while the positions
+// lead to the angles.
 #include "common.h"
 
 #include <string.h>

@@ -580,6 +580,16 @@ def test_distillation(how, dtype, rows, vocab, k, pad):
     c.untouched()
 
 
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+@pytest.mark.parametrize("vocab", [300, 600, 2048, 2049, 4096, 4097, 7001, 9000, 13001, 20011, 30011, 40009, 45001, 55001, 60001, 70001, 90001, 100003, 120011])
+def test_distillation_of_every_length_of_row(dtype, vocab):
+    c = Distill(dtype, 161, vocab, 5, pad=(3, 1), seed=4)
+    dz = c.call("both")
+    torch.cuda.synchronize()
+    c.check(dz)
+    c.untouched()
+
+
 @pytest.mark.parametrize("how", ["both", "apart"])
 @pytest.mark.parametrize("dtype", [BF16, FP32])
 @pytest.mark.parametrize("temperature,log_probs", [(2.0, 0), (0.25, 0), (1.0, 1), (3.0, 1)])
@@ -675,7 +685,7 @@ def test_distillation_of_a_row_of_alike_values(how, dtype, rows, vocab, size):
     c.check(torch.from_numpy(dz[fine]))
 
 
-@pytest.mark.parametrize("rows,vocab,k", [(40, 3000, 20), (2, 100003, 64), (700, 20000, 9)])
+@pytest.mark.parametrize("rows,vocab,k", [(40, 3000, 20), (2, 100003, 64), (700, 20000, 9), (301, 900, 1024)])
 def test_distillation_captured_replayed_and_repeated(rows, vocab, k):
     a, b = Distill(BF16, rows, vocab, k), Distill(BF16, rows, vocab, k, seed=1)
     s = torch.cuda.Stream()
