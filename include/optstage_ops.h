@@ -220,7 +220,7 @@ uint64_t optstage_op_cross_attn_ws_bytes(uint32_t dtype, uint32_t seq_q, uint32_
  *   dz[r][v] = dloss[r] / temperature * (p_v * sum of all t_j - sum of t_j with ids_j = v)
  * A teacher's entry of minus infinity has t = 0 and adds nothing.  A row without entries has loss 0 and gradient 0, and so has the gradient of a row whose
  * dloss is 0 (padding), whatever its logits are.  From lse (distill_bwd) p is off by its rounding, up to 2^-24 |lse|; a row whose |lse| is 16 and more (bf16: 4096) is summed
- * again instead, for the time of one more read.  dz rows lie lddz apart; columns past vocab are neither read nor written; dz may be z (with lddz = ldz).
+ * again instead, for the time of one more read, and one of up to 2048 words always is (from registers).  dz rows lie lddz apart; columns past vocab are neither read nor written; dz may be z (with lddz = ldz).
  * k is at most 1024, temperature from 1e-30 to 1e30.  z and dz: 16-byte aligned, any ldz and lddz >= vocab.  ws: DEVICE scratch of
  * at least optstage_op_distill_ws_bytes() bytes, belonging to a call until its work has run. */
 optstage_status optstage_op_distill_fwd(uint32_t dtype, const void* z, uint32_t ldz, const int32_t* ids, const float* teacher, float* loss, float* lse, void* ws,
