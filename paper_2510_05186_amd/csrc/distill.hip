@@ -507,7 +507,7 @@ template <typename T> constexpr float FAR_LSE = sizeof(T) == 4 ? 16.f : 4096.f;
 // ---- the gradient of a row's piece, from lse (JOIN: from the pieces' m and s, the first piece writes loss and lse).  Grid rows x pieces.
 // Without JOIN a row of FAR_LSE is summed again, by the workgroup of its first piece, which has the whole row then: dz may be z, so nobody else may write before.
 // PAST: stores (1), loads too (2) past the caches.
-template <typename T, int NT, bool JOIN, int PAST> __global__ __launch_bounds__(NT) void distill_grad(const Distill p) {
+template <typename T, int NT, bool JOIN, int PAST> __global__ __launch_bounds__(NT) void distill_grad(const Distill p, int slots) {
   constexpr int N = Vec16<T>::N, STEP = NT * N, U = 4;
   extern __shared__ float lds[];
   __shared__ Shared sh;
@@ -528,7 +528,9 @@ template <typename T, int NT, bool JOIN, int PAST> __global__ __launch_bounds__(
         if (piece == 0) finish(p, row, r, p.parts[row]);
       }
     }
-    const Teacher mine = read_entries<T, true, true>(p, row, e);
+    Teacher mine = read_entries<T, true, true>(p, row, e);
+    // few entries are gone through sooner than asked about (4096 rows of 32000 words, forward and backward: 256 entries 193 -> 183 us, 1024 750 -> 290)
+    mine.twice = p.k <= 64 || names_twice(e, p.k, (int*)lds + 4 * p.k, slots);
     if (threadIdx.x == 0) sh.teacher = mine;
   }
   __syncthreads();
@@ -598,7 +600,7 @@ template <typename T, int NT, bool JOIN, int PAST> __global__ __launch_bounds__(
   __syncthreads();
   for (int j = threadIdx.x; j < p.k; j += NT) {
     const int id = e.id[j];
-    if (id >= begin && id < end) dz[id] = (T)((sound ? prob(e.z[j]) : f * __builtin_amdgcn_exp2f((e.z[j] - r.m) * p.c)) - w * teacher_at(e, p.k, id));
+    if (id >= begin && id < end) dz[id] = (T)((sound ? prob(e.z[j]) : f * __builtin_amdgcn_exp2f((e.z[j] - r.m) * p.c)) - w * (sh.teacher.twice ? teacher_at(e, p.k, id) : e.t[j]));
   }
 }
 
@@ -700,18 +702,20 @@ template <typename T> hipError_t run_parts(Distill p, bool whole, hipStream_t s)
   p.stats = (float2*)(p.parts + p.rows);
   const dim3 grid((unsigned)p.rows * p.pieces);
   const size_t lds = entries_bytes(p.k);
+  const int slots = table_slots(p.k);
+  const size_t lds_grad = lds + (p.k <= 64 ? 0 : sizeof(int) * slots);
   if (p.loss) {
     hipLaunchKernelGGL((distill_stats<T, 256>), grid, dim3(256), lds, s, p);
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-    if (p.dz) hipLaunchKernelGGL((distill_grad<T, 256, true, 0>), grid, dim3(256), lds, s, p);
+    if (p.dz) hipLaunchKernelGGL((distill_grad<T, 256, true, 0>), grid, dim3(256), lds_grad, s, p, slots);
     else if (p.pieces > 1) hipLaunchKernelGGL(distill_finish, dim3((p.rows + 3) / 4), dim3(256), 0, s, p);
   } else {
     // what the caches do not keep anyway: 300 rows of 131072 words (79 MB) 43.7 -> 34.2 us (41.3 with the loads), 4096 rows of 32000 124 -> 115 (103), of 131072
     // 445 -> 423 (406); 4096 rows of 1000 (8 MB) 16.5 either way, and whoever reads them next finds them there
     const double bytes = (double)p.rows * p.vocab * sizeof(T);
-    if (bytes >= 160e6) hipLaunchKernelGGL((distill_grad<T, 256, false, 2>), grid, dim3(256), lds, s, p);
-    else if (bytes >= 32e6) hipLaunchKernelGGL((distill_grad<T, 256, false, 1>), grid, dim3(256), lds, s, p);
-    else hipLaunchKernelGGL((distill_grad<T, 256, false, 0>), grid, dim3(256), lds, s, p);
+    if (bytes >= 160e6) hipLaunchKernelGGL((distill_grad<T, 256, false, 2>), grid, dim3(256), lds_grad, s, p, slots);
+    else if (bytes >= 32e6) hipLaunchKernelGGL((distill_grad<T, 256, false, 1>), grid, dim3(256), lds_grad, s, p, slots);
+    else hipLaunchKernelGGL((distill_grad<T, 256, false, 0>), grid, dim3(256), lds_grad, s, p, slots);
   }
   return hipGetLastError();
 }
