@@ -571,7 +571,8 @@ class Distill:
 @pytest.mark.parametrize("how", ["both", "apart"])
 @pytest.mark.parametrize("dtype", [BF16, FP32])
 @pytest.mark.parametrize("rows,vocab,k,pad", [(1, 1, 1, (0, 0)), (3, 2, 3, (0, 0)), (5, 7, 4, (1, 3)), (128, 1000, 8, (0, 0)), (9, 1001, 64, (0, 0)), (4, 4096, 100, (8, 16)), (300, 513, 5, (7, 0)),
-                                              (2, 32000, 64, (0, 0)), (7, 50001, 50, (23, 0)), (3, 151003, 300, (5, 9)), (1, 262144, 1024, (0, 0)), (600, 3001, 17, (3, 3)), (270, 66000, 9, (0, 8))])
+                                              (2, 32000, 64, (0, 0)), (7, 50001, 50, (23, 0)), (3, 151003, 300, (5, 9)), (1, 262144, 1024, (0, 0)), (600, 3001, 17, (3, 3)), (270, 66000, 9, (0, 8)),
+                                              (5, 9000, 300, (0, 0)), (200, 9000, 300, (0, 1)), (200, 1500, 1024, (0, 0))])   # many words given twice
 def test_distillation(how, dtype, rows, vocab, k, pad):
     c = Distill(dtype, rows, vocab, k, pad=pad)
     dz = c.call(how)
