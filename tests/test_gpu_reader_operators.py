@@ -686,6 +686,30 @@ def test_distillation_of_a_row_of_alike_values(how, dtype, rows, vocab, size):
     c.check(torch.from_numpy(dz[fine]))
 
 
+@pytest.mark.parametrize("how", ["both", "apart"])
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+@pytest.mark.parametrize("rows,vocab,every", [(3, 50000, 2000), (100, 50000, 4552), (161, 9001, 4000), (161, 40009, 12000)])
+@pytest.mark.parametrize("gap", [75.0, 88.0])
+@pytest.mark.parametrize("dloss", [1.0 / 4096, 1e-8])
+def test_distillation_of_words_whose_exponential_is_just_within_range(how, dtype, rows, vocab, every, gap, dloss):
+    """Logits that lie almost as far above the first words' as an exponential in 32 bits reaches (88.7): one of them at the end, and one in every stretch of words that few rows are divided into, whose
+    sums come together; against weights of the loss with which 1 / the sum against the first words is below the normal numbers."""
+    c = Distill(dtype, rows, vocab, 6, bare=True, seed=9)
+    c.Z /= 64
+    at = np.arange(3 * every // 4, vocab, every)
+    c.Z[0, vocab - 5] = gap
+    c.Z[1, at] = gap
+    c.Z[2, at] = gap - np.arange(len(at)) % 3
+    c.Z = q(c.Z, dtype)
+    c.ids[0, 0], c.ids[1, :2], c.ids[2, :2] = vocab - 5, at[:2], at[-2:]
+    c.w = (np.float32(dloss) * np.sign(c.w)).astype(np.float32)
+    c.upload()
+    dz = c.call(how)
+    torch.cuda.synchronize()
+    c.check(dz)
+    c.untouched()
+
+
 @pytest.mark.parametrize("rows,vocab,k", [(40, 3000, 20), (2, 100003, 64), (700, 20000, 9), (301, 900, 1024)])
 def test_distillation_captured_replayed_and_repeated(rows, vocab, k):
     a, b = Distill(BF16, rows, vocab, k), Distill(BF16, rows, vocab, k, seed=1)
