@@ -18,6 +18,9 @@
 namespace {
 
 constexpr float LOG2E = 1.4426950408889634f, LOWEST = -3.402823466e38f;
+// A row's factor, weight / sum, below which it is not formed (its reference's rest may take 2^-16 more, and 2^-126 is the least number of full precision): the row's
+// probabilities come first then, and the weight last.
+constexpr float LEAST_FACTOR = 0x1p-100f;
 
 // 16 bytes of a row at any address of its elements
 template <typename T> struct Any16;
@@ -373,15 +376,16 @@ template <typename T, int NT, int R> __global__ __launch_bounds__(NT) __attribut
     const bool twice = teacher.twice;
     const float w = p.dloss[row] * p.inv_t;
     const bool none = w == 0.f || mass == 0.0;
-    const bool sound = all.sound(p.c);
-    const float f = none ? 0.f : w * (float)mass / all.s, fr = sound ? f * all.rest(p.c) : f, mc = all.reference(p.c);
+    const float wm = w * (float)mass, f = none ? 0.f : wm / all.s, inv = 1.f / all.s;
+    const bool sound = all.sound(p.c) && (none || fabsf(f) >= LEAST_FACTOR);
+    const float fr = sound ? f * all.rest(p.c) : f, mc = all.reference(p.c);
     if (!sound) {
 #pragma unroll 1
       for (int at = first; at < p.vocab; at += STEP) {
         float x[N];
         load_chunk(z, at, p.vocab, x);
 #pragma unroll
-        for (int e = 0; e < N; ++e) x[e] = none ? 0.f : f * __builtin_amdgcn_exp2f((x[e] - all.m) * p.c);
+        for (int e = 0; e < N; ++e) x[e] = none ? 0.f : wm * (inv * __builtin_amdgcn_exp2f((x[e] - all.m) * p.c));
         store_chunk(dz, at, p.vocab, x);
       }
     }
@@ -421,7 +425,9 @@ template <typename T, int NT, int R> __global__ __launch_bounds__(NT) __attribut
     if (!none)
       for (int j = threadIdx.x; j < p.k; j += NT) {
         const int id = en.id[j];
-        if (id >= 0) dz[id] = (T)(f * __builtin_amdgcn_exp2f((en.z[j] - all.m) * p.c) - w * (twice ? teacher_at(en, p.k, id) : en.t[j]));
+        if (id < 0) continue;
+        const float e = __builtin_amdgcn_exp2f((en.z[j] - all.m) * p.c);
+        dz[id] = (T)((sound ? f * e : wm * (inv * e)) - w * (twice ? teacher_at(en, p.k, id) : en.t[j]));
       }
   }
 }
@@ -540,7 +546,8 @@ template <typename T, int NT, bool JOIN, int PAST> __global__ __launch_bounds__(
   const bool none = w == 0.f || mass == 0.0;
   // p = exp((z - m) / T) / s, or, from lse, exp(z / T - lse): f exp2(z c - shift), with what the shift's rounding leaves out in f
   Running r;
-  float f = w * (float)mass, shift;
+  const float wm = w * (float)mass;
+  float f = wm, inv = 1.f, shift;
   bool sound = true;
   if (JOIN) {
     r.m = sh.m[0];
@@ -550,7 +557,8 @@ template <typename T, int NT, bool JOIN, int PAST> __global__ __launch_bounds__(
   }
   if (JOIN || again) {
     f /= r.s;
-    sound = r.sound(p.c);
+    inv = 1.f / r.s;
+    sound = r.sound(p.c) && fabsf(f) >= LEAST_FACTOR;
     shift = r.reference(p.c);
     if (sound) f *= r.rest(p.c);
   } else {
@@ -559,6 +567,7 @@ template <typename T, int NT, bool JOIN, int PAST> __global__ __launch_bounds__(
     f *= __builtin_amdgcn_exp2f((float)((double)shift - exact));
   }
   auto prob = [&](float x) { return f * __builtin_amdgcn_exp2f(fmaf(x, p.c, -shift)); };
+  auto prob_slow = [&](float x) { return wm * (inv * __builtin_amdgcn_exp2f((x - r.m) * p.c)); };
   int at = begin + threadIdx.x * N;
   if (none) {
     const float x[N] = {};
@@ -570,7 +579,7 @@ template <typename T, int NT, bool JOIN, int PAST> __global__ __launch_bounds__(
       float x[N];
       load_chunk(z, at, end, x);
 #pragma unroll
-      for (int e = 0; e < N; ++e) x[e] = f * __builtin_amdgcn_exp2f((x[e] - r.m) * p.c);
+      for (int e = 0; e < N; ++e) x[e] = prob_slow(x[e]);
       store_chunk(dz, at, end, x);
     }
   }
@@ -601,7 +610,7 @@ template <typename T, int NT, bool JOIN, int PAST> __global__ __launch_bounds__(
   __syncthreads();
   for (int j = threadIdx.x; j < p.k; j += NT) {
     const int id = e.id[j];
-    if (id >= begin && id < end) dz[id] = (T)((sound ? prob(e.z[j]) : f * __builtin_amdgcn_exp2f((e.z[j] - r.m) * p.c)) - w * (sh.teacher.twice ? teacher_at(e, p.k, id) : e.t[j]));
+    if (id >= begin && id < end) dz[id] = (T)((sound ? prob(e.z[j]) : prob_slow(e.z[j])) - w * (sh.teacher.twice ? teacher_at(e, p.k, id) : e.t[j]));
   }
 }
 

@@ -710,6 +710,24 @@ def test_distillation_of_words_whose_exponential_is_just_within_range(how, dtype
     c.untouched()
 
 
+@pytest.mark.parametrize("how", ["both", "apart"])
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+@pytest.mark.parametrize("rows,vocab", [(3, 900), (3, 50000), (161, 9001), (161, 40009)])
+def test_distillation_of_weights_near_the_least_numbers(how, dtype, rows, vocab):
+    """The gradient's values are numbers of 32 bits as long as weight times probability is; weight over the sum against the first words need not be."""
+    c = Distill(dtype, rows, vocab, 6, bare=True, seed=10)
+    c.Z[:2] /= 64
+    c.Z[:2, vocab - 5] = 20.0
+    c.Z = q(c.Z, dtype)
+    c.ids[:2, 0] = vocab - 5
+    c.w = (np.float32(1e-35) * np.sign(c.w)).astype(np.float32)
+    c.upload()
+    dz = c.call(how)
+    torch.cuda.synchronize()
+    c.check(dz)
+    c.untouched()
+
+
 @pytest.mark.parametrize("rows,vocab,k", [(40, 3000, 20), (2, 100003, 64), (700, 20000, 9), (301, 900, 1024)])
 def test_distillation_captured_replayed_and_repeated(rows, vocab, k):
     a, b = Distill(BF16, rows, vocab, k), Distill(BF16, rows, vocab, k, seed=1)
