@@ -28,14 +28,15 @@ template <> struct Any16<bf16_t> { typedef bf16_t t __attribute__((ext_vector_ty
 template <> struct Any16<float> { typedef float t __attribute__((ext_vector_type(4), aligned(4))); };
 
 // what a row's entries make of its loss: sum + mass (log of the sum of exp(z / T) - z0 / T), with sum = sum of t (log t - (z - z0) / T), mass = sum of t and z0 one of
-// their own logits, so that nothing large cancels; log t = the teacher's value - log_norm; twice: a word is named twice
-struct Teacher { double sum, mass, z0, log_norm; int twice, unused; };
+// their own logits, so that nothing large cancels; log t = (the teacher's value - most) / T - log_norm, with T = 1 for log-probabilities; twice: a word is named twice
+struct Teacher { double sum, mass, z0, log_norm; float most; int twice; };
 
 struct Distill {
   const void* z; const int* ids; const float* teacher; const float* dloss;
   float* loss; float* lse; void* dz;
   size_t ldz, lddz;
   int rows, vocab, k;
+  double teacher_inv_t;                                 // 1 / T, or 1 where the teacher gives log-probabilities
   float inv_t, c;                                       // 1 / T, log2(e) / T
   int log_probs;
   int pieces, piece;                                    // of a row, and elements of one (a multiple of a chunk)
@@ -117,7 +118,7 @@ __device__ __forceinline__ double wave_sum64(double v) {
 // exp of a 64-bit number: of its 32-bit part, times one plus the rest (two roundings of 32 bits; the 64-bit functions take a wave a microsecond)
 __device__ __forceinline__ float exp_of(double x) {
   const float hi = (float)x;
-  return x == -INFINITY ? 0.f : expf(hi) * (1.f + (float)(x - (double)hi));
+  return x < -150.0 ? 0.f : expf(hi) * (1.f + (float)(x - (double)hi));   // below: less than half of the least number
 }
 // log of a positive 32-bit number to 2^-26: its exponent times log 2 in 64 bits, the rest near one
 __device__ __forceinline__ double log_of(float x) {
@@ -130,14 +131,17 @@ __device__ __forceinline__ double log_of(float x) {
   return (double)k * 0.69314718055994531 + (double)logf(f);
 }
 
-// entry j's logit of the teacher ahead of its normalisation, minus infinity where it is not there
+// entry j's value of the teacher, minus infinity where it is not there
 __device__ __forceinline__ float entry(const Distill& p, size_t row, int j, int& id) {
   id = p.ids[row * p.k + j];
   const float a = p.teacher[row * p.k + j];
-  if ((unsigned)id < (unsigned)p.vocab) return p.log_probs ? a : a * p.inv_t;
+  if ((unsigned)id < (unsigned)p.vocab) return a;
   id = -1;
   return -INFINITY;
 }
+// log t of a value.  In 64 bits and from the difference: a logit over T in 32 bits is off by 2^-24 of itself, which is an error of t by as much as the logits have in common
+// (1e4 at T 0.7: 5e-4 of t), and past the range for small T.
+__device__ __forceinline__ double log_weight(const Distill& p, float a, float most, double log_norm) { return ((double)a - (double)most) * p.teacher_inv_t - log_norm; }
 
 // One wave: a row's entries into LDS and what they come to.  WEIGHTS: t takes the place of the teacher's values there.  GATHER: with the logits at the words, read
 // before anything of the row is written (dz may be z); without them `sum` is that of t log t alone.
@@ -161,25 +165,25 @@ template <typename T, bool WEIGHTS, bool GATHER> __device__ __forceinline__ Teac
   most = wave_max(most);
   z0 = wave_max(z0);
   if (!(fabsf(z0) < INFINITY)) z0 = 0.f;
-  const double shift = p.log_probs || most == -INFINITY ? 0.0 : (double)most;
+  if (p.log_probs || most == -INFINITY) most = 0.f;
   double norm = 1.0;
   if (!p.log_probs) {
     norm = 0.0;
 #pragma unroll 1
-    for (int j = lane; j < p.k; j += 64) norm += (double)exp_of((double)e.t[j] - shift);
+    for (int j = lane; j < p.k; j += 64) norm += (double)exp_of(log_weight(p, e.t[j], most, 0.0));
     norm = wave_sum64(norm);
     if (norm == 0.0) norm = 1.0;                        // no entries
   }
-  const double log_norm = shift + (p.log_probs ? 0.0 : log_of((float)norm));
+  const double log_norm = p.log_probs ? 0.0 : log_of((float)norm);
   double sum = 0.0, mass = 0.0;
 #pragma unroll 1
   for (int j = lane; j < p.k; j += 64) {
-    const double lt = (double)e.t[j] - log_norm, t = (double)exp_of(lt);
+    const double lt = log_weight(p, e.t[j], most, log_norm), t = (double)exp_of(lt);
     if (t != 0.0) sum += t * (GATHER ? lt - ((double)e.z[j] - (double)z0) * (double)p.inv_t : lt);
     mass += t;
     if (WEIGHTS) e.t[j] = (float)t;
   }
-  return {wave_sum64(sum), wave_sum64(mass), z0, log_norm, 0, 0};
+  return {wave_sum64(sum), wave_sum64(mass), z0, log_norm, most, 0};
 }
 
 // all that the row's entries give a word
@@ -323,6 +327,7 @@ template <typename T, int NT, int R> __global__ __launch_bounds__(NT) __attribut
     const Entries en(lds, turn, p.k);
     const Teacher& teacher = p.parts[row];
     const double log_norm = teacher.log_norm;
+    const float most = teacher.most;
     const int id = id_next;                             // this thread's entry, requested a row ahead
     const float a = a_next, zid = id >= 0 ? (float)z[id] : -INFINITY;
     Running part;
@@ -356,7 +361,7 @@ template <typename T, int NT, int R> __global__ __launch_bounds__(NT) __attribut
     for (int r = 0; r < R; ++r) asm volatile("" : "+v"(held[r]));   // kept as they came: their values in 32 bits would take twice the registers
     if ((int)threadIdx.x < p.k) {
       en.id[threadIdx.x] = id;
-      en.t[threadIdx.x] = exp_of((double)a - log_norm);
+      en.t[threadIdx.x] = exp_of(log_weight(p, a, most, log_norm));
       en.z[threadIdx.x] = zid;
       en.value[threadIdx.x] = a;
 #pragma unroll 1
@@ -364,7 +369,7 @@ template <typename T, int NT, int R> __global__ __launch_bounds__(NT) __attribut
         int other;
         const float v = entry(p, row, j, other);
         en.id[j] = other;
-        en.t[j] = exp_of((double)v - log_norm);
+        en.t[j] = exp_of(log_weight(p, v, most, log_norm));
         en.value[j] = v;
         en.z[j] = other >= 0 ? (float)z[other] : -INFINITY;
       }
@@ -376,16 +381,17 @@ template <typename T, int NT, int R> __global__ __launch_bounds__(NT) __attribut
     const bool twice = teacher.twice;
     const float w = p.dloss[row] * p.inv_t;
     const bool none = w == 0.f || mass == 0.0;
-    const float wm = w * (float)mass, f = none ? 0.f : wm / all.s, inv = 1.f / all.s;
+    const float f = none ? 0.f : w * (float)mass / all.s;
     const bool sound = all.sound(p.c) && (none || fabsf(f) >= LEAST_FACTOR);
     const float fr = sound ? f * all.rest(p.c) : f, mc = all.reference(p.c);
+    auto prob_slow = [&](float x) { return w * (float)mass * (__builtin_amdgcn_exp2f((x - all.m) * p.c) / all.s); };
     if (!sound) {
 #pragma unroll 1
       for (int at = first; at < p.vocab; at += STEP) {
         float x[N];
         load_chunk(z, at, p.vocab, x);
 #pragma unroll
-        for (int e = 0; e < N; ++e) x[e] = none ? 0.f : wm * (inv * __builtin_amdgcn_exp2f((x[e] - all.m) * p.c));
+        for (int e = 0; e < N; ++e) x[e] = none ? 0.f : prob_slow(x[e]);
         store_chunk(dz, at, p.vocab, x);
       }
     }
@@ -417,17 +423,16 @@ template <typename T, int NT, int R> __global__ __launch_bounds__(NT) __attribut
 #pragma unroll 1
       for (int j = threadIdx.x - (NT - 64); j < p.k; j += 64) {
         const double t = (double)en.t[j];
-        if (t != 0.0) sum += t * ((double)en.value[j] - log_norm - ((double)en.z[j] - (double)all.m) * (double)p.inv_t);
+        if (t != 0.0) sum += t * (log_weight(p, en.value[j], most, log_norm) - ((double)en.z[j] - (double)all.m) * (double)p.inv_t);
       }
       sum = wave_sum64(sum);
-      if (threadIdx.x == NT - 1) finish(p, row, all, {sum, mass, all.m, 0.0, 0, 0});
+      if (threadIdx.x == NT - 1) finish(p, row, all, {sum, mass, all.m, 0.0, 0.f, 0});
     }
     if (!none)
       for (int j = threadIdx.x; j < p.k; j += NT) {
         const int id = en.id[j];
         if (id < 0) continue;
-        const float e = __builtin_amdgcn_exp2f((en.z[j] - all.m) * p.c);
-        dz[id] = (T)((sound ? f * e : wm * (inv * e)) - w * (twice ? teacher_at(en, p.k, id) : en.t[j]));
+        dz[id] = (T)((sound ? f * __builtin_amdgcn_exp2f((en.z[j] - all.m) * p.c) : prob_slow(en.z[j])) - w * (twice ? teacher_at(en, p.k, id) : en.t[j]));
       }
   }
 }
@@ -547,7 +552,7 @@ template <typename T, int NT, bool JOIN, int PAST> __global__ __launch_bounds__(
   // p = exp((z - m) / T) / s, or, from lse, exp(z / T - lse): f exp2(z c - shift), with what the shift's rounding leaves out in f
   Running r;
   const float wm = w * (float)mass;
-  float f = wm, inv = 1.f, shift;
+  float f = wm, shift;
   bool sound = true;
   if (JOIN) {
     r.m = sh.m[0];
@@ -557,7 +562,6 @@ template <typename T, int NT, bool JOIN, int PAST> __global__ __launch_bounds__(
   }
   if (JOIN || again) {
     f /= r.s;
-    inv = 1.f / r.s;
     sound = r.sound(p.c) && fabsf(f) >= LEAST_FACTOR;
     shift = r.reference(p.c);
     if (sound) f *= r.rest(p.c);
@@ -567,7 +571,7 @@ template <typename T, int NT, bool JOIN, int PAST> __global__ __launch_bounds__(
     f *= __builtin_amdgcn_exp2f((float)((double)shift - exact));
   }
   auto prob = [&](float x) { return f * __builtin_amdgcn_exp2f(fmaf(x, p.c, -shift)); };
-  auto prob_slow = [&](float x) { return wm * (inv * __builtin_amdgcn_exp2f((x - r.m) * p.c)); };
+  auto prob_slow = [&](float x) { return wm * (__builtin_amdgcn_exp2f((x - r.m) * p.c) / r.s); };
   int at = begin + threadIdx.x * N;
   if (none) {
     const float x[N] = {};
@@ -775,7 +779,7 @@ uint64_t distill_ws_bytes(int rows, int vocab, int) {
 
 hipError_t launch_distill(int dtype, const void* z, size_t ldz, const int* ids, const float* teacher, const float* dloss, float* loss, float* lse, void* dz, size_t lddz,
                           void* ws, int rows, int vocab, int k, float temperature, int log_probs, hipStream_t s) {
-  Distill p = {z, ids, teacher, dloss, loss, lse, dz, ldz, lddz, rows, vocab, k, 1.f / temperature, LOG2E / temperature, log_probs, 1, vocab, nullptr, nullptr};
+  Distill p = {z, ids, teacher, dloss, loss, lse, dz, ldz, lddz, rows, vocab, k, log_probs ? 1.0 : 1.0 / (double)temperature, 1.f / temperature, LOG2E / temperature, log_probs, 1, vocab, nullptr, nullptr};
   p.parts = (Teacher*)ws;
   return dtype == DT_BF16 ? run<bf16_t>(p, s) : run<float>(p, s);
 }

@@ -728,6 +728,21 @@ def test_distillation_of_weights_near_the_least_numbers(how, dtype, rows, vocab)
     c.untouched()
 
 
+@pytest.mark.parametrize("how", ["both", "apart"])
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+@pytest.mark.parametrize("rows,vocab", [(5, 500), (5, 9001), (200, 9001)])
+@pytest.mark.parametrize("offset,size,temperature", [(1e4, 1.0, 0.7), (-3e5, 1.0, 3.0), (0.0, 1e9, 1e-30)])
+def test_distillation_of_teacher_logits_far_from_zero(how, dtype, rows, vocab, offset, size, temperature):
+    """What a teacher's logits have in common does not show in its probabilities, nor does their size over the temperature have to be a number of 32 bits."""
+    c = Distill(dtype, rows, vocab, 12, float(np.float32(temperature)), seed=10)
+    c.T = (c.T * np.float32(size) + np.float32(offset)).astype(np.float32)
+    c.upload()
+    dz = c.call(how)
+    torch.cuda.synchronize()
+    c.check(dz)
+    c.untouched()
+
+
 @pytest.mark.parametrize("rows,vocab,k", [(40, 3000, 20), (2, 100003, 64), (700, 20000, 9), (301, 900, 1024)])
 def test_distillation_captured_replayed_and_repeated(rows, vocab, k):
     a, b = Distill(BF16, rows, vocab, k), Distill(BF16, rows, vocab, k, seed=1)
