@@ -4,7 +4,7 @@
 // one wave) runs while the row's loads are in flight.
 //
 // A row's reference and sum are one pass: every wave keeps m, the largest of its first 16 bytes a lane, and s = sum of exp((z - m) / T).  Where a later logit lies so far
-// above m that s reaches 2^32 (22 T), or nothing but the lowest values is left of a row, the row (its piece) is summed again with the running maximum.
+// above m that s reaches 2^64 (44 T), or nothing but the lowest values is left of a row, the row (its piece) is summed again with the running maximum.
 // A logit costs a conversion, a multiply-add, an exponential and an addition in each direction, half of what the running maximum would: at 4096 rows of 131072 words
 // the vector units are busy half of the time that memory takes.
 //  * Rows of a few words: a wave has one in its registers, in every direction.
@@ -69,9 +69,11 @@ struct Running {
   // m c as one number, and what that rounding left out: exp2((x - m) c) = exp2(x c - reference) * rest
   __device__ __forceinline__ float reference(float c) const { return m * c; }
   __device__ __forceinline__ float rest(float c) const { return __builtin_amdgcn_exp2f(fmaf(-m, c, m * c)); }
-  // Whether the sum holds, and rest is some 2^16 at most.  Against the maximum s is below 2^30, the number of words.  From 2^32 on the reference is not near enough: the
-  // exponents' rounding is 2^-20 there and grows, 1 / s falls towards the least numbers (a weight of 1e-6 over 2^122 has 7 bits), and sums of pieces overflow when they are joined.
-  __device__ __forceinline__ bool sound(float c) const { return s > 0.f && s < 0x1p32f && fabsf(m * c) < 0x1p28f; }
+  // Whether the sum holds, and rest is some 2^16 at most.  Against the maximum s is below 2^30, the number of words.  Where a later word lies far above the reference, 1 / s falls
+  // towards the least numbers (a weight of 1e-6 over 2^122 has 7 bits), and sums of pieces overflow when they are joined.  Up to 2^64 neither is near, and what the exponents lose to
+  // rounding, 2^-19, is about what such a row's lse loses.  A row with a word 44 T above the first ones is read once more (if every row has one, 4096 of 131072 words bf16
+  // 440 -> 618 us, 4096 of 32000 fp32 218 -> 281): a bound of 2^32 would have that from 22 T on.
+  __device__ __forceinline__ bool sound(float c) const { return s > 0.f && s < 0x1p64f && fabsf(m * c) < 0x1p28f; }
 };
 // The same against a reference that a wave has taken from its first chunks.
 struct Quick {
