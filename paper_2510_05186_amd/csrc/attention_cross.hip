@@ -1501,12 +1501,20 @@ template <int D> __global__ __launch_bounds__(256) void cross_dkv_f32_wide(const
 // 64 rows (states) to a workgroup (`waves` 4), or 16 whose waves divide the other side (1).  Forward and backward, us, 16 / 64: 16 heads of 64 x 512 x 512 (128 workgroups of 64)
 // 84 / 97, 4 x 16 heads x 512 x 1024 508 / 411, 8 heads of 128 x 2048 x 2048 1017 / 773, 4 heads x 4096 x 4096 1984 / 1486; fewer workgroups but a long other side, 8 / 2
 // heads x 2048 x 2048 (64 of states, 512 tiles of rows) 1022 / 801.
-bool wide_pays(long wide_wgs, long others) { return wide_wgs > 128 || (wide_wgs >= 48 && others >= 128); }
+// Few rows (states) of many sequences and heads leave 64 mostly empty, while every workgroup reads the other side: up to 16 of them in the form of 16, where the other side is two
+// tiles at least (less leaves its waves idle: 64 x 16 heads of 128 x 32 queries x 4 states 62 / 99), and up to 32 rows where it is eight.  Forward / backward: one token of 16 sequences, 32 / 8
+// heads of 128 x 16384 states 332 / 1381 as 16, 784 / 1870 as 64; 32 rows x 4096 130 / 507, 206 / 539 (48 rows: 174 / 635, 208 / 586); 2000 queries x 16 heads x 16 sequences
+// x 16 states 140 / 420, 140 / 512 (40 states: 197 / 860, 197 / 576).
+bool wide_pays(long mine, long others, bool states, long groups) {
+  if (mine <= 16 ? others >= 2 : !states && mine <= 32 && others >= 8) return false;
+  const long wgs = groups * ((mine + 63) / 64);
+  return wgs > 128 || (wgs >= 48 && others >= 128);
+}
 CrossPlan plan_f32(const CrossShape& c, bool states) {
   const long mine = states ? c.seq_kv : (long)(c.n_q / c.n_kv) * c.seq_q, others = ((states ? (long)(c.n_q / c.n_kv) * c.seq_q : c.seq_kv) + ROWS - 1) / ROWS;
   const long groups = (long)c.n_kv * c.batch;
   CrossPlan p;
-  p.waves = wide_pays(groups * ((mine + 63) / 64), others) ? 4 : 1;
+  p.waves = wide_pays(mine, others, states, groups) ? 4 : 1;
   p.tiles = (int)((mine + ROWS * p.waves - 1) / (ROWS * p.waves));
   const long wgs = groups * p.tiles;
   long splits = p.waves == 4 ? (wgs >= 384 ? 1 : 512 / wgs) : (wgs >= 512 ? 1 : 1024 / wgs);

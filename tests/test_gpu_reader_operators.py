@@ -347,7 +347,7 @@ def test_cross_attention_of_every_division(dtype, shape):
 @pytest.mark.parametrize("b,nq,nk,hq,hkv,d,lens", [(16, 1, 300, 32, 16, 64, None), (12, 15, 140, 16, 16, 128, [140, 0, 1, 16, 17, 139, 64, 33, 140, 2, 128, 100]), (16, 3, 5, 12, 12, 64, None),
                                                    (16, 70, 4, 16, 16, 64, [4, 3, 2, 1] * 4), (12, 100, 20, 12, 12, 128, [0, 20, 1, 16, 17, 19, 20, 5, 20, 2, 15, 20])])
 def test_cross_attention_of_many_short_sequences(dtype, b, nq, nk, hq, hkv, d, lens):
-    """So many sequences and heads that fp32 calls take the form of 64 rows, or states, to a workgroup, of which a few are there."""
+    """So many sequences and heads that every one has a workgroup of its own with 1 to 20 rows, or states, of 64 (or of 16) in it."""
     cross_both(Cross(dtype, b, nq, nk, hq, hkv, d, lens))
 
 

@@ -125,3 +125,13 @@ def test_the_sizes_tested_take_every_form():
         for dt in (FP32, BF16):
             assert 1 <= form(dt, 0, b, nq, nk, hq, hkv, d)[1] <= 64
             assert 1 <= form(dt, 1, b, nq, nk, hq, hkv, d)[1] <= 256
+
+
+@pytest.mark.parametrize("b,nq,nk,hq,hkv,d", [(16, 1, 16384, 32, 8, 128), (16, 1, 16384, 8, 8, 128), (16, 15, 2000, 16, 16, 128), (16, 8, 4096, 32, 8, 128), (64, 1, 32, 16, 16, 64)])
+def test_fp32_calls_of_few_rows_take_the_form_of_16(b, nq, nk, hq, hkv, d):
+    """64 rows to a workgroup would be mostly empty, and likewise of few states; many of them, or a short other side, keep their form."""
+    f = ctypes.CDLL(B.LIB_PATH)["_Z15cross_attn_formiiiiiiii"]
+    assert f(FP32, 0, nq, nk, b, hq, hkv, d) // 1000 == 1
+    assert f(FP32, 1, nk, nq, b, hkv, hkv, d) // 1000 == (1 if nq <= 16 else 4)
+    assert f(FP32, 0, 64, nk, b, hkv, hkv, d) // 1000 == 4 and f(FP32, 1, nk, 64, b, hkv, hkv, d) // 1000 == 4
+    assert f(FP32, 0, nq, 16, 4 * b, hq, hkv, d) // 1000 == 4
