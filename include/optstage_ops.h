@@ -201,7 +201,8 @@ optstage_status optstage_op_rope_axes(uint32_t dtype, const void* src, uint32_t 
  * o, dout [batch*seq_q, n_q*d]; lse fp32 [batch][n_q][seq_q] (natural log).  kv_len: DEVICE int32 [batch] (any address of an int32), or null for all states; below 0
  * counts as 0, above seq_kv as seq_kv.  States past it are not read: they may hold anything.  A sequence without states has o = 0, lse = -infinity and
  * no gradients (0).  A padded query computes as any other; finite and with dout = 0 it adds nothing to dk and dv.  head_dim 64 or 128.  ws: DEVICE scratch of at
- * least optstage_op_cross_attn_ws_bytes() bytes for either direction, belonging to a call until its work has run.  bf16: products on the matrix units, sums and softmax in fp32. */
+ * least optstage_op_cross_attn_ws_bytes() bytes for either direction, belonging to a call until its work has run.  bf16: products on the matrix units, their sums and the softmax
+ * in fp32; the probabilities, and in the gradient dS, are rounded to bf16 ahead of the products with v, dout, k and q. */
 optstage_status optstage_op_cross_attn_fwd(uint32_t dtype, const void* q, uint32_t ldq, const void* k, const void* v, uint32_t ldkv, const int32_t* kv_len, void* o,
                                            float* lse, void* ws, uint64_t ws_bytes, uint32_t seq_q, uint32_t seq_kv, uint32_t batch, uint32_t n_q, uint32_t n_kv,
                                            uint32_t head_dim, void* stream);

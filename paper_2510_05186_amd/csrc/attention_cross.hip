@@ -9,7 +9,9 @@
 //  * Work is split where rows alone do not fill the chip: forward and dQ over the states, dK / dV over the queries.  Parts leave fp32 sums in the workspace that
 //    a second launch joins in a fixed order.
 // The probabilities and dS enter the second products as one bf16 number (2^-8 of each at most, which adds about as much to the result's error as its own
-// rounding does); sums, softmax and D are fp32.  A single state has no gradient of its score: dS = p (dP - D) is 0 by definition and is not computed, since D
+// rounding does: 0.0024 of a tensor's norm from 64 bits, where rounding the result alone leaves 0.0017); sums, softmax and D are fp32.  Two numbers, as the causal
+// kernels of heads of 64 take, bring heads of 64 to 0.0018 and less for another half of the second products and their packing (forward and backward, one / two, us: 16 / 8 heads x 8
+// x 1024 x 1500 264 / 365, 16 heads x 4096 x 4096 339 / 477, 16 x 700 x 700 53 / 60, one token of 16 sequences x 16384 forward 74 / 80).  A single state has no gradient of its score: dS = p (dP - D) is 0 by definition and is not computed, since D
 // comes from the rounded o.
 #include "attention_f32_tiles.h"
 #include "attention_tiles.h"

@@ -674,7 +674,7 @@ constexpr int FEW_ROWS = 160;
 // Rows of up to this many words go a wave each, of twice as many in both directions at once (against a workgroup a row or pieces, us: bf16, both, 16384 rows of 200 words 68 -> 17,
 // of 1000 75 -> 23, of 4000 102 -> 88, 100 of 4000 10.6 -> 8.4; each by itself 16384 of 1000 81 -> 38, of 2048 94 -> 55, but 4096 of 3096 29.4 -> 34.5).
 constexpr int SHORT = 2048;
-// A row's pieces: some 1024 workgroups in all, pieces of 2048 elements and more
+// A row's pieces: some 1024 workgroups in all, and at most one for every 2048 elements begun (pieces of 1368 elements for 4097, of 2000 for 50000)
 int pieces_of(int rows, int vocab) {
   const int most = (vocab + 2047) / 2048, want = (1024 + rows - 1) / rows;
   return most < want ? most : want;
